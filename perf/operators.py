@@ -220,8 +220,7 @@ def prepare(c, seed):
         q, k, v = (x.view(n, -1, d) for x in qkv.split([hq * d, H * d, H * d], dim=1))
         n_pages = _pages(n, page) + 3
         f, m = frequencies(c)
-        turns = torch.tensor(f, dtype=torch.float64) / (2 * math.pi)
-        hi = turns.float()
+        turns = [round(x / (2 * math.pi) * 2 ** 64) % 2 ** 64 for x in f]                   # in 2^-64 of a turn
         pool = torch.randn(2, n_pages, H, page, d, device="cuda", generator=gen).to(dt)
         ids = torch.randperm(n_pages, device="cuda", generator=gen)
         t = torch.arange(n, device="cuda")
@@ -230,7 +229,7 @@ def prepare(c, seed):
         return dict(c=c, q=q, k=k, v=v, pool=pool, q_out=empty((n, hq, d), dt), positions=pos.to(torch.int32),
                     slots=ids[t // page] * page + t % page, mscale=m,
                     inv_freq=torch.tensor(f, dtype=torch.float32, device="cuda"),
-                    table=torch.stack([hi, (turns - hi.double()).float()], 1).cuda().contiguous())
+                    table=torch.tensor([x - 2 ** 64 if x >= 2 ** 63 else x for x in turns], dtype=torch.int64, device="cuda"))
     ctx, new = lengths(c)
     lens = [a + b for a, b in zip(ctx, new)]
     n, need = sum(new), [_pages(x, page) for x in lens]
