@@ -19,11 +19,14 @@ from dataclasses import dataclass
 __all__ = ["CG_BLOCK_UNIFORM", "CG_KIVI", "CG_NONE", "CG_BLOCK_TILE", "CG_TILE_TOKENS", "Shape", "Params",
            "packed_bytes", "encode", "decode", "get_status", "lib_path", "load", "CodecGaugeError",
            "kivi_stream_bytes", "kivi_stream_alloc", "kivi_append", "kivi_stream_decode",
-           "attention_workspace_bytes", "attention", "encode_hadamard", "decode_hadamard"]
+           "attention_workspace_bytes", "attention", "encode_hadamard", "decode_hadamard",
+           "Pages", "Rotary", "RopeScaling", "PagedAttention", "page_plan", "page_release", "rotary_table", "rotary",
+           "rotary_append", "paged_attention_workspace_bytes", "paged_attention"]
 
 CG_BLOCK_UNIFORM, CG_KIVI, CG_NONE, CG_BLOCK_TILE = 0, 1, 2, 3
 CG_TILE_TOKENS = 16
 CG_FLAG_NONFINITE_INPUT, CG_FLAG_FP16_OVERFLOW, CG_FLAG_PIPE_TIMEOUT = 1, 2, 4
+CG_FLAG_PAGES_EXHAUSTED, CG_FLAG_PAGED_RANGE = 8, 16
 _STATUS = {0: "CG_OK", -1: "CG_EINVAL", -2: "CG_EUNSUPPORTED", -3: "CG_ECUDA", -4: "CG_ERANGE"}
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -227,3 +230,7 @@ def alloc_outputs(shape: Shape, params: Params, device="cuda"):
     scales = torch.zeros(max(ns // 4, 4), dtype=torch.int32, device=device)
     resid = torch.zeros(max(nr // 2, 8), dtype=torch.int16, device=device)
     return codes, scales, resid
+
+
+from .paged import (Pages, PagedAttention, RopeScaling, Rotary, page_plan, page_release, paged_attention,  # noqa: E402
+                    paged_attention_workspace_bytes, rotary, rotary_append, rotary_table)

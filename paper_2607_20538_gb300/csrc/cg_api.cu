@@ -399,6 +399,9 @@ MoveArgs move_args(const cg_shape* sh, int64_t W) {
 
 }  // namespace
 
+int device_status(int32_t** out) { return status_ptr(out); }
+uint64_t wait_limit_ns() { return pipe_wait_ns(); }
+
 int set_error(int code, const char* fmt, ...) {
     char buf[512];
     va_list ap;

@@ -89,6 +89,11 @@ constexpr int kAttnChunk = 128;  // tokens per chunk of the chunk kernels
 size_t attn_workspace_bytes(int64_t units, int n_rep, int d, int64_t T);
 cudaError_t launch_attention(const AttnArgs& a, cudaStream_t st);
 
+// Address of the current device's status word (CG_OK, or the code of the failure).
+int device_status(int32_t** out);
+// Limit of each bounded pipeline wait (CODECGAUGE_PIPE_WAIT_NS or the default).
+uint64_t wait_limit_ns();
+
 // Sets the message cg_last_error() returns on this host thread; returns code.
 int set_error(int code, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
 

@@ -1,0 +1,33 @@
+// cg_paged.h -- internal interface between the paged-cache entry points and their kernels.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "../../include/codecgauge_paged.h"
+#include "cg_launch.h"
+
+namespace cg {
+
+// Paged attention of one layer (cg_paged_attention's arguments, with log2(page)).
+struct PagedArgs {
+    const uint16_t* q;
+    const uint16_t* pool;
+    const int32_t* table;
+    const int32_t* seq_lens;
+    const int32_t* cu_new;
+    uint16_t* out;
+    float* lse;
+    int32_t* status;
+    int dtype, n_pages, page, page_log2, H, d, n_req, max_pages;
+    int n_tok, n_rep, max_new, window, sinks;
+    float scale;
+    int64_t q_tok, q_head, o_tok, o_head;
+    uint64_t wait_ns;
+};
+
+// Workspace of the paged attention: bytes, and the launch (workspace of that size).
+size_t paged_attn_workspace(const PagedArgs& a);
+cudaError_t launch_paged_attn(const PagedArgs& a, void* workspace, cudaStream_t st);
+
+}  // namespace cg

@@ -1,0 +1,250 @@
+"""Paged KV cache: page plan, rotary append and paged attention (``include/codecgauge_paged.h``).
+
+Bindings of the C entry points with the same names; the tensors' shapes, types and strides are
+checked here, everything else by the library. A pool is a tensor [2][n_pages][H][page][d] (bf16 or
+fp16; 0 keys, 1 values), the codec's cache layout with one layer and the pages as the batch.
+"""
+from __future__ import annotations
+
+import ctypes
+from dataclasses import dataclass
+
+from . import CodecGaugeError, _check, _stream, load
+
+CG_BF16, CG_FP16 = 0, 1
+CG_ROPE_NONE, CG_ROPE_LINEAR, CG_ROPE_BANDS, CG_ROPE_YARN = 0, 1, 2, 3
+
+
+class _CPages(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "n_pages", "page", "H", "d", "n_req", "max_pages")]
+
+
+class _CRotary(ctypes.Structure):
+    _fields_ = [("rot", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("transpose", ctypes.c_int32),
+                ("mscale", ctypes.c_float)]
+
+
+class _CScaling(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32)] + [(n, ctypes.c_double) for n in ("base", "factor", "original", "low", "high")]
+
+
+class _CStrides(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("q_tok", "q_head", "k_tok", "k_head", "v_tok", "v_head", "o_tok", "o_head")]
+
+
+class _CPagedAttn(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_tok", "n_rep", "max_new", "window", "sinks")] + \
+        [("scale", ctypes.c_float)] + [(n, ctypes.c_int64) for n in ("q_tok", "q_head", "o_tok", "o_head")]
+
+
+@dataclass(frozen=True)
+class Pages:
+    """Pool geometry (n_pages pages of `page` tokens, H KV heads of d channels) and block table
+    [n_req][max_pages]. The plan and the release use neither H nor d."""
+    n_pages: int
+    page: int
+    H: int = 1
+    d: int = 128
+    n_req: int = 1
+    max_pages: int = 1
+
+    def c(self, dtype: int = CG_BF16) -> _CPages:
+        return _CPages(dtype, self.n_pages, self.page, self.H, self.d, self.n_req, self.max_pages)
+
+
+@dataclass(frozen=True)
+class Rotary:
+    """The first `rot` channels of a head turn; see cg_rotary_params."""
+    rot: int
+    interleaved: bool = False
+    mscale: float = 1.0
+    transpose: bool = False
+
+    def c(self) -> _CRotary:
+        return _CRotary(self.rot, int(self.interleaved), int(self.transpose), self.mscale)
+
+
+@dataclass(frozen=True)
+class RopeScaling:
+    """Frequency rule of rotary_table: kind CG_ROPE_NONE, _LINEAR, _BANDS or _YARN."""
+    kind: int = CG_ROPE_NONE
+    base: float = 10000.0
+    factor: float = 1.0
+    original: float = 8192.0
+    low: float = 1.0
+    high: float = 4.0
+
+
+@dataclass(frozen=True)
+class PagedAttention:
+    """n_rep query heads per KV head, at most max_new new tokens per request; see cg_paged_attn."""
+    n_rep: int
+    max_new: int
+    scale: float
+    window: int = 0
+    sinks: int = 0
+
+
+_P = ctypes.POINTER
+_vp, _i32, _i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
+_ARGS = {
+    "cg_page_plan": [_P(_CPages), _i32] + [_vp] * 11,
+    "cg_page_release": [_P(_CPages)] + [_vp] * 8,
+    "cg_rotary_table": [_i32, _P(_CScaling), _vp, _P(ctypes.c_float)],
+    "cg_rotary": [_P(_CRotary), _i32, _i32, _i32, _i32, _vp, _i64, _i64, _vp, _vp, _vp, _i64, _i64, _vp],
+    "cg_rotary_append": [_P(_CPages), _P(_CRotary), _i32, _i32, _P(_CStrides)] + [_vp] * 9,
+    "cg_paged_attention_workspace_bytes": [_P(_CPages), _P(_CPagedAttn), _P(ctypes.c_size_t)],
+    "cg_paged_attention": [_P(_CPages), _P(_CPagedAttn)] + [_vp] * 8 + [ctypes.c_size_t, _vp],
+}
+_fns = {}
+
+
+def _fn(name: str):
+    f = _fns.get(name)
+    if f is None:
+        f = getattr(load(), name)
+        f.restype = ctypes.c_int
+        f.argtypes = _ARGS[name]
+        _fns[name] = f
+    return f
+
+
+def _bad(msg: str):
+    raise CodecGaugeError(-1, msg)
+
+
+def _elem(t) -> int:
+    import torch
+    if t.dtype is torch.bfloat16:
+        return CG_BF16
+    if t.dtype is torch.float16:
+        return CG_FP16
+    _bad(f"expected a bfloat16 or float16 tensor, got {t.dtype}")
+
+
+def _ints(name: str, t, n: int, bits: int = 32) -> int:
+    """Address of a contiguous device array of at least n integers."""
+    import torch
+    if t.dtype is not (torch.int32 if bits == 32 else torch.int64) or not t.is_cuda or not t.is_contiguous() or t.numel() < n:
+        _bad(f"{name}: expected a contiguous int{bits} device tensor of at least {n} elements")
+    return t.data_ptr()
+
+
+def _heads(name: str, t, n_tok: int, heads: int, d: int, like):
+    """Checks a [n_tok][heads][d] device tensor; returns its address and its two strides."""
+    if t.dim() != 3 or t.shape[0] != n_tok or t.shape[1] != heads or t.shape[2] != d:
+        _bad(f"{name}: expected shape [{n_tok}, {heads}, {d}], got {list(t.shape)}")
+    if t.dtype is not like.dtype or not t.is_cuda:
+        _bad(f"{name}: expected a {like.dtype} device tensor")
+    s = t.stride()
+    if s[2] != 1:
+        _bad(f"{name}: the last dimension must be contiguous")
+    # the stride of a dimension of one element is never used
+    return t.data_ptr(), (s[0] if n_tok > 1 else 0), (s[1] if heads > 1 else 0)
+
+
+def _pool(pages: Pages, pool) -> int:
+    if list(pool.shape) != [2, pages.n_pages, pages.H, pages.page, pages.d] or not pool.is_contiguous() or not pool.is_cuda:
+        _bad(f"pool: expected a contiguous device tensor [2, {pages.n_pages}, {pages.H}, {pages.page}, {pages.d}], "
+             f"got {list(pool.shape)}")
+    return pool.data_ptr()
+
+
+def page_plan(pages: Pages, ctx_lens, new_lens, free_pages, free_count, block_table, seq_lens, cu_new, positions, slots,
+              free_left, stream=None) -> None:
+    """Pages for the new tokens of every request, and positions and slots of all new tokens (cg_page_plan).
+    The number of tokens planned for is positions.numel()."""
+    n, r = positions.numel(), pages.n_req
+    _check(_fn("cg_page_plan")(
+        pages.c(), n, _ints("ctx_lens", ctx_lens, r), _ints("new_lens", new_lens, r),
+        # a stack that is full of used pages may be an empty tensor: no entry of it is read
+        _ints("free_pages", free_pages, 0) or free_count.data_ptr(), _ints("free_count", free_count, 1),
+        _ints("block_table", block_table, r * pages.max_pages), _ints("seq_lens", seq_lens, r),
+        _ints("cu_new", cu_new, r + 1), _ints("positions", positions, n), _ints("slots", slots, n, 64),
+        _ints("free_left", free_left, 1), _stream(stream)))
+
+
+def page_release(pages: Pages, lens, done, block_table, free_pages, free_count, lens_left, free_left, stream=None) -> None:
+    """Give back the pages of the requests whose done flag (int32) is set (cg_page_release)."""
+    r = pages.n_req
+    _check(_fn("cg_page_release")(
+        pages.c(), _ints("lens", lens, r), _ints("done", done, r), _ints("block_table", block_table, r * pages.max_pages),
+        _ints("free_pages", free_pages, pages.n_pages), _ints("free_count", free_count, 1),
+        _ints("lens_left", lens_left, r), _ints("free_left", free_left, 1), _stream(stream)))
+
+
+def rotary_table(rot: int, scaling: RopeScaling = RopeScaling(), device="cuda"):
+    """Frequencies of rot / 2 pairs as a device tensor (int64, 2^-64 of a turn per position), and mscale."""
+    import torch
+    host = torch.empty(max(rot // 2, 0), dtype=torch.int64)
+    m = ctypes.c_float()
+    c = _CScaling(scaling.kind, scaling.base, scaling.factor, scaling.original, scaling.low, scaling.high)
+    _check(_fn("cg_rotary_table")(rot, c, host.data_ptr(), m))
+    return host.to(device), m.value
+
+
+def rotary(turn: Rotary, x, positions, table, out, stream=None) -> None:
+    """out = rotary(x), [n_tok][heads][d] (cg_rotary); out may be x."""
+    if x.dim() != 3:
+        _bad("x: expected [n_tok, heads, d]")
+    n, heads, d = x.shape
+    xp, xt, xh = _heads("x", x, n, heads, d, x)
+    op, ot, oh = _heads("out", out, n, heads, d, x)
+    _check(_fn("cg_rotary")(turn.c(), _elem(x), n, heads, d, xp, xt, xh, _ints("positions", positions, n),
+                            _ints("table", table, turn.rot // 2, 64) if turn.rot else None, op, ot, oh, _stream(stream)))
+
+
+def rotary_append(pages: Pages, turn: Rotary, q, k, v, positions, slots, table, q_out, pool, stream=None) -> None:
+    """q_out = rotary(q); rotary(k) and v into the pool at their slots (cg_rotary_append). q and
+    q_out may be None, or the same tensor."""
+    n = k.shape[0]
+    hq = 0 if q is None else q.shape[1]
+    if k.dtype is not pool.dtype:
+        _bad(f"k: expected the pool's type {pool.dtype}, got {k.dtype}")
+    kp, kt, kh = _heads("k", k, n, pages.H, pages.d, pool)
+    vp, vt, vh = _heads("v", v, n, pages.H, pages.d, pool)
+    qp, qt, qh = _heads("q", q, n, hq, pages.d, pool) if hq else (None, 0, 0)
+    op, ot, oh = _heads("q_out", q_out, n, hq, pages.d, pool) if hq else (None, 0, 0)
+    _check(_fn("cg_rotary_append")(
+        pages.c(_elem(pool)), turn.c(), n, hq, _CStrides(qt, qh, kt, kh, vt, vh, ot, oh), qp, kp, vp,
+        _ints("positions", positions, n), _ints("slots", slots, n, 64),
+        _ints("table", table, turn.rot // 2, 64) if turn.rot else None, op, _pool(pages, pool), _stream(stream)))
+
+
+def _attn(pages: Pages, how: PagedAttention, n: int, qt=0, qh=0, ot=0, oh=0) -> _CPagedAttn:
+    return _CPagedAttn(n, how.n_rep, how.max_new, how.window, how.sinks, how.scale, qt, qh, ot, oh)
+
+
+def paged_attention_workspace_bytes(pages: Pages, how: PagedAttention, n_tok: int) -> int:
+    """Workspace bytes of paged_attention for n_tok query rows."""
+    v = ctypes.c_size_t()
+    _check(_fn("cg_paged_attention_workspace_bytes")(pages.c(), _attn(pages, how, n_tok), v))
+    return v.value
+
+
+def paged_attention(pages: Pages, how: PagedAttention, q, pool, block_table, seq_lens, cu_new, out, lse=None,
+                    workspace=None, stream=None) -> None:
+    """Attention of the new tokens' queries q [n_tok][H * n_rep][d] over their requests' pages
+    (cg_paged_attention). Without a workspace the call takes one from torch's allocator, on the
+    current stream (pass one to run on another)."""
+    import torch
+    n, hq = q.shape[0], pages.H * how.n_rep
+    qp, qt, qh = _heads("q", q, n, hq, pages.d, pool)
+    op, ot, oh = _heads("out", out, n, hq, pages.d, pool)
+    lp = None
+    if lse is not None:
+        if lse.dtype is not torch.float32 or not lse.is_cuda or not lse.is_contiguous() or lse.numel() < n * hq:
+            _bad(f"lse: expected a contiguous float32 device tensor [{n}, {hq}]")
+        lp = lse.data_ptr()
+    cp, ca = pages.c(_elem(pool)), _attn(pages, how, n, qt, qh, ot, oh)
+    if workspace is None:
+        if stream is not None and stream != torch.cuda.current_stream():
+            _bad("workspace: needed on a stream that is not the current one")
+        need = ctypes.c_size_t()
+        _check(_fn("cg_paged_attention_workspace_bytes")(cp, ca, need))
+        workspace = torch.empty(need.value, dtype=torch.uint8, device=q.device)
+    r = pages.n_req
+    _check(_fn("cg_paged_attention")(
+        cp, ca, qp, _pool(pages, pool), _ints("block_table", block_table, r * pages.max_pages),
+        _ints("seq_lens", seq_lens, r), _ints("cu_new", cu_new, r + 1), op, lp, workspace.data_ptr(),
+        workspace.numel() * workspace.element_size(), _stream(stream)))
