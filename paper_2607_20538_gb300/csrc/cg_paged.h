@@ -1,6 +1,7 @@
 // cg_paged.h -- internal interface between the paged-cache entry points and their kernels.
 #pragma once
 
+#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -29,5 +30,12 @@ struct PagedArgs {
 // Workspace of the paged attention: bytes, and the launch (workspace of that size).
 size_t paged_attn_workspace(const PagedArgs& a);
 cudaError_t launch_paged_attn(const PagedArgs& a, void* workspace, cudaStream_t st);
+
+// Tensor map of the pool with boxes of box_rows tokens x 64 channels.
+bool paged_pool_map(CUtensorMap* map, const PagedArgs& a, uint32_t box_rows);
+
+// Requests of at least min_rows query rows on the tensor cores (d = 64, 128).
+size_t paged_chunk_workspace(int d);
+cudaError_t launch_paged_chunk(const PagedArgs& a, int min_rows, void* workspace, cudaStream_t st);
 
 }  // namespace cg

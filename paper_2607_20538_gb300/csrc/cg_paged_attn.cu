@@ -635,23 +635,10 @@ __global__ void __launch_bounds__(kMergeWarps * 32) paged_merge_kernel(const __g
 
 int rows_ctas(int d) { return tc::num_sms() * (d == 256 ? 1 : 2); }
 
-// Tensor map of the pool as [2 n_pages][H page][d], boxes of box_rows x 64 channels, 128-byte swizzle.
-bool make_pool_map(CUtensorMap* map, const PagedArgs& a, uint32_t box_rows) {
-    auto fn = tmap_encode_fn();
-    if (!fn) return false;
-    cuuint64_t dims[3] = {(cuuint64_t)a.d, (cuuint64_t)a.H * a.page, 2ull * a.n_pages};
-    cuuint64_t strides[2] = {(cuuint64_t)a.d * 2, (cuuint64_t)a.H * a.page * a.d * 2};
-    cuuint32_t box[3] = {64, box_rows, 1}, estr[3] = {1, 1, 1};
-    return fn(map, a.dtype == CG_FP16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3,
-              const_cast<uint16_t*>(a.pool), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 template <bool FP16, int D>
 cudaError_t launch_rows(const RowsParams& P, cudaStream_t st) {
     CUtensorMap map;
-    if (!make_pool_map(&map, P.a, P.box_rows)) return cudaErrorInvalidValue;
+    if (!paged_pool_map(&map, P.a, P.box_rows)) return cudaErrorInvalidValue;
     constexpr size_t smem = RowsSmem<D>::total;
     cudaError_t e = cudaFuncSetAttribute(paged_rows_kernel<FP16, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
@@ -676,24 +663,57 @@ size_t rows_workspace(int d) {
     return n * 2 * part_floats(d) * sizeof(float) + n * sizeof(Meta);
 }
 
+// Requests of at most this many query rows run in 16-row tiles here, longer ones on the 128-row
+// tensor-core tiles of cg_paged_chunk.cu. d = 256 does not fit those (tensor memory holds two
+// 128 x 256 accumulators and nothing else).
+int rows_limit(int d) { return d == 256 ? 0x7fffffff : kRows; }
+
 }  // namespace
 
-size_t paged_attn_workspace(const PagedArgs& a) { return rows_workspace(a.d); }
+// Tensor map of the pool as [2 n_pages][H page][d], boxes of box_rows x 64 channels, 128-byte swizzle.
+bool paged_pool_map(CUtensorMap* map, const PagedArgs& a, uint32_t box_rows) {
+    auto fn = tmap_encode_fn();
+    if (!fn) return false;
+    cuuint64_t dims[3] = {(cuuint64_t)a.d, (cuuint64_t)a.H * a.page, 2ull * a.n_pages};
+    cuuint64_t strides[2] = {(cuuint64_t)a.d * 2, (cuuint64_t)a.H * a.page * a.d * 2};
+    cuuint32_t box[3] = {64, box_rows, 1}, estr[3] = {1, 1, 1};
+    return fn(map, a.dtype == CG_FP16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3,
+              const_cast<uint16_t*>(a.pool), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// The two kernels follow one another on the stream, so they share the workspace.
+size_t paged_attn_workspace(const PagedArgs& a) {
+    const size_t r = rows_workspace(a.d);
+    if ((int64_t)a.max_new * a.n_rep <= rows_limit(a.d)) return r;
+    const size_t c = paged_chunk_workspace(a.d);
+    return r > c ? r : c;
+}
 
 cudaError_t launch_paged_attn(const PagedArgs& a, void* workspace, cudaStream_t st) {
-    RowsParams P{};
-    P.a = a;
-    P.parts = static_cast<float*>(workspace);
-    P.meta = reinterpret_cast<Meta*>(P.parts + (size_t)rows_ctas(a.d) * 2 * part_floats(a.d));
-    P.max_rows = 0x7fffffff;
-    P.min_share = 1;
-    P.box_rows = a.page < kTK ? a.page : kTK;
-    const bool h = a.dtype == CG_FP16;
-    switch (a.d) {
-        case 64: return h ? launch_rows<true, 64>(P, st) : launch_rows<false, 64>(P, st);
-        case 128: return h ? launch_rows<true, 128>(P, st) : launch_rows<false, 128>(P, st);
-        default: return h ? launch_rows<true, 256>(P, st) : launch_rows<false, 256>(P, st);
+    const int limit = rows_limit(a.d);
+    const bool long_ones = (int64_t)a.max_new * a.n_rep > limit;
+    cudaError_t e = cudaSuccess;
+    // one request that may be long: the rows kernel is still needed where it may turn out short
+    if (!long_ones || limit >= a.n_rep) {
+        RowsParams P{};
+        P.a = a;
+        P.parts = static_cast<float*>(workspace);
+        P.meta = reinterpret_cast<Meta*>(P.parts + (size_t)rows_ctas(a.d) * 2 * part_floats(a.d));
+        P.max_rows = limit;
+        P.min_share = 1;
+        P.box_rows = a.page < kTK ? a.page : kTK;
+        const bool h = a.dtype == CG_FP16;
+        switch (a.d) {
+            case 64: e = h ? launch_rows<true, 64>(P, st) : launch_rows<false, 64>(P, st); break;
+            case 128: e = h ? launch_rows<true, 128>(P, st) : launch_rows<false, 128>(P, st); break;
+            default: e = h ? launch_rows<true, 256>(P, st) : launch_rows<false, 256>(P, st); break;
+        }
+        if (e != cudaSuccess) return e;
     }
+    if (long_ones) e = launch_paged_chunk(a, limit + 1, workspace, st);
+    return e;
 }
 
 namespace {
