@@ -61,7 +61,7 @@ struct ChunkSmem {
 
 struct ChunkMisc {
     uint64_t full[kMaxStages], empty[kMaxStages];
-    uint64_t sfull[2], pfull[2], ofull[2], qfull[2], qempty[2], vok[4], drain;
+    uint64_t sfull[2], pfull[2][2], ofull[2], qfull[2], qempty[2], vok[4], drain;
     int64_t warp_sum[kChunkThreads / 32];
     int start[4];            // request, head, tile, key tile of the share's beginning
     int special[4];          // the inspected tile held special values
@@ -78,17 +78,16 @@ struct ChunkParams {
     int min_rows;      // requests with fewer query rows are left to the other kernel
     int min_share;     // key tiles
     int box_rows;
+    int q_boxes;       // the queries of a half are whole boxes of qmap
 };
 
-// Rows [row0, row0 + n_rows) of a request: their positions.
+// Rows of a request at positions p0 .. p1, and the key tiles (by number) that they see: some token
+// of tiles [s0, s1) and those below ss, every token for every row of [f0, f1) and those below fs.
 struct Span {
     int p0, p1, n;
-    __device__ __forceinline__ bool sees(const PagedArgs& a, int t0) const {
-        return n > 0 && t0 <= p1 && (!a.window || t0 + kKT > p0 - a.window + 1 || t0 < a.sinks);
-    }
-    __device__ __forceinline__ bool sees_all(const PagedArgs& a, int t0) const {
-        return t0 + kKT <= p0 + 1 && (!a.window || t0 > p1 - a.window || t0 + kKT <= a.sinks);
-    }
+    int s0, s1, ss, f0, f1, fs;
+    __device__ __forceinline__ bool sees(int id) const { return id < s1 && (id >= s0 || id < ss); }
+    __device__ __forceinline__ bool sees_all(int id) const { return id < f1 && (id >= f0 || id < fs); }
     // token t is seen by some rows and not by others, or by none
     __device__ __forceinline__ bool partial(const PagedArgs& a, int t) const {
         return t > p0 || (a.window && t >= a.sinks && p1 - a.window >= t);
@@ -101,26 +100,86 @@ __device__ __forceinline__ Span span_of(const PagedArgs& a, const Request& r, in
     s.n = rows < 0 ? 0 : rows < rows_max ? rows : rows_max;
     s.p0 = r.len - r.n + row0 / a.n_rep;
     s.p1 = s.n ? r.len - r.n + (row0 + s.n - 1) / a.n_rep : s.p0 - 1;
+    s.s0 = s.ss = s.f0 = s.fs = 0;
+    s.s1 = s.n && s.p1 >= 0 ? s.p1 / kKT + 1 : 0;
+    s.f1 = s.p0 < 0 ? 0 : (s.p0 + 1) / kKT;
+    if (a.window) {
+        const int from = s.p0 - a.window + 1, last = s.p1 - a.window;   // first token row p0 sees; last one p1 does not
+        s.s0 = from > 0 ? from / kKT : 0;
+        s.f0 = last >= 0 ? last / kKT + 1 : 0;
+        s.ss = (int)(((int64_t)a.sinks + kKT - 1) / kKT);
+        s.fs = a.sinks / kKT;
+    }
     return s;
 }
 
 __device__ __forceinline__ Tiles tile_tiles(const PagedArgs& a, const Request& r, int m) {
-    const Span s = span_of(a, r, m * kTileRows, kTileRows);
-    return visible_tiles<kKT>(a.window, a.sinks, s.p0, s.p1);
+    const int rows = r.n * a.n_rep - m * kTileRows, n = rows < kTileRows ? rows : kTileRows;
+    return visible_tiles<kKT>(a.window, a.sinks, r.len - r.n + m * kTileRows / a.n_rep,
+                              r.len - r.n + (m * kTileRows + n - 1) / a.n_rep);
 }
 
-// Key tiles of one KV head of a request (all its row tiles).
-__device__ __forceinline__ int64_t head_cost(const ChunkParams& P, const Request& r) {
+// A work tile costs its key tiles plus kTileCost (queries in, first scores, output out), in units of
+// a key tile. A cut of the line inside those kTileCost units falls before the tile.
+constexpr int kTileCost = 4;
+
+__device__ __forceinline__ int row_tiles(const ChunkParams& P, const Request& r) {
     const int64_t rows = (int64_t)r.n * P.a.n_rep;
-    if (rows < P.min_rows || r.n <= 0) return 0;
+    return r.n <= 0 || rows < P.min_rows ? 0 : (int)((rows + kTileRows - 1) / kTileRows);
+}
+
+// Cost of one KV head of each lane's request. All lanes call: requests of many tiles are summed by
+// the whole warp.
+__device__ __forceinline__ int64_t head_cost(const ChunkParams& P, const Request& r) {
+    const int lane = threadIdx.x & 31, n_m = row_tiles(P, r);
     int64_t sum = 0;
-    for (int m = 0; m < (int)((rows + kTileRows - 1) / kTileRows); m++) sum += tile_tiles(P.a, r, m).count();
+    if (n_m <= 2)
+        for (int m = 0; m < n_m; m++) sum += tile_tiles(P.a, r, m).count() + kTileCost;
+    for (uint32_t big = __ballot_sync(0xffffffffu, n_m > 2); big; big &= big - 1) {
+        const int src = __ffs(big) - 1;
+        Request q;
+        q.len = __shfl_sync(0xffffffffu, r.len, src);
+        q.n = __shfl_sync(0xffffffffu, r.n, src);
+        const int n = __shfl_sync(0xffffffffu, n_m, src);
+        int64_t part = 0;
+        for (int m = lane; m < n; m += 32) part += tile_tiles(P.a, q, m).count() + kTileCost;
+#pragma unroll
+        for (int off = 16; off; off >>= 1) part += __shfl_xor_sync(0xffffffffu, part, off);
+        if (lane == src) sum = part;
+    }
     return sum;
+}
+
+// Row tile of one KV head at offset *off of its line; *off becomes the offset within the tile.
+__device__ __forceinline__ int tile_at(const ChunkParams& P, const Request& r, int64_t* off) {
+    const int lane = threadIdx.x & 31, n_m = row_tiles(P, r);
+    for (int m0 = 0;; m0 += 32) {
+        const int m = m0 + lane;
+        const int64_t mine = m < n_m ? tile_tiles(P.a, r, m).count() + kTileCost : 0;
+        int64_t incl = mine;
+#pragma unroll
+        for (int k = 1; k < 32; k *= 2) {
+            const int64_t v = __shfl_up_sync(0xffffffffu, incl, k);
+            if (lane >= k) incl += v;
+        }
+        const int64_t total = __shfl_sync(0xffffffffu, incl, 31);
+        if (*off < total || m0 + 32 >= n_m) {
+            const uint32_t here = __ballot_sync(0xffffffffu, *off >= incl - mine && *off < incl);
+            const int src = here ? __ffs(here) - 1 : 0;
+            *off -= __shfl_sync(0xffffffffu, incl - mine, src);
+            return m0 + src;
+        }
+        *off -= total;
+    }
 }
 
 // Walk over a share: request, KV head, row tile, key tile.
 struct ChunkWalk {
-    int i, h, m, c, n_m, n_chunks;
+    int i, h, m, n_m;
+    int c, take, n;       // first key tile of the current work tile, how many of it, of how many
+    int left, x;          // of the share, in line units; offset of the share in the work tile
+    bool goes_on;         // the work tile goes on past the share
+    int64_t rest;         // by so many line units
     Request r;
     Tiles t;
 
@@ -129,23 +188,32 @@ struct ChunkWalk {
         n_m = 0;
         if (i >= P.a.n_req) return;
         r = load_request(P.a, i, &flag);
-        const int64_t rows = (int64_t)r.n * P.a.n_rep;
-        n_m = r.n <= 0 || rows < P.min_rows ? 0 : (int)((rows + kTileRows - 1) / kTileRows);
+        n_m = row_tiles(P, r);
     }
     __device__ __forceinline__ void tile(const ChunkParams& P) {
         t = tile_tiles(P.a, r, m);
-        n_chunks = t.count();
+        n = t.count();
+        c = x > kTileCost ? x - kTileCost : 0;
+        goes_on = n + kTileCost - x > left;
+        const int e = goes_on ? x + left - kTileCost : n;   // the share's end in the tile
+        take = e > c ? e - c : 0;
+        rest = n + kTileCost - x - left;
+        if (take == 0) left = 0;                            // the tile begins in the next share
     }
-    __device__ __forceinline__ void start(const ChunkParams& P, const int (&s)[4]) {
+    __device__ __forceinline__ void start(const ChunkParams& P, const int (&s)[4], int units) {
+        left = units;
         i = s[0];
         h = s[1];
         m = s[2];
-        c = s[3];
+        x = s[3];
+        if (left <= 0) return;
         load(P);
         tile(P);
     }
     __device__ __forceinline__ void next(const ChunkParams& P) {
-        c = 0;
+        left -= n + kTileCost - x;
+        x = 0;
+        if (left <= 0) return;
         if (++m >= n_m) {
             m = 0;
             if (++h >= P.a.H) {
@@ -154,21 +222,48 @@ struct ChunkWalk {
                     i++;
                     load(P);
                 } while (i < P.a.n_req && n_m == 0);
-                if (i >= P.a.n_req) return;
+                if (i >= P.a.n_req) {
+                    left = 0;
+                    return;
+                }
             }
         }
         tile(P);
     }
 };
 
-// ---------------------------------------------------------------- tcgen05 pieces
-__device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t acc) {
+__device__ __forceinline__ void tma_load_4d(void* dst, const void* tmap, uint64_t* bar, int x, int y, int z, int w) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
-        "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(acc)
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+        "[%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(smem_u32(dst)),
+        "l"(reinterpret_cast<uint64_t>(tmap)), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z), "r"(w)
         : "memory");
+}
+
+// ---------------------------------------------------------------- tcgen05 pieces
+// Descriptors as halves: a step of the product only adds to the low one.
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t acc) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
+        "mov.b64 da, {%1, %3};\n\tmov.b64 db, {%2, %3};\n\t"
+        "setp.ne.b32 p, %5, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, p;\n\t}" ::"r"(d),
+        "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(acc)
+        : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a_tmem, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t acc) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 db;\n\t"
+        "mov.b64 db, {%2, %3};\n\t"
+        "setp.ne.b32 p, %5, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, p;\n\t}" ::"r"(d),
+        "r"(a_tmem), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(acc)
+        : "memory");
+}
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
 }
 
 __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
@@ -196,22 +291,28 @@ __device__ __forceinline__ void tmem_ld32p(uint32_t taddr, uint32_t* r) {
         : "r"(taddr));
 }
 
-// 16 columns times f, in place
-__device__ __forceinline__ void tmem_scale16(uint32_t taddr, float f) {
-    uint32_t r[16];
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
         : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
           "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
         : "r"(taddr));
-    tmem_wait_ld();
-#pragma unroll
-    for (int k = 0; k < 16; k++) r[k] = __float_as_uint(__uint_as_float(r[k]) * f);
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
         "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
         "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
+}
+// 16 columns times f, in place
+__device__ __forceinline__ void tmem_scale16(uint32_t taddr, float f) {
+    uint32_t r[16];
+    tmem_ld16(taddr, r);
+    tmem_wait_ld();
+#pragma unroll
+    for (int k = 0; k < 16; k++) r[k] = __float_as_uint(__uint_as_float(r[k]) * f);
+    tmem_st16(taddr, r);
 }
 
 __device__ __forceinline__ void tmem_ld32f(uint32_t taddr, float (&r)[32]) {
@@ -232,30 +333,7 @@ __device__ __forceinline__ void settle(float (&r)[32]) {
                  "+f"(r[16]), "+f"(r[17]), "+f"(r[18]), "+f"(r[19]), "+f"(r[20]), "+f"(r[21]), "+f"(r[22]), "+f"(r[23]),
                  "+f"(r[24]), "+f"(r[25]), "+f"(r[26]), "+f"(r[27]), "+f"(r[28]), "+f"(r[29]), "+f"(r[30]), "+f"(r[31]));
 }
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
-        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-        : "memory");
-}
 
-// Scores of 32 columns from c0: sign (a negative scale), and where EDGE the columns that the row does
-// not see set to -inf: it sees [lo, hi] and those below sk.
-template <bool EDGE>
-__device__ __forceinline__ void prepare32(float (&s)[32], int c0, bool flip, int lo, int hi, int sk) {
-    if (flip) {
-#pragma unroll
-        for (int k = 0; k < 32; k++) s[k] = -s[k];
-    }
-    if (EDGE) {
-#pragma unroll
-        for (int k = 0; k < 32; k++) {
-            const int c = c0 + k;
-            s[k] = c <= hi && (c >= lo || c < sk) ? s[k] : -INFINITY;
-        }
-    }
-}
 __device__ __forceinline__ float max32(const float (&s)[32], float m) {
     float m0 = fmaxf(m, fmaxf(s[0], s[1])), m1 = fmaxf(s[2], s[3]);
 #pragma unroll
@@ -267,75 +345,61 @@ __device__ __forceinline__ float max32(const float (&s)[32], float m) {
 }
 
 // The row's largest score of a tile (128 columns).
-template <bool EDGE>
-__device__ __forceinline__ float row_max(uint32_t s_tm, bool flip, int lo, int hi, int sk) {
+__device__ __forceinline__ float row_max(uint32_t s_tm) {
     float u[32], v[32];
     tmem_ld32f(s_tm, u);
     tmem_ld32f(s_tm + 32, v);
     tmem_wait_ld();
     settle(u);
     settle(v);
-    prepare32<EDGE>(u, 0, flip, lo, hi, sk);
     float m = max32(u, -INFINITY);
     tmem_ld32f(s_tm + 64, u);
-    prepare32<EDGE>(v, 32, flip, lo, hi, sk);
     m = max32(v, m);
     tmem_ld32f(s_tm + 96, v);
     tmem_wait_ld();
     settle(u);
     settle(v);
-    prepare32<EDGE>(u, 64, flip, lo, hi, sk);
     m = max32(u, m);
-    prepare32<EDGE>(v, 96, flip, lo, hi, sk);
     return max32(v, m);
 }
 
+// Sets the columns that the row does not see to -inf: it sees [lo, hi] and those below sk.
+__device__ __forceinline__ void mask_row(uint32_t s_tm, int lo, int hi, int sk) {
+#pragma unroll 1
+    for (int c0 = 0; c0 < kKT; c0 += 16) {
+        uint32_t r[16];
+        tmem_ld16(s_tm + c0, r);
+        tmem_wait_ld();
+#pragma unroll
+        for (int k = 0; k < 16; k++) {
+            const int c = c0 + k;
+            if (!(c <= hi && (c >= lo || c < sk))) r[k] = 0xff800000u;
+        }
+        tmem_st16(s_tm + c0, r);
+    }
+    tmem_wait_st();
+}
+
+// Weights 2^(s sl2 + neg_ref) of 32 scores in 16 bits, and their sum.
 template <bool FP16>
-__device__ __forceinline__ void weights32(const float (&s)[32], uint32_t p_tm, float sl2, float neg_ref, float2& acc) {
+__device__ __forceinline__ void weights32(const float (&s)[32], uint32_t p_tm, float sl2, float neg_ref, float2& acc0, float2& acc1) {
     uint32_t p[16];
 #pragma unroll
     for (int k = 0; k < 16; k++) {
         const float2 e = __ffma2_rn(make_float2(s[2 * k], s[2 * k + 1]), make_float2(sl2, sl2), make_float2(neg_ref, neg_ref));
         const float2 w = make_float2(ex2(e.x), ex2(e.y));
-        acc = __fadd2_rn(acc, w);
+        if (k & 1) acc1 = __fadd2_rn(acc1, w);
+        else acc0 = __fadd2_rn(acc0, w);
         p[k] = pack2<FP16>(w.x, w.y);
     }
     tmem_st16(p_tm, p);
-}
-
-// Weights 2^(s sl2 + neg_ref) of the tile in 16 bits over the scores (columns [0, 64)), and their
-// sum. The scores are read again: 128 of them kept in registers would not leave room for the rest,
-// and each group of weights lies over scores already read.
-template <bool FP16, bool EDGE>
-__device__ __forceinline__ float row_weights(uint32_t s_tm, bool flip, int lo, int hi, int sk, float sl2, float neg_ref) {
-    float u[32], v[32];
-    float2 acc = make_float2(0.0f, 0.0f);
-    tmem_ld32f(s_tm, u);
-    tmem_ld32f(s_tm + 32, v);
-    tmem_wait_ld();
-    settle(u);
-    settle(v);
-    prepare32<EDGE>(u, 0, flip, lo, hi, sk);
-    weights32<FP16>(u, s_tm, sl2, neg_ref, acc);
-    tmem_ld32f(s_tm + 64, u);
-    prepare32<EDGE>(v, 32, flip, lo, hi, sk);
-    weights32<FP16>(v, s_tm + 16, sl2, neg_ref, acc);
-    tmem_ld32f(s_tm + 96, v);
-    tmem_wait_ld();
-    settle(u);
-    settle(v);
-    prepare32<EDGE>(u, 64, flip, lo, hi, sk);
-    weights32<FP16>(u, s_tm + 32, sl2, neg_ref, acc);
-    prepare32<EDGE>(v, 96, flip, lo, hi, sk);
-    weights32<FP16>(v, s_tm + 48, sl2, neg_ref, acc);
-    return acc.x + acc.y;
 }
 
 template <bool FP16>
 __host__ __device__ constexpr uint32_t idesc16(int M, int N) {
     return (1u << 4) | ((FP16 ? 0u : 1u) << 7) | ((FP16 ? 0u : 1u) << 10) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
 }
-constexpr uint32_t kIdescBMnMajor = 1u << 16;
+constexpr uint32_t kIdescBMnMajor = 1u << 16, kIdescNegateA = 1u << 13;
 
 template <bool FP16>
 __device__ __forceinline__ bool any_special(uint4 v) {
@@ -389,7 +453,8 @@ __device__ __noinline__ void add_special(const PagedArgs& a, const Request& r, i
 
 template <bool FP16, int D>
 __global__ void __launch_bounds__(kChunkThreads, 1)
-paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant__ CUtensorMap map) {
+paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant__ CUtensorMap map,
+                   const __grid_constant__ CUtensorMap qmap) {
     using L = ChunkSmem<D>;
     extern __shared__ __align__(1024) unsigned char smem[];
     ChunkMisc* M = reinterpret_cast<ChunkMisc*>(smem + L::misc);
@@ -402,7 +467,14 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
     const int i_lo = tid * per < a.n_req ? tid * per : a.n_req;
     const int i_hi = i_lo + per < a.n_req ? i_lo + per : a.n_req;
     int64_t mine = 0;
-    for (int i = i_lo; i < i_hi; i++) mine += head_cost(P, load_request(a, i, &flag)) * a.H;
+    int64_t first_cost = 0;
+    for (int k = 0; k < per; k++) {
+        Request r{};
+        if (i_lo + k < i_hi) r = load_request(a, i_lo + k, &flag);
+        const int64_t c = head_cost(P, r);
+        if (k == 0) first_cost = c;
+        mine += c * a.H;
+    }
     int64_t incl = mine;
 #pragma unroll
     for (int off = 1; off < 32; off *= 2) {
@@ -417,7 +489,8 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
         }
         for (int x = 0; x < 2; x++) {
             mbar_init(&M->sfull[x], 1);
-            mbar_init(&M->pfull[x], 4);
+            mbar_init(&M->pfull[x][0], 4);
+            mbar_init(&M->pfull[x][1], 4);
             mbar_init(&M->ofull[x], 1);
             mbar_init(&M->qfull[x], 1);
             mbar_init(&M->qempty[x], 1);
@@ -446,37 +519,44 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
     if (share < P.min_share) share = P.min_share;
     const int64_t begin = share * blockIdx.x;
     const int64_t end = begin + share < total ? begin + share : total;
-    if (begin >= before && begin < before + mine) {
-        int64_t at = before;
-        for (int i = i_lo; i < i_hi; i++) {
-            const Request r = load_request(a, i, &flag);
-            const int64_t hc = head_cost(P, r);
-            if (begin < at + hc * a.H) {
-                int64_t off = begin - at;
-                const int h = (int)(off / hc);
-                off -= h * hc;
-                int m = 0;
-                for (;; m++) {
-                    const int n = tile_tiles(a, r, m).count();
-                    if (off < n) break;
-                    off -= n;
-                }
-                M->start[0] = i;
-                M->start[1] = h;
-                M->start[2] = m;
-                M->start[3] = (int)off;
-                break;
+    if (__any_sync(0xffffffffu, begin >= before && begin < before + mine)) {   // one warp: its lanes look together
+        Request r{};
+        int req = -1;
+        int64_t at = before, hc = 0, off = 0;
+        for (int k = 0; k < per; k++) {
+            Request q{};
+            if (i_lo + k < i_hi) q = load_request(a, i_lo + k, &flag);
+            const int64_t c = per == 1 ? first_cost : head_cost(P, q);
+            if (begin >= at && begin < at + c * a.H) {
+                req = i_lo + k;
+                r = q;
+                hc = c;
+                off = begin - at;
             }
-            at += hc * a.H;
+            at += c * a.H;
+        }
+        const int src = __ffs(__ballot_sync(0xffffffffu, req >= 0)) - 1;
+        req = __shfl_sync(0xffffffffu, req, src);
+        r.len = __shfl_sync(0xffffffffu, r.len, src);
+        r.n = __shfl_sync(0xffffffffu, r.n, src);
+        hc = __shfl_sync(0xffffffffu, hc, src);
+        off = __shfl_sync(0xffffffffu, off, src);
+        const int h = (int)(off / hc);
+        off -= h * hc;
+        const int m = tile_at(P, r, &off);
+        if (lane == 0) {
+            M->start[0] = req;
+            M->start[1] = h;
+            M->start[2] = m;
+            M->start[3] = (int)off;
         }
     }
     __syncthreads();
     if (blockIdx.x == 0) raise_flag(a.status, flag);
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     volatile int* abort_flag = &M->abort_flag;
-    int left = begin < end ? (int)(end - begin) : 0;
     ChunkWalk w;
-    if (left) w.start(P, M->start);
+    w.start(P, M->start, begin < end ? (int)(end - begin) : 0);
     const uint32_t kS = tmem, kO = tmem + 256;
 
     if (warp < 8) {
@@ -486,16 +566,14 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
         const uint32_t s_tm = kS + x * 128 + lanes, o_tm = kO + x * D + lanes;
         // a scale of 0 becomes the least number, so that a masked -inf stays one
         const float sl2 = fmaxf(fabsf(a.scale) * kLog2e, 1.17549435e-38f);
-        const bool flip = a.scale < 0.0f;
         constexpr float kBias = Weights<FP16>::kBias;
         int ns = 0, no = 0, nv = 0;   // active steps, tiles and value tiles so far
-        bool head_part = left && w.c > 0, dead = *abort_flag != 0;
+        bool head_part = w.left > 0 && w.c > 0, dead = *abort_flag != 0;
         int meta_last = -1;
-        while (left > 0 && !dead) {
+        while (w.left > 0 && !dead) {
             const int row0 = w.m * kTileRows + x * kHalfRows;
             const Span sp = span_of(a, w.r, row0, kHalfRows), item = span_of(a, w.r, w.m * kTileRows, kTileRows);
-            const int take = w.n_chunks - w.c < left ? w.n_chunks - w.c : left;
-            const bool goes_on = w.c + take < w.n_chunks;
+            const int take = w.take;
             if (sp.n > 0) {
                 const int row = (warp & 3) * 32 + lane;
                 const bool have = row < sp.n;
@@ -504,17 +582,17 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                 float ref = -INFINITY, sum = 0.0f;
                 bool started = false;
                 for (int kc = 0; kc < take; kc++) {
-                    const int t0 = w.t.id(w.c + kc) * kKT;
-                    if (!sp.sees(a, t0)) continue;
+                    const int id = w.t.id(w.c + kc);
+                    if (!sp.sees(id)) continue;
                     if (!__all_sync(0xffffffffu, mbar_wait(&M->sfull[x], ns & 1, abort_flag, a.wait_ns))) {
                         dead = true;
                         break;
                     }
                     ns++;
                     tc_fence_after();
-                    const bool edge = !sp.sees_all(a, t0);
-                    const int hi = pos - t0, lo = a.window ? pos - a.window + 1 - t0 : 0, sk = a.sinks - t0;
-                    const float mx = sl2 * (edge ? row_max<true>(s_tm, flip, lo, hi, sk) : row_max<false>(s_tm, flip, 0, 0, 0));
+                    const int t0 = id * kKT;
+                    if (!sp.sees_all(id)) mask_row(s_tm, a.window ? pos - a.window + 1 - t0 : 0, pos - t0, a.sinks - t0);
+                    const float mx = sl2 * row_max(s_tm);
                     if (__any_sync(0xffffffffu, mx > ref + (kBias + kLazy))) {
                         const float nr = fmaxf(ref, mx - kBias);
                         // never 0 x inf in O: a factor below all numbers becomes the least one
@@ -526,10 +604,7 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                         sum *= ref == -INFINITY ? 0.0f : f;
                         ref = nr;
                     }
-                    const float nr = ref == -INFINITY ? 0.0f : -ref;
-                    sum += edge ? row_weights<FP16, true>(s_tm, flip, lo, hi, sk, sl2, nr)
-                                : row_weights<FP16, false>(s_tm, flip, 0, 0, 0, sl2, nr);
-                    if (!item.sees_all(a, t0)) {
+                    if (!item.sees_all(id)) {
                         // the inspected value tile held special values: add those the row sees
                         const int v = nv + kc;
                         if (!__all_sync(0xffffffffu, mbar_wait(&M->vok[v & 3], (v >> 2) & 1, abort_flag, a.wait_ns))) {
@@ -542,10 +617,35 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                         }
                     }
                     started = true;
+                    // The scores are read again: 128 of them kept in registers would not leave room
+                    // for the rest, and each group of weights lies over scores already read. The
+                    // product starts on the first half of the weights.
+                    const float nr = ref == -INFINITY ? 0.0f : -ref;
+                    float2 acc0 = make_float2(0.0f, 0.0f), acc1 = acc0;
+                    float u[32], v[32];
+                    tmem_ld32f(s_tm, u);
+                    tmem_ld32f(s_tm + 32, v);
+                    tmem_wait_ld();
+                    settle(u);
+                    settle(v);
+                    weights32<FP16>(u, s_tm, sl2, nr, acc0, acc1);
+                    tmem_ld32f(s_tm + 64, u);
+                    weights32<FP16>(v, s_tm + 16, sl2, nr, acc0, acc1);
                     tmem_wait_st();
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(&M->pfull[x]);
+                    if (lane == 0) mbar_arrive(&M->pfull[x][0]);
+                    tmem_ld32f(s_tm + 96, v);
+                    tmem_wait_ld();
+                    settle(u);
+                    settle(v);
+                    weights32<FP16>(u, s_tm + 32, sl2, nr, acc0, acc1);
+                    weights32<FP16>(v, s_tm + 48, sl2, nr, acc0, acc1);
+                    tmem_wait_st();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&M->pfull[x][1]);
+                    sum += (acc0.x + acc0.y) + (acc1.x + acc1.y);
                 }
                 if (dead || !__all_sync(0xffffffffu, mbar_wait(&M->ofull[x], no & 1, abort_flag, a.wait_ns))) {
                     dead = true;
@@ -553,7 +653,7 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                 }
                 no++;
                 tc_fence_after();
-                if (!head_part && !goes_on) {
+                if (!head_part && !w.goes_on) {
                     const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
                     uint16_t* dst = a.out + (int64_t)(w.r.tok0 + tk) * a.o_tok + hd * a.o_head;
 #pragma unroll 1
@@ -593,9 +693,8 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                     }
                 }
             }
-            if (!head_part && goes_on) {   // it starts here and goes on
-                const int64_t rest = (int64_t)w.n_chunks - w.c - take;
-                meta_last = (int)(blockIdx.x + (rest + share - 1) / share);
+            if (!head_part && w.goes_on) {   // it starts here and goes on
+                meta_last = (int)(blockIdx.x + (w.rest + share - 1) / share);
                 if (tid == 0) {
                     ChunkMeta* m = P.meta + blockIdx.x;
                     m->last = meta_last;
@@ -607,8 +706,7 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
             }
             head_part = false;
             nv += take;
-            left -= take;
-            if (left > 0) w.next(P);
+            w.next(P);
         }
         if (tid == 0 && meta_last < 0) P.meta[blockIdx.x].last = -1;
         if (dead) {
@@ -623,29 +721,35 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
             int32_t pflag = 0;
             int st = 0, ph = 1, issued = 0;
             bool dead = *abort_flag != 0;
-            while (left > 0 && !dead) {
+            while (w.left > 0 && !dead) {
                 const int wlo = a.window ? w.r.len - w.r.n - a.window + 1 : 0;
                 const int32_t* row = a.table + (int64_t)w.i * a.max_pages;
-                const int take = w.n_chunks - w.c < left ? w.n_chunks - w.c : left;
-                auto place = [&](int kc, int* z, int* y) {
-                    *z = 2 * a.n_pages;                  // past the pool: the copy fills with zeros
-                    *y = 0;
-                    const int t = w.t.id(w.c + kc) * kKT + lane * P.box_rows;
-                    if (lane < n_box && t < w.r.len && (t + P.box_rows > wlo || t < a.sinks)) {
-                        const int pg = __ldg(row + (t >> a.page_log2));
-                        if (pg >= 0 && pg < a.n_pages) {
-                            *z = pg;
-                            *y = w.h * a.page + (t & (a.page - 1));
-                        } else {
-                            pflag |= CG_FLAG_PAGED_RANGE;
-                        }
+                const int take = w.take;
+                // the places of a group of tiles are looked up at once, lane = tile * n_box + box,
+                // one group ahead of its use
+                const int group = 32 / n_box, mine = lane / n_box, mybox = lane - mine * n_box;
+                auto look = [&](int kc0) {               // page of the lane's box, or -1: zeros
+                    const int kc = kc0 + mine;
+                    if (mine >= group || kc >= take) return -1;
+                    const int t = w.t.id(w.c + kc) * kKT + mybox * P.box_rows;
+                    if (!(t < w.r.len && (t + P.box_rows > wlo || t < a.sinks))) return -1;
+                    const int pg = __ldg(row + (t >> a.page_log2));
+                    if (pg < 0 || pg >= a.n_pages) {
+                        pflag |= CG_FLAG_PAGED_RANGE;
+                        return -1;
                     }
+                    return pg;
                 };
-                int z, y;
-                place(0, &z, &y);
+                int now = look(0), ahead = 0;
                 for (int kc = 0; kc < take && !dead; kc++) {
-                    int zn = 0, yn = 0;
-                    if (kc + 1 < take) place(kc + 1, &zn, &yn);   // the next tile's pages, ahead of the waits
+                    const int in = kc % group;
+                    if (in == 0) {
+                        if (kc) now = ahead;
+                        ahead = look(kc + group);
+                    }
+                    const int pg = __shfl_sync(0xffffffffu, now, (in * n_box + lane) & 31);
+                    const int t = w.t.id(w.c + kc) * kKT + lane * P.box_rows;
+                    const int z = pg < 0 ? 2 * a.n_pages : pg, y = pg < 0 ? 0 : w.h * a.page + (t & (a.page - 1));
 #pragma unroll
                     for (int kv = 0; kv < 2; kv++) {
                         if (!__all_sync(0xffffffffu, mbar_wait(&M->empty[st], ph, abort_flag, a.wait_ns))) {
@@ -656,7 +760,7 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                         __syncwarp();
                         if (lane < n_box) {
                             unsigned char* dst = smem + L::stages + st * L::kStage + lane * P.box_rows * 128;
-                            const int zz = kv && z < a.n_pages ? z + a.n_pages : z;
+                            const int zz = kv && pg >= 0 ? z + a.n_pages : z;
 #pragma unroll
                             for (int hf = 0; hf < D / 64; hf++) tma_load_3d(dst + hf * L::kPiece, &map, &M->full[st], hf * 64, y, zz);
                         }
@@ -666,11 +770,8 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                             ph ^= 1;
                         }
                     }
-                    z = zn;
-                    y = yn;
                 }
-                left -= take;
-                if (left > 0) w.next(P);
+                w.next(P);
             }
             raise_flag(a.status, pflag);
             if (dead) {   // copies in flight land before the CTA ends
@@ -681,128 +782,126 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
             }
         } else if (warp == 9) {
             // -------------------------------------------------------- MMA issuer
-            if (lane == 0) {
-                constexpr uint32_t idesc_s = idesc16<FP16>(128, kKT);
-                constexpr uint32_t idesc_o = idesc16<FP16>(128, D) | kIdescBMnMajor;
-                const uint64_t qd[2] = {sdesc_sw128(smem_u32(smem + L::q)), sdesc_sw128(smem_u32(smem + L::q + L::kQ))};
-                const uint64_t kd = sdesc_sw128(smem_u32(smem + L::stages));
-                const uint64_t vd = sdesc_sw128_mn(smem_u32(smem + L::stages), L::kPiece, 1024u);
-                int st = 0, ph = 0;                // ring position of the next tile to wait for
-                int np[2] = {0, 0}, nq[2] = {0, 0}, nv = 0;
-                bool dead = *abort_flag != 0;
-                while (left > 0 && !dead) {
-                    const Span sp[2] = {span_of(a, w.r, w.m * kTileRows, kHalfRows),
-                                        span_of(a, w.r, w.m * kTileRows + kHalfRows, kHalfRows)};
-                    const int take = w.n_chunks - w.c < left ? w.n_chunks - w.c : left;
-                    bool first[2] = {true, true}, have_q[2] = {false, false};
-                    int vst = 0, vph = 0, t_prev = 0;
-                    for (int j = 0; j <= take && !dead; j++) {
-                        // keys of step j at ring slot kst; values of step j - 1 at vst
-                        const int t0 = j < take ? w.t.id(w.c + j) * kKT : 0;
-                        const int kst = st, kph = ph;
-                        bool k_ok = false;
-                        if (j > 0) {   // landed, and inspected
-                            const int v = nv + j - 1;
-                            if (!mbar_wait(&M->full[vst], vph, abort_flag, a.wait_ns) ||
-                                !mbar_wait(&M->vok[v & 3], (v >> 2) & 1, abort_flag, a.wait_ns)) {
-                                dead = true;
-                                break;
+            // The whole warp walks and waits, so that descriptors stay in uniform registers; one
+            // thread issues.
+            const bool issue = elect_one();
+            const uint32_t idesc_s = idesc16<FP16>(128, kKT) | (a.scale < 0.0f ? kIdescNegateA : 0u);
+            constexpr uint32_t idesc_o = idesc16<FP16>(128, D) | kIdescBMnMajor;
+            const uint64_t qd = sdesc_sw128(smem_u32(smem + L::q)), kd = sdesc_sw128(smem_u32(smem + L::stages));
+            const uint64_t vd = sdesc_sw128_mn(smem_u32(smem + L::stages), L::kPiece, 1024u);
+            const uint32_t q_lo = (uint32_t)qd, k_lo = (uint32_t)kd, hi = (uint32_t)(kd >> 32);
+            const uint32_t v_lo = (uint32_t)vd, v_hi = (uint32_t)(vd >> 32);
+            int st = 0, ph = 0;                // ring position of the next tile to wait for
+            int np[2] = {0, 0}, nq[2] = {0, 0}, nv = 0;
+            bool dead = *abort_flag != 0;
+            auto wait = [&](uint64_t* bar, int parity) {
+                if (!__all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, a.wait_ns))) dead = true;
+                return !dead;
+            };
+            while (w.left > 0 && !dead) {
+                const Span sp[2] = {span_of(a, w.r, w.m * kTileRows, kHalfRows),
+                                    span_of(a, w.r, w.m * kTileRows + kHalfRows, kHalfRows)};
+                const int take = w.take;
+                bool first[2] = {true, true}, have_q[2] = {false, false}, prev[2] = {false, false};
+                int vst = 0, vph = 0;
+                for (int j = 0; j <= take; j++) {
+                    // keys of step j at ring slot kst; values of step j - 1 at vst
+                    const int id = j < take ? w.t.id(w.c + j) : 0;
+                    const int kst = st, kph = ph;
+                    if (j > 0) {   // landed, and inspected
+                        const int v = nv + j - 1;
+                        if (!wait(&M->full[vst], vph) || !wait(&M->vok[v & 3], (v >> 2) & 1)) break;
+                    }
+#pragma unroll
+                    for (int x = 0; x < 2; x++) {
+                        if (prev[x]) {
+                            if (!wait(&M->pfull[x][0], np[x] & 1)) break;
+                            tc_fence_after();
+                            uint32_t acc = first[x] ? 0u : 1u;
+                            if (first[x] && *(volatile int*)&M->accum0[x]) {
+                                acc = 1u;
+                                __syncwarp();
+                                *(volatile int*)&M->accum0[x] = 0;
+                            }
+                            first[x] = false;
+                            const uint32_t bl = v_lo + ((vst * L::kStage) >> 4);
+                            if (issue) {
+#pragma unroll
+                                for (int k = 0; k < kKT / 32; k++)
+                                    mma_ts(kO + x * D, kS + x * 128 + 8 * k, bl + ((k * 2048) >> 4), v_hi, idesc_o, k ? 1u : acc);
+                            }
+                            if (!wait(&M->pfull[x][1], np[x] & 1)) break;
+                            tc_fence_after();
+                            np[x]++;
+                            if (issue) {
+#pragma unroll
+                                for (int k = kKT / 32; k < kKT / 16; k++)
+                                    mma_ts(kO + x * D, kS + x * 128 + 8 * k, bl + ((k * 2048) >> 4), v_hi, idesc_o, 1u);
                             }
                         }
-#pragma unroll
-                        for (int x = 0; x < 2; x++) {
-                            if (j > 0 && sp[x].sees(a, t_prev)) {
-                                if (!mbar_wait(&M->pfull[x], np[x] & 1, abort_flag, a.wait_ns)) {
-                                    dead = true;
-                                    break;
-                                }
-                                np[x]++;
-                                tc_fence_after();
-                                uint32_t acc = first[x] ? 0u : 1u;
-                                if (first[x] && *(volatile int*)&M->accum0[x]) {
-                                    acc = 1u;
-                                    *(volatile int*)&M->accum0[x] = 0;
-                                }
-                                first[x] = false;
-                                const uint64_t bd = vd + (uint64_t)((vst * L::kStage) >> 4);
-#pragma unroll
-                                for (int k = 0; k < kKT / 16; k++) {
-                                    mma_ts(kO + x * D, kS + x * 128 + 8 * k, bd + (uint64_t)(k * 2048 >> 4), idesc_o, acc);
-                                    acc = 1u;
-                                }
+                        prev[x] = j < take && sp[x].sees(id);
+                        if (prev[x]) {
+                            if (!have_q[x]) {
+                                if (!wait(&M->qfull[x], nq[x] & 1)) break;
+                                have_q[x] = true;
                             }
-                            if (j < take && sp[x].sees(a, t0)) {
-                                if (!have_q[x]) {
-                                    if (!mbar_wait(&M->qfull[x], nq[x] & 1, abort_flag, a.wait_ns)) {
-                                        dead = true;
-                                        break;
-                                    }
-                                    have_q[x] = true;
-                                }
-                                if (!k_ok) {
-                                    if (!mbar_wait(&M->full[kst], kph, abort_flag, a.wait_ns)) {
-                                        dead = true;
-                                        break;
-                                    }
-                                    k_ok = true;
-                                    tc_fence_after();
-                                }
-                                const uint64_t bd = kd + (uint64_t)((kst * L::kStage) >> 4);
+                            if (!wait(&M->full[kst], kph)) break;
+                            tc_fence_after();
+                            const uint32_t al = q_lo + ((x * L::kQ) >> 4), bl = k_lo + ((kst * L::kStage) >> 4);
+                            if (issue) {
 #pragma unroll
                                 for (int k = 0; k < D / 16; k++) {
-                                    const uint64_t o = (uint64_t)(((k >> 2) * L::kPiece + (k & 3) * 32) >> 4);
-                                    mma_bf16(kS + x * 128, qd[x] + o, bd + o, idesc_s, k > 0);
+                                    const uint32_t o = ((k >> 2) * L::kPiece + (k & 3) * 32) >> 4;
+                                    mma_ss(kS + x * 128, al + o, bl + o, hi, idesc_s, k ? 1u : 0u);
                                 }
                                 mma_commit(&M->sfull[x]);
                             }
                         }
-                        if (dead) break;
-                        if (j > 0) mma_commit(&M->empty[vst]);
-                        if (j < take) {
-                            if (!k_ok && !mbar_wait(&M->full[kst], kph, abort_flag, a.wait_ns)) {
-                                dead = true;
-                                break;
-                            }
-                            mma_commit(&M->empty[kst]);
-                            if (++st == L::kStages) {
-                                st = 0;
-                                ph ^= 1;
-                            }
-                            vst = st;   // the values follow the keys
-                            vph = ph;
-                            if (++st == L::kStages) {
-                                st = 0;
-                                ph ^= 1;
-                            }
-                        }
-                        t_prev = t0;
                     }
                     if (dead) break;
+                    if (j == take - 1) {   // the queries were read
 #pragma unroll
-                    for (int x = 0; x < 2; x++)
-                        if (sp[x].n > 0) {
-                            // a half whose rows see nothing of this share still takes its queries' turn
-                            if (!have_q[x] && !mbar_wait(&M->qfull[x], nq[x] & 1, abort_flag, a.wait_ns)) dead = true;
-                            nq[x]++;
-                            mma_commit(&M->qempty[x]);
-                            mma_commit(&M->ofull[x]);
+                        for (int x = 0; x < 2; x++)
+                            if (sp[x].n > 0) {
+                                if (!have_q[x] && !wait(&M->qfull[x], nq[x] & 1)) break;
+                                nq[x]++;
+                                if (issue) mma_commit(&M->qempty[x]);
+                            }
+                        if (dead) break;
+                    }
+                    if (j > 0 && issue) mma_commit(&M->empty[vst]);
+                    if (j < take) {
+                        if (!wait(&M->full[kst], kph)) break;
+                        if (issue) mma_commit(&M->empty[kst]);
+                        if (++st == L::kStages) {
+                            st = 0;
+                            ph ^= 1;
                         }
-                    nv += take;
-                    left -= take;
-                    if (left > 0) w.next(P);
+                        vst = st;   // the values follow the keys
+                        vph = ph;
+                        if (++st == L::kStages) {
+                            st = 0;
+                            ph ^= 1;
+                        }
+                    }
                 }
-                if (dead) *abort_flag = 1;
-                mma_commit(&M->drain);   // products in flight end before tensor memory is given back
-                const int zero = 0;
-                mbar_wait(&M->drain, 0, &zero, tc::kWaitLimitNs);
+                if (dead) break;
+#pragma unroll
+                for (int x = 0; x < 2; x++)
+                    if (sp[x].n > 0 && issue) mma_commit(&M->ofull[x]);
+                nv += take;
+                w.next(P);
             }
+            if (dead) *abort_flag = 1;
+            if (issue) mma_commit(&M->drain);   // products in flight end before tensor memory is given back
+            const int zero = 0;
+            mbar_wait(&M->drain, 0, &zero, tc::kWaitLimitNs);
             __syncwarp();
         } else if (warp == 10) {
             // -------------------------------------------------------- queries
             int nq[2] = {0, 0};
-            bool dead = *abort_flag != 0;
-            while (left > 0 && !dead) {
-                const int take = w.n_chunks - w.c < left ? w.n_chunks - w.c : left;
+            bool dead = *abort_flag != 0, q_bytes = false;
+            while (w.left > 0 && !dead) {
                 for (int x = 0; x < 2 && !dead; x++) {
                     const int row0 = w.m * kTileRows + x * kHalfRows;
                     const Span sp = span_of(a, w.r, row0, kHalfRows);
@@ -811,32 +910,54 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                         dead = true;
                         break;
                     }
-                    constexpr int kPer = D / 8;            // 16-byte pieces of a row
-                    const uint32_t base = smem_u32(smem + L::q + x * L::kQ);
+                    nq[x]++;
+                    unsigned char* dst0 = smem + L::q + x * L::kQ;
+                    if (P.q_boxes) {   // 128 / n_rep tokens x n_rep heads: whole boxes
+                        if (lane == 0) {
+                            mbar_arrive_expect_tx(&M->qfull[x], L::kQ);
+#pragma unroll
+                            for (int hf = 0; hf < D / 64; hf++)
+                                tma_load_4d(dst0 + hf * L::kPiece, &qmap, &M->qfull[x], hf * 64, 0, w.h, w.r.tok0 + row0 / a.n_rep);
+                        }
+                        q_bytes = true;
+                        continue;
+                    }
+                    constexpr int kPer = D / 8, kStep = 32 / kPer;   // 16-byte pieces of a row, rows at a time
+                    const uint32_t base = smem_u32(dst0);
                     const int ch = lane % kPer;
-                    for (int r = lane / kPer; r < sp.n; r += 32 / kPer) {
-                        const int tk = (row0 + r) / a.n_rep, hd = w.h * a.n_rep + (row0 + r - tk * a.n_rep);
-                        const uint16_t* src = a.q + (int64_t)(w.r.tok0 + tk) * a.q_tok + hd * a.q_head + ch * 8;
-                        const uint32_t dst = base + (ch >> 3) * L::kPiece + r * 128 + (((ch & 7) ^ (r & 7)) << 4);
-                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+                    int r = lane / kPer, tk = (row0 + r) / a.n_rep, rep = row0 + r - tk * a.n_rep;
+                    const uint16_t* src = a.q + (int64_t)(w.r.tok0 + tk) * a.q_tok + (int64_t)w.h * a.n_rep * a.q_head + ch * 8;
+                    const uint32_t col = base + (ch >> 3) * L::kPiece;
+                    for (; r < sp.n; r += kStep) {
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(col + r * 128 + (((ch & 7) ^ (r & 7)) << 4)),
+                                     "l"(src + rep * a.q_head)
+                                     : "memory");
+                        rep += kStep;
+                        while (rep >= a.n_rep) {
+                            rep -= a.n_rep;
+                            src += a.q_tok;
+                        }
                     }
                     asm volatile("cp.async.wait_all;" ::: "memory");
                     fence_proxy_async_smem();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&M->qfull[x]);
-                    nq[x]++;
                 }
-                left -= take;
-                if (left > 0) w.next(P);
+                w.next(P);
             }
             if (dead) *abort_flag = 1;
+            if (q_bytes && *abort_flag) {   // boxes in flight land before the CTA ends
+                const int zero = 0;
+                for (int x = 0; x < 2; x++)
+                    if (nq[x]) mbar_wait(&M->qfull[x], (nq[x] - 1) & 1, &zero, tc::kWaitLimitNs);
+            }
         } else {
             // -------------------------------------------------------- inspector of values
             int st = 0, ph = 0, nv = 0;
             bool dead = *abort_flag != 0;
-            while (left > 0 && !dead) {
+            while (w.left > 0 && !dead) {
                 const Span item = span_of(a, w.r, w.m * kTileRows, kTileRows);
-                const int take = w.n_chunks - w.c < left ? w.n_chunks - w.c : left;
+                const int take = w.take;
                 for (int kc = 0; kc < take; kc++, nv++) {
                     if (++st == L::kStages) {   // past the keys
                         st = 0;
@@ -846,9 +967,9 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                         dead = true;
                         break;
                     }
-                    const int t0 = w.t.id(w.c + kc) * kKT;
+                    const int id = w.t.id(w.c + kc), t0 = id * kKT;
                     int found = 0;
-                    if (!item.sees_all(a, t0)) {
+                    if (!item.sees_all(id)) {
                         unsigned char* tile = smem + L::stages + st * L::kStage;
                         constexpr int kPer = D / 8;
                         const int ch = lane % kPer;
@@ -879,8 +1000,7 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                         ph ^= 1;
                     }
                 }
-                left -= take;
-                if (left > 0) w.next(P);
+                w.next(P);
             }
             if (dead) *abort_flag = 1;
         }
@@ -938,15 +1058,32 @@ __global__ void __launch_bounds__(kTileRows) paged_chunk_merge_kernel(const __gr
         a.lse[(int64_t)(m.tok0 + tk) * a.H * a.n_rep + hd] = inv == 0.0f ? -INFINITY : (R + log2f(l)) * kLn2;
 }
 
+// Queries as [n_tok][H][n_rep][d] (their strides), boxes of 128 / n_rep tokens x n_rep heads x 64
+// channels: 128 rows in the order of a half. For head groups that divide 128 and strides that a
+// tensor map can hold; other queries are gathered by a warp.
+bool query_map(CUtensorMap* map, const PagedArgs& a) {
+    auto fn = tmap_encode_fn();
+    const int64_t most = (int64_t)1 << 39;
+    if (!fn || kHalfRows % a.n_rep || a.q_head <= 0 || a.q_tok <= 0 || a.q_head * a.n_rep * 2 >= most || a.q_tok * 2 >= most) return false;
+    cuuint64_t dims[4] = {(cuuint64_t)a.d, (cuuint64_t)a.n_rep, (cuuint64_t)a.H, (cuuint64_t)a.n_tok};
+    cuuint64_t strides[3] = {(cuuint64_t)a.q_head * 2, (cuuint64_t)a.q_head * a.n_rep * 2, (cuuint64_t)a.q_tok * 2};
+    cuuint32_t box[4] = {64, (cuuint32_t)a.n_rep, 1, (cuuint32_t)(kHalfRows / a.n_rep)}, estr[4] = {1, 1, 1, 1};
+    return fn(map, a.dtype == CG_FP16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4,
+              const_cast<uint16_t*>(a.q), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <bool FP16, int D>
-cudaError_t launch_chunk(const ChunkParams& P, cudaStream_t st) {
-    CUtensorMap map;
+cudaError_t launch_chunk(ChunkParams P, cudaStream_t st) {
+    CUtensorMap map, qmap{};
     if (!paged_pool_map(&map, P.a, P.box_rows)) return cudaErrorInvalidValue;
+    P.q_boxes = query_map(&qmap, P.a);
     constexpr size_t smem = ChunkSmem<D>::total;
     cudaError_t e = cudaFuncSetAttribute(paged_chunk_kernel<FP16, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
     const unsigned grid = (unsigned)tc::num_sms();
-    paged_chunk_kernel<FP16, D><<<grid, kChunkThreads, smem, st>>>(P, map);
+    paged_chunk_kernel<FP16, D><<<grid, kChunkThreads, smem, st>>>(P, map, qmap);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(grid, D / 8);
