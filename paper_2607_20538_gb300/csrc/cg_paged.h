@@ -25,6 +25,8 @@ struct PagedArgs {
     float scale;
     int64_t q_tok, q_head, o_tok, o_head;
     uint64_t wait_ns;
+    uint32_t rep_mul;     // x / n_rep = x * rep_mul >> rep_shift for 0 <= x < 2^31
+    int rep_shift;
 };
 
 // Workspace of the paged attention: bytes, and the launch (workspace of that size).

@@ -127,8 +127,8 @@ struct TileSpan {
         row0 = w.row0(P);
         const int rows = w.r.n * P.a.n_rep;
         n_rows = rows - row0 < kRows ? rows - row0 : kRows;
-        p0 = w.r.len - w.r.n + row0 / P.a.n_rep;
-        p1 = w.r.len - w.r.n + (row0 + n_rows - 1) / P.a.n_rep;
+        p0 = w.r.len - w.r.n + token_of(P.a, row0);
+        p1 = w.r.len - w.r.n + token_of(P.a, row0 + n_rows - 1);
     }
     __device__ __forceinline__ bool sees(const PagedArgs& a, int id) const {
         const int t0 = id * kTK;
@@ -292,7 +292,7 @@ paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ 
             for (int hf = 0; hf < 2; hf++) {
                 const int r = sp.row0 + g + 8 * hf;
                 const bool have = g + 8 * hf < sp.n_rows;
-                const int tk = r / a.n_rep, hd = sp.h * a.n_rep + (r - tk * a.n_rep);
+                const int tk = token_of(a, r), hd = sp.h * a.n_rep + (r - tk * a.n_rep);
                 pos[hf] = have ? w.r.len - w.r.n + tk : -1;
                 const uint16_t* src = a.q + (int64_t)(w.r.tok0 + tk) * a.q_tok + hd * a.q_head + 2 * j;
 #pragma unroll
@@ -523,7 +523,7 @@ paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ 
 #pragma unroll
                     for (int hf = 0; hf < 2; hf++) {
                         if (g + 8 * hf >= sp.n_rows) continue;
-                        const int r = sp.row0 + g + 8 * hf, tk = r / a.n_rep, hd = sp.h * a.n_rep + (r - tk * a.n_rep);
+                        const int r = sp.row0 + g + 8 * hf, tk = token_of(a, r), hd = sp.h * a.n_rep + (r - tk * a.n_rep);
                         const float inv = sum[hf] > 0.0f || sum[hf] != sum[hf] ? 1.0f / sum[hf] : 0.0f;
                         uint16_t* dst = a.out + (int64_t)(w.r.tok0 + tk) * a.o_tok + hd * a.o_head + 2 * j;
 #pragma unroll
@@ -615,7 +615,7 @@ __global__ void __launch_bounds__(kMergeWarps * 32) paged_merge_kernel(const __g
     for (int k = 0; k < D / 32; k++) acc[warp][lane + 32 * k] = o[k];
     __syncthreads();
     if (row < m.n_rows && sub == 0) {
-        const int r = m.row0 + row, tk = r / a.n_rep, hd = m.h * a.n_rep + (r - tk * a.n_rep);
+        const int r = m.row0 + row, tk = token_of(a, r), hd = m.h * a.n_rep + (r - tk * a.n_rep);
         const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
         uint16_t* dst = a.out + (int64_t)(m.tok0 + tk) * a.o_tok + hd * a.o_head;
 #pragma unroll
@@ -742,6 +742,10 @@ int check_attn(const cg_pages* p, const cg_paged_attn* h, PagedArgs* a) {
     a->max_pages = p->max_pages;
     a->n_tok = h->n_tok;
     a->n_rep = h->n_rep;
+    int up = 0;
+    while ((1 << up) < h->n_rep) up++;
+    a->rep_shift = 31 + up;
+    a->rep_mul = (uint32_t)((((uint64_t)1 << a->rep_shift) + h->n_rep - 1) / h->n_rep);
     a->max_new = h->max_new;
     // a window as long as the longest request cuts nothing
     const bool cuts = h->window > 0 && h->window < (int64_t)p->max_pages * p->page;

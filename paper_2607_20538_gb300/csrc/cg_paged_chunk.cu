@@ -6,14 +6,17 @@
 //   warps 0-3, 4-7  softmax of half A, half B: a thread owns a row: 128 scores from tensor memory,
 //                   running reference and sum in registers, weights back to tensor memory;
 //   warp 8          TMA: 128-token tiles of keys and values, K0 V0 K1 V1 ..., boxes of pages;
-//   warp 9          one thread issues tcgen05.mma: S = Q K^T (both operands in shared memory) and
-//                   O += P V (P in tensor memory over S, V token-major as it lies in the page);
-//   warp 10         loads the queries of a tile (any strides, any n_rep);
-//   warp 11         inspects the values of tiles that not every row sees whole (below).
-// The MMA order is PV_A(j-1) S_A(j) PV_B(j-1) S_B(j): while one half's softmax runs, the tensor
-// cores work for the other. S_x(j) follows PV_x(j-1) in issue order, so S may overwrite P, and its
-// completion tells the softmax that O_x is quiescent: the thread rescales its row of O itself on the
-// rare steps that raise the reference by more than 2^8.
+//   warps 9, 10     one thread each issues half A's, half B's tcgen05.mma: S = Q K^T (both operands in
+//                   shared memory) and O += P V (P in tensor memory over S, V token-major as it
+//                   lies in the page);
+//   warp 11         loads the queries of a tile (TMA boxes, or gathered: any strides, any n_rep) and
+//                   inspects the values of tiles that not every row sees whole (below).
+// A half's order is PV(j-1) S(j): while its softmax runs, the tensor cores work for the other half.
+// (Both halves from one warp were slower, 0.89 ms against 0.79 ms on 2048 tokens after 32k: its own
+// instructions between the products of the two halves, about 900 cycles a step, kept the tensor cores
+// idle.) S(j) follows PV(j-1) in issue order, so S may overwrite P, and its completion tells the
+// softmax that O is quiescent: the thread rescales its row of O itself on the rare steps that raise
+// the reference by more than 2^8.
 // Bound: the tensor cores (4 x 128 x 128 x d multiply-adds per key tile against 128 x 256
 // exponentials and about four times as many other operations).
 //
@@ -61,12 +64,13 @@ struct ChunkSmem {
 
 struct ChunkMisc {
     uint64_t full[kMaxStages], empty[kMaxStages];
-    uint64_t sfull[2], pfull[2][2], ofull[2], qfull[2], qempty[2], vok[4], drain;
+    uint64_t sfull[2], pfull[2][2], ofull[2], qfull[2], qempty[2], vok[4], drain[2];
     int64_t warp_sum[kChunkThreads / 32];
     int start[4];            // request, head, tile, key tile of the share's beginning
     int special[4];          // the inspected tile held special values
     int accum0[2];           // the half's O was prepared by its softmax before the first product
     int abort_flag;
+    int turn;                // 1 while a half's second products and next scores are being issued
     uint32_t tmem;
 };
 static_assert(sizeof(ChunkMisc) <= 512, "misc block");
@@ -98,8 +102,8 @@ __device__ __forceinline__ Span span_of(const PagedArgs& a, const Request& r, in
     Span s;
     const int rows = r.n * a.n_rep - row0;
     s.n = rows < 0 ? 0 : rows < rows_max ? rows : rows_max;
-    s.p0 = r.len - r.n + row0 / a.n_rep;
-    s.p1 = s.n ? r.len - r.n + (row0 + s.n - 1) / a.n_rep : s.p0 - 1;
+    s.p0 = r.len - r.n + token_of(a, row0);
+    s.p1 = s.n ? r.len - r.n + token_of(a, row0 + s.n - 1) : s.p0 - 1;
     s.s0 = s.ss = s.f0 = s.fs = 0;
     s.s1 = s.n && s.p1 >= 0 ? s.p1 / kKT + 1 : 0;
     s.f1 = s.p0 < 0 ? 0 : (s.p0 + 1) / kKT;
@@ -115,13 +119,13 @@ __device__ __forceinline__ Span span_of(const PagedArgs& a, const Request& r, in
 
 __device__ __forceinline__ Tiles tile_tiles(const PagedArgs& a, const Request& r, int m) {
     const int rows = r.n * a.n_rep - m * kTileRows, n = rows < kTileRows ? rows : kTileRows;
-    return visible_tiles<kKT>(a.window, a.sinks, r.len - r.n + m * kTileRows / a.n_rep,
-                              r.len - r.n + (m * kTileRows + n - 1) / a.n_rep);
+    return visible_tiles<kKT>(a.window, a.sinks, r.len - r.n + token_of(a, m * kTileRows),
+                              r.len - r.n + token_of(a, m * kTileRows + n - 1));
 }
 
 // A work tile costs its key tiles plus kTileCost (queries in, first scores, output out), in units of
 // a key tile. A cut of the line inside those kTileCost units falls before the tile.
-constexpr int kTileCost = 4;
+constexpr int kTileCost = 3;
 
 __device__ __forceinline__ int row_tiles(const ChunkParams& P, const Request& r) {
     const int64_t rows = (int64_t)r.n * P.a.n_rep;
@@ -344,18 +348,17 @@ __device__ __forceinline__ float max32(const float (&s)[32], float m) {
     return fmaxf(m0, m1);
 }
 
-// The row's largest score of a tile (128 columns).
-__device__ __forceinline__ float row_max(uint32_t s_tm) {
-    float u[32], v[32];
-    tmem_ld32f(s_tm, u);
-    tmem_ld32f(s_tm + 32, v);
+// The row's largest score of a tile (128 columns); the first 64 scores stay in u and v.
+__device__ __forceinline__ float row_max(uint32_t s_tm, float (&u)[32], float (&v)[32]) {
+    tmem_ld32f(s_tm + 64, u);
+    tmem_ld32f(s_tm + 96, v);
     tmem_wait_ld();
     settle(u);
     settle(v);
     float m = max32(u, -INFINITY);
-    tmem_ld32f(s_tm + 64, u);
+    tmem_ld32f(s_tm, u);
     m = max32(v, m);
-    tmem_ld32f(s_tm + 96, v);
+    tmem_ld32f(s_tm + 32, v);
     tmem_wait_ld();
     settle(u);
     settle(v);
@@ -363,21 +366,60 @@ __device__ __forceinline__ float row_max(uint32_t s_tm) {
     return max32(v, m);
 }
 
-// Sets the columns that the row does not see to -inf: it sees [lo, hi] and those below sk.
-__device__ __forceinline__ void mask_row(uint32_t s_tm, int lo, int hi, int sk) {
+// A tile that not every row sees whole: the row sees the columns [lo, hi] and those below sk; the
+// others are set to -inf.
+__device__ __noinline__ void mask_row(uint32_t s_tm, int lo, int hi, int sk) {
 #pragma unroll 1
-    for (int c0 = 0; c0 < kKT; c0 += 16) {
-        uint32_t r[16];
-        tmem_ld16(s_tm + c0, r);
+    for (int c0 = 0; c0 < kKT; c0 += 32) {
+        float u[32];
+        tmem_ld32f(s_tm + c0, u);
+        const int h = hi - c0, l = lo - c0, k0 = sk - c0;
+        const bool all = h >= 31 && (l <= 0 || k0 > 31), none_cut = l <= 0;
         tmem_wait_ld();
+        settle(u);
+        if (!__all_sync(0xffffffffu, all)) {
+            if (__all_sync(0xffffffffu, none_cut)) {
 #pragma unroll
-        for (int k = 0; k < 16; k++) {
-            const int c = c0 + k;
-            if (!(c <= hi && (c >= lo || c < sk))) r[k] = 0xff800000u;
+                for (int k = 0; k < 32; k++) u[k] = k <= h ? u[k] : -INFINITY;
+            } else {
+#pragma unroll
+                for (int k = 0; k < 32; k++) u[k] = k <= h && (k >= l || k < k0) ? u[k] : -INFINITY;
+            }
+            uint32_t r[32];
+#pragma unroll
+            for (int k = 0; k < 32; k++) r[k] = __float_as_uint(u[k]);
+            tmem_st32(s_tm + c0, r);
         }
-        tmem_st16(s_tm + c0, r);
     }
     tmem_wait_st();
+}
+
+// Each lane holds 8 pieces of 16 bytes of its row (128 bytes). The 8 lanes of a group transpose them
+// (piece k of lane l to lane k, place l), so that a store instruction covers 4 whole lines instead of
+// a piece of 32. dst: the row's address, or 0 (not written); off: bytes into the row.
+__device__ __forceinline__ void store_rows(uint32_t (&b)[32], uint64_t dst, int off) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int step = 1; step < 8; step *= 2) {
+        const bool up = lane & step;
+#pragma unroll
+        for (int k = 0; k < 8; k++) {
+            if (k & step) continue;
+#pragma unroll
+            for (int e = 0; e < 4; e++) {   // pieces k of the upper lane and k + step of the lower one change places
+                uint32_t &x = b[4 * k + e], &y = b[4 * (k + step) + e];
+                const uint32_t other = __shfl_xor_sync(0xffffffffu, up ? x : y, step);
+                if (up) x = other;
+                else y = other;
+            }
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < 8; k++) {
+        const uint64_t row = __shfl_sync(0xffffffffu, dst, (lane & 24) + k);
+        if (row)
+            *reinterpret_cast<uint4*>(row + off + 16 * (lane & 7)) = make_uint4(b[4 * k], b[4 * k + 1], b[4 * k + 2], b[4 * k + 3]);
+    }
 }
 
 // Weights 2^(s sl2 + neg_ref) of 32 scores in 16 bits, and their sum.
@@ -401,12 +443,12 @@ __host__ __device__ constexpr uint32_t idesc16(int M, int N) {
 }
 constexpr uint32_t kIdescBMnMajor = 1u << 16, kIdescNegateA = 1u << 13;
 
+// Not 0 if a 16-bit value of v is an infinity or NaN (all exponent bits set: adding the lowest of
+// them carries into the sign's place).
 template <bool FP16>
-__device__ __forceinline__ bool any_special(uint4 v) {
-    constexpr uint32_t e = FP16 ? 0x7c00u : 0x7f80u;
-    bool s = false;
-    for (uint32_t w : {v.x, v.y, v.z, v.w}) s |= (w & e) == e || (w & (e << 16)) == (e << 16);
-    return s;
+__device__ __forceinline__ uint32_t special_bits(uint4 v) {
+    constexpr uint32_t e = FP16 ? 0x7c007c00u : 0x7f807f80u, c = FP16 ? 0x04000400u : 0x00800080u;
+    return (((v.x & e) + c) | ((v.y & e) + c) | ((v.z & e) + c) | ((v.w & e) + c)) & 0x80008000u;
 }
 template <bool FP16>
 __device__ __forceinline__ uint32_t drop_special(uint32_t w) {
@@ -451,6 +493,23 @@ __device__ __noinline__ void add_special(const PagedArgs& a, const Request& r, i
     tmem_wait_st();
 }
 
+// Takes the CTA's turn to issue (a bounded wait). Without it the two halves' products interleave
+// when both are ready, both softmaxes then run at the same time, and the halves stay in step: 2900 to
+// 3300 cycles per key tile instead of 2600.
+__device__ __forceinline__ bool take_turn(int* turn, bool issue, const volatile int* abort, uint64_t limit_ns) {
+    bool ok = true;
+    if (issue && atomicCAS(turn, 0, 1) != 0) {
+        const uint64_t t0 = globaltimer_ns();
+        while (atomicCAS(turn, 0, 1) != 0) {
+            if (*abort || globaltimer_ns() - t0 > limit_ns) {
+                ok = false;
+                break;
+            }
+        }
+    }
+    return __all_sync(0xffffffffu, ok);
+}
+
 template <bool FP16, int D>
 __global__ void __launch_bounds__(kChunkThreads, 1)
 paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant__ CUtensorMap map,
@@ -485,7 +544,7 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
     if (tid == 0) {
         for (int s = 0; s < L::kStages; s++) {
             mbar_init(&M->full[s], 1);
-            mbar_init(&M->empty[s], 1);
+            mbar_init(&M->empty[s], 2);
         }
         for (int x = 0; x < 2; x++) {
             mbar_init(&M->sfull[x], 1);
@@ -494,10 +553,11 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
             mbar_init(&M->ofull[x], 1);
             mbar_init(&M->qfull[x], 1);
             mbar_init(&M->qempty[x], 1);
+            mbar_init(&M->drain[x], 1);
             M->accum0[x] = 0;
         }
         for (int s = 0; s < 4; s++) mbar_init(&M->vok[s], 1);
-        mbar_init(&M->drain, 1);
+        M->turn = 0;
         M->abort_flag = (smem_u32(smem) & 1023u) != 0;   // the swizzle needs the alignment asked for
         fence_barrier_init();
         prefetch_tmap(&map);
@@ -577,7 +637,7 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
             if (sp.n > 0) {
                 const int row = (warp & 3) * 32 + lane;
                 const bool have = row < sp.n;
-                const int tk = (row0 + row) / a.n_rep, hd = w.h * a.n_rep + (row0 + row - tk * a.n_rep);
+                const int tk = token_of(a, row0 + row), hd = w.h * a.n_rep + (row0 + row - tk * a.n_rep);
                 const int pos = have ? w.r.len - w.r.n + tk : -1;
                 float ref = -INFINITY, sum = 0.0f;
                 bool started = false;
@@ -592,7 +652,8 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                     tc_fence_after();
                     const int t0 = id * kKT;
                     if (!sp.sees_all(id)) mask_row(s_tm, a.window ? pos - a.window + 1 - t0 : 0, pos - t0, a.sinks - t0);
-                    const float mx = sl2 * row_max(s_tm);
+                    float u[32], v[32];
+                    const float mx = sl2 * row_max(s_tm, u, v);
                     if (__any_sync(0xffffffffu, mx > ref + (kBias + kLazy))) {
                         const float nr = fmaxf(ref, mx - kBias);
                         // never 0 x inf in O: a factor below all numbers becomes the least one
@@ -606,28 +667,22 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                     }
                     if (!item.sees_all(id)) {
                         // the inspected value tile held special values: add those the row sees
-                        const int v = nv + kc;
-                        if (!__all_sync(0xffffffffu, mbar_wait(&M->vok[v & 3], (v >> 2) & 1, abort_flag, a.wait_ns))) {
+                        const int nth = nv + kc;
+                        if (!__all_sync(0xffffffffu, mbar_wait(&M->vok[nth & 3], (nth >> 2) & 1, abort_flag, a.wait_ns))) {
                             dead = true;
                             break;
                         }
-                        if (*(volatile int*)&M->special[v & 3]) {
+                        if (*(volatile int*)&M->special[nth & 3]) {
                             add_special<FP16, D>(a, w.r, w.i, w.h, item, t0, pos, o_tm, !started);
                             if (!started && lane == 0) *(volatile int*)&M->accum0[x] = 1;
                         }
                     }
                     started = true;
-                    // The scores are read again: 128 of them kept in registers would not leave room
-                    // for the rest, and each group of weights lies over scores already read. The
-                    // product starts on the first half of the weights.
+                    // The last 64 scores are read again: 128 of them kept in registers would not leave
+                    // room for the rest, and each group of weights lies over scores already read.
+                    // The product starts on the first half of the weights.
                     const float nr = ref == -INFINITY ? 0.0f : -ref;
                     float2 acc0 = make_float2(0.0f, 0.0f), acc1 = acc0;
-                    float u[32], v[32];
-                    tmem_ld32f(s_tm, u);
-                    tmem_ld32f(s_tm + 32, v);
-                    tmem_wait_ld();
-                    settle(u);
-                    settle(v);
                     weights32<FP16>(u, s_tm, sl2, nr, acc0, acc1);
                     tmem_ld32f(s_tm + 64, u);
                     weights32<FP16>(v, s_tm + 16, sl2, nr, acc0, acc1);
@@ -656,19 +711,21 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                 if (!head_part && !w.goes_on) {
                     const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
                     uint16_t* dst = a.out + (int64_t)(w.r.tok0 + tk) * a.o_tok + hd * a.o_head;
+                    const uint64_t my_dst = have ? reinterpret_cast<uint64_t>(dst) : 0;
 #pragma unroll 1
-                    for (int c0 = 0; c0 < D; c0 += 32) {
-                        uint32_t o[32], b[16];
-                        tmem_ld32p(o_tm + c0, o);
-                        tmem_wait_ld();
+                    for (int c0 = 0; c0 < D; c0 += 64) {
+                        uint32_t b[32];
 #pragma unroll
-                        for (int k = 0; k < 16; k++)
-                            b[k] = started && inv != 0.0f ? pack2<FP16>(__uint_as_float(o[2 * k]) * inv, __uint_as_float(o[2 * k + 1]) * inv) : 0u;
-                        if (have) {
+                        for (int q = 0; q < 2; q++) {
+                            float o[32];
+                            tmem_ld32f(o_tm + c0 + 32 * q, o);
+                            tmem_wait_ld();
+                            settle(o);
 #pragma unroll
-                            for (int k = 0; k < 4; k++)
-                                *reinterpret_cast<uint4*>(dst + c0 + 8 * k) = make_uint4(b[4 * k], b[4 * k + 1], b[4 * k + 2], b[4 * k + 3]);
+                            for (int k = 0; k < 16; k++)
+                                b[16 * q + k] = started && inv != 0.0f ? pack2<FP16>(o[2 * k] * inv, o[2 * k + 1] * inv) : 0u;
                         }
+                        store_rows(b, my_dst, 2 * c0);
                     }
                     if (a.lse && have)
                         a.lse[(int64_t)(w.r.tok0 + tk) * a.H * a.n_rep + hd] = inv == 0.0f ? -INFINITY : (ref + log2f(sum)) * kLn2;
@@ -780,99 +837,89 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                 for (int k = issued > L::kStages ? issued - L::kStages : 0; k < issued; k++)
                     mbar_wait(&M->full[k % L::kStages], (k / L::kStages) & 1, &zero, tc::kWaitLimitNs);
             }
-        } else if (warp == 9) {
-            // -------------------------------------------------------- MMA issuer
+        } else if (warp < 11) {
+            // -------------------------------------------------------- MMA issuer of one half
             // The whole warp walks and waits, so that descriptors stay in uniform registers; one
-            // thread issues.
+            // thread issues. Everything a step needs is waited for ahead of the weights.
+            const int x = warp - 9;
             const bool issue = elect_one();
             const uint32_t idesc_s = idesc16<FP16>(128, kKT) | (a.scale < 0.0f ? kIdescNegateA : 0u);
             constexpr uint32_t idesc_o = idesc16<FP16>(128, D) | kIdescBMnMajor;
             const uint64_t qd = sdesc_sw128(smem_u32(smem + L::q)), kd = sdesc_sw128(smem_u32(smem + L::stages));
             const uint64_t vd = sdesc_sw128_mn(smem_u32(smem + L::stages), L::kPiece, 1024u);
-            const uint32_t q_lo = (uint32_t)qd, k_lo = (uint32_t)kd, hi = (uint32_t)(kd >> 32);
+            const uint32_t al = (uint32_t)qd + ((x * L::kQ) >> 4), k_lo = (uint32_t)kd, hi = (uint32_t)(kd >> 32);
             const uint32_t v_lo = (uint32_t)vd, v_hi = (uint32_t)(vd >> 32);
+            const uint32_t sx = kS + x * 128, ox = kO + x * D;
             int st = 0, ph = 0;                // ring position of the next tile to wait for
-            int np[2] = {0, 0}, nq[2] = {0, 0}, nv = 0;
+            int np = 0, nq = 0, nv = 0;
             bool dead = *abort_flag != 0;
             auto wait = [&](uint64_t* bar, int parity) {
                 if (!__all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, a.wait_ns))) dead = true;
                 return !dead;
             };
             while (w.left > 0 && !dead) {
-                const Span sp[2] = {span_of(a, w.r, w.m * kTileRows, kHalfRows),
-                                    span_of(a, w.r, w.m * kTileRows + kHalfRows, kHalfRows)};
+                const Span sp = span_of(a, w.r, w.m * kTileRows + x * kHalfRows, kHalfRows);
                 const int take = w.take;
-                bool first[2] = {true, true}, have_q[2] = {false, false}, prev[2] = {false, false};
+                bool first = true, prev = false;
                 int vst = 0, vph = 0;
+                if (sp.n > 0 && !wait(&M->qfull[x], nq & 1)) break;
                 for (int j = 0; j <= take; j++) {
                     // keys of step j at ring slot kst; values of step j - 1 at vst
                     const int id = j < take ? w.t.id(w.c + j) : 0;
-                    const int kst = st, kph = ph;
+                    const int kst = st;
+                    const bool next = j < take && sp.sees(id);
                     if (j > 0) {   // landed, and inspected
                         const int v = nv + j - 1;
                         if (!wait(&M->full[vst], vph) || !wait(&M->vok[v & 3], (v >> 2) & 1)) break;
                     }
-#pragma unroll
-                    for (int x = 0; x < 2; x++) {
-                        if (prev[x]) {
-                            if (!wait(&M->pfull[x][0], np[x] & 1)) break;
-                            tc_fence_after();
-                            uint32_t acc = first[x] ? 0u : 1u;
-                            if (first[x] && *(volatile int*)&M->accum0[x]) {
-                                acc = 1u;
-                                __syncwarp();
-                                *(volatile int*)&M->accum0[x] = 0;
-                            }
-                            first[x] = false;
-                            const uint32_t bl = v_lo + ((vst * L::kStage) >> 4);
-                            if (issue) {
-#pragma unroll
-                                for (int k = 0; k < kKT / 32; k++)
-                                    mma_ts(kO + x * D, kS + x * 128 + 8 * k, bl + ((k * 2048) >> 4), v_hi, idesc_o, k ? 1u : acc);
-                            }
-                            if (!wait(&M->pfull[x][1], np[x] & 1)) break;
-                            tc_fence_after();
-                            np[x]++;
-                            if (issue) {
-#pragma unroll
-                                for (int k = kKT / 32; k < kKT / 16; k++)
-                                    mma_ts(kO + x * D, kS + x * 128 + 8 * k, bl + ((k * 2048) >> 4), v_hi, idesc_o, 1u);
-                            }
+                    if (j < take && !wait(&M->full[kst], ph)) break;
+                    const uint32_t bv = v_lo + ((vst * L::kStage) >> 4), bk = k_lo + ((kst * L::kStage) >> 4);
+                    uint32_t acc = first ? 0u : 1u;
+                    if (prev) {
+                        if (!wait(&M->pfull[x][0], np & 1)) break;
+                        tc_fence_after();
+                        if (first && *(volatile int*)&M->accum0[x]) {
+                            acc = 1u;
+                            __syncwarp();
+                            *(volatile int*)&M->accum0[x] = 0;
                         }
-                        prev[x] = j < take && sp[x].sees(id);
-                        if (prev[x]) {
-                            if (!have_q[x]) {
-                                if (!wait(&M->qfull[x], nq[x] & 1)) break;
-                                have_q[x] = true;
-                            }
-                            if (!wait(&M->full[kst], kph)) break;
-                            tc_fence_after();
-                            const uint32_t al = q_lo + ((x * L::kQ) >> 4), bl = k_lo + ((kst * L::kStage) >> 4);
-                            if (issue) {
+                        first = false;
+                        if (issue) {
 #pragma unroll
-                                for (int k = 0; k < D / 16; k++) {
-                                    const uint32_t o = ((k >> 2) * L::kPiece + (k & 3) * 32) >> 4;
-                                    mma_ss(kS + x * 128, al + o, bl + o, hi, idesc_s, k ? 1u : 0u);
-                                }
-                                mma_commit(&M->sfull[x]);
-                            }
+                            for (int k = 0; k < kKT / 32; k++)
+                                mma_ts(ox, sx + 8 * k, bv + ((k * 2048) >> 4), v_hi, idesc_o, k ? 1u : acc);
                         }
+                        if (!take_turn(&M->turn, issue, abort_flag, a.wait_ns)) {
+                            dead = true;
+                            break;
+                        }
+                        if (!wait(&M->pfull[x][1], np & 1)) break;
+                        np++;
                     }
-                    if (dead) break;
-                    if (j == take - 1) {   // the queries were read
+                    tc_fence_after();
+                    if (issue) {
+                        if (prev) {
 #pragma unroll
-                        for (int x = 0; x < 2; x++)
-                            if (sp[x].n > 0) {
-                                if (!have_q[x] && !wait(&M->qfull[x], nq[x] & 1)) break;
-                                nq[x]++;
-                                if (issue) mma_commit(&M->qempty[x]);
+                            for (int k = kKT / 32; k < kKT / 16; k++)
+                                mma_ts(ox, sx + 8 * k, bv + ((k * 2048) >> 4), v_hi, idesc_o, 1u);
+                        }
+                        if (next) {
+#pragma unroll
+                            for (int k = 0; k < D / 16; k++) {
+                                const uint32_t o = ((k >> 2) * L::kPiece + (k & 3) * 32) >> 4;
+                                mma_ss(sx, al + o, bk + o, hi, idesc_s, k ? 1u : 0u);
                             }
-                        if (dead) break;
+                            mma_commit(&M->sfull[x]);
+                        }
+                        if (prev) *(volatile int*)&M->turn = 0;
+                        if (j == take - 1 && sp.n > 0) mma_commit(&M->qempty[x]);   // the queries were read
+                        if (j > 0) mma_commit(&M->empty[vst]);
+                        if (j < take) mma_commit(&M->empty[kst]);
+                        if (j == take && sp.n > 0) mma_commit(&M->ofull[x]);
                     }
-                    if (j > 0 && issue) mma_commit(&M->empty[vst]);
+                    __syncwarp();
+                    prev = next;
                     if (j < take) {
-                        if (!wait(&M->full[kst], kph)) break;
-                        if (issue) mma_commit(&M->empty[kst]);
                         if (++st == L::kStages) {
                             st = 0;
                             ph ^= 1;
@@ -886,22 +933,23 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                     }
                 }
                 if (dead) break;
-#pragma unroll
-                for (int x = 0; x < 2; x++)
-                    if (sp[x].n > 0 && issue) mma_commit(&M->ofull[x]);
+                if (sp.n > 0) nq++;
                 nv += take;
                 w.next(P);
             }
             if (dead) *abort_flag = 1;
-            if (issue) mma_commit(&M->drain);   // products in flight end before tensor memory is given back
+            if (issue) mma_commit(&M->drain[x]);   // products in flight end before tensor memory is given back
             const int zero = 0;
-            mbar_wait(&M->drain, 0, &zero, tc::kWaitLimitNs);
+            mbar_wait(&M->drain[x], 0, &zero, tc::kWaitLimitNs);
             __syncwarp();
-        } else if (warp == 10) {
-            // -------------------------------------------------------- queries
-            int nq[2] = {0, 0};
+        } else {
+            // -------------------------------------------------------- queries, and inspector of values
+            // (one warp: a tile's queries are loaded once the last tile's values are inspected)
+            int st = 0, ph = 0, nv = 0, nq[2] = {0, 0};
             bool dead = *abort_flag != 0, q_bytes = false;
             while (w.left > 0 && !dead) {
+                const Span item = span_of(a, w.r, w.m * kTileRows, kTileRows);
+                const int take = w.take;
                 for (int x = 0; x < 2 && !dead; x++) {
                     const int row0 = w.m * kTileRows + x * kHalfRows;
                     const Span sp = span_of(a, w.r, row0, kHalfRows);
@@ -917,7 +965,7 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                             mbar_arrive_expect_tx(&M->qfull[x], L::kQ);
 #pragma unroll
                             for (int hf = 0; hf < D / 64; hf++)
-                                tma_load_4d(dst0 + hf * L::kPiece, &qmap, &M->qfull[x], hf * 64, 0, w.h, w.r.tok0 + row0 / a.n_rep);
+                                tma_load_4d(dst0 + hf * L::kPiece, &qmap, &M->qfull[x], hf * 64, 0, w.h, w.r.tok0 + token_of(a, row0));
                         }
                         q_bytes = true;
                         continue;
@@ -925,7 +973,7 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                     constexpr int kPer = D / 8, kStep = 32 / kPer;   // 16-byte pieces of a row, rows at a time
                     const uint32_t base = smem_u32(dst0);
                     const int ch = lane % kPer;
-                    int r = lane / kPer, tk = (row0 + r) / a.n_rep, rep = row0 + r - tk * a.n_rep;
+                    int r = lane / kPer, tk = token_of(a, row0 + r), rep = row0 + r - tk * a.n_rep;
                     const uint16_t* src = a.q + (int64_t)(w.r.tok0 + tk) * a.q_tok + (int64_t)w.h * a.n_rep * a.q_head + ch * 8;
                     const uint32_t col = base + (ch >> 3) * L::kPiece;
                     for (; r < sp.n; r += kStep) {
@@ -943,21 +991,7 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&M->qfull[x]);
                 }
-                w.next(P);
-            }
-            if (dead) *abort_flag = 1;
-            if (q_bytes && *abort_flag) {   // boxes in flight land before the CTA ends
-                const int zero = 0;
-                for (int x = 0; x < 2; x++)
-                    if (nq[x]) mbar_wait(&M->qfull[x], (nq[x] - 1) & 1, &zero, tc::kWaitLimitNs);
-            }
-        } else {
-            // -------------------------------------------------------- inspector of values
-            int st = 0, ph = 0, nv = 0;
-            bool dead = *abort_flag != 0;
-            while (w.left > 0 && !dead) {
-                const Span item = span_of(a, w.r, w.m * kTileRows, kTileRows);
-                const int take = w.take;
+                if (dead) break;
                 for (int kc = 0; kc < take; kc++, nv++) {
                     if (++st == L::kStages) {   // past the keys
                         st = 0;
@@ -971,21 +1005,41 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                     int found = 0;
                     if (!item.sees_all(id)) {
                         unsigned char* tile = smem + L::stages + st * L::kStage;
-                        constexpr int kPer = D / 8;
-                        const int ch = lane % kPer;
-                        for (int r = lane / kPer; r < kKT; r += 32 / kPer) {
-                            const int t = t0 + r;
-                            if (!item.partial(a, t)) continue;
-                            uint4* p = reinterpret_cast<uint4*>(tile + (ch >> 3) * L::kPiece + r * 128 + (((ch & 7) ^ (r & 7)) << 4));
-                            if (t >= w.r.len) {
-                                *p = make_uint4(0, 0, 0, 0);
-                            } else {
-                                const uint4 v = *p;
-                                if (any_special<FP16>(v)) {
-                                    *p = make_uint4(drop_special<FP16>(v.x), drop_special<FP16>(v.y), drop_special<FP16>(v.z), drop_special<FP16>(v.w));
+                        constexpr int kPer = D / 8, kStep = 32 / kPer;
+                        const int ch = lane % kPer, r0 = lane / kPer;
+                        auto at = [&](int r) {
+                            return reinterpret_cast<uint4*>(tile + (ch >> 3) * L::kPiece + r * 128 + (((ch & 7) ^ (r & 7)) << 4));
+                        };
+                        const int held = w.r.len - t0 < kKT ? w.r.len - t0 : kKT;
+                        for (int r = (held > 0 ? held : 0) + r0; r < kKT; r += kStep) *at(r) = make_uint4(0, 0, 0, 0);
+                        // rows [lo, hi) in batches of independent loads
+                        auto scan = [&](int lo, int hi) {
+                            constexpr int kBatch = 8;
+                            for (int rb = lo + r0; __any_sync(0xffffffffu, rb < hi); rb += kBatch * kStep) {
+                                uint4 v[kBatch];
+                                uint32_t seen = 0;
+#pragma unroll
+                                for (int k = 0; k < kBatch; k++) v[k] = rb + k * kStep < hi ? *at(rb + k * kStep) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                                for (int k = 0; k < kBatch; k++) seen |= special_bits<FP16>(v[k]);
+                                if (seen) {
                                     found = 1;
+#pragma unroll
+                                    for (int k = 0; k < kBatch; k++)
+                                        if (rb + k * kStep < hi)
+                                            *at(rb + k * kStep) = make_uint4(drop_special<FP16>(v[k].x), drop_special<FP16>(v[k].y),
+                                                                             drop_special<FP16>(v[k].z), drop_special<FP16>(v[k].w));
                                 }
                             }
+                        };
+                        // the partial tokens: those past the first row's position, and those that the
+                        // last row's window has left
+                        const int after = item.p0 + 1 - t0 > 0 ? item.p0 + 1 - t0 : 0;
+                        scan(after, held);
+                        if (a.window) {
+                            const int lo = a.sinks - t0 > 0 ? a.sinks - t0 : 0, gone = item.p1 - a.window + 1 - t0;
+                            const int hi = gone < after ? gone : after;
+                            scan(lo, hi < held ? hi : held);
                         }
                         found = __any_sync(0xffffffffu, found);
                         fence_proxy_async_smem();
@@ -1003,6 +1057,11 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                 w.next(P);
             }
             if (dead) *abort_flag = 1;
+            if (q_bytes && *abort_flag) {   // boxes in flight land before the CTA ends
+                const int zero = 0;
+                for (int x = 0; x < 2; x++)
+                    if (nq[x]) mbar_wait(&M->qfull[x], (nq[x] - 1) & 1, &zero, tc::kWaitLimitNs);
+            }
         }
     }
     __syncthreads();
@@ -1047,7 +1106,7 @@ __global__ void __launch_bounds__(kTileRows) paged_chunk_merge_kernel(const __gr
         o[6] += f * v.z;
         o[7] += f * v.w;
     }
-    const int r = m.row0 + row, tk = r / a.n_rep, hd = m.h * a.n_rep + (r - tk * a.n_rep);
+    const int r = m.row0 + row, tk = token_of(a, r), hd = m.h * a.n_rep + (r - tk * a.n_rep);
     const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
     uint32_t b[4];
 #pragma unroll

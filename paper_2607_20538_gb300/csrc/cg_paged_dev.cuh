@@ -42,6 +42,12 @@ __device__ __forceinline__ uint32_t pack2(float x, float y) {   // x in the low 
     return *reinterpret_cast<const uint32_t*>(&b);
 }
 
+// Row x of a request belongs to its token x / n_rep. rep_mul = ceil(2^shift / n_rep) with shift =
+// 31 + ceil(log2 n_rep): the product is off by less than n_rep x / 2^shift < 1 / n_rep.
+__device__ __forceinline__ int token_of(const PagedArgs& a, int x) {
+    return (int)(((uint64_t)(uint32_t)x * a.rep_mul) >> a.rep_shift);
+}
+
 // A request as the attention sees it.
 struct Request {
     int len, n, tok0;     // tokens in the pool, new ones, first query row
