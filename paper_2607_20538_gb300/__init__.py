@@ -232,5 +232,16 @@ def alloc_outputs(shape: Shape, params: Params, device="cuda"):
     return codes, scales, resid
 
 
-from .paged import (Pages, PagedAttention, RopeScaling, Rotary, page_plan, page_release, paged_attention,  # noqa: E402
-                    paged_attention_workspace_bytes, rotary, rotary_append, rotary_table)
+
+# The paged cache's binding checks torch tensors, so it (and torch) is loaded on first use.
+_PAGED = ("Pages", "PagedAttention", "RopeScaling", "Rotary", "page_plan", "page_release", "paged_attention",
+          "paged_attention_workspace_bytes", "rotary", "rotary_append", "rotary_table")
+
+
+def __getattr__(name):
+    if name == "paged" or name in _PAGED:
+        import importlib
+        paged = importlib.import_module(".paged", __name__)
+        globals().update({n: getattr(paged, n) for n in _PAGED})
+        return paged if name == "paged" else globals()[name]
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

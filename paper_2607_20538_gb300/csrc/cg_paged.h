@@ -1,6 +1,8 @@
 // cg_paged.h -- internal interface between the paged-cache entry points and their kernels.
 #pragma once
 
+#include <atomic>
+
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -32,6 +34,21 @@ struct PagedArgs {
 // Workspace of the paged attention: bytes, and the launch (workspace of that size).
 size_t paged_attn_workspace(const PagedArgs& a);
 cudaError_t launch_paged_attn(const PagedArgs& a, void* workspace, cudaStream_t st);
+
+// A kernel's dynamic shared memory limit, raised once per device.
+struct SmemOptIn {
+    std::atomic<uint64_t> done{0};
+    cudaError_t set(const void* kernel, int bytes) {
+        int dev = 0;
+        cudaError_t e = cudaGetDevice(&dev);
+        if (e != cudaSuccess) return e;
+        const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
+        if (bit && (done.load(std::memory_order_relaxed) & bit)) return cudaSuccess;
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+        return e;
+    }
+};
 
 // Tensor map of the pool with boxes of box_rows tokens x 64 channels.
 bool paged_pool_map(CUtensorMap* map, const PagedArgs& a, uint32_t box_rows);

@@ -640,7 +640,8 @@ cudaError_t launch_rows(const RowsParams& P, cudaStream_t st) {
     CUtensorMap map;
     if (!paged_pool_map(&map, P.a, P.box_rows)) return cudaErrorInvalidValue;
     constexpr size_t smem = RowsSmem<D>::total;
-    cudaError_t e = cudaFuncSetAttribute(paged_rows_kernel<FP16, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    static SmemOptIn opt_in;
+    cudaError_t e = opt_in.set(reinterpret_cast<const void*>(paged_rows_kernel<FP16, D>), (int)smem);
     if (e != cudaSuccess) return e;
     const unsigned grid = (unsigned)rows_ctas(D);
     paged_rows_kernel<FP16, D><<<grid, kThreads, smem, st>>>(P, map);

@@ -1139,7 +1139,8 @@ cudaError_t launch_chunk(ChunkParams P, cudaStream_t st) {
     if (!paged_pool_map(&map, P.a, P.box_rows)) return cudaErrorInvalidValue;
     P.q_boxes = query_map(&qmap, P.a);
     constexpr size_t smem = ChunkSmem<D>::total;
-    cudaError_t e = cudaFuncSetAttribute(paged_chunk_kernel<FP16, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    static SmemOptIn opt_in;
+    cudaError_t e = opt_in.set(reinterpret_cast<const void*>(paged_chunk_kernel<FP16, D>), (int)smem);
     if (e != cudaSuccess) return e;
     const unsigned grid = (unsigned)tc::num_sms();
     paged_chunk_kernel<FP16, D><<<grid, kChunkThreads, smem, st>>>(P, map, qmap);

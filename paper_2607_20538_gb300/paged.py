@@ -9,7 +9,9 @@ from __future__ import annotations
 import ctypes
 from dataclasses import dataclass
 
-from . import CodecGaugeError, _check, _stream, load
+import torch
+
+from . import CodecGaugeError, _check, load
 
 CG_BF16, CG_FP16 = 0, 1
 CG_ROPE_NONE, CG_ROPE_LINEAR, CG_ROPE_BANDS, CG_ROPE_YARN = 0, 1, 2, 3
@@ -86,17 +88,18 @@ class PagedAttention:
 
 
 _P = ctypes.POINTER
-_vp, _i32, _i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
+_vp, _ci32, _ci64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
 _ARGS = {
-    "cg_page_plan": [_P(_CPages), _i32] + [_vp] * 11,
+    "cg_page_plan": [_P(_CPages), _ci32] + [_vp] * 11,
     "cg_page_release": [_P(_CPages)] + [_vp] * 8,
-    "cg_rotary_table": [_i32, _P(_CScaling), _vp, _P(ctypes.c_float)],
-    "cg_rotary": [_P(_CRotary), _i32, _i32, _i32, _i32, _vp, _i64, _i64, _vp, _vp, _vp, _i64, _i64, _vp],
-    "cg_rotary_append": [_P(_CPages), _P(_CRotary), _i32, _i32, _P(_CStrides)] + [_vp] * 9,
+    "cg_rotary_table": [_ci32, _P(_CScaling), _vp, _P(ctypes.c_float)],
+    "cg_rotary": [_P(_CRotary), _ci32, _ci32, _ci32, _ci32, _vp, _ci64, _ci64, _vp, _vp, _vp, _ci64, _ci64, _vp],
+    "cg_rotary_append": [_P(_CPages), _P(_CRotary), _ci32, _ci32, _P(_CStrides)] + [_vp] * 9,
     "cg_paged_attention_workspace_bytes": [_P(_CPages), _P(_CPagedAttn), _P(ctypes.c_size_t)],
     "cg_paged_attention": [_P(_CPages), _P(_CPagedAttn)] + [_vp] * 8 + [ctypes.c_size_t, _vp],
 }
 _fns = {}
+_ws_bytes = {}
 
 
 def _fn(name: str):
@@ -113,38 +116,58 @@ def _bad(msg: str):
     raise CodecGaugeError(-1, msg)
 
 
+_INT32, _INT64, _FLOAT32 = torch.int32, torch.int64, torch.float32
+_ELEM = {torch.bfloat16: CG_BF16, torch.float16: CG_FP16}
+
+
 def _elem(t) -> int:
-    import torch
-    if t.dtype is torch.bfloat16:
-        return CG_BF16
-    if t.dtype is torch.float16:
-        return CG_FP16
-    _bad(f"expected a bfloat16 or float16 tensor, got {t.dtype}")
+    e = _ELEM.get(t.dtype)
+    if e is None:
+        _bad(f"expected a bfloat16 or float16 tensor, got {t.dtype}")
+    return e
 
 
-def _ints(name: str, t, n: int, bits: int = 32) -> int:
-    """Address of a contiguous device array of at least n integers."""
-    import torch
-    if t.dtype is not (torch.int32 if bits == 32 else torch.int64) or not t.is_cuda or not t.is_contiguous() or t.numel() < n:
-        _bad(f"{name}: expected a contiguous int{bits} device tensor of at least {n} elements")
+# The current stream's handle without a Stream object around it, where torch has that.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_device = getattr(torch._C, "_cuda_getDevice", None)
+
+
+def _stream(stream) -> int:
+    if stream is not None:
+        return stream.cuda_stream
+    if _raw_stream is not None and _device is not None:
+        return _raw_stream(_device())
+    return torch.cuda.current_stream().cuda_stream
+
+
+def _i32(name: str, t, n: int) -> int:
+    """Address of a contiguous device array of at least n 32-bit integers."""
+    if t.dtype is not _INT32 or not t.is_cuda or t.numel() < n or not t.is_contiguous():
+        _bad(f"{name}: expected a contiguous int32 device tensor of at least {n} elements")
     return t.data_ptr()
 
 
-def _heads(name: str, t, n_tok: int, heads: int, d: int, like):
+def _i64(name: str, t, n: int) -> int:
+    if t.dtype is not _INT64 or not t.is_cuda or t.numel() < n or not t.is_contiguous():
+        _bad(f"{name}: expected a contiguous int64 device tensor of at least {n} elements")
+    return t.data_ptr()
+
+
+def _heads(name: str, t, n_tok: int, heads: int, d: int, dtype):
     """Checks a [n_tok][heads][d] device tensor; returns its address and its two strides."""
-    if t.dim() != 3 or t.shape[0] != n_tok or t.shape[1] != heads or t.shape[2] != d:
+    if t.shape != (n_tok, heads, d):
         _bad(f"{name}: expected shape [{n_tok}, {heads}, {d}], got {list(t.shape)}")
-    if t.dtype is not like.dtype or not t.is_cuda:
-        _bad(f"{name}: expected a {like.dtype} device tensor")
-    s = t.stride()
-    if s[2] != 1:
+    if t.dtype is not dtype or not t.is_cuda:
+        _bad(f"{name}: expected a {dtype} device tensor")
+    tok, head, one = t.stride()
+    if one != 1:
         _bad(f"{name}: the last dimension must be contiguous")
     # the stride of a dimension of one element is never used
-    return t.data_ptr(), (s[0] if n_tok > 1 else 0), (s[1] if heads > 1 else 0)
+    return t.data_ptr(), (tok if n_tok > 1 else 0), (head if heads > 1 else 0)
 
 
 def _pool(pages: Pages, pool) -> int:
-    if list(pool.shape) != [2, pages.n_pages, pages.H, pages.page, pages.d] or not pool.is_contiguous() or not pool.is_cuda:
+    if pool.shape != (2, pages.n_pages, pages.H, pages.page, pages.d) or not pool.is_contiguous() or not pool.is_cuda:
         _bad(f"pool: expected a contiguous device tensor [2, {pages.n_pages}, {pages.H}, {pages.page}, {pages.d}], "
              f"got {list(pool.shape)}")
     return pool.data_ptr()
@@ -156,26 +179,25 @@ def page_plan(pages: Pages, ctx_lens, new_lens, free_pages, free_count, block_ta
     The number of tokens planned for is positions.numel()."""
     n, r = positions.numel(), pages.n_req
     _check(_fn("cg_page_plan")(
-        pages.c(), n, _ints("ctx_lens", ctx_lens, r), _ints("new_lens", new_lens, r),
+        pages.c(), n, _i32("ctx_lens", ctx_lens, r), _i32("new_lens", new_lens, r),
         # a stack that is full of used pages may be an empty tensor: no entry of it is read
-        _ints("free_pages", free_pages, 0) or free_count.data_ptr(), _ints("free_count", free_count, 1),
-        _ints("block_table", block_table, r * pages.max_pages), _ints("seq_lens", seq_lens, r),
-        _ints("cu_new", cu_new, r + 1), _ints("positions", positions, n), _ints("slots", slots, n, 64),
-        _ints("free_left", free_left, 1), _stream(stream)))
+        _i32("free_pages", free_pages, 0) or free_count.data_ptr(), _i32("free_count", free_count, 1),
+        _i32("block_table", block_table, r * pages.max_pages), _i32("seq_lens", seq_lens, r),
+        _i32("cu_new", cu_new, r + 1), _i32("positions", positions, n), _i64("slots", slots, n),
+        _i32("free_left", free_left, 1), _stream(stream)))
 
 
 def page_release(pages: Pages, lens, done, block_table, free_pages, free_count, lens_left, free_left, stream=None) -> None:
     """Give back the pages of the requests whose done flag (int32) is set (cg_page_release)."""
     r = pages.n_req
     _check(_fn("cg_page_release")(
-        pages.c(), _ints("lens", lens, r), _ints("done", done, r), _ints("block_table", block_table, r * pages.max_pages),
-        _ints("free_pages", free_pages, pages.n_pages), _ints("free_count", free_count, 1),
-        _ints("lens_left", lens_left, r), _ints("free_left", free_left, 1), _stream(stream)))
+        pages.c(), _i32("lens", lens, r), _i32("done", done, r), _i32("block_table", block_table, r * pages.max_pages),
+        _i32("free_pages", free_pages, pages.n_pages), _i32("free_count", free_count, 1),
+        _i32("lens_left", lens_left, r), _i32("free_left", free_left, 1), _stream(stream)))
 
 
 def rotary_table(rot: int, scaling: RopeScaling = RopeScaling(), device="cuda"):
     """Frequencies of rot / 2 pairs as a device tensor (int64, 2^-64 of a turn per position), and mscale."""
-    import torch
     host = torch.empty(max(rot // 2, 0), dtype=torch.int64)
     m = ctypes.c_float()
     c = _CScaling(scaling.kind, scaling.base, scaling.factor, scaling.original, scaling.low, scaling.high)
@@ -188,10 +210,10 @@ def rotary(turn: Rotary, x, positions, table, out, stream=None) -> None:
     if x.dim() != 3:
         _bad("x: expected [n_tok, heads, d]")
     n, heads, d = x.shape
-    xp, xt, xh = _heads("x", x, n, heads, d, x)
-    op, ot, oh = _heads("out", out, n, heads, d, x)
-    _check(_fn("cg_rotary")(turn.c(), _elem(x), n, heads, d, xp, xt, xh, _ints("positions", positions, n),
-                            _ints("table", table, turn.rot // 2, 64) if turn.rot else None, op, ot, oh, _stream(stream)))
+    xp, xt, xh = _heads("x", x, n, heads, d, x.dtype)
+    op, ot, oh = _heads("out", out, n, heads, d, x.dtype)
+    _check(_fn("cg_rotary")(turn.c(), _elem(x), n, heads, d, xp, xt, xh, _i32("positions", positions, n),
+                            _i64("table", table, turn.rot // 2) if turn.rot else None, op, ot, oh, _stream(stream)))
 
 
 def rotary_append(pages: Pages, turn: Rotary, q, k, v, positions, slots, table, q_out, pool, stream=None) -> None:
@@ -201,14 +223,14 @@ def rotary_append(pages: Pages, turn: Rotary, q, k, v, positions, slots, table, 
     hq = 0 if q is None else q.shape[1]
     if k.dtype is not pool.dtype:
         _bad(f"k: expected the pool's type {pool.dtype}, got {k.dtype}")
-    kp, kt, kh = _heads("k", k, n, pages.H, pages.d, pool)
-    vp, vt, vh = _heads("v", v, n, pages.H, pages.d, pool)
-    qp, qt, qh = _heads("q", q, n, hq, pages.d, pool) if hq else (None, 0, 0)
-    op, ot, oh = _heads("q_out", q_out, n, hq, pages.d, pool) if hq else (None, 0, 0)
+    kp, kt, kh = _heads("k", k, n, pages.H, pages.d, pool.dtype)
+    vp, vt, vh = _heads("v", v, n, pages.H, pages.d, pool.dtype)
+    qp, qt, qh = _heads("q", q, n, hq, pages.d, pool.dtype) if hq else (None, 0, 0)
+    op, ot, oh = _heads("q_out", q_out, n, hq, pages.d, pool.dtype) if hq else (None, 0, 0)
     _check(_fn("cg_rotary_append")(
         pages.c(_elem(pool)), turn.c(), n, hq, _CStrides(qt, qh, kt, kh, vt, vh, ot, oh), qp, kp, vp,
-        _ints("positions", positions, n), _ints("slots", slots, n, 64),
-        _ints("table", table, turn.rot // 2, 64) if turn.rot else None, op, _pool(pages, pool), _stream(stream)))
+        _i32("positions", positions, n), _i64("slots", slots, n),
+        _i64("table", table, turn.rot // 2) if turn.rot else None, op, _pool(pages, pool), _stream(stream)))
 
 
 def _attn(pages: Pages, how: PagedAttention, n: int, qt=0, qh=0, ot=0, oh=0) -> _CPagedAttn:
@@ -227,24 +249,25 @@ def paged_attention(pages: Pages, how: PagedAttention, q, pool, block_table, seq
     """Attention of the new tokens' queries q [n_tok][H * n_rep][d] over their requests' pages
     (cg_paged_attention). Without a workspace the call takes one from torch's allocator, on the
     current stream (pass one to run on another)."""
-    import torch
     n, hq = q.shape[0], pages.H * how.n_rep
-    qp, qt, qh = _heads("q", q, n, hq, pages.d, pool)
-    op, ot, oh = _heads("out", out, n, hq, pages.d, pool)
+    qp, qt, qh = _heads("q", q, n, hq, pages.d, pool.dtype)
+    op, ot, oh = _heads("out", out, n, hq, pages.d, pool.dtype)
     lp = None
     if lse is not None:
-        if lse.dtype is not torch.float32 or not lse.is_cuda or not lse.is_contiguous() or lse.numel() < n * hq:
+        if lse.dtype is not _FLOAT32 or not lse.is_cuda or not lse.is_contiguous() or lse.numel() < n * hq:
             _bad(f"lse: expected a contiguous float32 device tensor [{n}, {hq}]")
         lp = lse.data_ptr()
     cp, ca = pages.c(_elem(pool)), _attn(pages, how, n, qt, qh, ot, oh)
     if workspace is None:
         if stream is not None and stream != torch.cuda.current_stream():
             _bad("workspace: needed on a stream that is not the current one")
-        need = ctypes.c_size_t()
-        _check(_fn("cg_paged_attention_workspace_bytes")(cp, ca, need))
-        workspace = torch.empty(need.value, dtype=torch.uint8, device=q.device)
+        key = (pages.d, how.n_rep, how.max_new, q.device)   # all that the size depends on
+        nbytes = _ws_bytes.get(key)
+        if nbytes is None:
+            nbytes = _ws_bytes[key] = paged_attention_workspace_bytes(pages, how, n)
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
     r = pages.n_req
     _check(_fn("cg_paged_attention")(
-        cp, ca, qp, _pool(pages, pool), _ints("block_table", block_table, r * pages.max_pages),
-        _ints("seq_lens", seq_lens, r), _ints("cu_new", cu_new, r + 1), op, lp, workspace.data_ptr(),
+        cp, ca, qp, _pool(pages, pool), _i32("block_table", block_table, r * pages.max_pages),
+        _i32("seq_lens", seq_lens, r), _i32("cu_new", cu_new, r + 1), op, lp, workspace.data_ptr(),
         workspace.numel() * workspace.element_size(), _stream(stream)))
