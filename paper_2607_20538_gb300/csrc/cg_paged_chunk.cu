@@ -1,8 +1,8 @@
 // cg_paged_chunk.cu -- paged attention of requests with many query rows (a chunk or a whole prompt):
 // o = softmax(scale q K^T) V on the tensor cores (contract: include/codecgauge_paged.h).
 //
-// A tile of work is 256 query rows of one request and KV head, as two halves A and B of 128 rows
-// (rows are (token, query head of the group)). One CTA per SM walks its share of the key tiles:
+// A tile of work is up to 256 query rows of one request and KV head, as two halves A and B of 128
+// rows (rows are (token, query head of the group), a half the whole tokens that fit). One CTA per SM walks its share of the key tiles:
 //   warps 0-3, 4-7  softmax of half A, half B: a thread owns a row: 128 scores from tensor memory,
 //                   running reference and sum in registers, weights back to tensor memory;
 //   warp 8          TMA: 128-token tiles of keys and values, K0 V0 K1 V1 ..., boxes of pages;
@@ -36,7 +36,7 @@ namespace {
 
 using namespace paged;
 
-constexpr int kHalfRows = 128;
+constexpr int kHalfRows = 128;    // rows of a half: as many whole tokens (of n_rep rows) as fit
 constexpr int kTileRows = 256;
 constexpr int kKT = 128;          // tokens of a key tile
 constexpr int kChunkThreads = 384;
@@ -46,7 +46,8 @@ constexpr int kMaxStages = 8;
 constexpr int chunk_part_floats(int d) { return kTileRows * d + 2 * kTileRows; }
 
 struct ChunkMeta {
-    int last, tok0, row0, n_rows, h, pad[3];
+    int last;            // last CTA with a part of the tile that starts here, or -1: none
+    int tok0, n_tok, h;  // its first query row of the call, tokens and KV head
 };
 
 template <int D>
@@ -81,6 +82,7 @@ struct ChunkParams {
     ChunkMeta* meta;
     int min_rows;      // requests with fewer query rows are left to the other kernel
     int min_share;     // key tiles
+    int half_tok;      // tokens of a half: 128 / n_rep
     int box_rows;
     int q_boxes;       // the queries of a half are whole boxes of qmap
 };
@@ -98,12 +100,13 @@ struct Span {
     }
 };
 
-__device__ __forceinline__ Span span_of(const PagedArgs& a, const Request& r, int row0, int rows_max) {
+// Tokens [tok, tok + most) of a request's new ones.
+__device__ __forceinline__ Span span_of(const PagedArgs& a, const Request& r, int tok, int most) {
     Span s;
-    const int rows = r.n * a.n_rep - row0;
-    s.n = rows < 0 ? 0 : rows < rows_max ? rows : rows_max;
-    s.p0 = r.len - r.n + token_of(a, row0);
-    s.p1 = s.n ? r.len - r.n + token_of(a, row0 + s.n - 1) : s.p0 - 1;
+    const int left = r.n - tok, n = left < 0 ? 0 : left < most ? left : most;
+    s.n = n * a.n_rep;
+    s.p0 = r.len - r.n + tok;
+    s.p1 = s.p0 + n - 1;
     s.s0 = s.ss = s.f0 = s.fs = 0;
     s.s1 = s.n && s.p1 >= 0 ? s.p1 / kKT + 1 : 0;
     s.f1 = s.p0 < 0 ? 0 : (s.p0 + 1) / kKT;
@@ -117,10 +120,9 @@ __device__ __forceinline__ Span span_of(const PagedArgs& a, const Request& r, in
     return s;
 }
 
-__device__ __forceinline__ Tiles tile_tiles(const PagedArgs& a, const Request& r, int m) {
-    const int rows = r.n * a.n_rep - m * kTileRows, n = rows < kTileRows ? rows : kTileRows;
-    return visible_tiles<kKT>(a.window, a.sinks, r.len - r.n + token_of(a, m * kTileRows),
-                              r.len - r.n + token_of(a, m * kTileRows + n - 1));
+__device__ __forceinline__ Tiles tile_tiles(const ChunkParams& P, const Request& r, int m) {
+    const int tok = m * 2 * P.half_tok, left = r.n - tok, n = left < 2 * P.half_tok ? left : 2 * P.half_tok;
+    return visible_tiles<kKT>(P.a.window, P.a.sinks, r.len - r.n + tok, r.len - r.n + tok + n - 1);
 }
 
 // A work tile costs its key tiles plus kTileCost (queries in, first scores, output out), in units of
@@ -129,7 +131,7 @@ constexpr int kTileCost = 3;
 
 __device__ __forceinline__ int row_tiles(const ChunkParams& P, const Request& r) {
     const int64_t rows = (int64_t)r.n * P.a.n_rep;
-    return r.n <= 0 || rows < P.min_rows ? 0 : (int)((rows + kTileRows - 1) / kTileRows);
+    return r.n <= 0 || rows < P.min_rows ? 0 : (r.n + 2 * P.half_tok - 1) / (2 * P.half_tok);
 }
 
 // Cost of one KV head of each lane's request. All lanes call: requests of many tiles are summed by
@@ -138,7 +140,7 @@ __device__ __forceinline__ int64_t head_cost(const ChunkParams& P, const Request
     const int lane = threadIdx.x & 31, n_m = row_tiles(P, r);
     int64_t sum = 0;
     if (n_m <= 2)
-        for (int m = 0; m < n_m; m++) sum += tile_tiles(P.a, r, m).count() + kTileCost;
+        for (int m = 0; m < n_m; m++) sum += tile_tiles(P, r, m).count() + kTileCost;
     for (uint32_t big = __ballot_sync(0xffffffffu, n_m > 2); big; big &= big - 1) {
         const int src = __ffs(big) - 1;
         Request q;
@@ -146,7 +148,7 @@ __device__ __forceinline__ int64_t head_cost(const ChunkParams& P, const Request
         q.n = __shfl_sync(0xffffffffu, r.n, src);
         const int n = __shfl_sync(0xffffffffu, n_m, src);
         int64_t part = 0;
-        for (int m = lane; m < n; m += 32) part += tile_tiles(P.a, q, m).count() + kTileCost;
+        for (int m = lane; m < n; m += 32) part += tile_tiles(P, q, m).count() + kTileCost;
 #pragma unroll
         for (int off = 16; off; off >>= 1) part += __shfl_xor_sync(0xffffffffu, part, off);
         if (lane == src) sum = part;
@@ -159,7 +161,7 @@ __device__ __forceinline__ int tile_at(const ChunkParams& P, const Request& r, i
     const int lane = threadIdx.x & 31, n_m = row_tiles(P, r);
     for (int m0 = 0;; m0 += 32) {
         const int m = m0 + lane;
-        const int64_t mine = m < n_m ? tile_tiles(P.a, r, m).count() + kTileCost : 0;
+        const int64_t mine = m < n_m ? tile_tiles(P, r, m).count() + kTileCost : 0;
         int64_t incl = mine;
 #pragma unroll
         for (int k = 1; k < 32; k *= 2) {
@@ -195,7 +197,7 @@ struct ChunkWalk {
         n_m = row_tiles(P, r);
     }
     __device__ __forceinline__ void tile(const ChunkParams& P) {
-        t = tile_tiles(P.a, r, m);
+        t = tile_tiles(P, r, m);
         n = t.count();
         c = x > kTileCost ? x - kTileCost : 0;
         goes_on = n + kTileCost - x > left;
@@ -631,14 +633,14 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
         bool head_part = w.left > 0 && w.c > 0, dead = *abort_flag != 0;
         int meta_last = -1;
         while (w.left > 0 && !dead) {
-            const int row0 = w.m * kTileRows + x * kHalfRows;
-            const Span sp = span_of(a, w.r, row0, kHalfRows), item = span_of(a, w.r, w.m * kTileRows, kTileRows);
+            const int tok = (2 * w.m + x) * P.half_tok;   // the half's first new token
+            const Span sp = span_of(a, w.r, tok, P.half_tok), item = span_of(a, w.r, 2 * w.m * P.half_tok, 2 * P.half_tok);
             const int take = w.take;
             if (sp.n > 0) {
                 const int row = (warp & 3) * 32 + lane;
                 const bool have = row < sp.n;
-                const int tk = token_of(a, row0 + row), hd = w.h * a.n_rep + (row0 + row - tk * a.n_rep);
-                const int pos = have ? w.r.len - w.r.n + tk : -1;
+                const int rt = token_of(a, row), tk = tok + rt, hd = w.h * a.n_rep + (row - rt * a.n_rep);
+                const int pos = have ? sp.p0 + rt : -1;
                 float ref = -INFINITY, sum = 0.0f;
                 bool started = false;
                 for (int kc = 0; kc < take; kc++) {
@@ -755,9 +757,8 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                 if (tid == 0) {
                     ChunkMeta* m = P.meta + blockIdx.x;
                     m->last = meta_last;
-                    m->tok0 = w.r.tok0;
-                    m->row0 = w.m * kTileRows;
-                    m->n_rows = item.n;
+                    m->tok0 = w.r.tok0 + 2 * w.m * P.half_tok;
+                    m->n_tok = item.p1 - item.p0 + 1;
                     m->h = w.h;
                 }
             }
@@ -858,7 +859,7 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                 return !dead;
             };
             while (w.left > 0 && !dead) {
-                const Span sp = span_of(a, w.r, w.m * kTileRows + x * kHalfRows, kHalfRows);
+                const Span sp = span_of(a, w.r, (2 * w.m + x) * P.half_tok, P.half_tok);
                 const int take = w.take;
                 bool first = true, prev = false;
                 int vst = 0, vph = 0;
@@ -948,11 +949,11 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
             int st = 0, ph = 0, nv = 0, nq[2] = {0, 0};
             bool dead = *abort_flag != 0, q_bytes = false;
             while (w.left > 0 && !dead) {
-                const Span item = span_of(a, w.r, w.m * kTileRows, kTileRows);
+                const Span item = span_of(a, w.r, 2 * w.m * P.half_tok, 2 * P.half_tok);
                 const int take = w.take;
                 for (int x = 0; x < 2 && !dead; x++) {
-                    const int row0 = w.m * kTileRows + x * kHalfRows;
-                    const Span sp = span_of(a, w.r, row0, kHalfRows);
+                    const int tok = (2 * w.m + x) * P.half_tok;
+                    const Span sp = span_of(a, w.r, tok, P.half_tok);
                     if (sp.n <= 0) continue;
                     if (!__all_sync(0xffffffffu, mbar_wait(&M->qempty[x], (nq[x] & 1) ^ 1, abort_flag, a.wait_ns))) {
                         dead = true;
@@ -960,12 +961,12 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                     }
                     nq[x]++;
                     unsigned char* dst0 = smem + L::q + x * L::kQ;
-                    if (P.q_boxes) {   // 128 / n_rep tokens x n_rep heads: whole boxes
+                    if (P.q_boxes) {   // the half's tokens x n_rep heads
                         if (lane == 0) {
-                            mbar_arrive_expect_tx(&M->qfull[x], L::kQ);
+                            mbar_arrive_expect_tx(&M->qfull[x], (uint32_t)(P.half_tok * a.n_rep * D * 2));
 #pragma unroll
                             for (int hf = 0; hf < D / 64; hf++)
-                                tma_load_4d(dst0 + hf * L::kPiece, &qmap, &M->qfull[x], hf * 64, 0, w.h, w.r.tok0 + token_of(a, row0));
+                                tma_load_4d(dst0 + hf * L::kPiece, &qmap, &M->qfull[x], hf * 64, 0, w.h, w.r.tok0 + tok);
                         }
                         q_bytes = true;
                         continue;
@@ -973,8 +974,8 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                     constexpr int kPer = D / 8, kStep = 32 / kPer;   // 16-byte pieces of a row, rows at a time
                     const uint32_t base = smem_u32(dst0);
                     const int ch = lane % kPer;
-                    int r = lane / kPer, tk = token_of(a, row0 + r), rep = row0 + r - tk * a.n_rep;
-                    const uint16_t* src = a.q + (int64_t)(w.r.tok0 + tk) * a.q_tok + (int64_t)w.h * a.n_rep * a.q_head + ch * 8;
+                    int r = lane / kPer, rt = token_of(a, r), rep = r - rt * a.n_rep;
+                    const uint16_t* src = a.q + (int64_t)(w.r.tok0 + tok + rt) * a.q_tok + (int64_t)w.h * a.n_rep * a.q_head + ch * 8;
                     const uint32_t col = base + (ch >> 3) * L::kPiece;
                     for (; r < sp.n; r += kStep) {
                         asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(col + r * 128 + (((ch & 7) ^ (r & 7)) << 4)),
@@ -1079,8 +1080,10 @@ __global__ void __launch_bounds__(kTileRows) paged_chunk_merge_kernel(const __gr
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const PagedArgs& a = P.a;
     const ChunkMeta m = P.meta[blockIdx.x];
-    const int row = threadIdx.x;
-    if (m.last < 0 || row >= m.n_rows) return;
+    // thread = row of the tile: half row >> 7, token rt of the half
+    const int row = threadIdx.x, rr = row & (kHalfRows - 1), rt = token_of(a, rr);
+    const int tk = (row >> 7) * P.half_tok + rt;
+    if (m.last < 0 || rt >= P.half_tok || tk >= m.n_tok) return;
     const int parts = m.last - (int)blockIdx.x + 1;
     auto part = [&](int p) { return P.parts + ((int64_t)(blockIdx.x + p) * 2 + (p == 0 ? 1 : 0)) * chunk_part_floats(D); };
     float R = -INFINITY;
@@ -1106,7 +1109,7 @@ __global__ void __launch_bounds__(kTileRows) paged_chunk_merge_kernel(const __gr
         o[6] += f * v.z;
         o[7] += f * v.w;
     }
-    const int r = m.row0 + row, tk = token_of(a, r), hd = m.h * a.n_rep + (r - tk * a.n_rep);
+    const int hd = m.h * a.n_rep + (rr - rt * a.n_rep);
     const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
     uint32_t b[4];
 #pragma unroll
@@ -1117,15 +1120,17 @@ __global__ void __launch_bounds__(kTileRows) paged_chunk_merge_kernel(const __gr
         a.lse[(int64_t)(m.tok0 + tk) * a.H * a.n_rep + hd] = inv == 0.0f ? -INFINITY : (R + log2f(l)) * kLn2;
 }
 
-// Queries as [n_tok][H][n_rep][d] (their strides), boxes of 128 / n_rep tokens x n_rep heads x 64
-// channels: 128 rows in the order of a half. For head groups that divide 128 and strides that a
-// tensor map can hold; other queries are gathered by a warp.
+// Queries as [n_tok][H][n_rep][d] (their strides), boxes of a half's tokens x n_rep heads x 64
+// channels: its rows in their order. Queries with strides that a tensor map cannot hold (a broadcast
+// dimension) are gathered by a warp instead.
 bool query_map(CUtensorMap* map, const PagedArgs& a) {
     auto fn = tmap_encode_fn();
     const int64_t most = (int64_t)1 << 39;
-    if (!fn || kHalfRows % a.n_rep || a.q_head <= 0 || a.q_tok <= 0 || a.q_head * a.n_rep * 2 >= most || a.q_tok * 2 >= most) return false;
+    // the stride of a dimension of one element is free
+    const int64_t q_head = a.H * a.n_rep == 1 ? a.d : a.q_head, q_tok = a.n_tok == 1 ? a.d : a.q_tok;
+    if (!fn || q_head <= 0 || q_tok <= 0 || q_head * a.n_rep * 2 >= most || q_tok * 2 >= most) return false;
     cuuint64_t dims[4] = {(cuuint64_t)a.d, (cuuint64_t)a.n_rep, (cuuint64_t)a.H, (cuuint64_t)a.n_tok};
-    cuuint64_t strides[3] = {(cuuint64_t)a.q_head * 2, (cuuint64_t)a.q_head * a.n_rep * 2, (cuuint64_t)a.q_tok * 2};
+    cuuint64_t strides[3] = {(cuuint64_t)q_head * 2, (cuuint64_t)q_head * a.n_rep * 2, (cuuint64_t)q_tok * 2};
     cuuint32_t box[4] = {64, (cuuint32_t)a.n_rep, 1, (cuuint32_t)(kHalfRows / a.n_rep)}, estr[4] = {1, 1, 1, 1};
     return fn(map, a.dtype == CG_FP16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4,
               const_cast<uint16_t*>(a.q), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
@@ -1171,6 +1176,7 @@ cudaError_t launch_paged_chunk(const PagedArgs& a, int min_rows, void* workspace
     P.meta = reinterpret_cast<ChunkMeta*>(P.parts + (size_t)tc::num_sms() * 2 * chunk_part_floats(a.d));
     P.min_rows = min_rows;
     P.min_share = 4;
+    P.half_tok = kHalfRows / a.n_rep;
     P.box_rows = a.page < kKT ? a.page : kKT;
     const bool h = a.dtype == CG_FP16;
     if (a.d == 64) return h ? launch_chunk<true, 64>(P, st) : launch_chunk<false, 64>(P, st);

@@ -463,3 +463,20 @@ def test_binding_refusals():
         kw.update(bad)
         with pytest.raises(cg.CodecGaugeError):
             cg.paged_attention(pages, how, q, kw["pool"], kw["table"], kw["lens"], cu, out, None, kw["workspace"])
+
+
+@pytest.mark.parametrize("rep,new", [(4, 1), (4, 50), (7, 50)])
+def test_broadcast_queries(rep, new):
+    """Queries whose token or head stride is 0 (one query for every head, or for every token)."""
+    c = _case("bf16", 128, 2, rep, 16, [new + 70], [new], seed=17)
+    q = c["q"].cuda()
+    for b in (q[:, :1].expand(-1, 2 * rep, -1), q[:1].expand(new, -1, -1), q[:1, :1].expand(new, 2 * rep, -1)):
+        got, lse = _attend(c, q=b, out=torch.full_like(q, float("nan")))
+        _check(dict(c, q=b.contiguous().cpu()), got, lse)
+
+
+@pytest.mark.parametrize("rep", [1, 2, 3, 5, 6, 7, 9, 11, 16, 17, 31, 48, 63])
+def test_every_head_group(rep):
+    """Rows per tile are whole tokens of n_rep rows, which leaves some of the 128 empty."""
+    c = _case("bf16", 64, 1, rep, 16, [300, 20], [290, 3], seed=rep)
+    _check(c, *_attend(c))
