@@ -368,30 +368,32 @@ __device__ __forceinline__ float row_max(uint32_t s_tm, float (&u)[32], float (&
     return max32(v, m);
 }
 
+// Bits [lo, hi] of a word, for any lo, hi.
+__device__ __forceinline__ uint32_t bits_between(int lo, int hi) {
+    const uint32_t up = hi < 0 ? 0u : hi >= 31 ? ~0u : (2u << hi) - 1u;
+    return lo <= 0 ? up : lo > 31 ? 0u : up & (~0u << lo);
+}
+
 // A tile that not every row sees whole: the row sees the columns [lo, hi] and those below sk; the
 // others are set to -inf.
 __device__ __noinline__ void mask_row(uint32_t s_tm, int lo, int hi, int sk) {
 #pragma unroll 1
     for (int c0 = 0; c0 < kKT; c0 += 32) {
-        float u[32];
-        tmem_ld32f(s_tm + c0, u);
-        const int h = hi - c0, l = lo - c0, k0 = sk - c0;
-        const bool all = h >= 31 && (l <= 0 || k0 > 31), none_cut = l <= 0;
-        tmem_wait_ld();
-        settle(u);
-        if (!__all_sync(0xffffffffu, all)) {
-            if (__all_sync(0xffffffffu, none_cut)) {
+        const uint32_t see = bits_between(lo - c0, hi - c0) | bits_between(0, (sk - 1 < hi ? sk - 1 : hi) - c0);
+        if (__all_sync(0xffffffffu, see == ~0u)) continue;
+        uint32_t r[32];
+        if (__any_sync(0xffffffffu, see != 0)) {
+            float u[32];
+            tmem_ld32f(s_tm + c0, u);
+            tmem_wait_ld();
+            settle(u);
 #pragma unroll
-                for (int k = 0; k < 32; k++) u[k] = k <= h ? u[k] : -INFINITY;
-            } else {
+            for (int k = 0; k < 32; k++) r[k] = see >> k & 1 ? __float_as_uint(u[k]) : 0xff800000u;
+        } else {
 #pragma unroll
-                for (int k = 0; k < 32; k++) u[k] = k <= h && (k >= l || k < k0) ? u[k] : -INFINITY;
-            }
-            uint32_t r[32];
-#pragma unroll
-            for (int k = 0; k < 32; k++) r[k] = __float_as_uint(u[k]);
-            tmem_st32(s_tm + c0, r);
+            for (int k = 0; k < 32; k++) r[k] = 0xff800000u;
         }
+        tmem_st32(s_tm + c0, r);
     }
     tmem_wait_st();
 }
@@ -636,6 +638,16 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
             const int tok = (2 * w.m + x) * P.half_tok;   // the half's first new token
             const Span sp = span_of(a, w.r, tok, P.half_tok), item = span_of(a, w.r, 2 * w.m * P.half_tok, 2 * P.half_tok);
             const int take = w.take;
+            if (!head_part && w.goes_on) {   // it starts here and goes on
+                meta_last = (int)(blockIdx.x + (w.rest + share - 1) / share);
+                if (tid == 0) {
+                    ChunkMeta* m = P.meta + blockIdx.x;
+                    m->last = meta_last;
+                    m->tok0 = w.r.tok0 + 2 * w.m * P.half_tok;
+                    m->n_tok = item.p1 - item.p0 + 1;
+                    m->h = w.h;
+                }
+            }
             if (sp.n > 0) {
                 const int row = (warp & 3) * 32 + lane;
                 const bool have = row < sp.n;
@@ -704,15 +716,22 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                     if (lane == 0) mbar_arrive(&M->pfull[x][1]);
                     sum += (acc0.x + acc0.y) + (acc1.x + acc1.y);
                 }
-                if (dead || !__all_sync(0xffffffffu, mbar_wait(&M->ofull[x], no & 1, abort_flag, a.wait_ns))) {
-                    dead = true;
-                    break;
+                if (dead) break;
+                // on to the next tile while the last products run
+                const bool whole = !head_part && !w.goes_on;
+                const int tok0 = w.r.tok0;
+                w.next(P);
+                if (started) {
+                    if (!__all_sync(0xffffffffu, mbar_wait(&M->ofull[x], no & 1, abort_flag, a.wait_ns))) {
+                        dead = true;
+                        break;
+                    }
+                    no++;
                 }
-                no++;
                 tc_fence_after();
-                if (!head_part && !w.goes_on) {
+                if (whole) {
                     const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
-                    uint16_t* dst = a.out + (int64_t)(w.r.tok0 + tk) * a.o_tok + hd * a.o_head;
+                    uint16_t* dst = a.out + (int64_t)(tok0 + tk) * a.o_tok + hd * a.o_head;
                     const uint64_t my_dst = have ? reinterpret_cast<uint64_t>(dst) : 0;
 #pragma unroll 1
                     for (int c0 = 0; c0 < D; c0 += 64) {
@@ -730,7 +749,7 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                         store_rows(b, my_dst, 2 * c0);
                     }
                     if (a.lse && have)
-                        a.lse[(int64_t)(w.r.tok0 + tk) * a.H * a.n_rep + hd] = inv == 0.0f ? -INFINITY : (ref + log2f(sum)) * kLn2;
+                        a.lse[(int64_t)(tok0 + tk) * a.H * a.n_rep + hd] = inv == 0.0f ? -INFINITY : (ref + log2f(sum)) * kLn2;
                 } else {
                     float* part = P.parts + ((int64_t)blockIdx.x * 2 + (head_part ? 0 : 1)) * chunk_part_floats(D);
                     const int r = x * kHalfRows + row;
@@ -752,19 +771,9 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                     }
                 }
             }
-            if (!head_part && w.goes_on) {   // it starts here and goes on
-                meta_last = (int)(blockIdx.x + (w.rest + share - 1) / share);
-                if (tid == 0) {
-                    ChunkMeta* m = P.meta + blockIdx.x;
-                    m->last = meta_last;
-                    m->tok0 = w.r.tok0 + 2 * w.m * P.half_tok;
-                    m->n_tok = item.p1 - item.p0 + 1;
-                    m->h = w.h;
-                }
-            }
             head_part = false;
             nv += take;
-            w.next(P);
+            if (sp.n <= 0) w.next(P);
         }
         if (tid == 0 && meta_last < 0) P.meta[blockIdx.x].last = -1;
         if (dead) {
@@ -890,6 +899,7 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                             for (int k = 0; k < kKT / 32; k++)
                                 mma_ts(ox, sx + 8 * k, bv + ((k * 2048) >> 4), v_hi, idesc_o, k ? 1u : acc);
                         }
+                        // taken before the rest of the weights are there, which hides the atomic
                         if (!take_turn(&M->turn, issue, abort_flag, a.wait_ns)) {
                             dead = true;
                             break;
@@ -916,7 +926,8 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                         if (j == take - 1 && sp.n > 0) mma_commit(&M->qempty[x]);   // the queries were read
                         if (j > 0) mma_commit(&M->empty[vst]);
                         if (j < take) mma_commit(&M->empty[kst]);
-                        if (j == take && sp.n > 0) mma_commit(&M->ofull[x]);
+                        // only where the softmax had its turn: it could otherwise miss one of two
+                        if (j == take && !first) mma_commit(&M->ofull[x]);
                     }
                     __syncwarp();
                     prev = next;
@@ -994,14 +1005,16 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                 }
                 if (dead) break;
                 for (int kc = 0; kc < take; kc++, nv++) {
-                    if (++st == L::kStages) {   // past the keys
-                        st = 0;
-                        ph ^= 1;
+                    // Every use of a stage is waited for, the keys' too: a wait tells only even from
+                    // odd uses, and the values' copy may land before the keys that used the stage.
+                    for (int kv = 0; kv < 2 && !dead; kv++) {
+                        if (kv && ++st == L::kStages) {
+                            st = 0;
+                            ph ^= 1;
+                        }
+                        if (!__all_sync(0xffffffffu, mbar_wait(&M->full[st], ph, abort_flag, a.wait_ns))) dead = true;
                     }
-                    if (!__all_sync(0xffffffffu, mbar_wait(&M->full[st], ph, abort_flag, a.wait_ns))) {
-                        dead = true;
-                        break;
-                    }
+                    if (dead) break;
                     const int id = w.t.id(w.c + kc), t0 = id * kKT;
                     int found = 0;
                     if (!item.sees_all(id)) {

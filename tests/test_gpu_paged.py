@@ -480,3 +480,28 @@ def test_every_head_group(rep):
     """Rows per tile are whole tokens of n_rep rows, which leaves some of the 128 empty."""
     c = _case("bf16", 64, 1, rep, 16, [300, 20], [290, 3], seed=rep)
     _check(c, *_attend(c))
+
+
+@pytest.mark.parametrize("kw", [dict(lens=[9000], new=[64], H=8), dict(lens=[3000, 700, 2100], new=[300, 500, 41], H=2, window=600, sinks=5, rep=7, page=16),
+                                dict(lens=[4000, 900], new=[60, 900], H=2, d=64, page=16)])
+def test_many_calls_in_a_row(kw):
+    """No wait of the pipelines gives up, and every call gives the same bits, over many calls on two
+    caches in turn (copies land in any order)."""
+    base = dict(dtype="bf16", d=128, rep=4, page=64)
+    base.update(kw)
+    cases = [_case(**base, seed=s) for s in (21, 22)]
+    state = []
+    for c in cases:
+        pages = cg.Pages(n_pages=c["pool"].shape[1], page=c["page"], H=c["H"], d=c["d"], n_req=len(c["lens"]), max_pages=c["table"].shape[1])
+        how = cg.PagedAttention(c["rep"], int(np.diff(c["cu"]).max()), c["d"] ** -0.5, c["window"], c["sinks"])
+        q = c["q"].cuda()
+        state.append((pages, how, q, c["pool"].cuda(), i32(c["table"]), i32(c["lens"]), i32(c["cu"]), torch.empty_like(q), torch.empty(q.shape[:2], device="cuda")))
+        cg.paged_attention(*state[-1])
+    first = [(s[7].clone(), s[8].clone()) for s in state]
+    for k in range(400):
+        cg.paged_attention(*state[k % 2])
+        if k % 40 > 37:
+            assert torch.equal(state[k % 2][7], first[k % 2][0]) and torch.equal(state[k % 2][8], first[k % 2][1])
+    assert cg.get_status() == 0
+    for c, f in zip(cases, first):
+        _check(c, *f)
