@@ -53,7 +53,7 @@ struct SmemOptIn {
 // Tensor map of the pool with boxes of box_rows tokens x 64 channels.
 bool paged_pool_map(CUtensorMap* map, const PagedArgs& a, uint32_t box_rows);
 
-// Requests of at least min_rows query rows on the tensor cores (d = 64, 128).
+// Requests of at least min_rows query rows on the tcgen05 tiles.
 size_t paged_chunk_workspace(int d);
 cudaError_t launch_paged_chunk(const PagedArgs& a, int min_rows, void* workspace, cudaStream_t st);
 

@@ -664,11 +664,6 @@ size_t rows_workspace(int d) {
     return n * 2 * part_floats(d) * sizeof(float) + n * sizeof(Meta);
 }
 
-// Requests of at most this many query rows run in 16-row tiles here, longer ones on the 128-row
-// tensor-core tiles of cg_paged_chunk.cu. d = 256 does not fit those (tensor memory holds two
-// 128 x 256 accumulators and nothing else).
-int rows_limit(int d) { return d == 256 ? 0x7fffffff : kRows; }
-
 }  // namespace
 
 // Tensor map of the pool as [2 n_pages][H page][d], boxes of box_rows x 64 channels, 128-byte swizzle.
@@ -687,13 +682,13 @@ bool paged_pool_map(CUtensorMap* map, const PagedArgs& a, uint32_t box_rows) {
 // The two kernels follow one another on the stream, so they share the workspace.
 size_t paged_attn_workspace(const PagedArgs& a) {
     const size_t r = rows_workspace(a.d);
-    if ((int64_t)a.max_new * a.n_rep <= rows_limit(a.d)) return r;
+    if ((int64_t)a.max_new * a.n_rep <= kRows) return r;
     const size_t c = paged_chunk_workspace(a.d);
     return r > c ? r : c;
 }
 
 cudaError_t launch_paged_attn(const PagedArgs& a, void* workspace, cudaStream_t st) {
-    const int limit = rows_limit(a.d);
+    const int limit = kRows;   // longer requests run on the 128-row tiles of cg_paged_chunk.cu
     const bool long_ones = (int64_t)a.max_new * a.n_rep > limit;
     cudaError_t e = cudaSuccess;
     // one request that may be long: the rows kernel is still needed where it may turn out short

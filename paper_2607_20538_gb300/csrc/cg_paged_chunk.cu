@@ -37,13 +37,16 @@ namespace {
 using namespace paged;
 
 constexpr int kHalfRows = 128;    // rows of a half: as many whole tokens (of n_rep rows) as fit
-constexpr int kTileRows = 256;
+// Tensor memory (512 columns of 128 rows) holds scores and accumulators: two halves of 128 + d columns
+// for d <= 128; for d = 256 one half with two score buffers.
+constexpr int halves(int d) { return d == 256 ? 1 : 2; }
+constexpr int tile_rows(int d) { return halves(d) * kHalfRows; }
 constexpr int kKT = 128;          // tokens of a key tile
 constexpr int kChunkThreads = 384;
 constexpr int kMaxStages = 8;
 
-// One part: O as [d / 4][256 rows][4], then reference and sum of each row.
-constexpr int chunk_part_floats(int d) { return kTileRows * d + 2 * kTileRows; }
+// One part: O as [d / 4][rows of a tile][4], then reference and sum of each row.
+constexpr int chunk_part_floats(int d) { return tile_rows(d) * (d + 2); }
 
 struct ChunkMeta {
     int last;            // last CTA with a part of the tile that starts here, or -1: none
@@ -54,10 +57,12 @@ template <int D>
 struct ChunkSmem {
     static constexpr int kStages = D == 64 ? 8 : 5;
     static constexpr uint32_t kPiece = kKT * 128;                 // 128 rows x 64 channels
-    static constexpr uint32_t kStage = kKT * D * 2;               // one key or value tile
+    static constexpr int kCh = D < 128 ? D : 128;                 // channels of a stage
+    static constexpr int kParts = D / kCh;                        // stages of a key or value tile
+    static constexpr uint32_t kStage = kKT * kCh * 2;
     static constexpr uint32_t kQ = kHalfRows * D * 2;             // one half's queries
     static constexpr uint32_t q = 0;
-    static constexpr uint32_t stages = 2 * kQ;
+    static constexpr uint32_t stages = halves(D) * kQ;
     static constexpr uint32_t misc = stages + kStages * kStage;
     static constexpr uint32_t total = misc + 512;
     static_assert(total <= 232448, "shared memory budget");
@@ -65,7 +70,7 @@ struct ChunkSmem {
 
 struct ChunkMisc {
     uint64_t full[kMaxStages], empty[kMaxStages];
-    uint64_t sfull[2], pfull[2][2], ofull[2], qfull[2], qempty[2], vok[4], drain[2];
+    uint64_t sfull[2], pfull[2][2], ofull[2], qfull[2], qempty[2], vok[4], drain[2], pvdone;
     int64_t warp_sum[kChunkThreads / 32];
     int start[4];            // request, head, tile, key tile of the share's beginning
     int special[4];          // the inspected tile held special values
@@ -83,6 +88,7 @@ struct ChunkParams {
     int min_rows;      // requests with fewer query rows are left to the other kernel
     int min_share;     // key tiles
     int half_tok;      // tokens of a half: 128 / n_rep
+    int tile_tok;      // tokens of a work tile
     int box_rows;
     int q_boxes;       // the queries of a half are whole boxes of qmap
 };
@@ -121,7 +127,7 @@ __device__ __forceinline__ Span span_of(const PagedArgs& a, const Request& r, in
 }
 
 __device__ __forceinline__ Tiles tile_tiles(const ChunkParams& P, const Request& r, int m) {
-    const int tok = m * 2 * P.half_tok, left = r.n - tok, n = left < 2 * P.half_tok ? left : 2 * P.half_tok;
+    const int tok = m * P.tile_tok, left = r.n - tok, n = left < P.tile_tok ? left : P.tile_tok;
     return visible_tiles<kKT>(P.a.window, P.a.sinks, r.len - r.n + tok, r.len - r.n + tok + n - 1);
 }
 
@@ -131,7 +137,7 @@ constexpr int kTileCost = 3;
 
 __device__ __forceinline__ int row_tiles(const ChunkParams& P, const Request& r) {
     const int64_t rows = (int64_t)r.n * P.a.n_rep;
-    return r.n <= 0 || rows < P.min_rows ? 0 : (r.n + 2 * P.half_tok - 1) / (2 * P.half_tok);
+    return r.n <= 0 || rows < P.min_rows ? 0 : (r.n + P.tile_tok - 1) / P.tile_tok;
 }
 
 // Cost of one KV head of each lane's request. All lanes call: requests of many tiles are summed by
@@ -548,7 +554,7 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
     if (tid == 0) {
         for (int s = 0; s < L::kStages; s++) {
             mbar_init(&M->full[s], 1);
-            mbar_init(&M->empty[s], 2);
+            mbar_init(&M->empty[s], halves(D));
         }
         for (int x = 0; x < 2; x++) {
             mbar_init(&M->sfull[x], 1);
@@ -561,6 +567,7 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
             M->accum0[x] = 0;
         }
         for (int s = 0; s < 4; s++) mbar_init(&M->vok[s], 1);
+        mbar_init(&M->pvdone, 1);
         M->turn = 0;
         M->abort_flag = (smem_u32(smem) & 1023u) != 0;   // the swizzle needs the alignment asked for
         fence_barrier_init();
@@ -623,11 +630,12 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
     w.start(P, M->start, begin < end ? (int)(end - begin) : 0);
     const uint32_t kS = tmem, kO = tmem + 256;
 
-    if (warp < 8) {
+    constexpr bool kOne = halves(D) == 1;
+    if (warp < 4 * halves(D)) {
         // ------------------------------------------------------------ softmax
         const int x = warp >> 2;
         const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16;
-        const uint32_t s_tm = kS + x * 128 + lanes, o_tm = kO + x * D + lanes;
+        const uint32_t o_tm = kO + x * D + lanes;
         // a scale of 0 becomes the least number, so that a masked -inf stays one
         const float sl2 = fmaxf(fabsf(a.scale) * kLog2e, 1.17549435e-38f);
         constexpr float kBias = Weights<FP16>::kBias;
@@ -635,15 +643,15 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
         bool head_part = w.left > 0 && w.c > 0, dead = *abort_flag != 0;
         int meta_last = -1;
         while (w.left > 0 && !dead) {
-            const int tok = (2 * w.m + x) * P.half_tok;   // the half's first new token
-            const Span sp = span_of(a, w.r, tok, P.half_tok), item = span_of(a, w.r, 2 * w.m * P.half_tok, 2 * P.half_tok);
+            const int tok = w.m * P.tile_tok + x * P.half_tok;   // the half's first new token
+            const Span sp = span_of(a, w.r, tok, P.half_tok), item = span_of(a, w.r, w.m * P.tile_tok, P.tile_tok);
             const int take = w.take;
             if (!head_part && w.goes_on) {   // it starts here and goes on
                 meta_last = (int)(blockIdx.x + (w.rest + share - 1) / share);
                 if (tid == 0) {
                     ChunkMeta* m = P.meta + blockIdx.x;
                     m->last = meta_last;
-                    m->tok0 = w.r.tok0 + 2 * w.m * P.half_tok;
+                    m->tok0 = w.r.tok0 + w.m * P.tile_tok;
                     m->n_tok = item.p1 - item.p0 + 1;
                     m->h = w.h;
                 }
@@ -658,11 +666,20 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                 for (int kc = 0; kc < take; kc++) {
                     const int id = w.t.id(w.c + kc);
                     if (!sp.sees(id)) continue;
-                    if (!__all_sync(0xffffffffu, mbar_wait(&M->sfull[x], ns & 1, abort_flag, a.wait_ns))) {
+                    // scores and weights: one buffer a half, or (one half) two in turn
+                    const int buf = kOne ? ns & 1 : x, turn = kOne ? ns >> 1 : ns;
+                    const uint32_t s_tm = kS + buf * 128 + lanes;
+                    if (!__all_sync(0xffffffffu, mbar_wait(&M->sfull[buf], turn & 1, abort_flag, a.wait_ns))) {
                         dead = true;
                         break;
                     }
                     ns++;
+                    // O is quiescent once the last step's product is done. With one buffer the scores
+                    // came after it; with two it is waited for where O is touched.
+                    auto quiet = [&]() {
+                        if (kOne && started && !__all_sync(0xffffffffu, mbar_wait(&M->pvdone, ns & 1, abort_flag, a.wait_ns))) dead = true;
+                        return !dead;
+                    };
                     tc_fence_after();
                     const int t0 = id * kKT;
                     if (!sp.sees_all(id)) mask_row(s_tm, a.window ? pos - a.window + 1 - t0 : 0, pos - t0, a.sinks - t0);
@@ -673,6 +690,7 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                         // never 0 x inf in O: a factor below all numbers becomes the least one
                         const float f = ref == nr ? 1.0f : fmaxf(ex2(ref - nr), 1.17549435e-38f);
                         if (started) {
+                            if (!quiet()) break;
 #pragma unroll 1
                             for (int c0 = 0; c0 < D; c0 += 16) tmem_scale16(o_tm + c0, f);
                         }
@@ -681,12 +699,15 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                     }
                     if (!item.sees_all(id)) {
                         // the inspected value tile held special values: add those the row sees
-                        const int nth = nv + kc;
-                        if (!__all_sync(0xffffffffu, mbar_wait(&M->vok[nth & 3], (nth >> 2) & 1, abort_flag, a.wait_ns))) {
-                            dead = true;
-                            break;
+                        int special = 0;
+                        for (int c = 0; c < L::kParts && !dead; c++) {
+                            const int nth = (nv + kc) * L::kParts + c;
+                            if (!__all_sync(0xffffffffu, mbar_wait(&M->vok[nth & 3], (nth >> 2) & 1, abort_flag, a.wait_ns))) dead = true;
+                            special |= *(volatile int*)&M->special[nth & 3];
                         }
-                        if (*(volatile int*)&M->special[nth & 3]) {
+                        if (dead) break;
+                        if (special) {
+                            if (!quiet()) break;
                             add_special<FP16, D>(a, w.r, w.i, w.h, item, t0, pos, o_tm, !started);
                             if (!started && lane == 0) *(volatile int*)&M->accum0[x] = 1;
                         }
@@ -703,7 +724,7 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                     tmem_wait_st();
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(&M->pfull[x][0]);
+                    if (lane == 0) mbar_arrive(&M->pfull[buf][0]);
                     tmem_ld32f(s_tm + 96, v);
                     tmem_wait_ld();
                     settle(u);
@@ -713,7 +734,7 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                     tmem_wait_st();
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(&M->pfull[x][1]);
+                    if (lane == 0) mbar_arrive(&M->pfull[buf][1]);
                     sum += (acc0.x + acc0.y) + (acc1.x + acc1.y);
                 }
                 if (dead) break;
@@ -761,13 +782,13 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                         if (have) {
 #pragma unroll
                             for (int k = 0; k < 8; k++)
-                                reinterpret_cast<uint4*>(part)[(c0 / 4 + k) * kTileRows + r] =
+                                reinterpret_cast<uint4*>(part)[(c0 / 4 + k) * tile_rows(D) + r] =
                                     started ? make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]) : make_uint4(0, 0, 0, 0);
                         }
                     }
                     if (have) {
-                        part[kTileRows * D + r] = ref;
-                        part[kTileRows * D + kTileRows + r] = sum;
+                        part[tile_rows(D) * D + r] = ref;
+                        part[tile_rows(D) * (D + 1) + r] = sum;
                     }
                 }
             }
@@ -807,35 +828,43 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                     }
                     return pg;
                 };
-                int now = look(0), ahead = 0;
-                for (int kc = 0; kc < take && !dead; kc++) {
-                    const int in = kc % group;
-                    if (in == 0) {
-                        if (kc) now = ahead;
-                        ahead = look(kc + group);
-                    }
-                    const int pg = __shfl_sync(0xffffffffu, now, (in * n_box + lane) & 31);
+                int now = look(0), ahead = look(group), base = 0;   // base: first tile of `now`
+                // the stages of the keys (kv = 0) or values of tile kc
+                auto load = [&](int kc, int kv) {
+                    const int in = kc - base;
+                    const int pg = __shfl_sync(0xffffffffu, in < group ? now : ahead, ((in % group) * n_box + lane) & 31);
                     const int t = w.t.id(w.c + kc) * kKT + lane * P.box_rows;
-                    const int z = pg < 0 ? 2 * a.n_pages : pg, y = pg < 0 ? 0 : w.h * a.page + (t & (a.page - 1));
+                    const int z = pg < 0 ? 2 * a.n_pages : kv ? pg + a.n_pages : pg, y = pg < 0 ? 0 : w.h * a.page + (t & (a.page - 1));
 #pragma unroll
-                    for (int kv = 0; kv < 2; kv++) {
-                        if (!__all_sync(0xffffffffu, mbar_wait(&M->empty[st], ph, abort_flag, a.wait_ns))) {
+                    for (int c = 0; c < L::kParts; c++) {
+                        if (dead || !__all_sync(0xffffffffu, mbar_wait(&M->empty[st], ph, abort_flag, a.wait_ns))) {
                             dead = true;
-                            break;
+                            return;
                         }
                         if (lane == 0) mbar_arrive_expect_tx(&M->full[st], L::kStage);
                         __syncwarp();
                         if (lane < n_box) {
                             unsigned char* dst = smem + L::stages + st * L::kStage + lane * P.box_rows * 128;
-                            const int zz = kv && pg >= 0 ? z + a.n_pages : z;
 #pragma unroll
-                            for (int hf = 0; hf < D / 64; hf++) tma_load_3d(dst + hf * L::kPiece, &map, &M->full[st], hf * 64, y, zz);
+                            for (int hf = 0; hf < L::kCh / 64; hf++)
+                                tma_load_3d(dst + hf * L::kPiece, &map, &M->full[st], c * L::kCh + hf * 64, y, z);
                         }
                         issued++;
                         if (++st == L::kStages) {
                             st = 0;
                             ph ^= 1;
                         }
+                    }
+                };
+                if (kOne) load(0, 0);   // with two score buffers the keys are one tile ahead
+                for (int kc = 0; kc < take && !dead; kc++) {
+                    if (!kOne) load(kc, 0);
+                    else if (kc + 1 < take) load(kc + 1, 0);
+                    load(kc, 1);
+                    if (kc + 1 - base == group) {
+                        base += group;
+                        now = ahead;
+                        ahead = look(base + group);
                     }
                 }
                 w.next(P);
@@ -847,19 +876,21 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                 for (int k = issued > L::kStages ? issued - L::kStages : 0; k < issued; k++)
                     mbar_wait(&M->full[k % L::kStages], (k / L::kStages) & 1, &zero, tc::kWaitLimitNs);
             }
-        } else if (warp < 11) {
+        } else if (warp == 9 || (warp == 10 && !kOne)) {
             // -------------------------------------------------------- MMA issuer of one half
+            // One half alone (d = 256): S(0) S(1) PV(0) S(2) PV(1) ..., the next scores in the other
+            // buffer while a step's softmax runs; its step takes as long as the products.
             // The whole warp walks and waits, so that descriptors stay in uniform registers; one
             // thread issues. Everything a step needs is waited for ahead of the weights.
             const int x = warp - 9;
             const bool issue = elect_one();
             const uint32_t idesc_s = idesc16<FP16>(128, kKT) | (a.scale < 0.0f ? kIdescNegateA : 0u);
-            constexpr uint32_t idesc_o = idesc16<FP16>(128, D) | kIdescBMnMajor;
+            constexpr uint32_t idesc_o = idesc16<FP16>(128, L::kCh) | kIdescBMnMajor;
             const uint64_t qd = sdesc_sw128(smem_u32(smem + L::q)), kd = sdesc_sw128(smem_u32(smem + L::stages));
             const uint64_t vd = sdesc_sw128_mn(smem_u32(smem + L::stages), L::kPiece, 1024u);
             const uint32_t al = (uint32_t)qd + ((x * L::kQ) >> 4), k_lo = (uint32_t)kd, hi = (uint32_t)(kd >> 32);
             const uint32_t v_lo = (uint32_t)vd, v_hi = (uint32_t)(vd >> 32);
-            const uint32_t sx = kS + x * 128, ox = kO + x * D;
+            const uint32_t ox = kO + x * D;
             int st = 0, ph = 0;                // ring position of the next tile to wait for
             int np = 0, nq = 0, nv = 0;
             bool dead = *abort_flag != 0;
@@ -867,86 +898,144 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                 if (!__all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, a.wait_ns))) dead = true;
                 return !dead;
             };
-            while (w.left > 0 && !dead) {
-                const Span sp = span_of(a, w.r, (2 * w.m + x) * P.half_tok, P.half_tok);
-                const int take = w.take;
-                bool first = true, prev = false;
-                int vst = 0, vph = 0;
-                if (sp.n > 0 && !wait(&M->qfull[x], nq & 1)) break;
-                for (int j = 0; j <= take; j++) {
-                    // keys of step j at ring slot kst; values of step j - 1 at vst
-                    const int id = j < take ? w.t.id(w.c + j) : 0;
-                    const int kst = st;
-                    const bool next = j < take && sp.sees(id);
-                    if (j > 0) {   // landed, and inspected
-                        const int v = nv + j - 1;
-                        if (!wait(&M->full[vst], vph) || !wait(&M->vok[v & 3], (v >> 2) & 1)) break;
-                    }
-                    if (j < take && !wait(&M->full[kst], ph)) break;
-                    const uint32_t bv = v_lo + ((vst * L::kStage) >> 4), bk = k_lo + ((kst * L::kStage) >> 4);
-                    uint32_t acc = first ? 0u : 1u;
-                    if (prev) {
-                        if (!wait(&M->pfull[x][0], np & 1)) break;
-                        tc_fence_after();
-                        if (first && *(volatile int*)&M->accum0[x]) {
-                            acc = 1u;
-                            __syncwarp();
-                            *(volatile int*)&M->accum0[x] = 0;
-                        }
-                        first = false;
-                        if (issue) {
+            int ns = 0;                        // scores issued (np: products)
+            bool first = true;                 // of the tile's products
+            auto advance = [&]() {
+                if (++st == L::kStages) {
+                    st = 0;
+                    ph ^= 1;
+                }
+            };
+            // Scores of the keys at the ring's position into their buffer; the stages are released.
+            // Where the half sees nothing of the tile the stages are only waited for.
+            auto scores = [&](bool go, bool last) {
+                const int buf = kOne ? ns & 1 : x;
 #pragma unroll
-                            for (int k = 0; k < kKT / 32; k++)
-                                mma_ts(ox, sx + 8 * k, bv + ((k * 2048) >> 4), v_hi, idesc_o, k ? 1u : acc);
-                        }
-                        // taken before the rest of the weights are there, which hides the atomic
-                        if (!take_turn(&M->turn, issue, abort_flag, a.wait_ns)) {
-                            dead = true;
-                            break;
-                        }
-                        if (!wait(&M->pfull[x][1], np & 1)) break;
-                        np++;
-                    }
+                for (int c = 0; c < L::kParts; c++) {
+                    if (!wait(&M->full[st], ph)) return;
                     tc_fence_after();
+                    const uint32_t bk = k_lo + ((st * L::kStage) >> 4);
                     if (issue) {
-                        if (prev) {
+                        if (go) {
 #pragma unroll
-                            for (int k = kKT / 32; k < kKT / 16; k++)
-                                mma_ts(ox, sx + 8 * k, bv + ((k * 2048) >> 4), v_hi, idesc_o, 1u);
-                        }
-                        if (next) {
-#pragma unroll
-                            for (int k = 0; k < D / 16; k++) {
+                            for (int k = 0; k < L::kCh / 16; k++) {
                                 const uint32_t o = ((k >> 2) * L::kPiece + (k & 3) * 32) >> 4;
-                                mma_ss(sx, al + o, bk + o, hi, idesc_s, k ? 1u : 0u);
+                                mma_ss(kS + buf * 128, al + ((c * L::kCh / 64 * L::kPiece) >> 4) + o, bk + o, hi, idesc_s, c + k ? 1u : 0u);
                             }
-                            mma_commit(&M->sfull[x]);
+                            if (c == L::kParts - 1) mma_commit(&M->sfull[buf]);
                         }
-                        if (prev) *(volatile int*)&M->turn = 0;
-                        if (j == take - 1 && sp.n > 0) mma_commit(&M->qempty[x]);   // the queries were read
-                        if (j > 0) mma_commit(&M->empty[vst]);
-                        if (j < take) mma_commit(&M->empty[kst]);
-                        // only where the softmax had its turn: it could otherwise miss one of two
-                        if (j == take && !first) mma_commit(&M->ofull[x]);
+                        if (last && c == L::kParts - 1) mma_commit(&M->qempty[x]);   // the queries were read
+                        mma_commit(&M->empty[st]);
                     }
                     __syncwarp();
-                    prev = next;
-                    if (j < take) {
-                        if (++st == L::kStages) {
-                            st = 0;
-                            ph ^= 1;
+                    advance();
+                }
+                if (go) ns++;
+            };
+            // O += P V with the values at stages vst ...; in two steps, as the weights come.
+            auto products = [&](int vst, uint32_t half, int buf) {
+#pragma unroll
+                for (int c = 0; c < L::kParts; c++) {
+                    const uint32_t bv = v_lo + (((vst + c) % L::kStages * L::kStage) >> 4);
+                    const bool clear = first && half == 0;
+#pragma unroll
+                    for (int k = 0; k < kKT / 32; k++)
+                        mma_ts(ox + c * L::kCh, kS + buf * 128 + 8 * (k + half * (kKT / 32)), bv + (((k + half * (kKT / 32)) * 2048) >> 4), v_hi,
+                               idesc_o, clear && k == 0 ? 0u : 1u);
+                }
+            };
+            // Waits for the values at the ring's position: landed, and inspected.
+            auto values = [&]() {
+#pragma unroll
+                for (int c = 0; c < L::kParts; c++) {
+                    const int vs = (st + c) % L::kStages, vp = st + c >= L::kStages ? ph ^ 1 : ph;
+                    if (!wait(&M->full[vs], vp) || !wait(&M->vok[nv & 3], (nv >> 2) & 1)) return;
+                    nv++;
+                }
+            };
+            // First half of the weights of the next product.
+            auto product0 = [&](int vst) {
+                const int buf = kOne ? np & 1 : x, turn = kOne ? np >> 1 : np;
+                if (!wait(&M->pfull[buf][0], turn & 1)) return;
+                tc_fence_after();
+                if (first && *(volatile int*)&M->accum0[x]) {   // the softmax has put something into O
+                    __syncwarp();
+                    *(volatile int*)&M->accum0[x] = 0;
+                    first = false;
+                }
+                if (issue) products(vst, 0, buf);
+                first = false;
+            };
+            while (w.left > 0 && !dead) {
+                const Span sp = span_of(a, w.r, w.m * P.tile_tok + x * P.half_tok, P.half_tok);
+                const int take = w.take;
+                bool prev = false, any = false;
+                first = true;
+                if (sp.n > 0 && !wait(&M->qfull[x], nq & 1)) break;
+                if (kOne) {
+                    const bool go = sp.s1 > 0;   // rows that see any tile see all of the tile's list
+                    scores(go, sp.n > 0 && take == 1);
+                    for (int j = 0; j < take && !dead; j++) {
+                        // keys of step j + 1 are ahead of the values of step j in the ring
+                        if (j + 1 < take) scores(go, sp.n > 0 && j + 2 == take);
+                        if (dead) break;
+                        const int vst = st;
+                        values();
+                        if (dead) break;
+                        if (go) {
+                            product0(vst);
+                            if (dead || !wait(&M->pfull[np & 1][1], (np >> 1) & 1)) break;
+                            tc_fence_after();
+                            if (issue) {
+                                products(vst, 1, np & 1);
+                                mma_commit(&M->pvdone);
+                            }
+                            np++;
+                            any = true;
                         }
-                        vst = st;   // the values follow the keys
-                        vph = ph;
-                        if (++st == L::kStages) {
-                            st = 0;
-                            ph ^= 1;
+                        if (issue) {
+#pragma unroll
+                            for (int c = 0; c < L::kParts; c++) mma_commit(&M->empty[(vst + c) % L::kStages]);
                         }
+                        __syncwarp();
+#pragma unroll
+                        for (int c = 0; c < L::kParts; c++) advance();
+                    }
+                } else {
+                    for (int j = 0; j <= take; j++) {
+                        // the values of step j - 1 at vst, then the keys of step j
+                        const bool next = j < take && sp.sees(w.t.id(w.c + j));
+                        const int vst = st;
+                        if (j > 0) {
+                            values();
+                            advance();
+                        }
+                        if (dead || (j < take && !wait(&M->full[st], ph))) break;   // ahead of the weights
+                        if (prev) {
+                            product0(vst);
+                            // taken before the rest of the weights are there, which hides the atomic
+                            if (dead || !take_turn(&M->turn, issue, abort_flag, a.wait_ns)) {
+                                dead = true;
+                                break;
+                            }
+                            if (!wait(&M->pfull[x][1], np & 1)) break;
+                            np++;
+                            any = true;
+                            tc_fence_after();
+                            if (issue) products(vst, 1, x);
+                        }
+                        if (j > 0 && issue) mma_commit(&M->empty[vst]);
+                        if (j < take) scores(next, sp.n > 0 && j == take - 1);
+                        if (issue && prev) *(volatile int*)&M->turn = 0;
+                        __syncwarp();
+                        if (dead) break;
+                        prev = next;
                     }
                 }
                 if (dead) break;
+                // only where the softmax had its turn: it could otherwise miss one of two
+                if (any && issue) mma_commit(&M->ofull[x]);
                 if (sp.n > 0) nq++;
-                nv += take;
                 w.next(P);
             }
             if (dead) *abort_flag = 1;
@@ -954,16 +1043,16 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
             const int zero = 0;
             mbar_wait(&M->drain[x], 0, &zero, tc::kWaitLimitNs);
             __syncwarp();
-        } else {
+        } else if (warp == 11) {
             // -------------------------------------------------------- queries, and inspector of values
             // (one warp: a tile's queries are loaded once the last tile's values are inspected)
             int st = 0, ph = 0, nv = 0, nq[2] = {0, 0};
             bool dead = *abort_flag != 0, q_bytes = false;
             while (w.left > 0 && !dead) {
-                const Span item = span_of(a, w.r, 2 * w.m * P.half_tok, 2 * P.half_tok);
+                const Span item = span_of(a, w.r, w.m * P.tile_tok, P.tile_tok);
                 const int take = w.take;
-                for (int x = 0; x < 2 && !dead; x++) {
-                    const int tok = (2 * w.m + x) * P.half_tok;
+                for (int x = 0; x < halves(D) && !dead; x++) {
+                    const int tok = w.m * P.tile_tok + x * P.half_tok;
                     const Span sp = span_of(a, w.r, tok, P.half_tok);
                     if (sp.n <= 0) continue;
                     if (!__all_sync(0xffffffffu, mbar_wait(&M->qempty[x], (nq[x] & 1) ^ 1, abort_flag, a.wait_ns))) {
@@ -1004,22 +1093,34 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                     if (lane == 0) mbar_arrive(&M->qfull[x]);
                 }
                 if (dead) break;
-                for (int kc = 0; kc < take; kc++, nv++) {
-                    // Every use of a stage is waited for, the keys' too: a wait tells only even from
-                    // odd uses, and the values' copy may land before the keys that used the stage.
-                    for (int kv = 0; kv < 2 && !dead; kv++) {
-                        if (kv && ++st == L::kStages) {
-                            st = 0;
-                            ph ^= 1;
-                        }
-                        if (!__all_sync(0xffffffffu, mbar_wait(&M->full[st], ph, abort_flag, a.wait_ns))) dead = true;
+                // Every use of a stage is waited for, the keys' too: a wait tells only even from odd
+                // uses, and the values' copy may land before the keys that used the stage.
+                auto landed = [&]() {
+                    if (!dead && !__all_sync(0xffffffffu, mbar_wait(&M->full[st], ph, abort_flag, a.wait_ns))) dead = true;
+                };
+                auto past = [&]() {
+                    if (++st == L::kStages) {
+                        st = 0;
+                        ph ^= 1;
                     }
+                };
+                auto past_keys = [&]() {
+                    for (int c = 0; c < L::kParts; c++) {
+                        landed();
+                        past();
+                    }
+                };
+                if (kOne) past_keys();
+                for (int kv = 0; kv < take * L::kParts; kv++, nv++) {
+                    const int kc = kv / L::kParts;
+                    if (kv % L::kParts == 0 && (!kOne || kc + 1 < take)) past_keys();
+                    landed();
                     if (dead) break;
                     const int id = w.t.id(w.c + kc), t0 = id * kKT;
                     int found = 0;
                     if (!item.sees_all(id)) {
                         unsigned char* tile = smem + L::stages + st * L::kStage;
-                        constexpr int kPer = D / 8, kStep = 32 / kPer;
+                        constexpr int kPer = L::kCh / 8, kStep = 32 / kPer;
                         const int ch = lane % kPer, r0 = lane / kPer;
                         auto at = [&](int r) {
                             return reinterpret_cast<uint4*>(tile + (ch >> 3) * L::kPiece + r * 128 + (((ch & 7) ^ (r & 7)) << 4));
@@ -1063,17 +1164,15 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                         *(volatile int*)&M->special[nv & 3] = found;
                         mbar_arrive(&M->vok[nv & 3]);
                     }
-                    if (++st == L::kStages) {
-                        st = 0;
-                        ph ^= 1;
-                    }
+                    past();
                 }
+                if (dead) break;
                 w.next(P);
             }
             if (dead) *abort_flag = 1;
             if (q_bytes && *abort_flag) {   // boxes in flight land before the CTA ends
                 const int zero = 0;
-                for (int x = 0; x < 2; x++)
+                for (int x = 0; x < halves(D); x++)
                     if (nq[x]) mbar_wait(&M->qfull[x], (nq[x] - 1) & 1, &zero, tc::kWaitLimitNs);
             }
         }
@@ -1089,7 +1188,7 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
 // Joins the parts of the tile that starts in CTA b's share. A thread owns a row and 8 channels
 // (blockIdx.y): its parts' references, then one pass over the parts.
 template <bool FP16, int D>
-__global__ void __launch_bounds__(kTileRows) paged_chunk_merge_kernel(const __grid_constant__ ChunkParams P) {
+__global__ void __launch_bounds__(tile_rows(D)) paged_chunk_merge_kernel(const __grid_constant__ ChunkParams P) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const PagedArgs& a = P.a;
     const ChunkMeta m = P.meta[blockIdx.x];
@@ -1100,7 +1199,7 @@ __global__ void __launch_bounds__(kTileRows) paged_chunk_merge_kernel(const __gr
     const int parts = m.last - (int)blockIdx.x + 1;
     auto part = [&](int p) { return P.parts + ((int64_t)(blockIdx.x + p) * 2 + (p == 0 ? 1 : 0)) * chunk_part_floats(D); };
     float R = -INFINITY;
-    for (int p = 0; p < parts; p++) R = fmaxf(R, part(p)[kTileRows * D + row]);
+    for (int p = 0; p < parts; p++) R = fmaxf(R, part(p)[tile_rows(D) * D + row]);
     const float Rs = R == -INFINITY ? 0.0f : R;
     float l = 0.0f, o[8];
 #pragma unroll
@@ -1108,11 +1207,11 @@ __global__ void __launch_bounds__(kTileRows) paged_chunk_merge_kernel(const __gr
 #pragma unroll 4
     for (int p = 0; p < parts; p++) {
         const float* src = part(p);
-        const float ref = src[kTileRows * D + row];
+        const float ref = src[tile_rows(D) * D + row];
         const float f = ref == -INFINITY ? 0.0f : fmaxf(ex2(ref - Rs), 1.17549435e-38f);
-        l += f * src[kTileRows * D + kTileRows + row];
-        const float4 u = reinterpret_cast<const float4*>(src)[(2 * blockIdx.y) * kTileRows + row];
-        const float4 v = reinterpret_cast<const float4*>(src)[(2 * blockIdx.y + 1) * kTileRows + row];
+        l += f * src[tile_rows(D) * (D + 1) + row];
+        const float4 u = reinterpret_cast<const float4*>(src)[(2 * blockIdx.y) * tile_rows(D) + row];
+        const float4 v = reinterpret_cast<const float4*>(src)[(2 * blockIdx.y + 1) * tile_rows(D) + row];
         o[0] += f * u.x;
         o[1] += f * u.y;
         o[2] += f * u.z;
@@ -1165,7 +1264,7 @@ cudaError_t launch_chunk(ChunkParams P, cudaStream_t st) {
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(grid, D / 8);
-    cfg.blockDim = dim3(kTileRows);
+    cfg.blockDim = dim3(tile_rows(D));
     cfg.stream = st;
     cudaLaunchAttribute at{};
     at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -1190,9 +1289,11 @@ cudaError_t launch_paged_chunk(const PagedArgs& a, int min_rows, void* workspace
     P.min_rows = min_rows;
     P.min_share = 4;
     P.half_tok = kHalfRows / a.n_rep;
+    P.tile_tok = halves(a.d) * P.half_tok;
     P.box_rows = a.page < kKT ? a.page : kKT;
     const bool h = a.dtype == CG_FP16;
     if (a.d == 64) return h ? launch_chunk<true, 64>(P, st) : launch_chunk<false, 64>(P, st);
+    if (a.d == 256) return h ? launch_chunk<true, 256>(P, st) : launch_chunk<false, 256>(P, st);
     return h ? launch_chunk<true, 128>(P, st) : launch_chunk<false, 128>(P, st);
 }
 
