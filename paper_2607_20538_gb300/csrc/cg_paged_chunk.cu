@@ -936,7 +936,8 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
             auto products = [&](int vst, uint32_t half, int buf) {
 #pragma unroll
                 for (int c = 0; c < L::kParts; c++) {
-                    const uint32_t bv = v_lo + (((vst + c) % L::kStages * L::kStage) >> 4);
+                    const int vs = kOne ? (vst + c) % L::kStages : vst;
+                    const uint32_t bv = v_lo + ((vs * L::kStage) >> 4);
                     const bool clear = first && half == 0;
 #pragma unroll
                     for (int k = 0; k < kKT / 32; k++)
@@ -948,7 +949,7 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
             auto values = [&]() {
 #pragma unroll
                 for (int c = 0; c < L::kParts; c++) {
-                    const int vs = (st + c) % L::kStages, vp = st + c >= L::kStages ? ph ^ 1 : ph;
+                    const int vs = kOne ? (st + c) % L::kStages : st, vp = kOne && st + c >= L::kStages ? ph ^ 1 : ph;
                     if (!wait(&M->full[vs], vp) || !wait(&M->vok[nv & 3], (nv >> 2) & 1)) return;
                     nv++;
                 }
@@ -1003,14 +1004,17 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                     }
                 } else {
                     for (int j = 0; j <= take; j++) {
-                        // the values of step j - 1 at vst, then the keys of step j
+                        // the values of step j - 1 at vst, then the keys of step j at kst
                         const bool next = j < take && sp.sees(w.t.id(w.c + j));
                         const int vst = st;
                         if (j > 0) {
                             values();
                             advance();
                         }
-                        if (dead || (j < take && !wait(&M->full[st], ph))) break;   // ahead of the weights
+                        const int kst = st;
+                        if (dead || (j < take && !wait(&M->full[kst], ph))) break;
+                        const uint32_t bv = v_lo + ((vst * L::kStage) >> 4), bk = k_lo + ((kst * L::kStage) >> 4);
+                        const uint32_t sx = kS + x * 128;
                         if (prev) {
                             product0(vst);
                             // taken before the rest of the weights are there, which hides the atomic
@@ -1021,14 +1025,29 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                             if (!wait(&M->pfull[x][1], np & 1)) break;
                             np++;
                             any = true;
-                            tc_fence_after();
-                            if (issue) products(vst, 1, x);
                         }
-                        if (j > 0 && issue) mma_commit(&M->empty[vst]);
-                        if (j < take) scores(next, sp.n > 0 && j == take - 1);
-                        if (issue && prev) *(volatile int*)&M->turn = 0;
+                        tc_fence_after();
+                        if (issue) {   // the products' second half and the next scores without a pause
+                            if (prev) {
+#pragma unroll
+                                for (int k = kKT / 32; k < kKT / 16; k++)
+                                    mma_ts(ox, sx + 8 * k, bv + ((k * 2048) >> 4), v_hi, idesc_o, 1u);
+                            }
+                            if (next) {
+#pragma unroll
+                                for (int k = 0; k < D / 16; k++) {
+                                    const uint32_t o = ((k >> 2) * L::kPiece + (k & 3) * 32) >> 4;
+                                    mma_ss(sx, al + o, bk + o, hi, idesc_s, k ? 1u : 0u);
+                                }
+                                mma_commit(&M->sfull[x]);
+                            }
+                            if (prev) *(volatile int*)&M->turn = 0;
+                            if (j == take - 1 && sp.n > 0) mma_commit(&M->qempty[x]);   // the queries were read
+                            if (j > 0) mma_commit(&M->empty[vst]);
+                            if (j < take) mma_commit(&M->empty[kst]);
+                        }
                         __syncwarp();
-                        if (dead) break;
+                        if (j < take) advance();
                         prev = next;
                     }
                 }
