@@ -43,7 +43,6 @@ constexpr int halves(int d) { return d == 256 ? 1 : 2; }
 constexpr int tile_rows(int d) { return halves(d) * kHalfRows; }
 constexpr int kKT = 128;          // tokens of a key tile
 constexpr int kChunkThreads = 384;
-constexpr int kMaxStages = 8;
 
 // One part: O as [d / 4][rows of a tile][4], then reference and sum of each row.
 constexpr int chunk_part_floats(int d) { return tile_rows(d) * (d + 2); }
@@ -55,7 +54,10 @@ struct ChunkMeta {
 
 template <int D>
 struct ChunkSmem {
-    static constexpr int kStages = D == 64 ? 8 : 5;
+    // Keys and values have rings of their own: every stage is then waited for, use by use, by each
+    // warp that reads it and refilled only after all of them (a wait tells only even from odd uses).
+    static constexpr int kKeyStages = D == 64 ? 4 : 2, kValStages = D == 64 ? 4 : 3;
+    static constexpr int kStages = kKeyStages + kValStages;
     static constexpr uint32_t kPiece = kKT * 128;                 // 128 rows x 64 channels
     static constexpr int kCh = D < 128 ? D : 128;                 // channels of a stage
     static constexpr int kParts = D / kCh;                        // stages of a key or value tile
@@ -68,8 +70,20 @@ struct ChunkSmem {
     static_assert(total <= 232448, "shared memory budget");
 };
 
+// A position in a ring of N stages and the parity of its use.
+template <int N>
+struct Ring {
+    int st = 0, ph = 0;
+    __device__ __forceinline__ void next() {
+        if (++st == N) {
+            st = 0;
+            ph ^= 1;
+        }
+    }
+};
+
 struct ChunkMisc {
-    uint64_t full[kMaxStages], empty[kMaxStages];
+    uint64_t kfull[4], kempty[4], vfull[4], vempty[4];
     uint64_t sfull[2], pfull[2][2], ofull[2], qfull[2], qempty[2], vok[4], drain[2], pvdone;
     int64_t warp_sum[kChunkThreads / 32];
     int start[4];            // request, head, tile, key tile of the share's beginning
@@ -552,9 +566,11 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
     }
     if (lane == 31) M->warp_sum[warp] = incl;
     if (tid == 0) {
-        for (int s = 0; s < L::kStages; s++) {
-            mbar_init(&M->full[s], 1);
-            mbar_init(&M->empty[s], halves(D));
+        for (int s = 0; s < 4; s++) {
+            mbar_init(&M->kfull[s], 1);
+            mbar_init(&M->kempty[s], halves(D));
+            mbar_init(&M->vfull[s], 1);
+            mbar_init(&M->vempty[s], halves(D));
         }
         for (int x = 0; x < 2; x++) {
             mbar_init(&M->sfull[x], 1);
@@ -807,7 +823,9 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
             // lane k < n_box carries the boxes of token rows [k box_rows, ...) of a tile
             const int n_box = kKT / P.box_rows;
             int32_t pflag = 0;
-            int st = 0, ph = 1, issued = 0;
+            Ring<L::kKeyStages> kr;
+            Ring<L::kValStages> vr;
+            int ki = 0, vi = 0;      // stages issued
             bool dead = *abort_flag != 0;
             while (w.left > 0 && !dead) {
                 const int wlo = a.window ? w.r.len - w.r.n - a.window + 1 : 0;
@@ -837,22 +855,25 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                     const int z = pg < 0 ? 2 * a.n_pages : kv ? pg + a.n_pages : pg, y = pg < 0 ? 0 : w.h * a.page + (t & (a.page - 1));
 #pragma unroll
                     for (int c = 0; c < L::kParts; c++) {
-                        if (dead || !__all_sync(0xffffffffu, mbar_wait(&M->empty[st], ph, abort_flag, a.wait_ns))) {
+                        uint64_t *full = kv ? &M->vfull[vr.st] : &M->kfull[kr.st], *empty = kv ? &M->vempty[vr.st] : &M->kempty[kr.st];
+                        if (dead || !__all_sync(0xffffffffu, mbar_wait(empty, (kv ? vr.ph : kr.ph) ^ 1, abort_flag, a.wait_ns))) {
                             dead = true;
                             return;
                         }
-                        if (lane == 0) mbar_arrive_expect_tx(&M->full[st], L::kStage);
+                        if (lane == 0) mbar_arrive_expect_tx(full, L::kStage);
                         __syncwarp();
                         if (lane < n_box) {
-                            unsigned char* dst = smem + L::stages + st * L::kStage + lane * P.box_rows * 128;
+                            unsigned char* dst = smem + L::stages + (kv ? L::kKeyStages + vr.st : kr.st) * L::kStage + lane * P.box_rows * 128;
 #pragma unroll
                             for (int hf = 0; hf < L::kCh / 64; hf++)
-                                tma_load_3d(dst + hf * L::kPiece, &map, &M->full[st], c * L::kCh + hf * 64, y, z);
+                                tma_load_3d(dst + hf * L::kPiece, &map, full, c * L::kCh + hf * 64, y, z);
                         }
-                        issued++;
-                        if (++st == L::kStages) {
-                            st = 0;
-                            ph ^= 1;
+                        if (kv) {
+                            vi++;
+                            vr.next();
+                        } else {
+                            ki++;
+                            kr.next();
                         }
                     }
                 };
@@ -873,8 +894,10 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
             if (dead) {   // copies in flight land before the CTA ends
                 *abort_flag = 1;
                 const int zero = 0;
-                for (int k = issued > L::kStages ? issued - L::kStages : 0; k < issued; k++)
-                    mbar_wait(&M->full[k % L::kStages], (k / L::kStages) & 1, &zero, tc::kWaitLimitNs);
+                for (int k = ki > L::kKeyStages ? ki - L::kKeyStages : 0; k < ki; k++)
+                    mbar_wait(&M->kfull[k % L::kKeyStages], (k / L::kKeyStages) & 1, &zero, tc::kWaitLimitNs);
+                for (int k = vi > L::kValStages ? vi - L::kValStages : 0; k < vi; k++)
+                    mbar_wait(&M->vfull[k % L::kValStages], (k / L::kValStages) & 1, &zero, tc::kWaitLimitNs);
             }
         } else if (warp == 9 || (warp == 10 && !kOne)) {
             // -------------------------------------------------------- MMA issuer of one half
@@ -887,11 +910,12 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
             const uint32_t idesc_s = idesc16<FP16>(128, kKT) | (a.scale < 0.0f ? kIdescNegateA : 0u);
             constexpr uint32_t idesc_o = idesc16<FP16>(128, L::kCh) | kIdescBMnMajor;
             const uint64_t qd = sdesc_sw128(smem_u32(smem + L::q)), kd = sdesc_sw128(smem_u32(smem + L::stages));
-            const uint64_t vd = sdesc_sw128_mn(smem_u32(smem + L::stages), L::kPiece, 1024u);
+            const uint64_t vd = sdesc_sw128_mn(smem_u32(smem + L::stages + L::kKeyStages * L::kStage), L::kPiece, 1024u);
             const uint32_t al = (uint32_t)qd + ((x * L::kQ) >> 4), k_lo = (uint32_t)kd, hi = (uint32_t)(kd >> 32);
             const uint32_t v_lo = (uint32_t)vd, v_hi = (uint32_t)(vd >> 32);
             const uint32_t ox = kO + x * D;
-            int st = 0, ph = 0;                // ring position of the next tile to wait for
+            Ring<L::kKeyStages> kr;
+            Ring<L::kValStages> vr;
             int np = 0, nq = 0, nv = 0;
             bool dead = *abort_flag != 0;
             auto wait = [&](uint64_t* bar, int parity) {
@@ -900,21 +924,15 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
             };
             int ns = 0;                        // scores issued (np: products)
             bool first = true;                 // of the tile's products
-            auto advance = [&]() {
-                if (++st == L::kStages) {
-                    st = 0;
-                    ph ^= 1;
-                }
-            };
             // Scores of the keys at the ring's position into their buffer; the stages are released.
             // Where the half sees nothing of the tile the stages are only waited for.
             auto scores = [&](bool go, bool last) {
                 const int buf = kOne ? ns & 1 : x;
 #pragma unroll
                 for (int c = 0; c < L::kParts; c++) {
-                    if (!wait(&M->full[st], ph)) return;
+                    if (!wait(&M->kfull[kr.st], kr.ph)) return;
                     tc_fence_after();
-                    const uint32_t bk = k_lo + ((st * L::kStage) >> 4);
+                    const uint32_t bk = k_lo + ((kr.st * L::kStage) >> 4);
                     if (issue) {
                         if (go) {
 #pragma unroll
@@ -925,10 +943,10 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                             if (c == L::kParts - 1) mma_commit(&M->sfull[buf]);
                         }
                         if (last && c == L::kParts - 1) mma_commit(&M->qempty[x]);   // the queries were read
-                        mma_commit(&M->empty[st]);
+                        mma_commit(&M->kempty[kr.st]);
                     }
                     __syncwarp();
-                    advance();
+                    kr.next();
                 }
                 if (go) ns++;
             };
@@ -936,7 +954,7 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
             auto products = [&](int vst, uint32_t half, int buf) {
 #pragma unroll
                 for (int c = 0; c < L::kParts; c++) {
-                    const int vs = kOne ? (vst + c) % L::kStages : vst;
+                    const int vs = kOne ? (vst + c) % L::kValStages : vst;
                     const uint32_t bv = v_lo + ((vs * L::kStage) >> 4);
                     const bool clear = first && half == 0;
 #pragma unroll
@@ -949,8 +967,8 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
             auto values = [&]() {
 #pragma unroll
                 for (int c = 0; c < L::kParts; c++) {
-                    const int vs = kOne ? (st + c) % L::kStages : st, vp = kOne && st + c >= L::kStages ? ph ^ 1 : ph;
-                    if (!wait(&M->full[vs], vp) || !wait(&M->vok[nv & 3], (nv >> 2) & 1)) return;
+                    const int vs = kOne ? (vr.st + c) % L::kValStages : vr.st, vp = kOne && vr.st + c >= L::kValStages ? vr.ph ^ 1 : vr.ph;
+                    if (!wait(&M->vfull[vs], vp) || !wait(&M->vok[nv & 3], (nv >> 2) & 1)) return;
                     nv++;
                 }
             };
@@ -980,7 +998,7 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                         // keys of step j + 1 are ahead of the values of step j in the ring
                         if (j + 1 < take) scores(go, sp.n > 0 && j + 2 == take);
                         if (dead) break;
-                        const int vst = st;
+                        const int vst = vr.st;
                         values();
                         if (dead) break;
                         if (go) {
@@ -996,23 +1014,23 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                         }
                         if (issue) {
 #pragma unroll
-                            for (int c = 0; c < L::kParts; c++) mma_commit(&M->empty[(vst + c) % L::kStages]);
+                            for (int c = 0; c < L::kParts; c++) mma_commit(&M->vempty[(vst + c) % L::kValStages]);
                         }
                         __syncwarp();
 #pragma unroll
-                        for (int c = 0; c < L::kParts; c++) advance();
+                        for (int c = 0; c < L::kParts; c++) vr.next();
                     }
                 } else {
                     for (int j = 0; j <= take; j++) {
                         // the values of step j - 1 at vst, then the keys of step j at kst
                         const bool next = j < take && sp.sees(w.t.id(w.c + j));
-                        const int vst = st;
+                        const int vst = vr.st;
                         if (j > 0) {
                             values();
-                            advance();
+                            vr.next();
                         }
-                        const int kst = st;
-                        if (dead || (j < take && !wait(&M->full[kst], ph))) break;
+                        const int kst = kr.st;
+                        if (dead || (j < take && !wait(&M->kfull[kst], kr.ph))) break;
                         const uint32_t bv = v_lo + ((vst * L::kStage) >> 4), bk = k_lo + ((kst * L::kStage) >> 4);
                         const uint32_t sx = kS + x * 128;
                         if (prev) {
@@ -1043,11 +1061,11 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                             }
                             if (prev) *(volatile int*)&M->turn = 0;
                             if (j == take - 1 && sp.n > 0) mma_commit(&M->qempty[x]);   // the queries were read
-                            if (j > 0) mma_commit(&M->empty[vst]);
-                            if (j < take) mma_commit(&M->empty[kst]);
+                            if (j > 0) mma_commit(&M->vempty[vst]);
+                            if (j < take) mma_commit(&M->kempty[kst]);
                         }
                         __syncwarp();
-                        if (j < take) advance();
+                        if (j < take) kr.next();
                         prev = next;
                     }
                 }
@@ -1065,7 +1083,8 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
         } else if (warp == 11) {
             // -------------------------------------------------------- queries, and inspector of values
             // (one warp: a tile's queries are loaded once the last tile's values are inspected)
-            int st = 0, ph = 0, nv = 0, nq[2] = {0, 0};
+            Ring<L::kValStages> vr;
+            int nv = 0, nq[2] = {0, 0};
             bool dead = *abort_flag != 0, q_bytes = false;
             while (w.left > 0 && !dead) {
                 const Span item = span_of(a, w.r, w.m * P.tile_tok, P.tile_tok);
@@ -1112,33 +1131,16 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                     if (lane == 0) mbar_arrive(&M->qfull[x]);
                 }
                 if (dead) break;
-                // Every use of a stage is waited for, the keys' too: a wait tells only even from odd
-                // uses, and the values' copy may land before the keys that used the stage.
-                auto landed = [&]() {
-                    if (!dead && !__all_sync(0xffffffffu, mbar_wait(&M->full[st], ph, abort_flag, a.wait_ns))) dead = true;
-                };
-                auto past = [&]() {
-                    if (++st == L::kStages) {
-                        st = 0;
-                        ph ^= 1;
-                    }
-                };
-                auto past_keys = [&]() {
-                    for (int c = 0; c < L::kParts; c++) {
-                        landed();
-                        past();
-                    }
-                };
-                if (kOne) past_keys();
                 for (int kv = 0; kv < take * L::kParts; kv++, nv++) {
                     const int kc = kv / L::kParts;
-                    if (kv % L::kParts == 0 && (!kOne || kc + 1 < take)) past_keys();
-                    landed();
-                    if (dead) break;
+                    if (!__all_sync(0xffffffffu, mbar_wait(&M->vfull[vr.st], vr.ph, abort_flag, a.wait_ns))) {
+                        dead = true;
+                        break;
+                    }
                     const int id = w.t.id(w.c + kc), t0 = id * kKT;
                     int found = 0;
                     if (!item.sees_all(id)) {
-                        unsigned char* tile = smem + L::stages + st * L::kStage;
+                        unsigned char* tile = smem + L::stages + (L::kKeyStages + vr.st) * L::kStage;
                         constexpr int kPer = L::kCh / 8, kStep = 32 / kPer;
                         const int ch = lane % kPer, r0 = lane / kPer;
                         auto at = [&](int r) {
@@ -1183,7 +1185,7 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                         *(volatile int*)&M->special[nv & 3] = found;
                         mbar_arrive(&M->vok[nv & 3]);
                     }
-                    past();
+                    vr.next();
                 }
                 if (dead) break;
                 w.next(P);
