@@ -12,7 +12,11 @@
 // once per tile of work.
 // Split: the chunks of all tiles form one line that is cut into equal shares, one per CTA (two CTAs
 // per SM), so a batch of ragged lengths and a single long request both load every SM alike. A tile
-// that a cut goes through is written in parts and joined by paged_merge_kernel.
+// that a cut goes through is written in parts; the CTA that writes its last part joins them, in
+// their order whoever is last (a merge kernel of its own took 3 us of GPU and 4 us of host time more a
+// call). A tile is cut into at most kMaxParts.
+#include <chrono>
+
 #include "cg_paged_dev.cuh"
 #include "cg_tc_common.cuh"
 #include "cg_tmap.h"
@@ -35,11 +39,7 @@ constexpr int kThreads = 32 * (kWarps + 1);
 // One part's place in the workspace: O [16][d], then the reference and sum of each row.
 constexpr int part_floats(int d) { return kRows * d + 2 * kRows; }
 
-// What the merge needs of the tile that starts in a CTA's share and goes on past it.
-struct Meta {
-    int last;      // last CTA with a part of it, or -1: none
-    int tok0, row0, n_rows, h, pad[3];
-};
+constexpr int kMaxParts = 64;
 
 template <int D>
 struct RowsSmem {
@@ -58,7 +58,8 @@ struct RowsMisc {
     uint64_t full[6], empty[6];
     int64_t warp_sum[kThreads / 32];
     int64_t total, before;
-    int start_req, abort_flag;
+    int warp_longest[kThreads / 32];
+    int start_req, abort_flag, last_part;
     float ml[2][2 * kRows];
 };
 static_assert(sizeof(RowsMisc) <= 512, "misc block");
@@ -66,19 +67,19 @@ static_assert(sizeof(RowsMisc) <= 512, "misc block");
 struct RowsParams {
     PagedArgs a;
     float* parts;
-    Meta* meta;
+    unsigned long long* written;   // a word per part
+    uint64_t epoch;                // of the call
     int max_rows;     // requests with more query rows are left to the other kernel
-    int min_share;    // chunks
     int box_rows;
 };
 
 // Cost of a request in chunks: (row tiles) x H x (chunks that its rows see).
-__device__ __forceinline__ int64_t request_cost(const RowsParams& P, int i, int32_t* flag, Request* out) {
+__device__ __forceinline__ int64_t request_cost(const RowsParams& P, int i, int32_t* flag, int* longest) {
     const Request r = load_request(P.a, i, flag);
-    if (out) *out = r;
     const int64_t rows = (int64_t)r.n * P.a.n_rep;
     if (r.n <= 0 || rows > P.max_rows) return 0;
     const Tiles t = visible_tiles<kTK>(P.a.window, P.a.sinks, r.len - r.n, r.len - 1);
+    if (t.count() > *longest) *longest = t.count();
     return (rows + kRows - 1) / kRows * P.a.H * t.count();
 }
 
@@ -147,6 +148,86 @@ __device__ __forceinline__ uint32_t special_mask(uint32_t v) {
     return ((v & e) == e ? 0xffffu : 0u) | ((v & (e << 16)) == (e << 16) ? 0xffff0000u : 0u);
 }
 
+// A part's word, beside the part: the call's epoch once the part is written. Words of unused memory
+// and of earlier calls hold something else, and the joining CTA leaves 0, so that a replay of a
+// captured call starts without. Writes the word of this CTA's part and says whether those of all parts
+// are written: of the CTAs that finish at the same time at least one sees so (each writes its own word
+// before it reads the others', with a fence between); if two do, both join, to the same values. (A
+// counter instead cost up to 16 us: a compare-and-swap per arrival and retry.) One warp calls.
+__device__ __forceinline__ bool all_written(unsigned long long* words, int mine, int b0, int parts, uint64_t epoch) {
+    const int lane = threadIdx.x & 31;
+    auto word = [&](int p) { return reinterpret_cast<volatile unsigned long long*>(words) + ((int64_t)(b0 + p) * 2 + (p == 0 ? 1 : 0)); };
+    __threadfence();   // the part, by every lane
+    __syncwarp();
+    if (lane == 0) {
+        reinterpret_cast<volatile unsigned long long*>(words)[mine] = epoch;
+        __threadfence();
+    }
+    __syncwarp();
+    __threadfence();
+    bool all = true;
+    for (int p = lane; p < parts; p += 32) all &= *word(p) == epoch;
+    all = __all_sync(0xffffffffu, all);
+    if (all)
+        for (int p = lane; p < parts; p += 32) *word(p) = 0ull;
+    return all;
+}
+
+// Joins the parts of a tile: row r = sum_p 2^(ref_p - R) O_p / sum_p 2^(ref_p - R) l_p in the order of
+// the parts: CTA b0's second slot, then each next CTA's first. A row per warp and turn.
+template <bool FP16, int D>
+__device__ __noinline__ void join_parts(const RowsParams& P, int b0, int parts, int tok0, int row0, int n_rows, int h) {
+    const PagedArgs& a = P.a;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    constexpr int V = D / 32;   // channels of a lane: V lane .. V lane + V - 1
+    auto part = [&](int p) { return P.parts + ((int64_t)(b0 + p) * 2 + (p == 0 ? 1 : 0)) * part_floats(D); };
+    for (int row = warp; row < n_rows; row += kWarps) {
+        // references and sums of parts lane, lane + 32
+        float ref[kMaxParts / 32], l = 0.0f, R = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < kMaxParts / 32; k++) {
+            const int p = lane + 32 * k;
+            ref[k] = p < parts ? __ldcg(part(p) + kRows * D + row) : -INFINITY;
+            R = fmaxf(R, ref[k]);
+        }
+#pragma unroll
+        for (int off = 16; off; off >>= 1) R = fmaxf(R, __shfl_xor_sync(0xffffffffu, R, off));
+        const float Rs = R == -INFINITY ? 0.0f : R;
+#pragma unroll
+        for (int k = 0; k < kMaxParts / 32; k++) {
+            const int p = lane + 32 * k;
+            ref[k] = ex2(ref[k] - Rs);
+            if (p < parts) l += ref[k] * __ldcg(part(p) + kRows * D + kRows + row);
+        }
+#pragma unroll
+        for (int off = 16; off; off >>= 1) l += __shfl_xor_sync(0xffffffffu, l, off);
+        float o[V];
+#pragma unroll
+        for (int e = 0; e < V; e++) o[e] = 0.0f;
+#pragma unroll
+        for (int k = 0; k < kMaxParts / 32; k++) {
+            const int n = parts - 32 * k < 32 ? parts - 32 * k : 32;
+#pragma unroll 8
+            for (int q = 0; q < n; q++) {
+                const float f = __shfl_sync(0xffffffffu, ref[k], q);
+                const float* src = part(32 * k + q) + row * D + V * lane;
+                float x[V];
+#pragma unroll
+                for (int e = 0; e < V; e += 2) *reinterpret_cast<float2*>(x + e) = __ldcg(reinterpret_cast<const float2*>(src + e));
+#pragma unroll
+                for (int e = 0; e < V; e++) o[e] = fmaf(f, x[e], o[e]);   // a part with nothing in it: weight 0, zeros
+            }
+        }
+        const int r = row0 + row, tk = token_of(a, r), hd = h * a.n_rep + (r - tk * a.n_rep);
+        const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+        uint16_t* dst = a.out + (int64_t)(tok0 + tk) * a.o_tok + hd * a.o_head + V * lane;
+#pragma unroll
+        for (int e = 0; e < V; e += 2) *reinterpret_cast<uint32_t*>(dst + e) = pack2<FP16>(o[e] * inv, o[e + 1] * inv);
+        if (a.lse && lane == 0)
+            a.lse[(int64_t)(tok0 + tk) * a.H * a.n_rep + hd] = inv == 0.0f ? -INFINITY : (R + log2f(l)) * kLn2;
+    }
+}
+
 template <bool FP16, int D>
 __global__ void __launch_bounds__(kThreads, RowsSmem<D>::kCtas)
 paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ CUtensorMap map) {
@@ -163,14 +244,19 @@ paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ 
     const int i_lo = tid * per < a.n_req ? tid * per : a.n_req;
     const int i_hi = i_lo + per < a.n_req ? i_lo + per : a.n_req;
     int64_t mine = 0;
-    for (int i = i_lo; i < i_hi; i++) mine += request_cost(P, i, &flag, nullptr);
+    int longest = 1;
+    for (int i = i_lo; i < i_hi; i++) mine += request_cost(P, i, &flag, &longest);
+    longest = __reduce_max_sync(0xffffffffu, longest);
     int64_t incl = mine;
 #pragma unroll
     for (int off = 1; off < 32; off *= 2) {
         const int64_t v = __shfl_up_sync(0xffffffffu, incl, off);
         if (lane >= off) incl += v;
     }
-    if (lane == 31) M->warp_sum[warp] = incl;
+    if (lane == 31) {
+        M->warp_sum[warp] = incl;
+        M->warp_longest[warp] = longest;
+    }
     if (tid == 0) {
         for (int s = 0; s < L::kStages; s++) {
             mbar_init(&M->full[s], 1);
@@ -186,15 +272,17 @@ paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ 
     for (int w = 0; w < kThreads / 32; w++) {
         if (w < warp) before += M->warp_sum[w];
         total += M->warp_sum[w];
+        longest = max(longest, M->warp_longest[w]);
     }
     int64_t share = (total + gridDim.x - 1) / gridDim.x;
-    if (share < P.min_share) share = P.min_share;
+    const int least = (longest + kMaxParts - 3) / (kMaxParts - 2);   // cut ends make two parts more
+    if (share < least) share = least;
     const int64_t begin = share * blockIdx.x;
     const int64_t end = begin + share < total ? begin + share : total;
     if (begin >= before && begin < before + mine) {
         int64_t at = before;
         for (int i = i_lo; i < i_hi; i++) {
-            const int64_t c = request_cost(P, i, &flag, nullptr);
+            const int64_t c = request_cost(P, i, &flag, &longest);
             if (begin < at + c) {
                 M->start_req = i;
                 M->before = begin - at;
@@ -205,11 +293,7 @@ paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ 
     }
     __syncthreads();
     if (blockIdx.x == 0) raise_flag(a.status, flag);
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    if (begin >= end) {
-        if (tid == 0) P.meta[blockIdx.x].last = -1;
-        return;
-    }
+    if (begin >= end) return;
     volatile int* abort_flag = &M->abort_flag;
     int left = (int)(end - begin);
     Walk w;
@@ -227,22 +311,33 @@ paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ 
             const int wlo = a.window ? w.r.len - w.r.n - a.window + 1 : 0;   // first token the request still needs
             const int32_t* row = a.table + (int64_t)w.i * a.max_pages;
             const int take = w.n_chunks - w.c < left ? w.n_chunks - w.c : left;
-            for (int k = 0; k < take; k++) {
+            // the places of a group of chunks are looked up at once, lane = chunk * n_box + box, one
+            // group ahead of its use
+            const int group = 32 / n_box, mine = lane / n_box, mybox = lane - mine * n_box;
+            auto look = [&](int k0) {                // page of the lane's box, or -1: zeros
+                const int k = k0 + mine;
+                if (k >= take) return -1;
+                const int t = w.t.id(w.c + k) * kTK + mybox * P.box_rows;
+                if (!(t < w.r.len && (t + P.box_rows > wlo || t < a.sinks))) return -1;
+                const int pg = __ldg(row + (t >> a.page_log2));
+                if (pg < 0 || pg >= a.n_pages) {
+                    pflag |= CG_FLAG_PAGED_RANGE;
+                    return -1;
+                }
+                return pg;
+            };
+            int now = look(0), ahead = look(group), in = 0;
+            for (int k = 0; k < take; k++, in++) {
+                if (in == group) {
+                    in = 0;
+                    now = ahead;
+                    ahead = look(k + group);
+                }
+                const int pg = __shfl_sync(0xffffffffu, now, (in * n_box + lane) & 31);
                 const int id = w.t.id(w.c + k);
                 if (!sp.sees(a, id)) continue;
-                int z = 2 * a.n_pages, y = 0;           // past the pool: the copy fills with zeros
-                if (lane < n_box) {
-                    const int t = id * kTK + lane * P.box_rows;
-                    if (t < w.r.len && (t + P.box_rows > wlo || t < a.sinks)) {
-                        const int pg = __ldg(row + (t >> a.page_log2));
-                        if (pg >= 0 && pg < a.n_pages) {
-                            z = pg;
-                            y = sp.h * a.page + (t & (a.page - 1));
-                        } else {
-                            pflag |= CG_FLAG_PAGED_RANGE;
-                        }
-                    }
-                }
+                // past the pool (page 2 n_pages) the copy fills with zeros
+                const int z = pg < 0 ? 2 * a.n_pages : pg, y = pg < 0 ? 0 : sp.h * a.page + ((id * kTK + lane * P.box_rows) & (a.page - 1));
                 if (!dead && !__all_sync(0xffffffffu, mbar_wait(&M->empty[st], ph, abort_flag, a.wait_ns))) {
                     dead = true;
                     *abort_flag = 1;
@@ -281,7 +376,7 @@ paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ 
         const float sl2 = a.scale * kLog2e;
         int st = 0, ph = 0;
         bool dead = *abort_flag != 0, head_part = w.c > 0;
-        int meta_last = -1;
+        int64_t at = begin - w.c;   // the tile's place in the line
         while (left > 0) {
             const TileSpan sp(P, w);
             const int take = w.n_chunks - w.c < left ? w.n_chunks - w.c : left;
@@ -518,8 +613,9 @@ paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ 
                 asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");
             }
             const bool goes_on = w.c + take < w.n_chunks;
+            const bool whole = !head_part && !goes_on;
             if (warp == 0) {
-                if (!head_part && !goes_on) {
+                if (whole) {
 #pragma unroll
                     for (int hf = 0; hf < 2; hf++) {
                         if (g + 8 * hf >= sp.n_rows) continue;
@@ -546,91 +642,35 @@ paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ 
                             part[kRows * D + kRows + g + 8 * hf] = sum[hf];
                         }
                     }
-                    if (!head_part) {   // it starts here and goes on
-                        const int64_t rest = (int64_t)w.n_chunks - w.c - take;   // chunks past this share
-                        meta_last = (int)(blockIdx.x + (rest + share - 1) / share);
-                        if (lane == 0) {
-                            Meta* m = P.meta + blockIdx.x;
-                            m->last = meta_last;
-                            m->tok0 = w.r.tok0;
-                            m->row0 = sp.row0;
-                            m->n_rows = sp.n_rows;
-                            m->h = sp.h;
-                        }
-                    }
                 }
             }
+            if (!whole) {
+                const int b0 = (int)(at / share), parts = (int)((at + w.n_chunks - 1) / share) - b0 + 1;
+                if (warp == 0) {
+                    const bool all = all_written(P.written, blockIdx.x * 2 + (head_part ? 0 : 1), b0, parts, P.epoch);
+                    if (lane == 0) M->last_part = all;
+                }
+                asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");
+                if (*(volatile int*)&M->last_part) {
+                    __threadfence();
+                    join_parts<FP16, D>(P, b0, parts, w.r.tok0, sp.row0, sp.n_rows, sp.h);
+                }
+            }
+            at += w.n_chunks;
             head_part = false;
             left -= take;
             w.next_tile(P);
         }
-        if (warp == 0 && lane == 0 && meta_last < 0) P.meta[blockIdx.x].last = -1;
         if (dead && tid == 0) raise_flag(a.status, CG_FLAG_PIPE_TIMEOUT);
     }
 }
 
-// Joins the parts of the tile that starts in CTA b's share: row r = sum_p 2^(ref_p - R) O_p / sum_p
-// 2^(ref_p - R) l_p in the order of the parts. A few KB per tile, bound by one round of loads.
-constexpr int kMergeWarps = 16;
-
-template <bool FP16, int D>
-__global__ void __launch_bounds__(kMergeWarps * 32) paged_merge_kernel(const __grid_constant__ RowsParams P) {
-    __shared__ float acc[kMergeWarps][D];
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    const PagedArgs& a = P.a;
-    const Meta m = P.meta[blockIdx.x];
-    if (m.last < 0) return;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int parts = m.last - (int)blockIdx.x + 1;
-    int rows2 = 1;
-    while (rows2 < m.n_rows) rows2 *= 2;
-    const int groups = kMergeWarps / rows2, row = warp / groups, sub = warp - row * groups;
-    auto part = [&](int p) {   // the starting CTA's second slot, then each next CTA's first
-        return P.parts + ((int64_t)(blockIdx.x + p) * 2 + (p == 0 ? 1 : 0)) * part_floats(D);
-    };
-    float R = -INFINITY, l = 0.0f;
-    float o[D / 32];
-#pragma unroll
-    for (int k = 0; k < D / 32; k++) o[k] = 0.0f;
-    if (row < m.n_rows) {
-        for (int p = lane; p < parts; p += 32) R = fmaxf(R, part(p)[kRows * D + row]);
-#pragma unroll
-        for (int off = 16; off; off >>= 1) R = fmaxf(R, __shfl_xor_sync(0xffffffffu, R, off));
-        const float Rs = R == -INFINITY ? 0.0f : R;
-        for (int p = lane; p < parts; p += 32) l += part(p)[kRows * D + kRows + row] * ex2(part(p)[kRows * D + row] - Rs);
-#pragma unroll
-        for (int off = 16; off; off >>= 1) l += __shfl_xor_sync(0xffffffffu, l, off);
-#pragma unroll 4
-        for (int p = sub; p < parts; p += groups) {
-            const float* src = part(p);
-            const float f = ex2(src[kRows * D + row] - Rs);
-#pragma unroll
-            for (int k = 0; k < D / 32; k++) {
-                // a part with nothing in it has weight 0 and zeros
-                o[k] += f * src[row * D + lane + 32 * k];
-            }
-        }
-    }
-#pragma unroll
-    for (int k = 0; k < D / 32; k++) acc[warp][lane + 32 * k] = o[k];
-    __syncthreads();
-    if (row < m.n_rows && sub == 0) {
-        const int r = m.row0 + row, tk = token_of(a, r), hd = m.h * a.n_rep + (r - tk * a.n_rep);
-        const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-        uint16_t* dst = a.out + (int64_t)(m.tok0 + tk) * a.o_tok + hd * a.o_head;
-#pragma unroll
-        for (int k = 0; k < D / 64; k++) {
-            const int c = 2 * lane + 64 * k;
-            float x = 0.0f, y = 0.0f;
-            for (int s = 0; s < groups; s++) {
-                x += acc[warp + s][c];
-                y += acc[warp + s][c + 1];
-            }
-            *reinterpret_cast<uint32_t*>(dst + c) = pack2<FP16>(x * inv, y * inv);
-        }
-        if (a.lse && lane == 0)
-            a.lse[(int64_t)(m.tok0 + tk) * a.H * a.n_rep + hd] = inv == 0.0f ? -INFINITY : (R + log2f(l)) * kLn2;
-    }
+// A number for each call, unlike those of other calls and unlike what unused memory holds: 64 bits that
+// start at a hash of the clock, never 0.
+uint64_t next_epoch() {
+    static std::atomic<uint64_t> n{(uint64_t)std::chrono::high_resolution_clock::now().time_since_epoch().count() * 0x9e3779b97f4a7c15ull};
+    const uint64_t e = n.fetch_add(1, std::memory_order_relaxed);
+    return e ? e : next_epoch();
 }
 
 int rows_ctas(int d) { return tc::num_sms() * (d == 256 ? 1 : 2); }
@@ -645,23 +685,12 @@ cudaError_t launch_rows(const RowsParams& P, cudaStream_t st) {
     if (e != cudaSuccess) return e;
     const unsigned grid = (unsigned)rows_ctas(D);
     paged_rows_kernel<FP16, D><<<grid, kThreads, smem, st>>>(P, map);
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
-    // the merge may be scheduled while the last shares run; it waits for them on the device
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(grid);
-    cfg.blockDim = dim3(kMergeWarps * 32);
-    cfg.stream = st;
-    cudaLaunchAttribute at{};
-    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at.val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = &at;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, paged_merge_kernel<FP16, D>, P);
+    return cudaGetLastError();
 }
 
 size_t rows_workspace(int d) {
     const size_t n = (size_t)rows_ctas(d);
-    return n * 2 * part_floats(d) * sizeof(float) + n * sizeof(Meta);
+    return n * 2 * part_floats(d) * sizeof(float) + n * 2 * sizeof(unsigned long long);
 }
 
 }  // namespace
@@ -691,14 +720,15 @@ cudaError_t launch_paged_attn(const PagedArgs& a, void* workspace, cudaStream_t 
     const int limit = kRows;   // longer requests run on the 128-row tiles of cg_paged_chunk.cu
     const bool long_ones = (int64_t)a.max_new * a.n_rep > limit;
     cudaError_t e = cudaSuccess;
-    // one request that may be long: the rows kernel is still needed where it may turn out short
-    if (!long_ones || limit >= a.n_rep) {
+    // short requests beside long ones; one request alone goes to the tiles whatever its rows
+    const bool short_ones = !long_ones || (a.n_req > 1 && a.n_rep <= limit);
+    if (short_ones) {
         RowsParams P{};
         P.a = a;
         P.parts = static_cast<float*>(workspace);
-        P.meta = reinterpret_cast<Meta*>(P.parts + (size_t)rows_ctas(a.d) * 2 * part_floats(a.d));
+        P.written = reinterpret_cast<unsigned long long*>(P.parts + (size_t)rows_ctas(a.d) * 2 * part_floats(a.d));
+        P.epoch = next_epoch();
         P.max_rows = limit;
-        P.min_share = 1;
         P.box_rows = a.page < kTK ? a.page : kTK;
         const bool h = a.dtype == CG_FP16;
         switch (a.d) {
@@ -708,7 +738,7 @@ cudaError_t launch_paged_attn(const PagedArgs& a, void* workspace, cudaStream_t 
         }
         if (e != cudaSuccess) return e;
     }
-    if (long_ones) e = launch_paged_chunk(a, limit + 1, workspace, st);
+    if (long_ones) e = launch_paged_chunk(a, short_ones ? limit + 1 : 1, workspace, st);
     return e;
 }
 
