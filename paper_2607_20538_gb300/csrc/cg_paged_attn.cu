@@ -34,12 +34,12 @@ using namespace paged;
 constexpr int kRows = 16;        // query rows of a tile
 constexpr int kTK = 64;          // tokens of a stage
 constexpr int kWarps = 4;        // consumer warps, 16 tokens of a stage each
-constexpr int kThreads = 32 * (kWarps + 1);
+constexpr int kThreads = 256;    // the consumers' four warps, and four of which one issues the copies
 
 // One part's place in the workspace: O [16][d], then the reference and sum of each row.
 constexpr int part_floats(int d) { return kRows * d + 2 * kRows; }
 
-constexpr int kMaxParts = 64;
+constexpr int kMaxParts = 64;   // two a lane of the joining warp
 
 template <int D>
 struct RowsSmem {
@@ -57,9 +57,10 @@ struct RowsSmem {
 struct RowsMisc {
     uint64_t full[6], empty[6];
     int64_t warp_sum[kThreads / 32];
-    int64_t total, before;
+    int64_t share, begin, before;
     int warp_longest[kThreads / 32];
     int start_req, abort_flag, last_part;
+    Request start_r;
     float ml[2][2 * kRows];
 };
 static_assert(sizeof(RowsMisc) <= 512, "misc block");
@@ -93,19 +94,24 @@ struct Walk {
     __device__ __forceinline__ void load(const RowsParams& P, int req) {
         int32_t flag = 0;
         i = req;
-        u = c = 0;
         n_tiles = 0;
         n_chunks = 1;
-        if (i >= P.a.n_req) return;
-        r = load_request(P.a, i, &flag);
+        if (i < P.a.n_req) set(P, load_request(P.a, i, &flag));
+    }
+    __device__ __forceinline__ void set(const RowsParams& P, const Request& req) {
+        r = req;
+        u = c = 0;
         const int64_t rows = (int64_t)r.n * P.a.n_rep;
         if (r.n <= 0 || rows > P.max_rows) return;
         t = visible_tiles<kTK>(P.a.window, P.a.sinks, r.len - r.n, r.len - 1);
         n_chunks = t.count();
         n_tiles = (int)((rows + kRows - 1) / kRows) * P.a.H;
     }
-    __device__ __forceinline__ void start(const RowsParams& P, int req, int64_t off) {
-        load(P, req);
+    __device__ __forceinline__ void start(const RowsParams& P, int req, const Request& q, int64_t off) {
+        i = req;
+        n_tiles = 0;
+        n_chunks = 1;
+        set(P, q);
         u = (int)(off / n_chunks);
         c = (int)(off - (int64_t)u * n_chunks);
     }
@@ -141,6 +147,13 @@ struct TileSpan {
     }
 };
 
+// With registers exchanged (two CTAs per SM) a wait cannot be a call; with one CTA it is, which leaves
+// the loop more registers.
+template <int D>
+__device__ __forceinline__ bool bounded_wait(uint64_t* bar, uint32_t parity, const volatile int* abort, uint64_t limit_ns) {
+    return RowsSmem<D>::kCtas == 2 ? wait_here(bar, parity, abort, limit_ns) : mbar_wait(bar, parity, abort, limit_ns);
+}
+
 // Special values (infinities, NaN) of a 16-bit pair, as a mask of its halves.
 template <bool FP16>
 __device__ __forceinline__ uint32_t special_mask(uint32_t v) {
@@ -153,16 +166,13 @@ __device__ __forceinline__ uint32_t special_mask(uint32_t v) {
 // captured call starts without. Writes the word of this CTA's part and says whether those of all parts
 // are written: of the CTAs that finish at the same time at least one sees so (each writes its own word
 // before it reads the others', with a fence between); if two do, both join, to the same values. (A
-// counter instead cost up to 16 us: a compare-and-swap per arrival and retry.) One warp calls.
+// counter instead cost up to 16 us: a compare-and-swap per arrival and retry.) The warp that wrote the
+// part calls.
 __device__ __forceinline__ bool all_written(unsigned long long* words, int mine, int b0, int parts, uint64_t epoch) {
     const int lane = threadIdx.x & 31;
     auto word = [&](int p) { return reinterpret_cast<volatile unsigned long long*>(words) + ((int64_t)(b0 + p) * 2 + (p == 0 ? 1 : 0)); };
-    __threadfence();   // the part, by every lane
-    __syncwarp();
-    if (lane == 0) {
-        reinterpret_cast<volatile unsigned long long*>(words)[mine] = epoch;
-        __threadfence();
-    }
+    __threadfence();
+    if (lane == 0) reinterpret_cast<volatile unsigned long long*>(words)[mine] = epoch;
     __syncwarp();
     __threadfence();
     bool all = true;
@@ -182,41 +192,50 @@ __device__ __noinline__ void join_parts(const RowsParams& P, int b0, int parts, 
     constexpr int V = D / 32;   // channels of a lane: V lane .. V lane + V - 1
     auto part = [&](int p) { return P.parts + ((int64_t)(b0 + p) * 2 + (p == 0 ? 1 : 0)) * part_floats(D); };
     for (int row = warp; row < n_rows; row += kWarps) {
-        // references and sums of parts lane, lane + 32
-        float ref[kMaxParts / 32], l = 0.0f, R = -INFINITY;
+        // references and sums of parts lane, lane + 32, and the first parts' rows, in one round of loads
+        constexpr int kBatch = 32 / V;
+        float x[kBatch][V], ref[kMaxParts / 32], ls[kMaxParts / 32], l = 0.0f, R = -INFINITY;
+        auto fetch = [&](int p0) {
+#pragma unroll
+            for (int k = 0; k < kBatch; k++) {
+                if (p0 + k >= parts) break;
+                const float* src = part(p0 + k) + row * D + V * lane;
+#pragma unroll
+                for (int e = 0; e < V; e += 2) *reinterpret_cast<float2*>(&x[k][e]) = __ldcg(reinterpret_cast<const float2*>(src + e));
+            }
+        };
 #pragma unroll
         for (int k = 0; k < kMaxParts / 32; k++) {
             const int p = lane + 32 * k;
             ref[k] = p < parts ? __ldcg(part(p) + kRows * D + row) : -INFINITY;
-            R = fmaxf(R, ref[k]);
+            ls[k] = p < parts ? __ldcg(part(p) + kRows * D + kRows + row) : 0.0f;
         }
+        fetch(0);
+#pragma unroll
+        for (int k = 0; k < kMaxParts / 32; k++) R = fmaxf(R, ref[k]);
 #pragma unroll
         for (int off = 16; off; off >>= 1) R = fmaxf(R, __shfl_xor_sync(0xffffffffu, R, off));
         const float Rs = R == -INFINITY ? 0.0f : R;
 #pragma unroll
         for (int k = 0; k < kMaxParts / 32; k++) {
-            const int p = lane + 32 * k;
             ref[k] = ex2(ref[k] - Rs);
-            if (p < parts) l += ref[k] * __ldcg(part(p) + kRows * D + kRows + row);
+            l = fmaf(ref[k], ls[k], l);
         }
 #pragma unroll
         for (int off = 16; off; off >>= 1) l += __shfl_xor_sync(0xffffffffu, l, off);
         float o[V];
 #pragma unroll
         for (int e = 0; e < V; e++) o[e] = 0.0f;
+        for (int p0 = 0; p0 < parts; p0 += kBatch) {
 #pragma unroll
-        for (int k = 0; k < kMaxParts / 32; k++) {
-            const int n = parts - 32 * k < 32 ? parts - 32 * k : 32;
-#pragma unroll 8
-            for (int q = 0; q < n; q++) {
-                const float f = __shfl_sync(0xffffffffu, ref[k], q);
-                const float* src = part(32 * k + q) + row * D + V * lane;
-                float x[V];
+            for (int k = 0; k < kBatch; k++) {
+                const float f = __shfl_sync(0xffffffffu, p0 < 32 ? ref[0] : ref[1], (p0 + k) & 31);
+                if (p0 + k < parts) {   // a part with nothing in it: weight 0, zeros
 #pragma unroll
-                for (int e = 0; e < V; e += 2) *reinterpret_cast<float2*>(x + e) = __ldcg(reinterpret_cast<const float2*>(src + e));
-#pragma unroll
-                for (int e = 0; e < V; e++) o[e] = fmaf(f, x[e], o[e]);   // a part with nothing in it: weight 0, zeros
+                    for (int e = 0; e < V; e++) o[e] = fmaf(f, x[k][e], o[e]);
+                }
             }
+            fetch(p0 + kBatch);
         }
         const int r = row0 + row, tk = token_of(a, r), hd = h * a.n_rep + (r - tk * a.n_rep);
         const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
@@ -282,14 +301,19 @@ paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ 
     if (begin >= before && begin < before + mine) {
         int64_t at = before;
         for (int i = i_lo; i < i_hi; i++) {
-            const int64_t c = request_cost(P, i, &flag, &longest);
+            const int64_t c = per == 1 ? mine : request_cost(P, i, &flag, &longest);
             if (begin < at + c) {
                 M->start_req = i;
+                M->start_r = load_request(a, i, &flag);
                 M->before = begin - at;
                 break;
             }
             at += c;
         }
+    }
+    if (tid == 0) {
+        M->share = share;
+        M->begin = begin;
     }
     __syncthreads();
     if (blockIdx.x == 0) raise_flag(a.status, flag);
@@ -297,9 +321,13 @@ paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ 
     volatile int* abort_flag = &M->abort_flag;
     int left = (int)(end - begin);
     Walk w;
-    w.start(P, M->start_req, M->before);
+    w.start(P, M->start_req, M->start_r, M->before);
 
-    if (warp == kWarps) {
+    // Registers: 128 a thread at launch; the consumers take what the others give up (128 x 208 + 128 x 40
+    // of 256 x 128). With 168 each (five warps, no exchange) their loop spilled.
+    if (warp >= kWarps) {
+        if (L::kCtas == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+        if (warp > kWarps) return;
         // ------------------------------------------------------------ producer
         // lane k < n_box carries the boxes of token rows [k box_rows, ...) of a stage
         const int n_box = kTK / P.box_rows;
@@ -338,7 +366,7 @@ paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ 
                 if (!sp.sees(a, id)) continue;
                 // past the pool (page 2 n_pages) the copy fills with zeros
                 const int z = pg < 0 ? 2 * a.n_pages : pg, y = pg < 0 ? 0 : sp.h * a.page + ((id * kTK + lane * P.box_rows) & (a.page - 1));
-                if (!dead && !__all_sync(0xffffffffu, mbar_wait(&M->empty[st], ph, abort_flag, a.wait_ns))) {
+                if (!dead && !__all_sync(0xffffffffu, bounded_wait<D>(&M->empty[st], ph, abort_flag, a.wait_ns))) {
                     dead = true;
                     *abort_flag = 1;
                 }
@@ -368,15 +396,16 @@ paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ 
         if (dead) {   // copies in flight land before the CTA ends
             const int zero = 0;
             for (int k = issued > L::kStages ? issued - L::kStages : 0; k < issued; k++)
-                mbar_wait(&M->full[k % L::kStages], (k / L::kStages) & 1, &zero, tc::kWaitLimitNs);
+                bounded_wait<D>(&M->full[k % L::kStages], (k / L::kStages) & 1, &zero, tc::kWaitLimitNs);
         }
     } else {
         // ------------------------------------------------------------ consumers
+        if (L::kCtas == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
         const int g = lane >> 2, j = lane & 3;   // rows g and g + 8; columns 2j, 2j + 1
         const float sl2 = a.scale * kLog2e;
         int st = 0, ph = 0;
         bool dead = *abort_flag != 0, head_part = w.c > 0;
-        int64_t at = begin - w.c;   // the tile's place in the line
+        int from = -w.c;            // the tile's place in the line, from the share's beginning
         while (left > 0) {
             const TileSpan sp(P, w);
             const int take = w.n_chunks - w.c < left ? w.n_chunks - w.c : left;
@@ -406,7 +435,7 @@ paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ 
             for (int kc = 0; kc < take; kc++) {
                 const int id = w.t.id(w.c + kc);
                 if (!sp.sees(a, id)) continue;
-                if (!dead && !__all_sync(0xffffffffu, mbar_wait(&M->full[st], ph, abort_flag, a.wait_ns))) {
+                if (!dead && !__all_sync(0xffffffffu, bounded_wait<D>(&M->full[st], ph, abort_flag, a.wait_ns))) {
                     dead = true;
                     *abort_flag = 1;
                 }
@@ -459,7 +488,7 @@ paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ 
                         float f[2];
 #pragma unroll
                         for (int hf = 0; hf < 2; hf++) {
-                            const float nr = fmaxf(ref[hf], mx[hf] - kBias);
+                            const float nr = mx[hf] > ref[hf] + (kBias + kLazy) ? mx[hf] - kBias : ref[hf];
                             f[hf] = ref[hf] == nr ? 1.0f : ex2(ref[hf] - nr);   // 0 at a row's first token
                             ref[hf] = nr;
                             sum[hf] *= f[hf];
@@ -645,7 +674,8 @@ paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ 
                 }
             }
             if (!whole) {
-                const int b0 = (int)(at / share), parts = (int)((at + w.n_chunks - 1) / share) - b0 + 1;
+                const int64_t at = M->begin + from;
+                const int b0 = (int)(at / M->share), parts = (int)((at + w.n_chunks - 1) / M->share) - b0 + 1;
                 if (warp == 0) {
                     const bool all = all_written(P.written, blockIdx.x * 2 + (head_part ? 0 : 1), b0, parts, P.epoch);
                     if (lane == 0) M->last_part = all;
@@ -656,7 +686,7 @@ paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ 
                     join_parts<FP16, D>(P, b0, parts, w.r.tok0, sp.row0, sp.n_rows, sp.h);
                 }
             }
-            at += w.n_chunks;
+            from += w.n_chunks;
             head_part = false;
             left -= take;
             w.next_tile(P);

@@ -701,8 +701,10 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                     if (!sp.sees_all(id)) mask_row(s_tm, a.window ? pos - a.window + 1 - t0 : 0, pos - t0, a.sinks - t0);
                     float u[32], v[32];
                     const float mx = sl2 * row_max(s_tm, u, v);
-                    if (__any_sync(0xffffffffu, mx > ref + (kBias + kLazy))) {
-                        const float nr = fmaxf(ref, mx - kBias);
+                    // each row by its own scores alone: rows past the tile's end hold anything
+                    const bool raise = have && mx > ref + (kBias + kLazy);
+                    if (__any_sync(0xffffffffu, raise)) {
+                        const float nr = raise ? mx - kBias : ref;
                         // never 0 x inf in O: a factor below all numbers becomes the least one
                         const float f = ref == nr ? 1.0f : fmaxf(ex2(ref - nr), 1.17549435e-38f);
                         if (started) {

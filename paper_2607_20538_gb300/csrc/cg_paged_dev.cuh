@@ -26,6 +26,21 @@ struct Weights {
     static constexpr float kBias = FP16 ? 7.0f : 0.0f;
 };
 
+// mbar_wait, whole in its place: kernels that exchange registers between warps (setmaxnreg) cannot
+// call functions.
+__device__ __forceinline__ bool wait_here(uint64_t* bar, uint32_t parity, const volatile int* abort, uint64_t limit_ns) {
+    const bool poll = limit_ns < 1000000ull;   // the diagnostic setting of mbar_wait
+    if (!poll && mbar_try_wait(bar, parity)) return true;
+    const uint64_t t0 = globaltimer_ns();
+    for (uint32_t it = 0;; it++) {
+        if (poll ? mbar_test_wait(bar, parity) : mbar_try_wait(bar, parity)) return true;
+        if (poll || (it & 63u) == 63u) {
+            if (*abort) return false;
+            if (globaltimer_ns() - t0 > limit_ns) return false;
+        }
+    }
+}
+
 __device__ __forceinline__ float ex2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -51,7 +66,6 @@ __device__ __forceinline__ int token_of(const PagedArgs& a, int x) {
 // A request as the attention sees it.
 struct Request {
     int len, n, tok0;     // tokens in the pool, new ones, first query row
-    bool ok;
 };
 
 // Loads and checks a request: lengths that are not covered by the arrays raise the flag.
@@ -61,9 +75,9 @@ __device__ __forceinline__ Request load_request(const PagedArgs& a, int i, int32
     r.len = __ldg(a.seq_lens + i);
     r.tok0 = c0;
     r.n = c1 - c0;
-    r.ok = c0 >= 0 && c1 >= c0 && c1 <= a.n_tok && r.n <= a.max_new && r.len >= 0 &&
+    const bool ok = c0 >= 0 && c1 >= c0 && c1 <= a.n_tok && r.n <= a.max_new && r.len >= 0 &&
            (int64_t)r.len <= (int64_t)a.max_pages << a.page_log2;
-    if (!r.ok) {
+    if (!ok) {
         *flag |= CG_FLAG_PAGED_RANGE;
         r.n = 0;
     }
