@@ -55,6 +55,7 @@ bool paged_pool_map(CUtensorMap* map, const PagedArgs& a, uint32_t box_rows);
 
 // Requests of at least min_rows query rows on the tcgen05 tiles.
 size_t paged_chunk_workspace(int d);
-cudaError_t launch_paged_chunk(const PagedArgs& a, int min_rows, void* workspace, cudaStream_t st);
+// after_rows: the last launch on the stream is this call's paged_rows_kernel.
+cudaError_t launch_paged_chunk(const PagedArgs& a, int min_rows, bool after_rows, void* workspace, cudaStream_t st);
 
 }  // namespace cg

@@ -251,6 +251,7 @@ template <bool FP16, int D>
 __global__ void __launch_bounds__(kThreads, RowsSmem<D>::kCtas)
 paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ CUtensorMap map) {
     using L = RowsSmem<D>;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the tiles kernel of the call may come beside
     extern __shared__ __align__(1024) unsigned char smem[];
     RowsMisc* M = reinterpret_cast<RowsMisc*>(smem + L::misc);
     float* merge = reinterpret_cast<float*>(smem + L::merge);
@@ -738,12 +739,10 @@ bool paged_pool_map(CUtensorMap* map, const PagedArgs& a, uint32_t box_rows) {
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// The two kernels follow one another on the stream, so they share the workspace.
+// The two kernels of a call may run beside each other: each has its own part of the workspace.
 size_t paged_attn_workspace(const PagedArgs& a) {
-    const size_t r = rows_workspace(a.d);
-    if ((int64_t)a.max_new * a.n_rep <= kRows) return r;
-    const size_t c = paged_chunk_workspace(a.d);
-    return r > c ? r : c;
+    const size_t r = (rows_workspace(a.d) + 255) / 256 * 256;
+    return (int64_t)a.max_new * a.n_rep <= kRows ? r : r + paged_chunk_workspace(a.d);
 }
 
 cudaError_t launch_paged_attn(const PagedArgs& a, void* workspace, cudaStream_t st) {
@@ -768,7 +767,9 @@ cudaError_t launch_paged_attn(const PagedArgs& a, void* workspace, cudaStream_t 
         }
         if (e != cudaSuccess) return e;
     }
-    if (long_ones) e = launch_paged_chunk(a, short_ones ? limit + 1 : 1, workspace, st);
+    if (long_ones)
+        e = launch_paged_chunk(a, short_ones ? limit + 1 : 1, short_ones,
+                               static_cast<unsigned char*>(workspace) + (rows_workspace(a.d) + 255) / 256 * 256, st);
     return e;
 }
 

@@ -1206,10 +1206,12 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
         tc_fence_after();
         tmem_dealloc(tmem, 512);
     }
+    asm volatile("griddepcontrol.wait;" ::: "memory");   // not done before the rows kernel of the call
 }
 
-// Joins the parts of the tile that starts in CTA b's share. A thread owns a row and 8 channels
-// (blockIdx.y): its parts' references, then one pass over the parts.
+// Joins the parts of the tile that starts in CTA b's share. A thread owns a row and 16 channels
+// (blockIdx.y). The first parts' values are asked for together with the references, so that the usual
+// two or three parts take one round of loads.
 template <bool FP16, int D>
 __global__ void __launch_bounds__(tile_rows(D)) paged_chunk_merge_kernel(const __grid_constant__ ChunkParams P) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -1221,36 +1223,59 @@ __global__ void __launch_bounds__(tile_rows(D)) paged_chunk_merge_kernel(const _
     if (m.last < 0 || rt >= P.half_tok || tk >= m.n_tok) return;
     const int parts = m.last - (int)blockIdx.x + 1;
     auto part = [&](int p) { return P.parts + ((int64_t)(blockIdx.x + p) * 2 + (p == 0 ? 1 : 0)) * chunk_part_floats(D); };
-    float R = -INFINITY;
-    for (int p = 0; p < parts; p++) R = fmaxf(R, part(p)[tile_rows(D) * D + row]);
-    const float Rs = R == -INFINITY ? 0.0f : R;
-    float l = 0.0f, o[8];
+    constexpr int kFirst = 3;
+    float ref[kFirst], sum[kFirst];
+    float4 x[kFirst][4];
 #pragma unroll
-    for (int k = 0; k < 8; k++) o[k] = 0.0f;
-#pragma unroll 4
-    for (int p = 0; p < parts; p++) {
+    for (int p = 0; p < kFirst; p++) {
+        ref[p] = -INFINITY;
+        sum[p] = 0.0f;
+        if (p < parts) {
+            const float* src = part(p);
+            ref[p] = src[tile_rows(D) * D + row];
+            sum[p] = src[tile_rows(D) * (D + 1) + row];
+#pragma unroll
+            for (int k = 0; k < 4; k++) x[p][k] = reinterpret_cast<const float4*>(src)[(4 * blockIdx.y + k) * tile_rows(D) + row];
+        }
+    }
+    float R = fmaxf(fmaxf(ref[0], ref[1]), ref[2]);
+    for (int p = kFirst; p < parts; p++) R = fmaxf(R, part(p)[tile_rows(D) * D + row]);
+    const float Rs = R == -INFINITY ? 0.0f : R;
+    float l = 0.0f, o[16];
+#pragma unroll
+    for (int k = 0; k < 16; k++) o[k] = 0.0f;
+    auto add = [&](float r, float s, const float4 (&v)[4]) {
+        const float f = r == -INFINITY ? 0.0f : fmaxf(ex2(r - Rs), 1.17549435e-38f);
+        l = fmaf(f, s, l);
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            o[4 * k] = fmaf(f, v[k].x, o[4 * k]);
+            o[4 * k + 1] = fmaf(f, v[k].y, o[4 * k + 1]);
+            o[4 * k + 2] = fmaf(f, v[k].z, o[4 * k + 2]);
+            o[4 * k + 3] = fmaf(f, v[k].w, o[4 * k + 3]);
+        }
+    };
+#pragma unroll
+    for (int p = 0; p < kFirst; p++)
+        if (p < parts) add(ref[p], sum[p], x[p]);
+#pragma unroll 2
+    for (int p = kFirst; p < parts; p++) {
         const float* src = part(p);
-        const float ref = src[tile_rows(D) * D + row];
-        const float f = ref == -INFINITY ? 0.0f : fmaxf(ex2(ref - Rs), 1.17549435e-38f);
-        l += f * src[tile_rows(D) * (D + 1) + row];
-        const float4 u = reinterpret_cast<const float4*>(src)[(2 * blockIdx.y) * tile_rows(D) + row];
-        const float4 v = reinterpret_cast<const float4*>(src)[(2 * blockIdx.y + 1) * tile_rows(D) + row];
-        o[0] += f * u.x;
-        o[1] += f * u.y;
-        o[2] += f * u.z;
-        o[3] += f * u.w;
-        o[4] += f * v.x;
-        o[5] += f * v.y;
-        o[6] += f * v.z;
-        o[7] += f * v.w;
+        float4 v[4];
+#pragma unroll
+        for (int k = 0; k < 4; k++) v[k] = reinterpret_cast<const float4*>(src)[(4 * blockIdx.y + k) * tile_rows(D) + row];
+        add(src[tile_rows(D) * D + row], src[tile_rows(D) * (D + 1) + row], v);
     }
     const int hd = m.h * a.n_rep + (rr - rt * a.n_rep);
     const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-    uint32_t b[4];
+    uint4* dst = reinterpret_cast<uint4*>(a.out + (int64_t)(m.tok0 + tk) * a.o_tok + hd * a.o_head + 16 * blockIdx.y);
 #pragma unroll
-    for (int k = 0; k < 4; k++) b[k] = inv == 0.0f ? 0u : pack2<FP16>(o[2 * k] * inv, o[2 * k + 1] * inv);
-    *reinterpret_cast<uint4*>(a.out + (int64_t)(m.tok0 + tk) * a.o_tok + hd * a.o_head + 8 * blockIdx.y) =
-        make_uint4(b[0], b[1], b[2], b[3]);
+    for (int q = 0; q < 2; q++) {
+        uint32_t b[4];
+#pragma unroll
+        for (int k = 0; k < 4; k++) b[k] = inv == 0.0f ? 0u : pack2<FP16>(o[8 * q + 2 * k] * inv, o[8 * q + 2 * k + 1] * inv);
+        dst[q] = make_uint4(b[0], b[1], b[2], b[3]);
+    }
     if (a.lse && blockIdx.y == 0)
         a.lse[(int64_t)(m.tok0 + tk) * a.H * a.n_rep + hd] = inv == 0.0f ? -INFINITY : (R + log2f(l)) * kLn2;
 }
@@ -1274,7 +1299,7 @@ bool query_map(CUtensorMap* map, const PagedArgs& a) {
 }
 
 template <bool FP16, int D>
-cudaError_t launch_chunk(ChunkParams P, cudaStream_t st) {
+cudaError_t launch_chunk(ChunkParams P, bool after_rows, cudaStream_t st) {
     CUtensorMap map, qmap{};
     if (!paged_pool_map(&map, P.a, P.box_rows)) return cudaErrorInvalidValue;
     P.q_boxes = query_map(&qmap, P.a);
@@ -1283,16 +1308,23 @@ cudaError_t launch_chunk(ChunkParams P, cudaStream_t st) {
     cudaError_t e = opt_in.set(reinterpret_cast<const void*>(paged_chunk_kernel<FP16, D>), (int)smem);
     if (e != cudaSuccess) return e;
     const unsigned grid = (unsigned)tc::num_sms();
-    paged_chunk_kernel<FP16, D><<<grid, kChunkThreads, smem, st>>>(P, map, qmap);
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(grid, D / 8);
-    cfg.blockDim = dim3(tile_rows(D));
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(kChunkThreads);
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute at{};
     at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at.val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = &at;
+    // Beside the rows kernel of the same call this one starts as soon as that one's CTAs leave room: it
+    // reads none of its results (and ends after it, see its end).
+    cfg.numAttrs = after_rows ? 1 : 0;
+    if ((e = cudaLaunchKernelEx(&cfg, paged_chunk_kernel<FP16, D>, P, map, qmap)) != cudaSuccess) return e;
+    // the merge is scheduled while the last shares run; it waits for them on the device
+    cfg.gridDim = dim3(grid, D / 16);
+    cfg.blockDim = dim3(tile_rows(D));
+    cfg.dynamicSmemBytes = 0;
     cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, paged_chunk_merge_kernel<FP16, D>, P);
 }
@@ -1304,7 +1336,7 @@ size_t paged_chunk_workspace(int d) {
     return n * 2 * chunk_part_floats(d) * sizeof(float) + n * sizeof(ChunkMeta);
 }
 
-cudaError_t launch_paged_chunk(const PagedArgs& a, int min_rows, void* workspace, cudaStream_t st) {
+cudaError_t launch_paged_chunk(const PagedArgs& a, int min_rows, bool after_rows, void* workspace, cudaStream_t st) {
     ChunkParams P{};
     P.a = a;
     P.parts = static_cast<float*>(workspace);
@@ -1315,9 +1347,9 @@ cudaError_t launch_paged_chunk(const PagedArgs& a, int min_rows, void* workspace
     P.tile_tok = halves(a.d) * P.half_tok;
     P.box_rows = a.page < kKT ? a.page : kKT;
     const bool h = a.dtype == CG_FP16;
-    if (a.d == 64) return h ? launch_chunk<true, 64>(P, st) : launch_chunk<false, 64>(P, st);
-    if (a.d == 256) return h ? launch_chunk<true, 256>(P, st) : launch_chunk<false, 256>(P, st);
-    return h ? launch_chunk<true, 128>(P, st) : launch_chunk<false, 128>(P, st);
+    if (a.d == 64) return h ? launch_chunk<true, 64>(P, after_rows, st) : launch_chunk<false, 64>(P, after_rows, st);
+    if (a.d == 256) return h ? launch_chunk<true, 256>(P, after_rows, st) : launch_chunk<false, 256>(P, after_rows, st);
+    return h ? launch_chunk<true, 128>(P, after_rows, st) : launch_chunk<false, 128>(P, after_rows, st);
 }
 
 }  // namespace cg
