@@ -266,11 +266,15 @@ __global__ void __launch_bounds__(kPT) plan_kernel(PlanArgs a) {
 }
 
 // ------------------------------------------------------------------------------------
-// Rotary. A thread owns two 16-byte pieces (8 channels each) of a head, at channels 8c and
-// rot / 2 + 8c: for the half layout these are the two sides of 8 pairs, for the interleaved layout
-// 4 pairs each. So both layouts load and store whole 128-byte lines. It turns these pieces of HPT
-// heads of one token with the same 8 sines and cosines. Past rot the pieces are copied; value heads
-// are copied whole. Bound: HBM (every byte is read once and written once).
+// Rotary. A CTA takes a few tokens: first the cosine and sine of every pair of each token, once, into
+// shared memory, then the heads. A unit of work is two 16-byte pieces (8 channels each) of two heads of
+// a token, at channels 8c and rot / 2 + 8c: for the half layout these are the two sides of 8 pairs, for
+// the interleaved layout 4 pairs each, so both layouts load and store whole 128-byte lines. The next
+// unit's loads are issued ahead of a unit's stores, the first unit's ahead of the cosines. Past rot the
+// pieces are copied; value heads are copied whole. Bound: HBM (every byte is read once and written
+// once). A 16384-token prompt, 32 + 8 + 8 heads of 128, 403 MB: 66.6 us, 6.05 TB/s; with the cosines and
+// sines computed by every thread for the heads that it turns, 68 us (two heads a thread), 70 (four) and
+// 103 (one: the arithmetic then bounds it). 193 decode tokens: 12.5 us, most of it the call's latency.
 // The angle is exact modulo a turn: position times the frequency in 2^-64 of a turn, in integers.
 // ------------------------------------------------------------------------------------
 struct RotArgs {
@@ -283,7 +287,8 @@ struct RotArgs {
     int64_t q_tok, q_head, k_tok, k_head, v_tok, v_head, o_tok, o_head;
     int64_t n_slots, v_half;     // slots of the pool; elements from the key to the value half
     int n_tok, q_heads, H, d, rot, page, page_log2, transpose;
-    int turn_groups, groups;     // groups of HPT heads that turn, and of all heads, per token
+    int turn_groups, groups;     // pairs of heads that turn, and of all heads, per token
+    int tokens;                  // of a CTA
     float mscale;
 };
 
@@ -303,106 +308,135 @@ __device__ __forceinline__ uint32_t pack2(float x, float y) {
     return *reinterpret_cast<const uint32_t*>(&b);
 }
 
-constexpr int kRotThreads = 128;
+constexpr int kRotThreads = 128, kRotTokens = 2;
 
-template <bool FP16, bool INTER, int HPT>
+template <bool FP16, bool INTER>
 __global__ void __launch_bounds__(kRotThreads) rotary_kernel(RotArgs a) {
-    const int C = a.d >> 4;                                       // threads along a head
-    const int c = threadIdx.x & (C - 1), per_cta = kRotThreads / C;
-    const uint32_t w = blockIdx.x * per_cta + threadIdx.x / C;
-    const uint32_t tok = w / (uint32_t)a.groups, grp = w - tok * a.groups;
-    if (tok >= (uint32_t)a.n_tok) return;
-    const bool is_v = (int)grp >= a.turn_groups;
-    const bool turns = !is_v && c < (a.rot >> 4);
-    const int o0 = turns || is_v ? 8 * c : a.rot + 16 * (c - (a.rot >> 4));
-    const int o1 = turns ? (a.rot >> 1) + 8 * c : is_v ? (a.d >> 1) + 8 * c : o0 + 8;
-    const int head0 = (is_v ? (int)grp - a.turn_groups : (int)grp) * HPT;
-    const int heads = is_v ? a.H : a.q_heads + a.H;
-
-    int64_t dst0 = -1;   // element of the token's slot in the key half, head 0
-    if (a.pool && head0 + HPT > (is_v ? 0 : a.q_heads)) {
-        const int64_t slot = __ldg(a.slots + tok);
-        if (slot >= 0 && slot < a.n_slots)
-            dst0 = (((slot >> a.page_log2) * a.H << a.page_log2) + (slot & (a.page - 1))) * a.d;
-        else if (slot != -1 && c == 0)
-            raise_flag(a.status, CG_FLAG_PAGED_RANGE);
-    }
+    extern __shared__ __align__(16) float2 turns_sm[];            // [tokens][rot / 2] (cosine, sine) x mscale
+    const int C = a.d >> 4, tid = threadIdx.x;                    // C units along a pair of heads
+    const int64_t tok0 = (int64_t)blockIdx.x * a.tokens;
+    const int n_tok = a.n_tok - tok0 < a.tokens ? (int)(a.n_tok - tok0) : a.tokens;
+    const int units = n_tok * a.groups * C, pairs = a.rot >> 1;
     const int64_t head_step = (int64_t)a.page * a.d;
 
-    uint4 x0[HPT], x1[HPT];
+    struct Unit {
+        int t, c, o0, o1, head0;
+        bool is_v, turns;
+        uint4 x0[2], x1[2];
+    };
+    auto heads_of = [&](const Unit& u) { return u.is_v ? a.H : a.q_heads + a.H; };
+    auto load = [&](int i, Unit& u) {
+        if (i >= units) return;
+        u.c = i & (C - 1);
+        const int g = i / C;
+        u.t = g / a.groups;
+        const int grp = g - u.t * a.groups;
+        u.is_v = grp >= a.turn_groups;
+        u.turns = !u.is_v && u.c < (a.rot >> 4);
+        u.o0 = u.turns || u.is_v ? 8 * u.c : a.rot + 16 * (u.c - (a.rot >> 4));
+        u.o1 = u.turns ? (a.rot >> 1) + 8 * u.c : u.is_v ? (a.d >> 1) + 8 * u.c : u.o0 + 8;
+        u.head0 = (u.is_v ? grp - a.turn_groups : grp) * 2;
+        const int64_t tok = tok0 + u.t;
 #pragma unroll
-    for (int k = 0; k < HPT; k++) {
-        const int h = head0 + k;
-        if (h < heads) {
-            const uint16_t* src = is_v ? a.v + tok * a.v_tok + h * a.v_head
-                                  : h < a.q_heads ? a.q + tok * a.q_tok + h * a.q_head
-                                                  : a.k + tok * a.k_tok + (h - a.q_heads) * a.k_head;
-            x0[k] = *reinterpret_cast<const uint4*>(src + o0);
-            x1[k] = *reinterpret_cast<const uint4*>(src + o1);
-        }
-    }
-    float cs[8], sn[8];
-    if (turns) {
-        const int64_t p = __ldg(a.pos + tok);
-#pragma unroll
-        for (int e = 0; e < 8; e++) {
-            const int pair = INTER ? ((e < 4 ? o0 : o1) >> 1) + (e & 3) : 8 * c + e;
-            const uint64_t turn = (uint64_t)p * (uint64_t)__ldg(a.table + pair);
-            const float f = (float)(int32_t)(turn >> 32) * 0x1p-31f;   // half turns, in [-1, 1]
-            sincospif(f, &sn[e], &cs[e]);
-            cs[e] *= a.mscale;
-            sn[e] *= a.transpose ? -a.mscale : a.mscale;
-        }
-    }
-#pragma unroll
-    for (int k = 0; k < HPT; k++) {
-        const int h = head0 + k;
-        if (h >= heads) break;
-        if (turns) {
-            uint32_t u[4] = {x0[k].x, x0[k].y, x0[k].z, x0[k].w}, v[4] = {x1[k].x, x1[k].y, x1[k].z, x1[k].w};
-#pragma unroll
-            for (int e = 0; e < 4; e++) {
-                const float2 f = unpack2<FP16>(u[e]), g = unpack2<FP16>(v[e]);
-                if (INTER) {   // pairs (f.x, f.y) and (g.x, g.y)
-                    u[e] = pack2<FP16>(f.x * cs[e] - f.y * sn[e], f.y * cs[e] + f.x * sn[e]);
-                    v[e] = pack2<FP16>(g.x * cs[4 + e] - g.y * sn[4 + e], g.y * cs[4 + e] + g.x * sn[4 + e]);
-                } else {       // pairs (f.x, g.x) and (f.y, g.y)
-                    const int i = 2 * e, j = 2 * e + 1;
-                    u[e] = pack2<FP16>(f.x * cs[i] - g.x * sn[i], f.y * cs[j] - g.y * sn[j]);
-                    v[e] = pack2<FP16>(g.x * cs[i] + f.x * sn[i], g.y * cs[j] + f.y * sn[j]);
-                }
+        for (int k = 0; k < 2; k++) {
+            const int h = u.head0 + k;
+            if (h < heads_of(u)) {
+                const uint16_t* src = u.is_v ? a.v + tok * a.v_tok + h * a.v_head
+                                      : h < a.q_heads ? a.q + tok * a.q_tok + h * a.q_head
+                                                      : a.k + tok * a.k_tok + (h - a.q_heads) * a.k_head;
+                u.x0[k] = *reinterpret_cast<const uint4*>(src + u.o0);
+                u.x1[k] = *reinterpret_cast<const uint4*>(src + u.o1);
             }
-            x0[k] = make_uint4(u[0], u[1], u[2], u[3]);
-            x1[k] = make_uint4(v[0], v[1], v[2], v[3]);
         }
-        uint16_t* dst = nullptr;
-        if (!is_v && h < a.q_heads) dst = a.q_out + tok * a.o_tok + h * a.o_head;
-        else if (dst0 >= 0) dst = a.pool + dst0 + (is_v ? a.v_half + h * head_step : (h - a.q_heads) * head_step);
-        if (dst) {
-            *reinterpret_cast<uint4*>(dst + o0) = x0[k];
-            *reinterpret_cast<uint4*>(dst + o1) = x1[k];
+    };
+    Unit now;
+    load(tid, now);
+
+    for (int i = tid; i < n_tok * pairs; i += kRotThreads) {
+        const int t = i / pairs, pair = i - t * pairs;
+        const int64_t p = __ldg(a.pos + tok0 + t);
+        const uint64_t turn = (uint64_t)p * (uint64_t)__ldg(a.table + pair);
+        const float f = (float)(int32_t)(turn >> 32) * 0x1p-31f;   // half turns, in [-1, 1]
+        float sn, cs;
+        sincospif(f, &sn, &cs);
+        turns_sm[i] = make_float2(cs * a.mscale, a.transpose ? -sn * a.mscale : sn * a.mscale);
+    }
+    __syncthreads();
+
+    for (int i = tid; i < units; i += kRotThreads) {
+        Unit next;
+        load(i + kRotThreads, next);
+        int64_t dst0 = -1;   // element of the token's slot in the key half, head 0
+        if (a.pool && now.head0 + 2 > (now.is_v ? 0 : a.q_heads)) {
+            const int64_t slot = __ldg(a.slots + tok0 + now.t);
+            if (slot >= 0 && slot < a.n_slots)
+                dst0 = (((slot >> a.page_log2) * a.H << a.page_log2) + (slot & (a.page - 1))) * a.d;
+            else if (slot != -1 && now.c == 0)
+                raise_flag(a.status, CG_FLAG_PAGED_RANGE);
         }
+        float cs[8], sn[8];
+        if (now.turns) {
+            // pairs of the pieces: 8 from 8c, or 4 each from o0 / 2 and o1 / 2
+            const float2* row = turns_sm + now.t * pairs;
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+                const float4 v = *reinterpret_cast<const float4*>(row + (INTER ? ((e < 4 ? now.o0 : now.o1) >> 1) + (e & 3) : 8 * now.c + e));
+                cs[e] = v.x;
+                sn[e] = v.y;
+                cs[e + 1] = v.z;
+                sn[e + 1] = v.w;
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 2; k++) {
+            const int h = now.head0 + k;
+            if (h >= heads_of(now)) break;
+            if (now.turns) {
+                uint32_t u[4] = {now.x0[k].x, now.x0[k].y, now.x0[k].z, now.x0[k].w}, v[4] = {now.x1[k].x, now.x1[k].y, now.x1[k].z, now.x1[k].w};
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    const float2 f = unpack2<FP16>(u[e]), g = unpack2<FP16>(v[e]);
+                    if (INTER) {   // pairs (f.x, f.y) and (g.x, g.y)
+                        u[e] = pack2<FP16>(f.x * cs[e] - f.y * sn[e], f.y * cs[e] + f.x * sn[e]);
+                        v[e] = pack2<FP16>(g.x * cs[4 + e] - g.y * sn[4 + e], g.y * cs[4 + e] + g.x * sn[4 + e]);
+                    } else {       // pairs (f.x, g.x) and (f.y, g.y)
+                        const int i0 = 2 * e, i1 = 2 * e + 1;
+                        u[e] = pack2<FP16>(f.x * cs[i0] - g.x * sn[i0], f.y * cs[i1] - g.y * sn[i1]);
+                        v[e] = pack2<FP16>(g.x * cs[i0] + f.x * sn[i0], g.y * cs[i1] + f.y * sn[i1]);
+                    }
+                }
+                now.x0[k] = make_uint4(u[0], u[1], u[2], u[3]);
+                now.x1[k] = make_uint4(v[0], v[1], v[2], v[3]);
+            }
+            uint16_t* dst = nullptr;
+            if (!now.is_v && h < a.q_heads) dst = a.q_out + (tok0 + now.t) * a.o_tok + h * a.o_head;
+            else if (dst0 >= 0) dst = a.pool + dst0 + (now.is_v ? a.v_half + h * head_step : (h - a.q_heads) * head_step);
+            if (dst) {
+                *reinterpret_cast<uint4*>(dst + now.o0) = now.x0[k];
+                *reinterpret_cast<uint4*>(dst + now.o1) = now.x1[k];
+            }
+        }
+        now = next;
     }
 }
 
-template <int HPT>
-cudaError_t launch_rotary_hpt(RotArgs a, bool fp16, bool inter, cudaStream_t st) {
-    a.turn_groups = (a.q_heads + a.H + HPT - 1) / HPT;
-    a.groups = a.turn_groups + (a.pool ? (a.H + HPT - 1) / HPT : 0);
-    const int64_t per_cta = kRotThreads / (a.d >> 4);
-    const unsigned grid = (unsigned)(((int64_t)a.n_tok * a.groups + per_cta - 1) / per_cta);
+cudaError_t launch_rotary(RotArgs a, bool fp16, bool inter, cudaStream_t st) {
+    a.turn_groups = (a.q_heads + a.H + 1) / 2;
+    a.groups = a.turn_groups + (a.pool ? (a.H + 1) / 2 : 0);
+    // Two tokens a CTA where that leaves no SM idle: 16384 tokens take 66.6 us with two, 66.1 with four and
+    // 68 with 256 threads and four; 4000 tokens 21.1, 22.8 and 22.8. One token a CTA below: 193 tokens take
+    // 12.5 us, 13.1 with more a CTA.
+    a.tokens = a.n_tok >= kRotTokens * 1024 ? kRotTokens : 1;
+    const unsigned grid = (unsigned)(((int64_t)a.n_tok + a.tokens - 1) / a.tokens);
+    const size_t smem = (size_t)a.tokens * (a.rot >> 1) * sizeof(float2);
     if (fp16) {
-        if (inter) rotary_kernel<true, true, HPT><<<grid, kRotThreads, 0, st>>>(a);
-        else rotary_kernel<true, false, HPT><<<grid, kRotThreads, 0, st>>>(a);
+        if (inter) rotary_kernel<true, true><<<grid, kRotThreads, smem, st>>>(a);
+        else rotary_kernel<true, false><<<grid, kRotThreads, smem, st>>>(a);
     } else {
-        if (inter) rotary_kernel<false, true, HPT><<<grid, kRotThreads, 0, st>>>(a);
-        else rotary_kernel<false, false, HPT><<<grid, kRotThreads, 0, st>>>(a);
+        if (inter) rotary_kernel<false, true><<<grid, kRotThreads, smem, st>>>(a);
+        else rotary_kernel<false, false><<<grid, kRotThreads, smem, st>>>(a);
     }
     return cudaGetLastError();
-}
-
-cudaError_t launch_rotary(const RotArgs& a, bool fp16, bool inter, cudaStream_t st) {
-    return launch_rotary_hpt<4>(a, fp16, inter, st);
 }
 
 bool al16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
