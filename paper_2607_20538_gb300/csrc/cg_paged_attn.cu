@@ -394,11 +394,10 @@ paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ 
             w.next_tile(P);
         }
         raise_flag(a.status, pflag);
-        if (dead) {   // copies in flight land before the CTA ends
-            const int zero = 0;
-            for (int k = issued > L::kStages ? issued - L::kStages : 0; k < issued; k++)
-                bounded_wait<D>(&M->full[k % L::kStages], (k / L::kStages) & 1, &zero, tc::kWaitLimitNs);
-        }
+        // copies in flight land before the CTA ends, also where the consumers gave up on them
+        const int zero = 0;
+        for (int k = issued > L::kStages ? issued - L::kStages : 0; k < issued; k++)
+            bounded_wait<D>(&M->full[k % L::kStages], (k / L::kStages) & 1, &zero, tc::kWaitLimitNs);
     } else {
         // ------------------------------------------------------------ consumers
         if (L::kCtas == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");

@@ -893,14 +893,13 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                 w.next(P);
             }
             raise_flag(a.status, pflag);
-            if (dead) {   // copies in flight land before the CTA ends
-                *abort_flag = 1;
-                const int zero = 0;
-                for (int k = ki > L::kKeyStages ? ki - L::kKeyStages : 0; k < ki; k++)
-                    mbar_wait(&M->kfull[k % L::kKeyStages], (k / L::kKeyStages) & 1, &zero, tc::kWaitLimitNs);
-                for (int k = vi > L::kValStages ? vi - L::kValStages : 0; k < vi; k++)
-                    mbar_wait(&M->vfull[k % L::kValStages], (k / L::kValStages) & 1, &zero, tc::kWaitLimitNs);
-            }
+            if (dead) *abort_flag = 1;
+            // copies in flight land before the CTA ends, also where the other warps gave up on them
+            const int zero = 0;
+            for (int k = ki > L::kKeyStages ? ki - L::kKeyStages : 0; k < ki; k++)
+                mbar_wait(&M->kfull[k % L::kKeyStages], (k / L::kKeyStages) & 1, &zero, tc::kWaitLimitNs);
+            for (int k = vi > L::kValStages ? vi - L::kValStages : 0; k < vi; k++)
+                mbar_wait(&M->vfull[k % L::kValStages], (k / L::kValStages) & 1, &zero, tc::kWaitLimitNs);
         } else if (warp == 9 || (warp == 10 && !kOne)) {
             // -------------------------------------------------------- MMA issuer of one half
             // One half alone (d = 256): S(0) S(1) PV(0) S(2) PV(1) ..., the next scores in the other
@@ -1193,7 +1192,7 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                 w.next(P);
             }
             if (dead) *abort_flag = 1;
-            if (q_bytes && *abort_flag) {   // boxes in flight land before the CTA ends
+            if (q_bytes) {   // boxes in flight land before the CTA ends
                 const int zero = 0;
                 for (int x = 0; x < halves(D); x++)
                     if (nq[x]) mbar_wait(&M->qfull[x], (nq[x] - 1) & 1, &zero, tc::kWaitLimitNs);
