@@ -7,7 +7,8 @@ fp16; 0 keys, 1 values), the codec's cache layout with one layer and the pages a
 from __future__ import annotations
 
 import ctypes
-from dataclasses import dataclass
+import struct
+from typing import NamedTuple
 
 import torch
 
@@ -17,30 +18,27 @@ CG_BF16, CG_FP16 = 0, 1
 CG_ROPE_NONE, CG_ROPE_LINEAR, CG_ROPE_BANDS, CG_ROPE_YARN = 0, 1, 2, 3
 
 
-class _CPages(ctypes.Structure):
-    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "n_pages", "page", "H", "d", "n_req", "max_pages")]
+def _packed(fmt: str):
+    """The C struct of these members (native sizes and alignment) as bytes: their address is what the
+    entry points take. A third of the time of a ctypes.Structure, in calls of a few microseconds."""
+    pack = struct.Struct("@" + fmt).pack
+
+    def make(*members) -> bytes:
+        try:
+            return pack(*members)
+        except (struct.error, OverflowError) as e:
+            raise CodecGaugeError(-1, f"a parameter does not fit its type: {e}") from None
+    return make
 
 
-class _CRotary(ctypes.Structure):
-    _fields_ = [("rot", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("transpose", ctypes.c_int32),
-                ("mscale", ctypes.c_float)]
+_CPages = _packed("7i")        # dtype, n_pages, page, H, d, n_req, max_pages
+_CRotary = _packed("3if")      # rot, interleaved, transpose, mscale
+_CScaling = _packed("i5d")     # kind, base, factor, original, low, high
+_CStrides = _packed("8q")      # q_tok, q_head, k_tok, k_head, v_tok, v_head, o_tok, o_head
+_CPagedAttn = _packed("5if4q")  # n_tok, n_rep, max_new, window, sinks, scale, q_tok, q_head, o_tok, o_head
 
 
-class _CScaling(ctypes.Structure):
-    _fields_ = [("kind", ctypes.c_int32)] + [(n, ctypes.c_double) for n in ("base", "factor", "original", "low", "high")]
-
-
-class _CStrides(ctypes.Structure):
-    _fields_ = [(n, ctypes.c_int64) for n in ("q_tok", "q_head", "k_tok", "k_head", "v_tok", "v_head", "o_tok", "o_head")]
-
-
-class _CPagedAttn(ctypes.Structure):
-    _fields_ = [(n, ctypes.c_int32) for n in ("n_tok", "n_rep", "max_new", "window", "sinks")] + \
-        [("scale", ctypes.c_float)] + [(n, ctypes.c_int64) for n in ("q_tok", "q_head", "o_tok", "o_head")]
-
-
-@dataclass(frozen=True)
-class Pages:
+class Pages(NamedTuple):
     """Pool geometry (n_pages pages of `page` tokens, H KV heads of d channels) and block table
     [n_req][max_pages]. The plan and the release use neither H nor d."""
     n_pages: int
@@ -50,24 +48,22 @@ class Pages:
     n_req: int = 1
     max_pages: int = 1
 
-    def c(self, dtype: int = CG_BF16) -> _CPages:
+    def c(self, dtype: int = CG_BF16) -> bytes:
         return _CPages(dtype, self.n_pages, self.page, self.H, self.d, self.n_req, self.max_pages)
 
 
-@dataclass(frozen=True)
-class Rotary:
+class Rotary(NamedTuple):
     """The first `rot` channels of a head turn; see cg_rotary_params."""
     rot: int
     interleaved: bool = False
     mscale: float = 1.0
     transpose: bool = False
 
-    def c(self) -> _CRotary:
+    def c(self) -> bytes:
         return _CRotary(self.rot, int(self.interleaved), int(self.transpose), self.mscale)
 
 
-@dataclass(frozen=True)
-class RopeScaling:
+class RopeScaling(NamedTuple):
     """Frequency rule of rotary_table: kind CG_ROPE_NONE, _LINEAR, _BANDS or _YARN."""
     kind: int = CG_ROPE_NONE
     base: float = 10000.0
@@ -77,8 +73,7 @@ class RopeScaling:
     high: float = 4.0
 
 
-@dataclass(frozen=True)
-class PagedAttention:
+class PagedAttention(NamedTuple):
     """n_rep query heads per KV head, at most max_new new tokens per request; see cg_paged_attn."""
     n_rep: int
     max_new: int
@@ -87,16 +82,15 @@ class PagedAttention:
     sinks: int = 0
 
 
-_P = ctypes.POINTER
 _vp, _ci32, _ci64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
-_ARGS = {
-    "cg_page_plan": [_P(_CPages), _ci32] + [_vp] * 11,
-    "cg_page_release": [_P(_CPages)] + [_vp] * 8,
-    "cg_rotary_table": [_ci32, _P(_CScaling), _vp, _P(ctypes.c_float)],
-    "cg_rotary": [_P(_CRotary), _ci32, _ci32, _ci32, _ci32, _vp, _ci64, _ci64, _vp, _vp, _vp, _ci64, _ci64, _vp],
-    "cg_rotary_append": [_P(_CPages), _P(_CRotary), _ci32, _ci32, _P(_CStrides)] + [_vp] * 9,
-    "cg_paged_attention_workspace_bytes": [_P(_CPages), _P(_CPagedAttn), _P(ctypes.c_size_t)],
-    "cg_paged_attention": [_P(_CPages), _P(_CPagedAttn)] + [_vp] * 8 + [ctypes.c_size_t, _vp],
+_ARGS = {   # the first pointers are to parameter structs
+    "cg_page_plan": [_vp, _ci32] + [_vp] * 11,
+    "cg_page_release": [_vp] + [_vp] * 8,
+    "cg_rotary_table": [_ci32, _vp, _vp, ctypes.POINTER(ctypes.c_float)],
+    "cg_rotary": [_vp, _ci32, _ci32, _ci32, _ci32, _vp, _ci64, _ci64, _vp, _vp, _vp, _ci64, _ci64, _vp],
+    "cg_rotary_append": [_vp, _vp, _ci32, _ci32, _vp] + [_vp] * 9,
+    "cg_paged_attention_workspace_bytes": [_vp, _vp, ctypes.POINTER(ctypes.c_size_t)],
+    "cg_paged_attention": [_vp, _vp] + [_vp] * 8 + [ctypes.c_size_t, _vp],
 }
 _fns = {}
 _ws_bytes = {}
@@ -233,7 +227,7 @@ def rotary_append(pages: Pages, turn: Rotary, q, k, v, positions, slots, table, 
         _i64("table", table, turn.rot // 2) if turn.rot else None, op, _pool(pages, pool), _stream(stream)))
 
 
-def _attn(pages: Pages, how: PagedAttention, n: int, qt=0, qh=0, ot=0, oh=0) -> _CPagedAttn:
+def _attn(pages: Pages, how: PagedAttention, n: int, qt=0, qh=0, ot=0, oh=0) -> bytes:
     return _CPagedAttn(n, how.n_rep, how.max_new, how.window, how.sinks, how.scale, qt, qh, ot, oh)
 
 
