@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(kPT) plan_kernel(PlanArgs a) {
         }
         __syncthreads();
 
-        // page items of this round in the CTA's range
+        // page items of this pass in the CTA's range
         {
             const int64_t lo = f_lo > page_base ? f_lo : page_base, hi = f_hi < total_p ? f_hi : total_p;
             for (int64_t f = lo + tid; f < hi; f += kPT) {
@@ -191,7 +191,7 @@ __global__ void __launch_bounds__(kPT) plan_kernel(PlanArgs a) {
                 }
             }
         }
-        // tokens of this round in the CTA's range, four in a row per thread
+        // tokens of this pass in the CTA's range, four in a row per thread
         if (!RELEASE) {
             const int64_t t0 = t_lo + tid * 4;
             if (t0 + 3 >= tok_base && t0 < total_t && t0 < t_hi) {

@@ -58,6 +58,7 @@ struct RowsMisc {
     uint64_t full[6], empty[6];
     int64_t warp_sum[kThreads / 32];
     int64_t share, begin, before;
+    int units;           // of the share: end - begin
     int warp_longest[kThreads / 32];
     int start_req, abort_flag, last_part;
     Request start_r;
@@ -74,51 +75,65 @@ struct RowsParams {
     int box_rows;
 };
 
-// Cost of a request in chunks: (row tiles) x H x (chunks that its rows see).
+// A tile costs its chunks and kLead more, for its queries, joining and output: the copies in flight meanwhile
+// fill the ring and no more, so that a CTA of many short tiles falls behind (by 2 to 3 us a tile, where
+// a chunk takes 1.5 us). A cut of the line inside the lead falls before the tile. 41 ragged requests of up to
+// 7000 tokens, 16 KV heads: 173 us with a lead of 2, 192 with 1, 229 without (172 with 3, which costs
+// 64 histories of 16k tokens 637 us against 632). 1640 equal requests of 101 tokens have nothing to
+// balance and take 508 us against 491.
+constexpr int kLead = 2;
+
+// Cost of a request in line units: (row tiles) x H x (chunks that its rows see, and their lead).
 __device__ __forceinline__ int64_t request_cost(const RowsParams& P, int i, int32_t* flag, int* longest) {
     const Request r = load_request(P.a, i, flag);
     const int64_t rows = (int64_t)r.n * P.a.n_rep;
     if (r.n <= 0 || rows > P.max_rows) return 0;
     const Tiles t = visible_tiles<kTK>(P.a.window, P.a.sinks, r.len - r.n, r.len - 1);
     if (t.count() > *longest) *longest = t.count();
-    return (rows + kRows - 1) / kRows * P.a.H * t.count();
+    return (rows + kRows - 1) / kRows * P.a.H * (t.count() + kLead);
 }
 
-// Walk over a share: request, tile of 16 rows within it (KV head outermost), chunk.
+// Walk over a share: request, tile of 16 rows within it (KV head outermost).
 struct Walk {
-    int i, u, c;          // request, tile, next chunk of the tile
+    int i, u;             // request, tile
+    int left, x;          // of the share, in line units; offset of the share in the tile
     int n_tiles, n_chunks;
     Request r;
     Tiles t;
 
-    __device__ __forceinline__ void load(const RowsParams& P, int req) {
-        int32_t flag = 0;
-        i = req;
-        n_tiles = 0;
-        n_chunks = 1;
-        if (i < P.a.n_req) set(P, load_request(P.a, i, &flag));
-    }
+    // the tile's first chunk in the share, and the one past its last; the tile goes on past the share
+    __device__ __forceinline__ int c() const { return x > kLead ? x - kLead : 0; }
+    __device__ __forceinline__ bool goes_on() const { return kLead + n_chunks - x > left; }
+    __device__ __forceinline__ int end() const { return goes_on() ? x + left - kLead : n_chunks; }
     __device__ __forceinline__ void set(const RowsParams& P, const Request& req) {
         r = req;
-        u = c = 0;
+        n_tiles = 0;
+        n_chunks = 1;
         const int64_t rows = (int64_t)r.n * P.a.n_rep;
         if (r.n <= 0 || rows > P.max_rows) return;
         t = visible_tiles<kTK>(P.a.window, P.a.sinks, r.len - r.n, r.len - 1);
         n_chunks = t.count();
         n_tiles = (int)((rows + kRows - 1) / kRows) * P.a.H;
     }
-    __device__ __forceinline__ void start(const RowsParams& P, int req, const Request& q, int64_t off) {
+    __device__ __forceinline__ void start(const RowsParams& P, int req, const Request& q, int64_t off, int share) {
         i = req;
-        n_tiles = 0;
-        n_chunks = 1;
+        left = share;
         set(P, q);
-        u = (int)(off / n_chunks);
-        c = (int)(off - (int64_t)u * n_chunks);
+        u = (int)(off / (kLead + n_chunks));
+        x = (int)(off - (int64_t)u * (kLead + n_chunks));
+        if (end() <= c()) left = 0;                           // the tile begins in the next share
     }
     __device__ __forceinline__ void next_tile(const RowsParams& P) {
-        c = 0;
+        left -= kLead + n_chunks - x;
+        x = 0;
         u++;
-        while (u >= n_tiles && i < P.a.n_req) load(P, i + 1);
+        while (u >= n_tiles && left > 0) {
+            int32_t flag = 0;
+            u = 0;
+            if (++i >= P.a.n_req) left = 0;
+            else set(P, load_request(P.a, i, &flag));
+        }
+        if (left <= kLead) left = 0;
     }
     // rows of the current tile
     __device__ __forceinline__ int per_head(const RowsParams& P) const { return n_tiles / P.a.H; }
@@ -315,19 +330,19 @@ paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ 
     if (tid == 0) {
         M->share = share;
         M->begin = begin;
+        M->units = (int)(end - begin);
     }
     __syncthreads();
     if (blockIdx.x == 0) raise_flag(a.status, flag);
     if (begin >= end) return;
     volatile int* abort_flag = &M->abort_flag;
-    int left = (int)(end - begin);
     Walk w;
-    w.start(P, M->start_req, M->start_r, M->before);
+    w.start(P, M->start_req, M->start_r, M->before, (int)(end - begin));
 
-    // Registers: 128 a thread at launch; the consumers take what the others give up (128 x 208 + 128 x 40
+    // Registers: 128 a thread at launch; the consumers take what the others give up (128 x 200 + 128 x 56
     // of 256 x 128). With 168 each (five warps, no exchange) their loop spilled.
     if (warp >= kWarps) {
-        if (L::kCtas == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+        if (L::kCtas == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         if (warp > kWarps) return;
         // ------------------------------------------------------------ producer
         // lane k < n_box carries the boxes of token rows [k box_rows, ...) of a stage
@@ -335,18 +350,18 @@ paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ 
         int st = 0, ph = 1, issued = 0;
         int32_t pflag = 0;
         bool dead = *abort_flag != 0;
-        while (left > 0) {
+        while (w.left > 0) {
             const TileSpan sp(P, w);
             const int wlo = a.window ? w.r.len - w.r.n - a.window + 1 : 0;   // first token the request still needs
             const int32_t* row = a.table + (int64_t)w.i * a.max_pages;
-            const int take = w.n_chunks - w.c < left ? w.n_chunks - w.c : left;
+            const int first = w.c(), take = w.end() - first;
             // the places of a group of chunks are looked up at once, lane = chunk * n_box + box, one
             // group ahead of its use
             const int group = 32 / n_box, mine = lane / n_box, mybox = lane - mine * n_box;
             auto look = [&](int k0) {                // page of the lane's box, or -1: zeros
                 const int k = k0 + mine;
                 if (k >= take) return -1;
-                const int t = w.t.id(w.c + k) * kTK + mybox * P.box_rows;
+                const int t = w.t.id(first + k) * kTK + mybox * P.box_rows;
                 if (!(t < w.r.len && (t + P.box_rows > wlo || t < a.sinks))) return -1;
                 const int pg = __ldg(row + (t >> a.page_log2));
                 if (pg < 0 || pg >= a.n_pages) {
@@ -363,7 +378,7 @@ paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ 
                     ahead = look(k + group);
                 }
                 const int pg = __shfl_sync(0xffffffffu, now, (in * n_box + lane) & 31);
-                const int id = w.t.id(w.c + k);
+                const int id = w.t.id(first + k);
                 if (!sp.sees(a, id)) continue;
                 // past the pool (page 2 n_pages) the copy fills with zeros
                 const int z = pg < 0 ? 2 * a.n_pages : pg, y = pg < 0 ? 0 : sp.h * a.page + ((id * kTK + lane * P.box_rows) & (a.page - 1));
@@ -390,7 +405,6 @@ paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ 
                     ph ^= 1;
                 }
             }
-            left -= take;
             w.next_tile(P);
         }
         raise_flag(a.status, pflag);
@@ -400,15 +414,14 @@ paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ 
             bounded_wait<D>(&M->full[k % L::kStages], (k / L::kStages) & 1, &zero, tc::kWaitLimitNs);
     } else {
         // ------------------------------------------------------------ consumers
-        if (L::kCtas == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+        if (L::kCtas == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
         const int g = lane >> 2, j = lane & 3;   // rows g and g + 8; columns 2j, 2j + 1
         const float sl2 = a.scale * kLog2e;
         int st = 0, ph = 0;
-        bool dead = *abort_flag != 0, head_part = w.c > 0;
-        int from = -w.c;            // the tile's place in the line, from the share's beginning
-        while (left > 0) {
+        bool dead = *abort_flag != 0;
+        while (w.left > 0) {
             const TileSpan sp(P, w);
-            const int take = w.n_chunks - w.c < left ? w.n_chunks - w.c : left;
+            const int first = w.c(), take = w.end() - first;
             // queries of rows g, g + 8 as MMA operands
             uint32_t q[D / 16][4];
             int pos[2];
@@ -433,7 +446,7 @@ paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ 
             float ref[2] = {-INFINITY, -INFINITY}, sum[2] = {0.0f, 0.0f};
 
             for (int kc = 0; kc < take; kc++) {
-                const int id = w.t.id(w.c + kc);
+                const int id = w.t.id(first + kc);
                 if (!sp.sees(a, id)) continue;
                 if (!dead && !__all_sync(0xffffffffu, bounded_wait<D>(&M->full[st], ph, abort_flag, a.wait_ns))) {
                     dead = true;
@@ -641,8 +654,7 @@ paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ 
                 }
                 asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");
             }
-            const bool goes_on = w.c + take < w.n_chunks;
-            const bool whole = !head_part && !goes_on;
+            const bool whole = first == 0 && !w.goes_on();
             if (warp == 0) {
                 if (whole) {
 #pragma unroll
@@ -659,7 +671,7 @@ paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ 
                                 inv == 0.0f ? -INFINITY : (ref[hf] + log2f(sum[hf])) * kLn2;
                     }
                 } else {
-                    float* part = P.parts + ((int64_t)blockIdx.x * 2 + (head_part ? 0 : 1)) * part_floats(D);
+                    float* part = P.parts + ((int64_t)blockIdx.x * 2 + (first ? 0 : 1)) * part_floats(D);
 #pragma unroll
                     for (int hf = 0; hf < 2; hf++) {
                         if (g + 8 * hf >= sp.n_rows) continue;
@@ -674,10 +686,10 @@ paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ 
                 }
             }
             if (!whole) {
-                const int64_t at = M->begin + from;
+                const int64_t at = M->begin + (M->units - w.left) - w.x + kLead;   // of the tile's first chunk in the line
                 const int b0 = (int)(at / M->share), parts = (int)((at + w.n_chunks - 1) / M->share) - b0 + 1;
                 if (warp == 0) {
-                    const bool all = all_written(P.written, blockIdx.x * 2 + (head_part ? 0 : 1), b0, parts, P.epoch);
+                    const bool all = all_written(P.written, blockIdx.x * 2 + (first ? 0 : 1), b0, parts, P.epoch);
                     if (lane == 0) M->last_part = all;
                 }
                 asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");
@@ -686,9 +698,6 @@ paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ 
                     join_parts<FP16, D>(P, b0, parts, w.r.tok0, sp.row0, sp.n_rows, sp.h);
                 }
             }
-            from += w.n_chunks;
-            head_part = false;
-            left -= take;
             w.next_tile(P);
         }
         if (dead && tid == 0) raise_flag(a.status, CG_FLAG_PIPE_TIMEOUT);
