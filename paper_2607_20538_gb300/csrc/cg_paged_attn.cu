@@ -496,7 +496,7 @@ paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ 
                         mx[hf] = fmaxf(mx[hf], __shfl_xor_sync(0xffffffffu, mx[hf], 1));
                         mx[hf] = fmaxf(mx[hf], __shfl_xor_sync(0xffffffffu, mx[hf], 2));
                     }
-                    constexpr float kBias = Weights<FP16>::kBias;
+                    constexpr float kBias = Weights<FP16>::kBias, kLazy = Weights<FP16>::kLazy;
                     if (__any_sync(0xffffffffu, mx[0] > ref[0] + (kBias + kLazy) || mx[1] > ref[1] + (kBias + kLazy))) {
                         float f[2];
 #pragma unroll

@@ -331,14 +331,14 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
         "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
 }
-// 16 columns times f, in place
-__device__ __forceinline__ void tmem_scale16(uint32_t taddr, float f) {
-    uint32_t r[16];
-    tmem_ld16(taddr, r);
+// 32 columns times f, in place
+__device__ __forceinline__ void tmem_scale32(uint32_t taddr, float f) {
+    uint32_t r[32];
+    tmem_ld32p(taddr, r);
     tmem_wait_ld();
 #pragma unroll
-    for (int k = 0; k < 16; k++) r[k] = __float_as_uint(__uint_as_float(r[k]) * f);
-    tmem_st16(taddr, r);
+    for (int k = 0; k < 32; k++) r[k] = __float_as_uint(__uint_as_float(r[k]) * f);
+    tmem_st32(taddr, r);
 }
 
 __device__ __forceinline__ void tmem_ld32f(uint32_t taddr, float (&r)[32]) {
@@ -395,25 +395,26 @@ __device__ __forceinline__ uint32_t bits_between(int lo, int hi) {
 }
 
 // A tile that not every row sees whole: the row sees the columns [lo, hi] and those below sk; the
-// others are set to -inf.
+// others are set to -inf. 64 columns a turn.
 __device__ __noinline__ void mask_row(uint32_t s_tm, int lo, int hi, int sk) {
 #pragma unroll 1
-    for (int c0 = 0; c0 < kKT; c0 += 32) {
-        const uint32_t see = bits_between(lo - c0, hi - c0) | bits_between(0, (sk - 1 < hi ? sk - 1 : hi) - c0);
-        if (__all_sync(0xffffffffu, see == ~0u)) continue;
+    for (int c0 = 0; c0 < kKT; c0 += 64) {
+        const uint32_t see0 = bits_between(lo - c0, hi - c0) | bits_between(0, (sk - 1 < hi ? sk - 1 : hi) - c0);
+        const uint32_t see1 = bits_between(lo - c0 - 32, hi - c0 - 32) | bits_between(0, (sk - 1 < hi ? sk - 1 : hi) - c0 - 32);
+        if (__all_sync(0xffffffffu, (see0 & see1) == ~0u)) continue;
+        float u[32], v[32];
+        tmem_ld32f(s_tm + c0, u);
+        tmem_ld32f(s_tm + c0 + 32, v);
+        tmem_wait_ld();
+        settle(u);
+        settle(v);
         uint32_t r[32];
-        if (__any_sync(0xffffffffu, see != 0)) {
-            float u[32];
-            tmem_ld32f(s_tm + c0, u);
-            tmem_wait_ld();
-            settle(u);
 #pragma unroll
-            for (int k = 0; k < 32; k++) r[k] = see >> k & 1 ? __float_as_uint(u[k]) : 0xff800000u;
-        } else {
-#pragma unroll
-            for (int k = 0; k < 32; k++) r[k] = 0xff800000u;
-        }
+        for (int k = 0; k < 32; k++) r[k] = see0 & (1u << k) ? __float_as_uint(u[k]) : 0xff800000u;
         tmem_st32(s_tm + c0, r);
+#pragma unroll
+        for (int k = 0; k < 32; k++) r[k] = see1 & (1u << k) ? __float_as_uint(v[k]) : 0xff800000u;
+        tmem_st32(s_tm + c0 + 32, r);
     }
     tmem_wait_st();
 }
@@ -654,7 +655,7 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
         const uint32_t o_tm = kO + x * D + lanes;
         // a scale of 0 becomes the least number, so that a masked -inf stays one
         const float sl2 = fmaxf(fabsf(a.scale) * kLog2e, 1.17549435e-38f);
-        constexpr float kBias = Weights<FP16>::kBias;
+        constexpr float kBias = Weights<FP16>::kBias, kLazy = Weights<FP16>::kLazy;
         int ns = 0, no = 0, nv = 0;   // active steps, tiles and value tiles so far
         bool head_part = w.left > 0 && w.c > 0, dead = *abort_flag != 0;
         int meta_last = -1;
@@ -707,10 +708,10 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                         const float nr = raise ? mx - kBias : ref;
                         // never 0 x inf in O: a factor below all numbers becomes the least one
                         const float f = ref == nr ? 1.0f : fmaxf(ex2(ref - nr), 1.17549435e-38f);
-                        if (started) {
+                        if (started && __any_sync(0xffffffffu, raise && ref != -INFINITY)) {   // (a row that has seen nothing holds 0)
                             if (!quiet()) break;
 #pragma unroll 1
-                            for (int c0 = 0; c0 < D; c0 += 16) tmem_scale16(o_tm + c0, f);
+                            for (int c0 = 0; c0 < D; c0 += 32) tmem_scale32(o_tm + c0, f);
                         }
                         sum *= ref == -INFINITY ? 0.0f : f;
                         ref = nr;
