@@ -331,14 +331,14 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
         "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
 }
-// 32 columns times f, in place
-__device__ __forceinline__ void tmem_scale32(uint32_t taddr, float f) {
-    uint32_t r[32];
-    tmem_ld32p(taddr, r);
+// 16 columns times f, in place
+__device__ __forceinline__ void tmem_scale16(uint32_t taddr, float f) {
+    uint32_t r[16];
+    tmem_ld16(taddr, r);
     tmem_wait_ld();
 #pragma unroll
-    for (int k = 0; k < 32; k++) r[k] = __float_as_uint(__uint_as_float(r[k]) * f);
-    tmem_st32(taddr, r);
+    for (int k = 0; k < 16; k++) r[k] = __float_as_uint(__uint_as_float(r[k]) * f);
+    tmem_st16(taddr, r);
 }
 
 __device__ __forceinline__ void tmem_ld32f(uint32_t taddr, float (&r)[32]) {
@@ -711,7 +711,7 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                         if (started && __any_sync(0xffffffffu, raise && ref != -INFINITY)) {   // (a row that has seen nothing holds 0)
                             if (!quiet()) break;
 #pragma unroll 1
-                            for (int c0 = 0; c0 < D; c0 += 32) tmem_scale32(o_tm + c0, f);
+                            for (int c0 = 0; c0 < D; c0 += 16) tmem_scale16(o_tm + c0, f);
                         }
                         sum *= ref == -INFINITY ? 0.0f : f;
                         ref = nr;
