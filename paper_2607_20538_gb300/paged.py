@@ -238,11 +238,27 @@ def paged_attention_workspace_bytes(pages: Pages, how: PagedAttention, n_tok: in
     return v.value
 
 
+_kept = {}   # device -> workspace of the default stream, where calls follow one another
+
+
+def _workspace(pages: Pages, how: PagedAttention, n: int, device):
+    key = (pages.d, how.n_rep, how.max_new, device)   # all that the size depends on
+    nbytes = _ws_bytes.get(key)
+    if nbytes is None:
+        nbytes = _ws_bytes[key] = paged_attention_workspace_bytes(pages, how, n)
+    if _stream(None) != 0:      # other streams end; the default one does not, and is never captured
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    kept = _kept.get(device)
+    if kept is None or kept.nbytes < nbytes:
+        kept = _kept[device] = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    return kept
+
+
 def paged_attention(pages: Pages, how: PagedAttention, q, pool, block_table, seq_lens, cu_new, out, lse=None,
                     workspace=None, stream=None) -> None:
     """Attention of the new tokens' queries q [n_tok][H * n_rep][d] over their requests' pages
     (cg_paged_attention). Without a workspace the call takes one from torch's allocator, on the
-    current stream (pass one to run on another)."""
+    current stream (pass one to run on another); the default stream's is kept for its next call."""
     n, hq = q.shape[0], pages.H * how.n_rep
     qp, qt, qh = _heads("q", q, n, hq, pages.d, pool.dtype)
     op, ot, oh = _heads("out", out, n, hq, pages.d, pool.dtype)
@@ -255,13 +271,9 @@ def paged_attention(pages: Pages, how: PagedAttention, q, pool, block_table, seq
     if workspace is None:
         if stream is not None and stream != torch.cuda.current_stream():
             _bad("workspace: needed on a stream that is not the current one")
-        key = (pages.d, how.n_rep, how.max_new, q.device)   # all that the size depends on
-        nbytes = _ws_bytes.get(key)
-        if nbytes is None:
-            nbytes = _ws_bytes[key] = paged_attention_workspace_bytes(pages, how, n)
-        workspace = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+        workspace = _workspace(pages, how, n, q.device)
     r = pages.n_req
     _check(_fn("cg_paged_attention")(
         cp, ca, qp, _pool(pages, pool), _i32("block_table", block_table, r * pages.max_pages),
         _i32("seq_lens", seq_lens, r), _i32("cu_new", cu_new, r + 1), op, lp, workspace.data_ptr(),
-        workspace.numel() * workspace.element_size(), _stream(stream)))
+        workspace.nbytes, _stream(stream)))

@@ -72,3 +72,27 @@ def test_program():
                        capture_output=True, text=True, timeout=300)
     assert r.returncode == 0, r.stderr
     assert "lengths [90, 37, 1504, 260]" in r.stdout and "attention off by" in r.stdout
+
+
+def test_kept_workspace():
+    """Calls of different workspace sizes one after the other on the default stream, against calls with
+    a workspace of their own."""
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    cases = []
+    for d, n_rep, lens, new in [(64, 2, [70, 300], [1, 1]), (128, 4, [500, 40, 333], [90, 1, 200]), (64, 2, [70, 300], [1, 1]),
+                                (256, 1, [200], [200]), (128, 4, [9, 1000], [1, 1])]:
+        H, page, per = 2, 16, 64
+        pages = cg.Pages(n_pages=len(lens) * per, page=page, H=H, d=d, n_req=len(lens), max_pages=per)
+        rnd = lambda *s: torch.randn(*s, generator=gen, device="cuda").to(torch.bfloat16)  # noqa: E731
+        i32 = lambda v: torch.tensor(np.asarray(v), dtype=torch.int32).cuda()  # noqa: E731
+        q = rnd(sum(new), H * n_rep, d)
+        cases.append((pages, cg.PagedAttention(n_rep, max(new), d ** -0.5), q, rnd(2, len(lens) * per, H, page, d),
+                      i32(np.arange(len(lens) * per).reshape(len(lens), per)), i32(lens), i32(np.concatenate([[0], np.cumsum(new)]))))
+    kept = [torch.empty_like(c[2]) for c in cases]
+    for c, o in zip(cases, kept):
+        cg.paged_attention(*c, o)
+    for c, o in zip(cases, kept):
+        own = torch.empty_like(o)
+        ws = torch.empty(cg.paged_attention_workspace_bytes(c[0], c[1], own.shape[0]), dtype=torch.uint8, device="cuda")
+        cg.paged_attention(*c, own, workspace=ws)
+        assert torch.equal(own, o)
