@@ -15,6 +15,10 @@
 // that a cut goes through is written in parts; the CTA that writes its last part joins them, in
 // their order whoever is last (a merge kernel of its own took 3 us of GPU and 4 us of host time more a
 // call). A tile is cut into at most kMaxParts.
+// Measured, 8 KV heads of 128 with 4 query heads each: 64 histories of 16384 tokens 632 us, 6.8 TB/s;
+// of 4096 174 us, 6.2 TB/s; 256 of 1001 177 us; one of 32768 44 us; one of 1000 14 us (start, four
+// copies' latency and the join). Up to 16 rows a request: above, the tiles of cg_paged_chunk.cu are
+// faster (4 query heads, 5 tokens = 20 rows: two tiles here read the keys twice).
 #include <chrono>
 
 #include "cg_paged_dev.cuh"
@@ -747,15 +751,23 @@ bool paged_pool_map(CUtensorMap* map, const PagedArgs& a, uint32_t box_rows) {
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Requests of more query rows run on the 128-row tiles of cg_paged_chunk.cu. Among others up to 16, a
+// tile here: 64 histories of 2000 tokens with 16 rows take 101 us here and 113 there, with 20 rows 175 and
+// 114 (two tiles read the keys twice). One request alone is cut into many parts, whose rows four warps
+// join here and many CTAs there: after 3000 tokens 8 rows take 21.0 us here and 19.5 there (300: 14.7, 16.3),
+// 16 rows 28.7 and 19.7; for d = 256 8 rows 26.9 and 22.6.
+static int rows_limit(const PagedArgs& a) { return a.n_req > 1 ? kRows : a.d == 256 ? 4 : 8; }
+static bool long_requests(const PagedArgs& a) { return (int64_t)a.max_new * a.n_rep > rows_limit(a); }
+
 // The two kernels of a call may run beside each other: each has its own part of the workspace.
 size_t paged_attn_workspace(const PagedArgs& a) {
     const size_t r = (rows_workspace(a.d) + 255) / 256 * 256;
-    return (int64_t)a.max_new * a.n_rep <= kRows ? r : r + paged_chunk_workspace(a.d);
+    return long_requests(a) ? r + paged_chunk_workspace(a.d) : r;
 }
 
 cudaError_t launch_paged_attn(const PagedArgs& a, void* workspace, cudaStream_t st) {
-    const int limit = kRows;   // longer requests run on the 128-row tiles of cg_paged_chunk.cu
-    const bool long_ones = (int64_t)a.max_new * a.n_rep > limit;
+    const int limit = rows_limit(a);
+    const bool long_ones = long_requests(a);
     cudaError_t e = cudaSuccess;
     // short requests beside long ones; one request alone goes to the tiles whatever its rows
     const bool short_ones = !long_ones || (a.n_req > 1 && a.n_rep <= limit);

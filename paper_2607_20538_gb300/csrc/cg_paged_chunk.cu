@@ -1,11 +1,12 @@
 // cg_paged_chunk.cu -- paged attention of requests with many query rows (a chunk or a whole prompt):
 // o = softmax(scale q K^T) V on the tensor cores (contract: include/codecgauge_paged.h).
 //
-// A tile of work is up to 256 query rows of one request and KV head, as two halves A and B of 128
-// rows (rows are (token, query head of the group), a half the whole tokens that fit). One CTA per SM walks its share of the key tiles:
+// A tile of work is up to 256 query rows of one request and KV head, as two halves A and B of 128 rows
+// (rows are (token, query head of the group), a half the whole tokens that fit); for d = 256 one half. One
+// CTA per SM walks its share of the key tiles:
 //   warps 0-3, 4-7  softmax of half A, half B: a thread owns a row: 128 scores from tensor memory,
 //                   running reference and sum in registers, weights back to tensor memory;
-//   warp 8          TMA: 128-token tiles of keys and values, K0 V0 K1 V1 ..., boxes of pages;
+//   warp 8          TMA: 128-token tiles of keys and values in rings of their own, boxes of pages;
 //   warps 9, 10     one thread each issues half A's, half B's tcgen05.mma: S = Q K^T (both operands in
 //                   shared memory) and O += P V (P in tensor memory over S, V token-major as it
 //                   lies in the page);
@@ -16,9 +17,16 @@
 // instructions between the products of the two halves, about 900 cycles a step, kept the tensor cores
 // idle.) S(j) follows PV(j-1) in issue order, so S may overwrite P, and its completion tells the
 // softmax that O is quiescent: the thread rescales its row of O itself on the rare steps that raise
-// the reference by more than 2^8.
-// Bound: the tensor cores (4 x 128 x 128 x d multiply-adds per key tile against 128 x 256
-// exponentials and about four times as many other operations).
+// the reference (by more than Weights::kLazy powers of two).
+// Bound: the tensor cores (4 x 128 x 128 x d multiply-adds per key tile against 128 x 256 exponentials
+// and about four times as many other operations), as far as a half's chain lets them: for d = 128 a
+// step takes 2500 cycles, its softmax 1400 of them, and both halves' products 2048. Tensor memory is
+// full (two halves of scores and accumulators), so that no scores are computed ahead. Measured, 32 query
+// heads on 8 KV heads: 2048 tokens after 32k 0.68 ms, 1.66 PFLOP/s (0.77 ms in a long run, under the
+// power cap); a prompt of 8192 0.365 ms, 1.5 PFLOP/s; d = 64 0.29 ms, 0.95 PFLOP/s (half the products for the
+// same softmax); d = 256 1.9 ms after 32k, 1.2 PFLOP/s: its tiles of 128 rows need 64 bytes a cycle
+// and SM from L2. Sixteen softmax warps (two threads a row, 96 registers) took 1.09 ms: their loop spilled. A
+// quarter of the exponentials as polynomials on the FMA units: 0.75 ms against 0.72 the same day.
 //
 // What a row does not see must not reach it, and 0 x inf would: in tiles that some rows see and
 // others do not, warp 11 takes special values (and whatever lies past the request's end) out of the
@@ -151,12 +159,13 @@ __device__ __forceinline__ Tiles tile_tiles(const ChunkParams& P, const Request&
 // a key tile. A cut of the line inside those kTileCost units falls before the tile.
 constexpr int kTileCost = 3;
 
-// A tile cut in two costs about as much as kSplitCost key tiles: a second start and end, and the
-// joining kernel. Where there are no more tiles than CTAs and the largest takes no longer than an equal share and
-// that, each CTA takes a whole tile: a prompt of 1024 tokens (128 tiles of 4 to 11 units) 26.9 us against
-// 30.4, of 300 18.8 against 20.7; with 12 instead of 7, 512 tokens after 1000 took 32.4 us against 29.2. (The
-// look at it costs calls of many tiles 0.7 us.)
-constexpr int kSplitCost = 7;
+// A tile cut in two costs about as much as kSplitCost key tiles: a second start and end, and the joining
+// kernel; with few CTAs at work kSplitLeast, as their parts join faster. Where there are no more tiles than
+// CTAs and the largest takes no longer than an equal share and that, each CTA takes a whole tile: a
+// prompt of 1024 tokens (128 tiles of 4 to 11 units) 26.9 us against 30.4, of 300 18.8 against 20.7. With 12
+// instead of 7, 512 tokens after 1000 took 32.4 us against 29.2; with 7 for few CTAs too, 4 tokens after 1000
+// took 22.3 us against 18.7. (The look at it costs calls of many tiles 0.7 us.)
+constexpr int kSplitCost = 7, kSplitLeast = 4;
 
 __device__ __forceinline__ int row_tiles(const ChunkParams& P, const Request& r) {
     const int64_t rows = (int64_t)r.n * P.a.n_rep;
@@ -646,7 +655,7 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
     const int64_t begin = share * blockIdx.x;
     const int64_t end = begin + share < total ? begin + share : total;
     // a tile for each CTA, or an equal share of the line
-    const bool whole_tiles = n_tiles <= gridDim.x && largest <= share + kSplitCost;
+    const bool whole_tiles = n_tiles <= gridDim.x && largest <= share + kSplitLeast + (int)((kSplitCost - kSplitLeast) * total / (share * gridDim.x));
     if (whole_tiles) {
         const uint32_t b = blockIdx.x;
         if (b >= tiles_before && b < tiles_before + tiles) {
