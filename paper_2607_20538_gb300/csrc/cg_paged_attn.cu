@@ -756,18 +756,18 @@ bool paged_pool_map(CUtensorMap* map, const PagedArgs& a, uint32_t box_rows) {
 // 114 (two tiles read the keys twice). One request alone is cut into many parts, whose rows four warps
 // join here and many CTAs there: after 3000 tokens 8 rows take 21.0 us here and 19.5 there (300: 14.7, 16.3),
 // 16 rows 28.7 and 19.7; for d = 256 8 rows 26.9 and 22.6.
-static int rows_limit(const PagedArgs& a) { return a.n_req > 1 ? kRows : a.d == 256 ? 4 : 8; }
-static bool long_requests(const PagedArgs& a) { return (int64_t)a.max_new * a.n_rep > rows_limit(a); }
+static int rows_limit(int d, bool alone) { return !alone ? kRows : d == 256 ? 4 : 8; }
 
-// The two kernels of a call may run beside each other: each has its own part of the workspace.
+// The two kernels of a call may run beside each other: each has its own part of the workspace. The same
+// for any number of requests, so that a program can size it once.
 size_t paged_attn_workspace(const PagedArgs& a) {
     const size_t r = (rows_workspace(a.d) + 255) / 256 * 256;
-    return long_requests(a) ? r + paged_chunk_workspace(a.d) : r;
+    return (int64_t)a.max_new * a.n_rep > rows_limit(a.d, true) ? r + paged_chunk_workspace(a.d) : r;
 }
 
 cudaError_t launch_paged_attn(const PagedArgs& a, void* workspace, cudaStream_t st) {
-    const int limit = rows_limit(a);
-    const bool long_ones = long_requests(a);
+    const int limit = rows_limit(a.d, a.n_req == 1);
+    const bool long_ones = (int64_t)a.max_new * a.n_rep > limit;
     cudaError_t e = cudaSuccess;
     // short requests beside long ones; one request alone goes to the tiles whatever its rows
     const bool short_ones = !long_ones || (a.n_req > 1 && a.n_rep <= limit);

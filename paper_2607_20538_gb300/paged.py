@@ -242,7 +242,7 @@ _kept = {}   # device -> workspace of the default stream, where calls follow one
 
 
 def _workspace(pages: Pages, how: PagedAttention, n: int, device):
-    key = (pages.d, how.n_rep, how.max_new, pages.n_req == 1, device)   # all that the size depends on
+    key = (pages.d, how.n_rep, how.max_new, device)   # all that the size depends on
     nbytes = _ws_bytes.get(key)
     if nbytes is None:
         nbytes = _ws_bytes[key] = paged_attention_workspace_bytes(pages, how, n)

@@ -52,3 +52,22 @@ def test_shares(name, dtype):
     again, lse2 = _attend(c)
     assert (again == out).all() and (lse2 == lse).all()
     assert cg.get_status() == 0
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_workspace_is_sized_once(d):
+    """A workspace sized for many requests serves one, and one for the most rows serves fewer."""
+    torch = pytest.importorskip("torch")
+    pages = cg.Pages(n_pages=64, page=16, H=2, d=d, n_req=50, max_pages=40)
+    sizes = [cg.paged_attention_workspace_bytes(pages, cg.PagedAttention(4, new, 0.1), 50 * new) for new in (1, 2, 3, 4, 5, 40)]
+    assert sizes == sorted(sizes)
+    for new in (1, 2, 4, 5, 40):
+        c = _case("bf16", d, 2, 4, 16, [500], [new])
+        one = cg.Pages(n_pages=c["pool"].shape[1], page=16, H=2, d=d, n_req=1, max_pages=c["table"].shape[1])
+        how = cg.PagedAttention(4, new, d ** -0.5)
+        ws = torch.empty(cg.paged_attention_workspace_bytes(pages, how, 50 * new), dtype=torch.uint8, device="cuda")
+        q = c["q"].cuda()
+        out, lse = torch.empty_like(q), torch.empty(new, 8, device="cuda")
+        t = lambda v: torch.tensor(np.asarray(v), dtype=torch.int32).cuda()  # noqa: E731
+        cg.paged_attention(one, how, q, c["pool"].cuda(), t(c["table"]), t(c["lens"]), t(c["cu"]), out, lse, workspace=ws)
+        _check(c, out, lse)
