@@ -166,8 +166,10 @@ int cg_rotary_append(const cg_pages* pages, const cg_rotary_params* rotary, int3
  *   strides in elements, multiples of 8. q [n_tok][H * n_rep][d], out alike, lse fp32
  *   [n_tok][H * n_rep] contiguous or NULL.
  * workspace: device scratch of cg_paged_attention_workspace_bytes, owned by the caller; needs no
- * initial value and may be shared by calls that follow one another on one stream. Its size does not
- * depend on n_req, n_tok or the pages, and does not shrink as n_rep or max_new grow. */
+ * initial value and may be shared by calls that are issued one after the other on one stream. (A call
+ * is up to three launches: two host threads that call at the same time, on one stream too, may mix
+ * theirs and need a workspace each.) Its size does not depend on n_req, n_tok or the pages, and does
+ * not shrink as n_rep or max_new grow. */
 typedef struct {
     int32_t n_tok, n_rep, max_new;
     int32_t window, sinks;

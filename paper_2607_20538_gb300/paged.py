@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import struct
+import threading
 from typing import NamedTuple
 
 import torch
@@ -238,7 +239,16 @@ def paged_attention_workspace_bytes(pages: Pages, how: PagedAttention, n_tok: in
     return v.value
 
 
-_kept = {}   # device -> workspace of the default stream, where calls follow one another
+class _Kept(threading.local):
+    """Workspaces (by device) of one host thread's calls on the default stream. The calls of one thread
+    follow one another there; those of two threads may mix their launches, of which a call has up to
+    three, so that each thread needs its own."""
+
+    def __init__(self):
+        self.by_device = {}
+
+
+_kept = _Kept()
 
 
 def _workspace(pages: Pages, how: PagedAttention, n: int, device):
@@ -248,9 +258,10 @@ def _workspace(pages: Pages, how: PagedAttention, n: int, device):
         nbytes = _ws_bytes[key] = paged_attention_workspace_bytes(pages, how, n)
     if _stream(None) != 0:      # other streams end; the default one does not, and is never captured
         return torch.empty(nbytes, dtype=torch.uint8, device=device)
-    kept = _kept.get(device)
+    mine = _kept.by_device
+    kept = mine.get(device)
     if kept is None or kept.nbytes < nbytes:
-        kept = _kept[device] = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        kept = mine[device] = torch.empty(nbytes, dtype=torch.uint8, device=device)
     return kept
 
 
@@ -258,7 +269,9 @@ def paged_attention(pages: Pages, how: PagedAttention, q, pool, block_table, seq
                     workspace=None, stream=None) -> None:
     """Attention of the new tokens' queries q [n_tok][H * n_rep][d] over their requests' pages
     (cg_paged_attention). Without a workspace the call takes one from torch's allocator, on the
-    current stream (pass one to run on another); the default stream's is kept for its next call."""
+    current stream (pass one to run on another); the default stream's is kept for the next call of the
+    same host thread, until the thread ends. A workspace that is passed serves calls made one after the
+    other: two threads must not pass the same one at the same time."""
     n, hq = q.shape[0], pages.H * how.n_rep
     qp, qt, qh = _heads("q", q, n, hq, pages.d, pool.dtype)
     op, ot, oh = _heads("out", out, n, hq, pages.d, pool.dtype)
