@@ -11,7 +11,16 @@
 
 namespace cg {
 
+// The encoder is a driver call and wants a current context, which a host thread gets with its first
+// runtime call that needs one: a thread whose first call is this library's has none yet.
+inline void bind_context() {
+    static thread_local int bound = -1;
+    int dev = -1;
+    if (cudaGetDevice(&dev) == cudaSuccess && dev != bound && cudaSetDevice(dev) == cudaSuccess) bound = dev;
+}
+
 inline PFN_cuTensorMapEncodeTiled_v12000 tmap_encode_fn() {
+    bind_context();
     static PFN_cuTensorMapEncodeTiled_v12000 fn = nullptr;
     static std::once_flag once;
     std::call_once(once, [] {

@@ -1,5 +1,6 @@
-"""Two host threads that attend on the default stream at the same time: each gets what it gets alone,
-bit for bit, and nothing is written past its outputs."""
+"""Calls from several host threads. Two that attend on the default stream at the same time: each gets
+what it gets alone, bit for bit, and nothing is written past its outputs. A thread whose first use of
+the GPU is a call of the library."""
 import threading
 
 import numpy as np
@@ -11,6 +12,21 @@ cg = pytest.importorskip("paper_2607_20538_gb300")
 pytestmark = pytest.mark.gpu
 
 CALLS = 150
+
+
+def _in_a_new_thread(call):
+    failed = []
+
+    def run():
+        try:
+            call()
+        except Exception as e:  # noqa: BLE001
+            failed.append(e)
+
+    t = threading.Thread(target=run)
+    t.start()
+    t.join()
+    assert not failed
 
 
 def _state(seed, lens, new, n_rep, d, window):
@@ -62,3 +78,32 @@ def test_two_threads_on_the_default_stream(other):
     for _, out, lse, n in states:
         assert torch.isnan(out[n:]).all() and torch.isnan(lse[n:]).all()
     assert cg.get_status() == 0
+
+
+@pytest.mark.parametrize("lens,new", [([300, 40], [1, 1]), ([300, 90], [60, 45])])
+def test_attention_as_a_threads_first_call(lens, new):
+    """Everything the call needs is there, so that nothing but the call itself touches the GPU."""
+    args, out, lse, n = _state(3, lens, new, 4, 128, 0)
+    cg.paged_attention(*args, out[:n], lse[:n])
+    want, o = out[:n].clone(), out[:n].zero_()
+    ws = torch.empty(cg.paged_attention_workspace_bytes(*args[:2], n), dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    _in_a_new_thread(lambda: cg.paged_attention(*args, o, lse[:n], ws))
+    assert torch.equal(o, want) and cg.get_status() == 0
+
+
+def test_codec_as_a_threads_first_call():
+    """The tensor-core encode and decode: tensor maps, like the attention."""
+    shape, params = cg.Shape(2, 1, 4, 256, 128), cg.Params(cg.CG_BLOCK_UNIFORM, 128, 4, block=64)
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    x = torch.randn(2, 2, 1, 4, 256, 128, generator=gen, device="cuda").bfloat16()
+    g = torch.linalg.qr(torch.randn(2 * 2 * 4, 128, 128, generator=gen, device="cuda"))[0].contiguous()
+    a, b = cg.alloc_outputs(shape, params), cg.alloc_outputs(shape, params)
+    y, z = torch.empty_like(x), torch.empty_like(x)
+    cg.encode(shape, params, x, g, *a[:2])
+    cg.decode(shape, params, *a[:2], None, g, y)
+    torch.cuda.synchronize()
+    _in_a_new_thread(lambda: cg.encode(shape, params, x, g, *b[:2]))
+    torch.cuda.synchronize()
+    _in_a_new_thread(lambda: cg.decode(shape, params, *b[:2], None, g, z))
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1]) and torch.equal(y, z) and cg.get_status() == 0
