@@ -186,16 +186,20 @@ __device__ __forceinline__ uint32_t special_mask(uint32_t v) {
 // are written: of the CTAs that finish at the same time at least one sees so (each writes its own word
 // before it reads the others', with a fence between); if two do, both join, to the same values. (A
 // counter instead cost up to 16 us: a compare-and-swap per arrival and retry.) The warp that wrote the
-// part calls.
+// part calls. Its lanes wrote pieces of it on different ways: each fences its own, and the word follows
+// when all have; the last fence stands between the words seen and the parts read (by this CTA, behind a
+// barrier).
 __device__ __forceinline__ bool all_written(unsigned long long* words, int mine, int b0, int parts, uint64_t epoch) {
     const int lane = threadIdx.x & 31;
     auto word = [&](int p) { return reinterpret_cast<volatile unsigned long long*>(words) + ((int64_t)(b0 + p) * 2 + (p == 0 ? 1 : 0)); };
     __threadfence();
+    __syncwarp();
     if (lane == 0) reinterpret_cast<volatile unsigned long long*>(words)[mine] = epoch;
     __syncwarp();
     __threadfence();
     bool all = true;
     for (int p = lane; p < parts; p += 32) all &= *word(p) == epoch;
+    __threadfence();
     all = __all_sync(0xffffffffu, all);
     if (all)
         for (int p = lane; p < parts; p += 32) *word(p) = 0ull;
@@ -697,10 +701,7 @@ paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ 
                     if (lane == 0) M->last_part = all;
                 }
                 asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");
-                if (*(volatile int*)&M->last_part) {
-                    __threadfence();
-                    join_parts<FP16, D>(P, b0, parts, w.r.tok0, sp.row0, sp.n_rows, sp.h);
-                }
+                if (*(volatile int*)&M->last_part) join_parts<FP16, D>(P, b0, parts, w.r.tok0, sp.row0, sp.n_rows, sp.h);
             }
             w.next_tile(P);
         }
