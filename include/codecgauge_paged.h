@@ -74,10 +74,15 @@ int cg_page_plan(const cg_pages* pages, int32_t n_tok, const int32_t* ctx_lens, 
                  int32_t* seq_lens, int32_t* cu_new, int32_t* positions, int64_t* slots,
                  int32_t* free_left, void* stream);
 
-/* Give back the pages of every request with done[i] != 0: with n = lens[i] tokens held, its P(n)
- * pages go on the stack in order of request and page, free_pages[free_count + k]; free_left =
- * free_count + their number; lens_left[i] = 0 for these and lens[i] for the others. block_table is
- * not changed. free_left and lens_left must not alias free_count and lens. */
+/* Give back the pages of every request with done[i] != 0: with n = lens[i] tokens held, the pages
+ * in its first P(n) table entries go on the stack in order of request and entry,
+ * free_pages[free_count + k]; free_left = free_count + their number; lens_left[i] = 0 for these and
+ * lens[i] for the others. An entry of -1 is no page and is passed over: what a plan that ran out of
+ * pages leaves, and what a program writes in place of a page that it has put back on the stack itself
+ * (a windowed request's old ones; an entry left standing would come on the stack a second time). Any
+ * other entry outside the pool is passed over too and raises CG_FLAG_PAGED_RANGE, as pages do that
+ * the stack of n_pages entries has no room for. block_table is not changed. free_left and lens_left
+ * must not alias free_count and lens. */
 int cg_page_release(const cg_pages* pages, const int32_t* lens, const int32_t* done, const int32_t* block_table,
                     int32_t* free_pages, const int32_t* free_count, int32_t* lens_left, int32_t* free_left,
                     void* stream);
@@ -155,8 +160,8 @@ int cg_rotary_append(const cg_pages* pages, const cg_rotary_params* rotary, int3
  * A query that sees nothing (a negative position) gives o = 0 and lse = -inf. Scores, softmax and
  * sums are fp32; the weights enter the value product rounded to the pool's type; o is rounded once.
  * Rows of the pool past a request's length are never used, whatever they hold (NaN and infinities
- * too); block table entries of pages that no query sees are not used either (a windowed request may
- * have given its old pages back).
+ * too); block table entries of pages that no query sees are not used either (a windowed request's old
+ * pages may be back on the stack, with -1 in their entries).
  *   n_tok   : rows of q, out and lse; cu_new[n_req] <= n_tok (rows from cu_new[n_req] on are left
  *             untouched)
  *   n_rep   : query heads per KV head, 1 .. 64
