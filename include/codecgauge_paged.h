@@ -67,7 +67,9 @@ typedef struct {
  * plan that ran out of pages can be dropped and made again: then CG_FLAG_PAGES_EXHAUSTED is
  * raised, free_left is negative (the pages that lack), and tokens without a page have slot -1.
  * A request that outgrows max_pages, a negative length, more than n_tok new tokens or a bad entry
- * of free_pages or block_table raises CG_FLAG_PAGED_RANGE; the tokens concerned get slot -1.
+ * of free_pages or block_table raises CG_FLAG_PAGED_RANGE; the tokens concerned get slot -1. More
+ * than n_tok tokens in all raise it too; of the pages that these would need, the first n_tok + n_req
+ * are dealt out.
  * One launch. Integer arithmetic only. n_tok may be 0. */
 int cg_page_plan(const cg_pages* pages, int32_t n_tok, const int32_t* ctx_lens, const int32_t* new_lens,
                  const int32_t* free_pages, const int32_t* free_count, int32_t* block_table,

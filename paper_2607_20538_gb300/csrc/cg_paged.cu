@@ -99,7 +99,10 @@ __global__ void __launch_bounds__(kPT) plan_kernel(PlanArgs a) {
     const int64_t t_hi = t_lo + kTokCta < a.n_tok ? t_lo + kTokCta : a.n_tok;
     const bool last_cta = blockIdx.x == gridDim.x - 1;
     const int64_t f_lo = (int64_t)blockIdx.x * a.pages_per_cta;
-    const int64_t f_hi = last_cta ? (int64_t)1 << 62 : f_lo + a.pages_per_cta;
+    // A plan whose tokens fit n_tok needs no more pages than tokens. Wrong lengths can ask for any number:
+    // those past this limit are not dealt out (the prefix in shared memory is right below 2^31 - 1 only).
+    const int64_t most = (int64_t)a.n_tok + a.n_req < 0x7fffffff ? (int64_t)a.n_tok + a.n_req : 0x7fffffff;
+    const int64_t f_hi = last_cta || f_lo + a.pages_per_cta > most ? most : f_lo + a.pages_per_cta;
     int64_t count = __ldg(a.count_in);
     if (count < 0 || count > a.n_pages) {
         flag |= CG_FLAG_PAGED_RANGE;
