@@ -60,7 +60,7 @@ typedef struct {
  * and for the tokens in order, request by request, token k of request i at t = cu_new[i] + k:
  *   positions[t] = ctx_i + k,  slots[t] = block_table[i][positions[t] / page] * page + positions[t] % page
  * free_left[0] = free_count[0] - sum of fresh. free_pages is a stack: [n_pages] entries, of which
- * the first free_count[0] are free.
+ * the first free_count[0] are free (a count outside 0 .. n_pages raises CG_FLAG_PAGED_RANGE).
  * n_tok is the size of positions and slots; entries past the last token get position 0 and slot -1
  * (a padded batch). seq_lens and free_left must not alias ctx_lens, new_lens and free_count: the
  * call changes nothing that it reads (block_table entries of tokens already held among them), so a
@@ -75,6 +75,14 @@ int cg_page_plan(const cg_pages* pages, int32_t n_tok, const int32_t* ctx_lens, 
                  const int32_t* free_pages, const int32_t* free_count, int32_t* block_table,
                  int32_t* seq_lens, int32_t* cu_new, int32_t* positions, int64_t* slots,
                  int32_t* free_left, void* stream);
+
+/* The same with a stack of n_stack entries, which may be fewer than n_pages (what a program never
+ * gives back needs no place; with n_stack 0 free_pages may be NULL). A free_count above n_stack
+ * raises CG_FLAG_PAGED_RANGE and counts as n_stack. */
+int cg_page_plan_stack(const cg_pages* pages, int32_t n_tok, const int32_t* ctx_lens, const int32_t* new_lens,
+                       const int32_t* free_pages, int32_t n_stack, const int32_t* free_count, int32_t* block_table,
+                       int32_t* seq_lens, int32_t* cu_new, int32_t* positions, int64_t* slots, int32_t* free_left,
+                       void* stream);
 
 /* Give back the pages of every request with done[i] != 0: with n = lens[i] tokens held, the pages
  * in its first P(n) table entries go on the stack in order of request and entry,

@@ -29,7 +29,7 @@ struct PlanArgs {
     int32_t *table, *lens_out, *cu, *pos, *count_out;
     int64_t* slots;
     int32_t* status;
-    int n_tok, n_pages, page, page_log2, n_req, max_pages;
+    int n_tok, n_pages, n_stack, page, page_log2, n_req, max_pages;
     int64_t pages_per_cta;
 };
 
@@ -104,9 +104,9 @@ __global__ void __launch_bounds__(kPT) plan_kernel(PlanArgs a) {
     const int64_t most = (int64_t)a.n_tok + a.n_req < 0x7fffffff ? (int64_t)a.n_tok + a.n_req : 0x7fffffff;
     const int64_t f_hi = last_cta || f_lo + a.pages_per_cta > most ? most : f_lo + a.pages_per_cta;
     int64_t count = __ldg(a.count_in);
-    if (count < 0 || count > a.n_pages) {
+    if (count < 0 || count > a.n_stack) {
         flag |= CG_FLAG_PAGED_RANGE;
-        count = count < 0 ? 0 : a.n_pages;
+        count = count < 0 ? 0 : a.n_stack;
     }
 
     int64_t tok_base = 0, page_base = 0;   // prefix at the start of the round
@@ -645,11 +645,22 @@ CG_EXPORT int cg_page_plan(const cg_pages* pages, int32_t n_tok, const int32_t* 
                            int32_t* seq_lens, int32_t* cu_new, int32_t* positions, int64_t* slots,
                            int32_t* free_left, void* stream) {
     set_error(CG_OK, "%s", "");
+    if (!free_pages) return set_error(CG_EINVAL, "null pointer");
+    return cg_page_plan_stack(pages, n_tok, ctx_lens, new_lens, free_pages, pages ? pages->n_pages : 0, free_count, block_table,
+                              seq_lens, cu_new, positions, slots, free_left, stream);
+}
+
+CG_EXPORT int cg_page_plan_stack(const cg_pages* pages, int32_t n_tok, const int32_t* ctx_lens, const int32_t* new_lens,
+                                 const int32_t* free_pages, int32_t n_stack, const int32_t* free_count,
+                                 int32_t* block_table, int32_t* seq_lens, int32_t* cu_new, int32_t* positions,
+                                 int64_t* slots, int32_t* free_left, void* stream) {
+    set_error(CG_OK, "%s", "");
     int rc = check_pages(pages, false);
     if (!rc) rc = check_table(pages);
     if (rc) return rc;
     if (n_tok < 0) return set_error(CG_EINVAL, "n_tok=%d: must be >= 0", n_tok);
-    if (!ctx_lens || !new_lens || !free_pages || !free_count || !block_table || !seq_lens || !cu_new || !free_left)
+    if (n_stack < 0) return set_error(CG_EINVAL, "n_stack=%d: must be >= 0", n_stack);
+    if (!ctx_lens || !new_lens || (n_stack && !free_pages) || !free_count || !block_table || !seq_lens || !cu_new || !free_left)
         return set_error(CG_EINVAL, "null pointer");
     if (n_tok && (!positions || !slots)) return set_error(CG_EINVAL, "null positions or slots");
     if (!al16(positions) || !al16(slots)) return set_error(CG_EINVAL, "positions and slots must be 16-byte aligned");
@@ -672,6 +683,7 @@ CG_EXPORT int cg_page_plan(const cg_pages* pages, int32_t n_tok, const int32_t* 
     a.count_out = free_left;
     a.n_tok = n_tok;
     a.n_pages = pages->n_pages;
+    a.n_stack = n_stack < pages->n_pages ? n_stack : pages->n_pages;
     a.page = pages->page;
     a.page_log2 = log2_of(pages->page);
     a.n_req = pages->n_req;

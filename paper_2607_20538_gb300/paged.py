@@ -86,6 +86,7 @@ class PagedAttention(NamedTuple):
 _vp, _ci32, _ci64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
 _ARGS = {   # the first pointers are to parameter structs
     "cg_page_plan": [_vp, _ci32] + [_vp] * 11,
+    "cg_page_plan_stack": [_vp, _ci32, _vp, _vp, _vp, _ci32] + [_vp] * 8,
     "cg_page_release": [_vp] + [_vp] * 8,
     "cg_rotary_table": [_ci32, _vp, _vp, ctypes.POINTER(ctypes.c_float)],
     "cg_rotary": [_vp, _ci32, _ci32, _ci32, _ci32, _vp, _ci64, _ci64, _vp, _vp, _vp, _ci64, _ci64, _vp],
@@ -170,13 +171,13 @@ def _pool(pages: Pages, pool) -> int:
 
 def page_plan(pages: Pages, ctx_lens, new_lens, free_pages, free_count, block_table, seq_lens, cu_new, positions, slots,
               free_left, stream=None) -> None:
-    """Pages for the new tokens of every request, and positions and slots of all new tokens (cg_page_plan).
-    The number of tokens planned for is positions.numel()."""
+    """Pages for the new tokens of every request, and positions and slots of all new tokens
+    (cg_page_plan_stack). The number of tokens planned for is positions.numel(), the stack's size
+    free_pages.numel(), which may be less than n_pages, and 0."""
     n, r = positions.numel(), pages.n_req
-    _check(_fn("cg_page_plan")(
+    _check(_fn("cg_page_plan_stack")(
         pages.c(), n, _i32("ctx_lens", ctx_lens, r), _i32("new_lens", new_lens, r),
-        # a stack that is full of used pages may be an empty tensor: no entry of it is read
-        _i32("free_pages", free_pages, 0) or free_count.data_ptr(), _i32("free_count", free_count, 1),
+        _i32("free_pages", free_pages, 0), min(free_pages.numel(), pages.n_pages), _i32("free_count", free_count, 1),
         _i32("block_table", block_table, r * pages.max_pages), _i32("seq_lens", seq_lens, r),
         _i32("cu_new", cu_new, r + 1), _i32("positions", positions, n), _i64("slots", slots, n),
         _i32("free_left", free_left, 1), _stream(stream)))
