@@ -286,6 +286,8 @@ def paged_attention(pages: Pages, how: PagedAttention, q, pool, block_table, seq
         if stream is not None and stream != torch.cuda.current_stream():
             _bad("workspace: needed on a stream that is not the current one")
         workspace = _workspace(pages, how, n, q.device)
+    elif not workspace.is_cuda or not workspace.is_contiguous():
+        _bad("workspace: expected a contiguous device tensor")
     r = pages.n_req
     _check(_fn("cg_paged_attention")(
         cp, ca, qp, _pool(pages, pool), _i32("block_table", block_table, r * pages.max_pages),
