@@ -125,36 +125,47 @@ def _elem(t) -> int:
 
 # The current stream's handle without a Stream object around it, where torch has that.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-_device = getattr(torch._C, "_cuda_getDevice", None)
+_get_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _device() -> int:
+    """The current device, on which a call launches; -2, where no tensor is, without a GPU."""
+    try:
+        return _get_device()
+    except RuntimeError:
+        return -2
 
 
 def _stream(stream) -> int:
     if stream is not None:
+        if getattr(stream, "device_index", _device()) != _device():
+            _bad(f"stream: on device {stream.device_index}, the current one is {_device()}")
         return stream.cuda_stream
-    if _raw_stream is not None and _device is not None:
-        return _raw_stream(_device())
+    if _raw_stream is not None:
+        return _raw_stream(_get_device())
     return torch.cuda.current_stream().cuda_stream
 
 
-def _i32(name: str, t, n: int) -> int:
-    """Address of a contiguous device array of at least n 32-bit integers."""
-    if t.dtype is not _INT32 or not t.is_cuda or t.numel() < n or not t.is_contiguous():
-        _bad(f"{name}: expected a contiguous int32 device tensor of at least {n} elements")
+# In the checks, dev is the device that the call launches on.
+def _i32(name: str, t, n: int, dev: int) -> int:
+    """Address of a contiguous array of at least n 32-bit integers on the device."""
+    if t.dtype is not _INT32 or t.get_device() != dev or t.numel() < n or not t.is_contiguous():
+        _bad(f"{name}: expected a contiguous int32 device tensor of at least {n} elements, on device {dev}")
     return t.data_ptr()
 
 
-def _i64(name: str, t, n: int) -> int:
-    if t.dtype is not _INT64 or not t.is_cuda or t.numel() < n or not t.is_contiguous():
-        _bad(f"{name}: expected a contiguous int64 device tensor of at least {n} elements")
+def _i64(name: str, t, n: int, dev: int) -> int:
+    if t.dtype is not _INT64 or t.get_device() != dev or t.numel() < n or not t.is_contiguous():
+        _bad(f"{name}: expected a contiguous int64 device tensor of at least {n} elements, on device {dev}")
     return t.data_ptr()
 
 
-def _heads(name: str, t, n_tok: int, heads: int, d: int, dtype):
-    """Checks a [n_tok][heads][d] device tensor; returns its address and its two strides."""
+def _heads(name: str, t, n_tok: int, heads: int, d: int, dtype, dev: int):
+    """Checks a [n_tok][heads][d] tensor on the device; returns its address and its two strides."""
     if t.shape != (n_tok, heads, d):
         _bad(f"{name}: expected shape [{n_tok}, {heads}, {d}], got {list(t.shape)}")
-    if t.dtype is not dtype or not t.is_cuda:
-        _bad(f"{name}: expected a {dtype} device tensor")
+    if t.dtype is not dtype or t.get_device() != dev:
+        _bad(f"{name}: expected a {dtype} tensor on device {dev}")
     tok, head, one = t.stride()
     if one != 1:
         _bad(f"{name}: the last dimension must be contiguous")
@@ -162,9 +173,9 @@ def _heads(name: str, t, n_tok: int, heads: int, d: int, dtype):
     return t.data_ptr(), (tok if n_tok > 1 else 0), (head if heads > 1 else 0)
 
 
-def _pool(pages: Pages, pool) -> int:
-    if pool.shape != (2, pages.n_pages, pages.H, pages.page, pages.d) or not pool.is_contiguous() or not pool.is_cuda:
-        _bad(f"pool: expected a contiguous device tensor [2, {pages.n_pages}, {pages.H}, {pages.page}, {pages.d}], "
+def _pool(pages: Pages, pool, dev: int) -> int:
+    if pool.shape != (2, pages.n_pages, pages.H, pages.page, pages.d) or not pool.is_contiguous() or pool.get_device() != dev:
+        _bad(f"pool: expected a contiguous tensor [2, {pages.n_pages}, {pages.H}, {pages.page}, {pages.d}] on device {dev}, "
              f"got {list(pool.shape)}")
     return pool.data_ptr()
 
@@ -174,22 +185,22 @@ def page_plan(pages: Pages, ctx_lens, new_lens, free_pages, free_count, block_ta
     """Pages for the new tokens of every request, and positions and slots of all new tokens
     (cg_page_plan_stack). The number of tokens planned for is positions.numel(), the stack's size
     free_pages.numel(), which may be less than n_pages, and 0."""
-    n, r = positions.numel(), pages.n_req
+    n, r, dev = positions.numel(), pages.n_req, _device()
     _check(_fn("cg_page_plan_stack")(
-        pages.c(), n, _i32("ctx_lens", ctx_lens, r), _i32("new_lens", new_lens, r),
-        _i32("free_pages", free_pages, 0), min(free_pages.numel(), pages.n_pages), _i32("free_count", free_count, 1),
-        _i32("block_table", block_table, r * pages.max_pages), _i32("seq_lens", seq_lens, r),
-        _i32("cu_new", cu_new, r + 1), _i32("positions", positions, n), _i64("slots", slots, n),
-        _i32("free_left", free_left, 1), _stream(stream)))
+        pages.c(), n, _i32("ctx_lens", ctx_lens, r, dev), _i32("new_lens", new_lens, r, dev),
+        _i32("free_pages", free_pages, 0, dev), free_pages.numel(), _i32("free_count", free_count, 1, dev),
+        _i32("block_table", block_table, r * pages.max_pages, dev), _i32("seq_lens", seq_lens, r, dev),
+        _i32("cu_new", cu_new, r + 1, dev), _i32("positions", positions, n, dev), _i64("slots", slots, n, dev),
+        _i32("free_left", free_left, 1, dev), _stream(stream)))
 
 
 def page_release(pages: Pages, lens, done, block_table, free_pages, free_count, lens_left, free_left, stream=None) -> None:
     """Give back the pages of the requests whose done flag (int32) is set (cg_page_release)."""
-    r = pages.n_req
+    r, dev = pages.n_req, _device()
     _check(_fn("cg_page_release")(
-        pages.c(), _i32("lens", lens, r), _i32("done", done, r), _i32("block_table", block_table, r * pages.max_pages),
-        _i32("free_pages", free_pages, pages.n_pages), _i32("free_count", free_count, 1),
-        _i32("lens_left", lens_left, r), _i32("free_left", free_left, 1), _stream(stream)))
+        pages.c(), _i32("lens", lens, r, dev), _i32("done", done, r, dev), _i32("block_table", block_table, r * pages.max_pages, dev),
+        _i32("free_pages", free_pages, pages.n_pages, dev), _i32("free_count", free_count, 1, dev),
+        _i32("lens_left", lens_left, r, dev), _i32("free_left", free_left, 1, dev), _stream(stream)))
 
 
 def rotary_table(rot: int, scaling: RopeScaling = RopeScaling(), device="cuda"):
@@ -205,28 +216,28 @@ def rotary(turn: Rotary, x, positions, table, out, stream=None) -> None:
     """out = rotary(x), [n_tok][heads][d] (cg_rotary); out may be x."""
     if x.dim() != 3:
         _bad("x: expected [n_tok, heads, d]")
-    n, heads, d = x.shape
-    xp, xt, xh = _heads("x", x, n, heads, d, x.dtype)
-    op, ot, oh = _heads("out", out, n, heads, d, x.dtype)
-    _check(_fn("cg_rotary")(turn.c(), _elem(x), n, heads, d, xp, xt, xh, _i32("positions", positions, n),
-                            _i64("table", table, turn.rot // 2) if turn.rot else None, op, ot, oh, _stream(stream)))
+    (n, heads, d), dev = x.shape, _device()
+    xp, xt, xh = _heads("x", x, n, heads, d, x.dtype, dev)
+    op, ot, oh = _heads("out", out, n, heads, d, x.dtype, dev)
+    _check(_fn("cg_rotary")(turn.c(), _elem(x), n, heads, d, xp, xt, xh, _i32("positions", positions, n, dev),
+                            _i64("table", table, turn.rot // 2, dev) if turn.rot else None, op, ot, oh, _stream(stream)))
 
 
 def rotary_append(pages: Pages, turn: Rotary, q, k, v, positions, slots, table, q_out, pool, stream=None) -> None:
     """q_out = rotary(q); rotary(k) and v into the pool at their slots (cg_rotary_append). q and
     q_out may be None, or the same tensor."""
-    n = k.shape[0]
+    n, dev = k.shape[0], _device()
     hq = 0 if q is None else q.shape[1]
     if k.dtype is not pool.dtype:
         _bad(f"k: expected the pool's type {pool.dtype}, got {k.dtype}")
-    kp, kt, kh = _heads("k", k, n, pages.H, pages.d, pool.dtype)
-    vp, vt, vh = _heads("v", v, n, pages.H, pages.d, pool.dtype)
-    qp, qt, qh = _heads("q", q, n, hq, pages.d, pool.dtype) if hq else (None, 0, 0)
-    op, ot, oh = _heads("q_out", q_out, n, hq, pages.d, pool.dtype) if hq else (None, 0, 0)
+    kp, kt, kh = _heads("k", k, n, pages.H, pages.d, pool.dtype, dev)
+    vp, vt, vh = _heads("v", v, n, pages.H, pages.d, pool.dtype, dev)
+    qp, qt, qh = _heads("q", q, n, hq, pages.d, pool.dtype, dev) if hq else (None, 0, 0)
+    op, ot, oh = _heads("q_out", q_out, n, hq, pages.d, pool.dtype, dev) if hq else (None, 0, 0)
     _check(_fn("cg_rotary_append")(
         pages.c(_elem(pool)), turn.c(), n, hq, _CStrides(qt, qh, kt, kh, vt, vh, ot, oh), qp, kp, vp,
-        _i32("positions", positions, n), _i64("slots", slots, n),
-        _i64("table", table, turn.rot // 2) if turn.rot else None, op, _pool(pages, pool), _stream(stream)))
+        _i32("positions", positions, n, dev), _i64("slots", slots, n, dev),
+        _i64("table", table, turn.rot // 2, dev) if turn.rot else None, op, _pool(pages, pool, dev), _stream(stream)))
 
 
 def _attn(pages: Pages, how: PagedAttention, n: int, qt=0, qh=0, ot=0, oh=0) -> bytes:
@@ -273,23 +284,23 @@ def paged_attention(pages: Pages, how: PagedAttention, q, pool, block_table, seq
     current stream (pass one to run on another); the default stream's is kept for the next call of the
     same host thread, until the thread ends. A workspace that is passed serves calls made one after the
     other: two threads must not pass the same one at the same time."""
-    n, hq = q.shape[0], pages.H * how.n_rep
-    qp, qt, qh = _heads("q", q, n, hq, pages.d, pool.dtype)
-    op, ot, oh = _heads("out", out, n, hq, pages.d, pool.dtype)
+    n, hq, dev = q.shape[0], pages.H * how.n_rep, _device()
+    qp, qt, qh = _heads("q", q, n, hq, pages.d, pool.dtype, dev)
+    op, ot, oh = _heads("out", out, n, hq, pages.d, pool.dtype, dev)
     lp = None
     if lse is not None:
-        if lse.dtype is not _FLOAT32 or not lse.is_cuda or not lse.is_contiguous() or lse.numel() < n * hq:
-            _bad(f"lse: expected a contiguous float32 device tensor [{n}, {hq}]")
+        if lse.dtype is not _FLOAT32 or lse.get_device() != dev or not lse.is_contiguous() or lse.numel() < n * hq:
+            _bad(f"lse: expected a contiguous float32 tensor [{n}, {hq}] on device {dev}")
         lp = lse.data_ptr()
     cp, ca = pages.c(_elem(pool)), _attn(pages, how, n, qt, qh, ot, oh)
     if workspace is None:
         if stream is not None and stream != torch.cuda.current_stream():
             _bad("workspace: needed on a stream that is not the current one")
         workspace = _workspace(pages, how, n, q.device)
-    elif not workspace.is_cuda or not workspace.is_contiguous():
-        _bad("workspace: expected a contiguous device tensor")
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
+        _bad(f"workspace: expected a contiguous tensor on device {dev}")
     r = pages.n_req
     _check(_fn("cg_paged_attention")(
-        cp, ca, qp, _pool(pages, pool), _i32("block_table", block_table, r * pages.max_pages),
-        _i32("seq_lens", seq_lens, r), _i32("cu_new", cu_new, r + 1), op, lp, workspace.data_ptr(),
+        cp, ca, qp, _pool(pages, pool, dev), _i32("block_table", block_table, r * pages.max_pages, dev),
+        _i32("seq_lens", seq_lens, r, dev), _i32("cu_new", cu_new, r + 1, dev), op, lp, workspace.data_ptr(),
         workspace.nbytes, _stream(stream)))

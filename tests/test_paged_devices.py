@@ -70,3 +70,45 @@ def test_a_workspace_on_the_host_is_refused(calls):
             _make("attention", dict(t, workspace=bad))
         assert e.value.code == -1 and "workspace" in str(e.value)
     assert len(calls) == 1
+
+
+@pytest.mark.parametrize("call", ["plan", "release", "rotary", "append", "attention"])
+def test_every_tensor_is_on_the_calls_device(call, calls):
+    shapes = _tensors(call)
+    make = lambda **index: {k: OnDevice(*v, index.get(k, 0)) for k, v in shapes.items()}  # noqa: E731
+    _make(call, make())
+    assert len(calls) == 1
+    for name in shapes:
+        for index in (1, -1):
+            with pytest.raises(cg.CodecGaugeError) as e:
+                _make(call, make(**{name: index}))
+            assert e.value.code == -1 and str(e.value).startswith(f"CG_EINVAL: {name}:"), name
+    assert len(calls) == 1
+
+
+@pytest.mark.parametrize("call", ["plan", "release", "rotary", "append", "attention"])
+def test_a_stream_of_another_device_is_refused(call, calls, monkeypatch):
+    monkeypatch.undo()
+    monkeypatch.setattr(paged, "_fn", lambda name: lambda *a: calls.append(name) or 0)
+    monkeypatch.setattr(paged, "_device", lambda: 0)
+
+    class Stream:
+        cuda_stream = 5
+
+        def __init__(self, index):
+            self.device_index = index
+
+    t = {k: OnDevice(*v) for k, v in _tensors(call).items()}
+    _make(call, t, stream=Stream(0))
+    with pytest.raises(cg.CodecGaugeError) as e:
+        _make(call, t, stream=Stream(1))
+    assert e.value.code == -1 and "stream" in str(e.value) and len(calls) == 1
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="a machine without a GPU is meant")
+def test_without_a_gpu_the_refusal_is_the_same(calls, monkeypatch):
+    monkeypatch.undo()
+    t = {k: torch.empty(shape, dtype=dt) for k, (shape, dt) in _tensors("attention").items()}
+    with pytest.raises(cg.CodecGaugeError) as e:
+        _make("attention", t)
+    assert e.value.code == -1
