@@ -266,7 +266,7 @@ __device__ __noinline__ void join_parts(const RowsParams& P, int b0, int parts, 
 #pragma unroll
         for (int e = 0; e < V; e += 2) *reinterpret_cast<uint32_t*>(dst + e) = pack2<FP16>(o[e] * inv, o[e + 1] * inv);
         if (a.lse && lane == 0)
-            a.lse[(int64_t)(tok0 + tk) * a.H * a.n_rep + hd] = inv == 0.0f ? -INFINITY : (R + log2f(l)) * kLn2;
+            a.lse[(int64_t)(tok0 + tk) * a.H * a.n_rep + hd] = inv == 0.0f ? -INFINITY : RowWeights<FP16>::lse(R, l);
     }
 }
 
@@ -504,7 +504,7 @@ paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ 
                         mx[hf] = fmaxf(mx[hf], __shfl_xor_sync(0xffffffffu, mx[hf], 1));
                         mx[hf] = fmaxf(mx[hf], __shfl_xor_sync(0xffffffffu, mx[hf], 2));
                     }
-                    constexpr float kBias = Weights<FP16>::kBias, kLazy = Weights<FP16>::kLazy;
+                    constexpr float kBias = RowWeights<FP16>::kBias, kLazy = RowWeights<FP16>::kLazy;
                     if (__any_sync(0xffffffffu, mx[0] > ref[0] + (kBias + kLazy) || mx[1] > ref[1] + (kBias + kLazy))) {
                         float f[2];
 #pragma unroll
@@ -676,7 +676,7 @@ paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ 
                             *reinterpret_cast<uint32_t*>(dst + 8 * k) = pack2<FP16>(o[k][2 * hf] * inv, o[k][2 * hf + 1] * inv);
                         if (a.lse && j == 0)
                             a.lse[(int64_t)(w.r.tok0 + tk) * a.H * a.n_rep + hd] =
-                                inv == 0.0f ? -INFINITY : (ref[hf] + log2f(sum[hf])) * kLn2;
+                                inv == 0.0f ? -INFINITY : RowWeights<FP16>::lse(ref[hf], sum[hf]);
                     }
                 } else {
                     float* part = P.parts + ((int64_t)blockIdx.x * 2 + (first ? 0 : 1)) * part_floats(D);

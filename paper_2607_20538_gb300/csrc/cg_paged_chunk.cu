@@ -17,7 +17,7 @@
 // instructions between the products of the two halves, about 900 cycles a step, kept the tensor cores
 // idle.) S(j) follows PV(j-1) in issue order, so S may overwrite P, and its completion tells the
 // softmax that O is quiescent: the thread rescales its row of O itself on the rare steps that raise
-// the reference (by more than Weights::kLazy powers of two).
+// the reference (by more than TileWeights::kLazy powers of two).
 // Bound: the tensor cores (4 x 128 x 128 x d multiply-adds per key tile against 128 x 256 exponentials
 // and about four times as many other operations), as far as a half's chain lets them: for d = 128 a
 // step takes 2500 cycles, its softmax 1400 of them, and both halves' products 2048. Tensor memory is
@@ -723,7 +723,7 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
         const uint32_t o_tm = kO + x * D + lanes;
         // a scale of 0 becomes the least number, so that a masked -inf stays one
         const float sl2 = fmaxf(fabsf(a.scale) * kLog2e, 1.17549435e-38f);
-        constexpr float kBias = Weights<FP16>::kBias, kLazy = Weights<FP16>::kLazy;
+        constexpr float kBias = TileWeights<FP16>::kBias, kLazy = TileWeights<FP16>::kLazy;
         int ns = 0, no = 0, nv = 0;   // active steps, tiles and value tiles so far
         bool head_part = w.left > 0 && w.c > 0, dead = *abort_flag != 0;
         int meta_last = -1;
@@ -857,7 +857,7 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                         store_rows(b, my_dst, 2 * c0);
                     }
                     if (a.lse && have)
-                        a.lse[(int64_t)(tok0 + tk) * a.H * a.n_rep + hd] = inv == 0.0f ? -INFINITY : (ref + log2f(sum)) * kLn2;
+                        a.lse[(int64_t)(tok0 + tk) * a.H * a.n_rep + hd] = inv == 0.0f ? -INFINITY : TileWeights<FP16>::lse(ref, sum);
                 } else {
                     float* part = P.parts + ((int64_t)blockIdx.x * 2 + (head_part ? 0 : 1)) * chunk_part_floats(D);
                     const int r = x * kHalfRows + row;
@@ -1345,7 +1345,7 @@ __global__ void __launch_bounds__(tile_rows(D)) paged_chunk_merge_kernel(const _
         dst[q] = make_uint4(b[0], b[1], b[2], b[3]);
     }
     if (a.lse && blockIdx.y == 0)
-        a.lse[(int64_t)(m.tok0 + tk) * a.H * a.n_rep + hd] = inv == 0.0f ? -INFINITY : (R + log2f(l)) * kLn2;
+        a.lse[(int64_t)(m.tok0 + tk) * a.H * a.n_rep + hd] = inv == 0.0f ? -INFINITY : TileWeights<FP16>::lse(R, l);
 }
 
 // Queries as [n_tok][H][n_rep][d] (their strides), boxes of a half's tokens x n_rep heads x 64
