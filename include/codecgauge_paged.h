@@ -168,7 +168,9 @@ int cg_rotary_append(const cg_pages* pages, const cg_rotary_params* rotary, int3
  * head j / n_rep:
  *   o = sum_t softmax_t(scale q . k_t) v_t,   lse = ln sum_t exp(scale q . k_t)
  * A query that sees nothing (a negative position) gives o = 0 and lse = -inf. Scores, softmax and
- * sums are fp32; the weights enter the value product rounded to the pool's type; o is rounded once.
+ * sums are fp32; the weights enter the value product rounded to the pool's type (summed before that), a
+ * row's largest among them but for requests of up to 16 query rows per KV head; o is rounded once.
+ * Values may be as large as fp32 has room for their sum over the visible tokens.
  * Rows of the pool past a request's length are never used, whatever they hold (NaN and infinities
  * too); block table entries of pages that no query sees are not used either (a windowed request's old
  * pages may be back on the stack, with -1 in their entries).

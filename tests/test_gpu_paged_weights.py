@@ -47,3 +47,26 @@ def test_the_largest_weight_is_not_rounded(dtype, rep, whole):
     err = np.abs(num(out) - want)
     assert (err <= tol).all(), f"worst error / bound {(err / tol).max():.3g}"
     assert cg.get_status() == 0
+
+
+@pytest.mark.parametrize("power", [118, 110, 0, -100, -120])
+@pytest.mark.parametrize("d,lens,new", [(128, [700], [1]), (128, [700], [300]), (64, [700, 300], [300, 40]), (256, [500], [200])])
+def test_the_range_of_values(d, lens, new, power):
+    """bf16 values of about 2^power under scores that climb by up to 2^15 from the first tokens to the last:
+    an output is a mean of values, finite wherever they leave fp32 room for the sum over the tokens. Off by
+    at most paged_ref.attention_tolerance, in units of 2^power (what fp32 does not hold below 2^-126 adds
+    2^-149 a token to a sum of weights of 2^-16 at least: 2^-123 for 1000 tokens)."""
+    c = _case("bf16", d, 2, 2, 16, lens, new, seed=7)
+    rng = np.random.default_rng(7)
+    scale = _set_scores(c, [np.sort(rng.uniform(0, 15, n)) for n in lens])
+    unit = c["pool"].clone()
+    c["pool"][1] = (c["pool"][1].double() * 2.0 ** power).to(c["pool"].dtype)
+    unit[1] = (c["pool"][1].double() * 2.0 ** -power).to(unit.dtype)
+    out, lse = _attend(c, scale)
+    want, wl, mag, big = ref.attention(num(c["q"]), num(unit), c["table"], c["lens"], c["cu"], 2, scale)
+    to, tl = ref.attention_tolerance(False, d, want, mag, big)
+    got = num(out) * 2.0 ** -power
+    assert np.isfinite(got).all()
+    err, to = np.abs(got - want), to + 2.0 ** (-123 - power) + 2.0 ** (-133 - power)
+    assert (err <= to).all(), f"worst error / bound {(err / to).max():.3g}"
+    assert (np.abs(num(lse) - wl) <= tl + 2.0 ** -22 * np.abs(wl)).all()
