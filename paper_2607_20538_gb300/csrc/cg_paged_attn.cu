@@ -166,8 +166,8 @@ struct TileSpan {
     }
 };
 
-// With registers exchanged (two CTAs per SM) a wait cannot be a call; with one CTA it is, which leaves
-// the loop more registers.
+// With registers exchanged (two CTAs per SM) a wait in the loops must not be a call (wait_here); with one
+// CTA it is, which leaves the loop more registers.
 template <int D>
 __device__ __forceinline__ bool bounded_wait(uint64_t* bar, uint32_t parity, const volatile int* abort, uint64_t limit_ns) {
     return RowsSmem<D>::kCtas == 2 ? wait_here(bar, parity, abort, limit_ns) : mbar_wait(bar, parity, abort, limit_ns);

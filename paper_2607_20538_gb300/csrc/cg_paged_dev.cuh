@@ -41,8 +41,9 @@ using TileWeights = Weights<FP16 ? 7 : -16, FP16 ? 8 : 16>;
 template <bool FP16>
 using RowWeights = Weights<FP16 ? 15 : 0, 0>;
 
-// mbar_wait, whole in its place: kernels that exchange registers between warps (setmaxnreg) cannot
-// call functions.
+// mbar_wait, whole in its place, for kernels that exchange registers between warps (setmaxnreg): with the
+// wait as a call inside their loops the compiler finds no allocation within the split (it does for a call
+// at the end of a tile).
 __device__ __forceinline__ bool wait_here(uint64_t* bar, uint32_t parity, const volatile int* abort, uint64_t limit_ns) {
     const bool poll = limit_ns < 1000000ull;   // the diagnostic setting of mbar_wait
     if (!poll && mbar_try_wait(bar, parity)) return true;
