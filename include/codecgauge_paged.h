@@ -141,13 +141,15 @@ typedef struct {
 int cg_rotary_table(int32_t rot, const cg_rope_scaling* scaling, int64_t* host_table, float* mscale);
 
 /* out = rotary(x), x and out [n_tok][heads][d] with the given strides in elements (multiples of 8;
- * the last dimension is contiguous). out may be x itself with the same strides. positions int32
+ * the last dimension is contiguous; 0 repeats an element of x, and is refused for out unless there is
+ * but one). out may be x itself with the same strides. positions int32
  * [n_tok]; dtype and d as in cg_pages (d 64, 128 or 256). Pointers 16-byte aligned. */
 int cg_rotary(const cg_rotary_params* rotary, int32_t dtype, int32_t n_tok, int32_t heads, int32_t d,
               const void* x, int64_t x_tok, int64_t x_head, const int32_t* positions, const int64_t* table,
               void* out, int64_t out_tok, int64_t out_head, void* stream);
 
-/* Strides in elements of the queries, keys and values of cg_rotary_append (multiples of 8). */
+/* Strides in elements of the queries, keys and values of cg_rotary_append (multiples of 8; o of q_out,
+ * not 0 over more than one element). */
 typedef struct {
     int64_t q_tok, q_head, k_tok, k_head, v_tok, v_head, o_tok, o_head;
 } cg_append_strides;
@@ -180,7 +182,8 @@ int cg_rotary_append(const cg_pages* pages, const cg_rotary_params* rotary, int3
  *   max_new : an upper bound of the n_i (sizes the launches; a request with more raises
  *             CG_FLAG_PAGED_RANGE and its output is not written)
  *   window  : >= 0, sinks : >= 0 (only with a window);  scale : finite
- *   strides in elements, multiples of 8. q [n_tok][H * n_rep][d], out alike, lse fp32
+ *   strides in elements, multiples of 8 (o of out, not 0 over more than one element).
+ *   q [n_tok][H * n_rep][d], out alike, lse fp32
  *   [n_tok][H * n_rep] contiguous or NULL.
  * workspace: device scratch of cg_paged_attention_workspace_bytes, owned by the caller; needs no
  * initial value and may be shared by calls that are issued one after the other on one stream. (A call

@@ -621,6 +621,13 @@ int check_rotary(const cg_rotary_params* r, int d, const void* table) {
 
 bool stride8(int64_t s) { return s >= 0 && s % 8 == 0; }
 
+// Rows of an output on one another: a stride of 0 over more than one element.
+int check_output(int64_t n_tok, int64_t tok, int64_t heads, int64_t head) {
+    if ((n_tok > 1 && heads > 0 && tok == 0) || (heads > 1 && n_tok > 0 && head == 0))
+        return set_error(CG_EINVAL, "an output stride is 0: rows of the output would lie on one another");
+    return CG_OK;
+}
+
 int check_units(int64_t n_tok, int64_t heads, int d) {
     if (n_tok * heads * (d >> 4) > ((int64_t)1 << 31) * 8)
         return set_error(CG_ERANGE, "n_tok * heads is too large for one call");
@@ -628,6 +635,8 @@ int check_units(int64_t n_tok, int64_t heads, int d) {
 }
 
 }  // namespace
+
+int paged_check_output(int64_t n_tok, int64_t tok, int64_t heads, int64_t head) { return check_output(n_tok, tok, heads, head); }
 
 int paged_check(const cg_pages* p) {
     int rc = check_pages(p, true);
@@ -779,6 +788,7 @@ CG_EXPORT int cg_rotary(const cg_rotary_params* rotary, int32_t dtype, int32_t n
     if (rc) return rc;
     if (!stride8(x_tok) || !stride8(x_head) || !stride8(out_tok) || !stride8(out_head))
         return set_error(CG_EINVAL, "strides must be non-negative multiples of 8 elements");
+    if ((rc = check_output(n_tok, out_tok, heads, out_head))) return rc;
     if (n_tok == 0 || heads == 0) return CG_OK;
     if (!x || !out || !positions) return set_error(CG_EINVAL, "null x, out or positions");
     if (!al16(x) || !al16(out) || !al4(positions)) return set_error(CG_EINVAL, "x and out must be 16-byte aligned");
@@ -819,6 +829,7 @@ CG_EXPORT int cg_rotary_append(const cg_pages* pages, const cg_rotary_params* ro
     if (!stride8(s->q_tok) || !stride8(s->q_head) || !stride8(s->k_tok) || !stride8(s->k_head) || !stride8(s->v_tok) ||
         !stride8(s->v_head) || !stride8(s->o_tok) || !stride8(s->o_head))
         return set_error(CG_EINVAL, "strides must be non-negative multiples of 8 elements");
+    if ((rc = check_output(n_tok, s->o_tok, q_heads, s->o_head))) return rc;
     if (n_tok == 0) return CG_OK;
     if (!k || !v || !positions || !slots || !pool || (q_heads && (!q || !q_out)))
         return set_error(CG_EINVAL, "null pointer");

@@ -30,6 +30,7 @@
 namespace cg {
 
 int paged_check(const cg_pages* p);
+int paged_check_output(int64_t n_tok, int64_t tok, int64_t heads, int64_t head);
 
 namespace {
 
@@ -860,6 +861,7 @@ CG_EXPORT int cg_paged_attention(const cg_pages* pages, const cg_paged_attn* how
     PagedArgs a{};
     int rc = check_attn(pages, how, &a);
     if (rc) return rc;
+    if ((rc = paged_check_output(a.n_tok, a.o_tok, (int64_t)a.H * a.n_rep, a.o_head))) return rc;
     if (a.n_tok == 0 || a.max_new == 0) return CG_OK;
     if (!q || !pool || !block_table || !seq_lens || !cu_new || !out || !workspace)
         return set_error(CG_EINVAL, "null q, pool, block_table, seq_lens, cu_new, out or workspace pointer");
