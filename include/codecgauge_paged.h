@@ -6,7 +6,7 @@
  *   pool : bf16 or fp16 [2][n_pages][H][page][d]      (0 = keys, 1 = values)
  * which is the codec's KV layout [L][2][B][H][T][d] with L = 1, B = n_pages and T = page: a bf16
  * pool (or a copy of a range of its pages) is coded by cg_encode and restored by cg_decode as it
- * stands. Token t of request i lives in page block_table[i][t / page], row t % page; its *slot*
+ * stands. (The attention reads pages, not codes: coded pages are decoded first.) Token t of request i lives in page block_table[i][t / page], row t % page; its *slot*
  * is page_id * page + t % page. The tables are the same for every layer.
  *
  * One step: cg_page_plan once (pages for the new tokens, positions, slots), then for each layer
@@ -170,12 +170,13 @@ int cg_rotary_append(const cg_pages* pages, const cg_rotary_params* rotary, int3
  * head j / n_rep:
  *   o = sum_t softmax_t(scale q . k_t) v_t,   lse = ln sum_t exp(scale q . k_t)
  * A query that sees nothing (a negative position) gives o = 0 and lse = -inf. Scores, softmax and
- * sums are fp32; the weights enter the value product rounded to the pool's type (summed before that), a
- * row's largest among them but for requests of up to 16 query rows per KV head; o is rounded once.
+ * sums are fp32; the weights enter the value product rounded to the pool's type (summed before that),
+ * the row's largest among them unless the request has few query rows; o is rounded once.
  * Values may be as large as fp32 has room for their sum over the visible tokens.
  * Rows of the pool past a request's length are never used, whatever they hold (NaN and infinities
  * too); block table entries of pages that no query sees are not used either (a windowed request's old
- * pages may be back on the stack, with -1 in their entries).
+ * pages may be back on the stack, with -1 in their entries). A visible token whose entry is no page
+ * raises CG_FLAG_PAGED_RANGE and counts with a key and a value of zeros.
  *   n_tok   : rows of q, out and lse; cu_new[n_req] <= n_tok (rows from cu_new[n_req] on are left
  *             untouched)
  *   n_rep   : query heads per KV head, 1 .. 64
