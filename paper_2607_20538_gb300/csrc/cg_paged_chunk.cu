@@ -20,10 +20,11 @@
 // the reference (by more than TileWeights::kLazy powers of two).
 // Bound: the tensor cores (4 x 128 x 128 x d multiply-adds per key tile against 128 x 256 exponentials
 // and about four times as many other operations), as far as a half's chain lets them: for d = 128 a
-// step takes 2500 cycles, its softmax 1400 of them, and both halves' products 2048. Tensor memory is
-// full (two halves of scores and accumulators), so that no scores are computed ahead. Measured, 32 query
-// heads on 8 KV heads: 2048 tokens after 32k 0.68 ms, 1.66 PFLOP/s (0.77 ms in a long run, under the
-// power cap); a prompt of 8192 0.365 ms, 1.5 PFLOP/s; d = 64 0.29 ms, 0.95 PFLOP/s (half the products for the
+// step takes 2500 cycles, its softmax 1400 of them, and both halves' products 2048. For d = 128 tensor
+// memory is full (two halves of scores and accumulators), so that no scores are computed ahead; d = 64 leaves
+// 128 columns of it unused. Measured, 32 query heads on 8 KV heads, in long runs (under the power cap):
+// 2048 tokens after 32k 0.77 ms, 1.47 PFLOP/s; a prompt of 8192 0.39 ms, 1.41 PFLOP/s (0.68 and 0.365 ms in
+// short ones); d = 64 0.29 ms, 0.96 PFLOP/s (half the products for the
 // same softmax); d = 256 1.9 ms after 32k, 1.2 PFLOP/s: its tiles of 128 rows need 64 bytes a cycle
 // and SM from L2. Sixteen softmax warps (two threads a row, 96 registers) took 1.09 ms: their loop spilled. A
 // quarter of the exponentials as polynomials on the FMA units: 0.75 ms against 0.72 the same day.
