@@ -11,26 +11,28 @@
 
 namespace cg {
 
-// The encoder is a driver call and wants a current context, which a host thread gets with its first
-// runtime call that needs one: a thread whose first call is this library's has none yet.
-inline void bind_context() {
-    static thread_local int bound = -1;
-    int dev = -1;
-    if (cudaGetDevice(&dev) == cudaSuccess && dev != bound && cudaSetDevice(dev) == cudaSuccess) bound = dev;
+template <class F>
+inline F driver_fn(const char* name) {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q{};
+    const bool found = cudaGetDriverEntryPointByVersion(name, &p, 12000, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess;
+    return found ? reinterpret_cast<F>(p) : nullptr;
 }
 
+// The tensor map encoder, or null. It is a driver call and wants a current context, which a host thread gets
+// with its first runtime call that needs one: a thread whose first call is this library's has none yet, and
+// gets its device's here. A context that is current stays so.
 inline PFN_cuTensorMapEncodeTiled_v12000 tmap_encode_fn() {
-    bind_context();
     static PFN_cuTensorMapEncodeTiled_v12000 fn = nullptr;
+    static PFN_cuCtxGetCurrent_v4000 current = nullptr;
     static std::once_flag once;
     std::call_once(once, [] {
-        void* p = nullptr;
-        cudaDriverEntryPointQueryResult q{};
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) ==
-                cudaSuccess &&
-            q == cudaDriverEntryPointSuccess)
-            fn = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(p);
+        fn = driver_fn<PFN_cuTensorMapEncodeTiled_v12000>("cuTensorMapEncodeTiled");
+        current = driver_fn<PFN_cuCtxGetCurrent_v4000>("cuCtxGetCurrent");
     });
+    CUcontext ctx = nullptr;
+    int dev = 0;
+    if (current && current(&ctx) == CUDA_SUCCESS && !ctx && cudaGetDevice(&dev) == cudaSuccess) cudaSetDevice(dev);
     return fn;
 }
 
