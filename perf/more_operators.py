@@ -366,7 +366,8 @@ def _plain_encode(s):
     M, K, rows = c["M"], c["K"], c["rows"]
     a = torch.zeros(_up(M, rows) * rows, _up(K, BLOCK) * BLOCK, device="cuda")
     a[:M, :K] = x.abs()
-    scales = a.view(_up(M, rows), rows, _up(K, BLOCK), BLOCK).amax((1, 3)) / TOP
+    # (by a tensor: a quotient by a number is a product with its rounded reciprocal)
+    scales = a.view(_up(M, rows), rows, _up(K, BLOCK), BLOCK).amax((1, 3)) / torch.full((), TOP, device="cuda")
     wide = scales.repeat_interleave(rows, 0)[:M].repeat_interleave(BLOCK, 1)[:, :K]
     return dict(codes=torch.where(wide > 0, x / wide, 0.0).to(E4M3), scales=scales)
 
