@@ -21,7 +21,7 @@ __all__ = ["CG_BLOCK_UNIFORM", "CG_KIVI", "CG_NONE", "CG_BLOCK_TILE", "CG_TILE_T
            "kivi_stream_bytes", "kivi_stream_alloc", "kivi_append", "kivi_stream_decode",
            "attention_workspace_bytes", "attention", "encode_hadamard", "decode_hadamard",
            "Pages", "Rotary", "RopeScaling", "PagedAttention", "page_plan", "page_release", "rotary_table", "rotary",
-           "rotary_append", "paged_attention_workspace_bytes", "paged_attention"]
+           "rotary_append", "paged_attention_workspace_bytes", "paged_attention", "tree_plan", "tree_attention", "tree_commit"]
 
 CG_BLOCK_UNIFORM, CG_KIVI, CG_NONE, CG_BLOCK_TILE = 0, 1, 2, 3
 CG_TILE_TOKENS = 16
@@ -232,16 +232,17 @@ def alloc_outputs(shape: Shape, params: Params, device="cuda"):
     return codes, scales, resid
 
 
-
-# The paged cache's binding checks torch tensors, so it (and torch) is loaded on first use.
-_PAGED = ("Pages", "PagedAttention", "RopeScaling", "Rotary", "page_plan", "page_release", "paged_attention",
-          "paged_attention_workspace_bytes", "rotary", "rotary_append", "rotary_table")
+# The bindings that check torch tensors are loaded (and torch with them) on first use.
+_LAZY = {"paged": ("Pages", "PagedAttention", "RopeScaling", "Rotary", "page_plan", "page_release", "paged_attention",
+                   "paged_attention_workspace_bytes", "rotary", "rotary_append", "rotary_table"),
+         "tree": ("tree_plan", "tree_attention", "tree_commit")}
 
 
 def __getattr__(name):
-    if name == "paged" or name in _PAGED:
-        import importlib
-        paged = importlib.import_module(".paged", __name__)
-        globals().update({n: getattr(paged, n) for n in _PAGED})
-        return paged if name == "paged" else globals()[name]
+    for module, names in _LAZY.items():
+        if name == module or name in names:
+            import importlib
+            m = importlib.import_module("." + module, __name__)
+            globals().update({n: getattr(m, n) for n in names})
+            return m if name == module else globals()[name]
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

@@ -3,9 +3,8 @@
 // Contract: include/codecgauge_paged.h.
 #include <cmath>
 
-#include <cooperative_groups.h>
-
 #include "cg_paged.h"
+#include "cg_paged_pages.cuh"
 
 #define CG_EXPORT __attribute__((visibility("default")))
 
@@ -41,18 +40,6 @@ struct PlanSmem {
 };
 
 __device__ __forceinline__ int32_t sat32(int64_t v) { return v > 0x7fffffff ? 0x7fffffff : (int32_t)v; }
-
-// Request k < n with prefix[k] <= v < prefix[k + 1].
-template <class T>
-__device__ __forceinline__ int find_request(const T* prefix, int n, T v) {
-    int lo = 0, hi = n;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (prefix[mid] <= v) lo = mid;
-        else hi = mid;
-    }
-    return lo;
-}
 
 // One request's tokens held, new tokens, and the pages that these need beyond those it has.
 __device__ __forceinline__ void plan_request(const PlanArgs& a, int i, int64_t* ctx, int64_t* add, int64_t* items,
@@ -253,154 +240,47 @@ __global__ void __launch_bounds__(kPT) plan_kernel(PlanArgs a) {
 }
 
 // ------------------------------------------------------------------------------------
-// Page release. The table entries of the finished requests form one line; those that are pages go on the
-// stack in its order, so that an entry's place is the number of pages before it, which only the entries
-// tell. One cluster: each of its 256 warps takes an equal piece of the line and counts its pages; after a
-// prefix over the CTA's warps and, through distributed shared memory, the cluster's CTAs it puts the
-// pages in their places (a piece of more than 128 entries is read once more). 4096 requests a round, each CTA with the prefix of
-// them all. Bound: launch latency and chains of dependent loads (length, entry). In a graph: 8 of 256
-// requests of 128 pages 5.8 us, all of them (32768 pages) 6.5, 102400 pages 18.4, 400 of 4096 requests 8.1.
+// Page release: the entries of the finished requests go on the stack (push_pages). Bound: launch latency and
+// chains of dependent loads (length, entry). In a graph: 8 of 256 requests of 128 pages 5.8 us, all of them
+// (32768 pages) 6.5, 102400 pages 18.4, 400 of 4096 requests 8.1.
 // ------------------------------------------------------------------------------------
-constexpr int kRelThreads = 1024, kRelCtas = 8, kRelWarps = 32;
-constexpr int kRelPer = 4;                         // requests of a thread and round
-constexpr int kRelRound = kRelThreads * kRelPer;   // requests per round
+constexpr int kRelThreads = 1024;
 
 struct ReleaseArgs {
-    const int32_t *lens, *done, *table, *count_in;
-    int32_t *free_pages, *lens_left, *count_out, *status;
-    int n_pages, page, page_log2, n_req, max_pages;
+    const int32_t *lens, *done;
+    int32_t *lens_left, *status;
+    int page, page_log2;
+    PushArgs push;
 };
 
-struct ReleaseSmem {
-    int64_t first[kRelRound + 1];   // place in the line of each request's first entry
-    int64_t entries[kRelWarps];     // of each warp's requests
-    int64_t pages[kRelWarps];       // in each warp's piece
-    int64_t total[2];               // pages in the CTA's pieces: this round's and the last one's
-};
-
-// Sum of the values of the lanes below `warp`, and of all (a value per warp of the CTA).
-__device__ __forceinline__ int64_t over_warps(int64_t v, int warp, int64_t* all) {
-    int64_t incl = v;
-#pragma unroll
-    for (int off = 1; off < 32; off *= 2) {
-        const int64_t u = __shfl_up_sync(0xffffffffu, incl, off);
-        if ((int)(threadIdx.x & 31) >= off) incl += u;
+// A finished request gives all its entries.
+struct Finished {
+    static constexpr bool kFromStart = true;
+    const ReleaseArgs& a;
+    int rank;
+    __device__ __forceinline__ void prepare(int, int) const {}
+    __device__ __forceinline__ int64_t entries(int i, int, int*, int32_t* flag) const {
+        int64_t c = __ldg(a.lens + i);
+        const bool done = __ldg(a.done + i) != 0;
+        int64_t have = (c + a.page - 1) >> a.page_log2;
+        if (c < 0) {
+            c = have = 0;
+            *flag |= CG_FLAG_PAGED_RANGE;
+        }
+        if (have > a.push.max_pages) {
+            have = a.push.max_pages;
+            *flag |= CG_FLAG_PAGED_RANGE;
+        }
+        if (rank == 0) a.lens_left[i] = done ? 0 : (int32_t)c;
+        return done ? have : 0;
     }
-    *all = __shfl_sync(0xffffffffu, incl, 31);
-    return __shfl_sync(0xffffffffu, incl - v, warp);
-}
+};
 
-__global__ void __cluster_dims__(kRelCtas, 1, 1) __launch_bounds__(kRelThreads) release_kernel(ReleaseArgs a) {
-    __shared__ ReleaseSmem S;
-    auto cluster = cooperative_groups::this_cluster();
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = (int)cluster.block_rank();
+__global__ void __cluster_dims__(kPushCtas, 1, 1) __launch_bounds__(kRelThreads) release_kernel(ReleaseArgs a) {
+    __shared__ PushSmem<kRelThreads, true> S;
     int32_t flag = 0;
-    int64_t count = __ldg(a.count_in);   // pages on the stack
-    if (count < 0 || count > a.n_pages) {
-        flag |= CG_FLAG_PAGED_RANGE;
-        count = count < 0 ? 0 : a.n_pages;
-    }
-    int round = 0;
-    for (int base = 0; base < a.n_req; base += kRelRound, round++) {
-        const int n = a.n_req - base < kRelRound ? a.n_req - base : kRelRound;
-        int64_t np[kRelPer], sum = 0;
-#pragma unroll
-        for (int k = 0; k < kRelPer; k++) {
-            const int i = tid * kRelPer + k;
-            np[k] = 0;
-            if (i < n) {
-                int64_t c = __ldg(a.lens + base + i);
-                const bool done = __ldg(a.done + base + i) != 0;
-                int64_t have = (c + a.page - 1) >> a.page_log2;
-                if (c < 0) {
-                    c = have = 0;
-                    flag |= CG_FLAG_PAGED_RANGE;
-                }
-                if (have > a.max_pages) {
-                    have = a.max_pages;
-                    flag |= CG_FLAG_PAGED_RANGE;
-                }
-                if (done) np[k] = have;
-                if (rank == 0) a.lens_left[base + i] = done ? 0 : (int32_t)c;
-            }
-            sum += np[k];
-        }
-        int64_t incl = sum;
-#pragma unroll
-        for (int off = 1; off < 32; off *= 2) {
-            const int64_t v = __shfl_up_sync(0xffffffffu, incl, off);
-            if (lane >= off) incl += v;
-        }
-        if (lane == 31) S.entries[warp] = incl;
-        __syncthreads();
-        int64_t all, at = over_warps(S.entries[lane], warp, &all) + incl - sum;
-#pragma unroll
-        for (int k = 0; k < kRelPer; k++) {
-            const int i = tid * kRelPer + k;
-            if (i < n) S.first[i] = at;
-            at += np[k];
-        }
-        if (tid == 0) S.first[n] = all;
-        __syncthreads();
-
-        // the warp's piece [lo, hi) of the line, whole groups of 32 entries
-        const int64_t groups = (all + 31) / 32, piece = (groups + kRelCtas * kRelWarps - 1) / (kRelCtas * kRelWarps) * 32;
-        const int64_t begin = (rank * kRelWarps + warp) * piece;
-        const int64_t lo = begin < all ? begin : all, hi = lo + piece < all ? lo + piece : all;
-        // lane's entries of four groups from f0 on; -1: none, or no page
-        auto fetch = [&](int64_t f0, int32_t (&id)[4]) {
-            int r = -1;
-#pragma unroll
-            for (int k = 0; k < 4; k++) {
-                const int64_t f = f0 + 32 * k + lane;
-                id[k] = -1;
-                if (f >= hi) continue;
-                if (r < 0 || S.first[r + 1] <= f) r = find_request(S.first, n, f);
-                id[k] = __ldg(a.table + (int64_t)(base + r) * a.max_pages + (f - S.first[r]));
-            }
-#pragma unroll
-            for (int k = 0; k < 4; k++)
-                if (id[k] < -1 || id[k] >= a.n_pages) {
-                    flag |= CG_FLAG_PAGED_RANGE;
-                    id[k] = -1;
-                }
-        };
-        int32_t id[4];
-        int64_t mine = 0;
-        for (int64_t f0 = lo; f0 < hi; f0 += 128) {
-            fetch(f0, id);
-#pragma unroll
-            for (int k = 0; k < 4; k++) mine += __popc(__ballot_sync(0xffffffffu, id[k] >= 0));
-        }
-        if (lane == 0) S.pages[warp] = mine;
-        __syncthreads();
-        int64_t here, to = count + over_warps(S.pages[lane], warp, &here);
-        if (tid == 0) S.total[round & 1] = here;
-        cluster.sync();
-#pragma unroll
-        for (int c = 0; c < kRelCtas; c++) {
-            const int64_t v = *cluster.map_shared_rank(&S.total[round & 1], c);
-            if (c < rank) to += v;
-            count += v;
-        }
-        for (int64_t f0 = lo; f0 < hi; f0 += 128) {
-            if (hi - lo > 128) fetch(f0, id);   // (else they are still there)
-#pragma unroll
-            for (int k = 0; k < 4; k++) {
-                const uint32_t mask = __ballot_sync(0xffffffffu, id[k] >= 0);
-                const int64_t place = to + __popc(mask & ((1u << lane) - 1u));
-                if (id[k] >= 0) {
-                    if (place < a.n_pages) a.free_pages[place] = id[k];
-                    else flag |= CG_FLAG_PAGED_RANGE;
-                }
-                to += __popc(mask);
-            }
-        }
-        __syncthreads();   // the round's prefix is free again
-    }
-    if (rank == 0 && tid == 0) *a.count_out = (int32_t)(count < a.n_pages ? count : a.n_pages);
+    push_pages<kRelThreads>(a.push, S, Finished{a, (int)cooperative_groups::this_cluster().block_rank()}, &flag);
     raise_flag(a.status, flag);
-    cluster.sync();        // no CTA ends while its count may be read
 }
 
 // ------------------------------------------------------------------------------------
@@ -638,6 +518,11 @@ int check_units(int64_t n_tok, int64_t heads, int d) {
 
 int paged_check_output(int64_t n_tok, int64_t tok, int64_t heads, int64_t head) { return check_output(n_tok, tok, heads, head); }
 
+int paged_check_sizes(const cg_pages* p) {
+    int rc = check_pages(p, false);
+    return rc ? rc : check_table(p);
+}
+
 int paged_check(const cg_pages* p) {
     int rc = check_pages(p, true);
     return rc ? rc : check_table(p);
@@ -723,17 +608,11 @@ CG_EXPORT int cg_page_release(const cg_pages* pages, const int32_t* lens, const 
     if ((rc = device_status(&a.status))) return rc;
     a.lens = lens;
     a.done = done;
-    a.table = block_table;
-    a.free_pages = free_pages;
-    a.count_in = free_count;
     a.lens_left = lens_left;
-    a.count_out = free_left;
-    a.n_pages = pages->n_pages;
     a.page = pages->page;
     a.page_log2 = log2_of(pages->page);
-    a.n_req = pages->n_req;
-    a.max_pages = pages->max_pages;
-    release_kernel<<<kRelCtas, kRelThreads, 0, static_cast<cudaStream_t>(stream)>>>(a);
+    a.push = PushArgs{block_table, free_count, free_pages, free_left, pages->n_pages, pages->n_req, pages->max_pages};
+    release_kernel<<<kPushCtas, kRelThreads, 0, static_cast<cudaStream_t>(stream)>>>(a);
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return set_error(CG_ECUDA, "page release launch: %s", cudaGetErrorString(e));
     return CG_OK;

@@ -27,9 +27,20 @@ struct PagedArgs {
     float scale;
     int64_t q_tok, q_head, o_tok, o_head;
     uint64_t wait_ns;
+    // A tree of drafted tokens (cg_tree_attention): the new tokens that a row sees are the bits of its
+    // mask, masks[n_tok][words]; masks null: those up to its own. positions: only with a window.
+    const uint32_t* masks;
+    const int32_t* positions;
+    int words;
     uint32_t rep_mul;     // x / n_rep = x * rep_mul >> rep_shift for 0 <= x < 2^31
     int rep_shift;
 };
+
+// Checks of cg_paged_attention's parameters; fills what of `a` they say.
+int paged_attn_check(const cg_pages* p, const cg_paged_attn* h, PagedArgs* a);
+// Checks of the pointers, and the launch (masks and positions are set in `a`, or null).
+int paged_attn_run(PagedArgs& a, const void* q, const void* pool, const int32_t* block_table, const int32_t* seq_lens,
+                   const int32_t* cu_new, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
 // Workspace of the paged attention: bytes, and the launch (workspace of that size).
 size_t paged_attn_workspace(const PagedArgs& a);

@@ -89,8 +89,9 @@ struct RowsParams {
 constexpr int kLead = 2;
 
 // Cost of a request in line units: (row tiles) x H x (chunks that its rows see, and their lead).
+template <bool TREE>
 __device__ __forceinline__ int64_t request_cost(const RowsParams& P, int i, int32_t* flag, int* longest) {
-    const Request r = load_request(P.a, i, flag);
+    const Request r = load_request<TREE>(P.a, i, flag);
     const int64_t rows = (int64_t)r.n * P.a.n_rep;
     if (r.n <= 0 || rows > P.max_rows) return 0;
     const Tiles t = visible_tiles<kTK>(P.a.window, P.a.sinks, r.len - r.n, r.len - 1);
@@ -99,6 +100,7 @@ __device__ __forceinline__ int64_t request_cost(const RowsParams& P, int i, int3
 }
 
 // Walk over a share: request, tile of 16 rows within it (KV head outermost).
+template <bool TREE>
 struct Walk {
     int i, u;             // request, tile
     int left, x;          // of the share, in line units; offset of the share in the tile
@@ -136,7 +138,7 @@ struct Walk {
             int32_t flag = 0;
             u = 0;
             if (++i >= P.a.n_req) left = 0;
-            else set(P, load_request(P.a, i, &flag));
+            else set(P, load_request<TREE>(P.a, i, &flag));
         }
         if (left <= kLead) left = 0;
     }
@@ -146,16 +148,18 @@ struct Walk {
     __device__ __forceinline__ int row0(const RowsParams& P) const { return (u - head(P) * per_head(P)) * kRows; }
 };
 
-// Positions of a tile's first and last row, and whether chunk `id` shows any of them a token.
+// Positions of a tile's first and last row, and whether chunk `id` shows any of them a token. A tree's rows
+// stand anywhere between its first node's position and its last place: every row may see each node.
+template <bool TREE>
 struct TileSpan {
     int p0, p1, h, row0, n_rows;
-    __device__ __forceinline__ TileSpan(const RowsParams& P, const Walk& w) {
+    __device__ __forceinline__ TileSpan(const RowsParams& P, const Walk<TREE>& w) {
         h = w.head(P);
         row0 = w.row0(P);
         const int rows = w.r.n * P.a.n_rep;
         n_rows = rows - row0 < kRows ? rows - row0 : kRows;
-        p0 = w.r.len - w.r.n + token_of(P.a, row0);
-        p1 = w.r.len - w.r.n + token_of(P.a, row0 + n_rows - 1);
+        p0 = w.r.len - w.r.n + (TREE ? 0 : token_of(P.a, row0));
+        p1 = TREE ? w.r.len - 1 : w.r.len - w.r.n + token_of(P.a, row0 + n_rows - 1);
     }
     __device__ __forceinline__ bool sees(const PagedArgs& a, int id) const {
         const int t0 = id * kTK;
@@ -163,7 +167,7 @@ struct TileSpan {
     }
     __device__ __forceinline__ bool sees_all(const PagedArgs& a, int id) const {
         const int t0 = id * kTK;
-        return t0 + kTK <= p0 + 1 && (!a.window || t0 > p1 - a.window || t0 + kTK <= a.sinks);
+        return t0 + kTK <= p0 + (TREE ? 0 : 1) && (!a.window || t0 > p1 - a.window || t0 + kTK <= a.sinks);
     }
 };
 
@@ -271,7 +275,7 @@ __device__ __noinline__ void join_parts(const RowsParams& P, int b0, int parts, 
     }
 }
 
-template <bool FP16, int D>
+template <bool FP16, int D, bool TREE>
 __global__ void __launch_bounds__(kThreads, RowsSmem<D>::kCtas)
 paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ CUtensorMap map) {
     using L = RowsSmem<D>;
@@ -289,7 +293,7 @@ paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ 
     const int i_hi = i_lo + per < a.n_req ? i_lo + per : a.n_req;
     int64_t mine = 0;
     int longest = 1;
-    for (int i = i_lo; i < i_hi; i++) mine += request_cost(P, i, &flag, &longest);
+    for (int i = i_lo; i < i_hi; i++) mine += request_cost<TREE>(P, i, &flag, &longest);
     longest = __reduce_max_sync(0xffffffffu, longest);
     int64_t incl = mine;
 #pragma unroll
@@ -326,10 +330,10 @@ paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ 
     if (begin >= before && begin < before + mine) {
         int64_t at = before;
         for (int i = i_lo; i < i_hi; i++) {
-            const int64_t c = per == 1 ? mine : request_cost(P, i, &flag, &longest);
+            const int64_t c = per == 1 ? mine : request_cost<TREE>(P, i, &flag, &longest);
             if (begin < at + c) {
                 M->start_req = i;
-                M->start_r = load_request(a, i, &flag);
+                M->start_r = load_request<TREE>(a, i, &flag);
                 M->before = begin - at;
                 break;
             }
@@ -345,7 +349,7 @@ paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ 
     if (blockIdx.x == 0) raise_flag(a.status, flag);
     if (begin >= end) return;
     volatile int* abort_flag = &M->abort_flag;
-    Walk w;
+    Walk<TREE> w;
     w.start(P, M->start_req, M->start_r, M->before, (int)(end - begin));
 
     // Registers: 128 a thread at launch; the consumers take what the others give up (128 x 200 + 128 x 56
@@ -360,7 +364,7 @@ paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ 
         int32_t pflag = 0;
         bool dead = *abort_flag != 0;
         while (w.left > 0) {
-            const TileSpan sp(P, w);
+            const TileSpan<TREE> sp(P, w);
             const int wlo = a.window ? w.r.len - w.r.n - a.window + 1 : 0;   // first token the request still needs
             const int32_t* row = a.table + (int64_t)w.i * a.max_pages;
             const int first = w.c(), take = w.end() - first;
@@ -427,19 +431,21 @@ paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ 
         const int g = lane >> 2, j = lane & 3;   // rows g and g + 8; columns 2j, 2j + 1
         const float sl2 = a.scale * kLog2e;
         int st = 0, ph = 0;
+        int32_t row_flag = 0;
         bool dead = *abort_flag != 0;
         while (w.left > 0) {
-            const TileSpan sp(P, w);
+            const TileSpan<TREE> sp(P, w);
             const int first = w.c(), take = w.end() - first;
             // queries of rows g, g + 8 as MMA operands
             uint32_t q[D / 16][4];
-            int pos[2];
+            int pos[2], node[2];
 #pragma unroll
             for (int hf = 0; hf < 2; hf++) {
                 const int r = sp.row0 + g + 8 * hf;
                 const bool have = g + 8 * hf < sp.n_rows;
                 const int tk = token_of(a, r), hd = sp.h * a.n_rep + (r - tk * a.n_rep);
-                pos[hf] = have ? w.r.len - w.r.n + tk : -1;
+                pos[hf] = !have ? -1 : TREE ? tree_position(a, w.r, tk, &row_flag) : w.r.len - w.r.n + tk;
+                node[hf] = have ? tk : -1;
                 const uint16_t* src = a.q + (int64_t)(w.r.tok0 + tk) * a.q_tok + hd * a.q_head + 2 * j;
 #pragma unroll
                 for (int k = 0; k < D / 16; k++) {
@@ -488,7 +494,23 @@ paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ 
                     for (int n = 0; n < 2; n++)
 #pragma unroll
                         for (int e = 0; e < 4; e++) s[n][e] *= sl2;
-                    if (edge) {
+                    if (TREE && edge) {
+#pragma unroll
+                        for (int hf = 0; hf < 2; hf++) {
+                            const int first = t0 - (w.r.len - w.r.n);   // node of column t0
+                            const uint32_t nodes = node[hf] >= 0 ? tree_word(a, w.r, node[hf], first) : 0u;
+#pragma unroll
+                            for (int n = 0; n < 2; n++)
+#pragma unroll
+                                for (int e = 0; e < 2; e++) {
+                                    const int c = 8 * n + e, t = t0 + c;
+                                    const bool old = !a.window || t > pos[hf] - a.window || t < a.sinks;
+                                    const bool see = first + c < 0 ? old && node[hf] >= 0 : (nodes >> c & 1u) != 0;
+                                    s[n][2 * hf + e] = see ? s[n][2 * hf + e] : -INFINITY;
+                                }
+                        }
+                    }
+                    if (!TREE && edge) {
 #pragma unroll
                         for (int n = 0; n < 2; n++)
 #pragma unroll
@@ -707,6 +729,7 @@ paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ 
             w.next_tile(P);
         }
         if (dead && tid == 0) raise_flag(a.status, CG_FLAG_PIPE_TIMEOUT);
+        if (TREE) raise_flag(a.status, row_flag);
     }
 }
 
@@ -720,17 +743,23 @@ uint64_t next_epoch() {
 
 int rows_ctas(int d) { return tc::num_sms() * (d == 256 ? 1 : 2); }
 
-template <bool FP16, int D>
+template <bool FP16, int D, bool TREE>
 cudaError_t launch_rows(const RowsParams& P, cudaStream_t st) {
     CUtensorMap map;
     if (!paged_pool_map(&map, P.a, P.box_rows)) return cudaErrorInvalidValue;
     constexpr size_t smem = RowsSmem<D>::total;
     static SmemOptIn opt_in;
-    cudaError_t e = opt_in.set(reinterpret_cast<const void*>(paged_rows_kernel<FP16, D>), (int)smem);
+    cudaError_t e = opt_in.set(reinterpret_cast<const void*>(paged_rows_kernel<FP16, D, TREE>), (int)smem);
     if (e != cudaSuccess) return e;
     const unsigned grid = (unsigned)rows_ctas(D);
-    paged_rows_kernel<FP16, D><<<grid, kThreads, smem, st>>>(P, map);
+    paged_rows_kernel<FP16, D, TREE><<<grid, kThreads, smem, st>>>(P, map);
     return cudaGetLastError();
+}
+
+template <int D>
+cudaError_t launch_rows(const RowsParams& P, cudaStream_t st) {
+    if (P.a.dtype == CG_FP16) return P.a.masks ? launch_rows<true, D, true>(P, st) : launch_rows<true, D, false>(P, st);
+    return P.a.masks ? launch_rows<false, D, true>(P, st) : launch_rows<false, D, false>(P, st);
 }
 
 size_t rows_workspace(int d) {
@@ -781,11 +810,10 @@ cudaError_t launch_paged_attn(const PagedArgs& a, void* workspace, cudaStream_t 
         P.epoch = next_epoch();
         P.max_rows = limit;
         P.box_rows = a.page < kTK ? a.page : kTK;
-        const bool h = a.dtype == CG_FP16;
         switch (a.d) {
-            case 64: e = h ? launch_rows<true, 64>(P, st) : launch_rows<false, 64>(P, st); break;
-            case 128: e = h ? launch_rows<true, 128>(P, st) : launch_rows<false, 128>(P, st); break;
-            default: e = h ? launch_rows<true, 256>(P, st) : launch_rows<false, 256>(P, st); break;
+            case 64: e = launch_rows<64>(P, st); break;
+            case 128: e = launch_rows<128>(P, st); break;
+            default: e = launch_rows<256>(P, st); break;
         }
         if (e != cudaSuccess) return e;
     }
@@ -795,9 +823,7 @@ cudaError_t launch_paged_attn(const PagedArgs& a, void* workspace, cudaStream_t 
     return e;
 }
 
-namespace {
-
-int check_attn(const cg_pages* p, const cg_paged_attn* h, PagedArgs* a) {
+int paged_attn_check(const cg_pages* p, const cg_paged_attn* h, PagedArgs* a) {
     int rc = paged_check(p);
     if (rc) return rc;
     if (!h) return set_error(CG_EINVAL, "null attention parameters");
@@ -838,31 +864,9 @@ int check_attn(const cg_pages* p, const cg_paged_attn* h, PagedArgs* a) {
     return CG_OK;
 }
 
-}  // namespace
-}  // namespace cg
-
-using namespace cg;
-
-extern "C" {
-
-CG_EXPORT int cg_paged_attention_workspace_bytes(const cg_pages* pages, const cg_paged_attn* how, size_t* bytes) {
-    set_error(CG_OK, "%s", "");
-    PagedArgs a{};
-    const int rc = check_attn(pages, how, &a);
-    if (rc) return rc;
-    if (bytes) *bytes = paged_attn_workspace(a);
-    return CG_OK;
-}
-
-CG_EXPORT int cg_paged_attention(const cg_pages* pages, const cg_paged_attn* how, const void* q, const void* pool,
-                                 const int32_t* block_table, const int32_t* seq_lens, const int32_t* cu_new, void* out,
-                                 float* lse, void* workspace, size_t workspace_bytes, void* stream) {
-    set_error(CG_OK, "%s", "");
-    PagedArgs a{};
-    int rc = check_attn(pages, how, &a);
-    if (rc) return rc;
-    if ((rc = paged_check_output(a.n_tok, a.o_tok, (int64_t)a.H * a.n_rep, a.o_head))) return rc;
-    if (a.n_tok == 0 || a.max_new == 0) return CG_OK;
+int paged_attn_run(PagedArgs& a, const void* q, const void* pool, const int32_t* block_table, const int32_t* seq_lens,
+                   const int32_t* cu_new, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+    int rc;
     if (!q || !pool || !block_table || !seq_lens || !cu_new || !out || !workspace)
         return set_error(CG_EINVAL, "null q, pool, block_table, seq_lens, cu_new, out or workspace pointer");
     for (const void* p : {q, pool, (const void*)out, (const void*)workspace})
@@ -884,6 +888,33 @@ CG_EXPORT int cg_paged_attention(const cg_pages* pages, const cg_paged_attn* how
     const cudaError_t e = launch_paged_attn(a, workspace, static_cast<cudaStream_t>(stream));
     if (e != cudaSuccess) return set_error(CG_ECUDA, "paged attention launch: %s", cudaGetErrorString(e));
     return CG_OK;
+}
+
+}  // namespace cg
+
+using namespace cg;
+
+extern "C" {
+
+CG_EXPORT int cg_paged_attention_workspace_bytes(const cg_pages* pages, const cg_paged_attn* how, size_t* bytes) {
+    set_error(CG_OK, "%s", "");
+    PagedArgs a{};
+    const int rc = paged_attn_check(pages, how, &a);
+    if (rc) return rc;
+    if (bytes) *bytes = paged_attn_workspace(a);
+    return CG_OK;
+}
+
+CG_EXPORT int cg_paged_attention(const cg_pages* pages, const cg_paged_attn* how, const void* q, const void* pool,
+                                 const int32_t* block_table, const int32_t* seq_lens, const int32_t* cu_new, void* out,
+                                 float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+    set_error(CG_OK, "%s", "");
+    PagedArgs a{};
+    int rc = paged_attn_check(pages, how, &a);
+    if (rc) return rc;
+    if ((rc = paged_check_output(a.n_tok, a.o_tok, (int64_t)a.H * a.n_rep, a.o_head))) return rc;
+    if (a.n_tok == 0 || a.max_new == 0) return CG_OK;
+    return paged_attn_run(a, q, pool, block_table, seq_lens, cu_new, out, lse, workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"

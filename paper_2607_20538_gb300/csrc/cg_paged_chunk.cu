@@ -121,7 +121,7 @@ struct ChunkParams {
 // Rows of a request at positions p0 .. p1, and the key tiles (by number) that they see: some token
 // of tiles [s0, s1) and those below ss, every token for every row of [f0, f1) and those below fs.
 struct Span {
-    int p0, p1, n;
+    int p0, p1, n, tok;   // (tok: tokens)
     int s0, s1, ss, f0, f1, fs;
     __device__ __forceinline__ bool sees(int id) const { return id < s1 && (id >= s0 || id < ss); }
     __device__ __forceinline__ bool sees_all(int id) const { return id < f1 && (id >= f0 || id < fs); }
@@ -131,18 +131,22 @@ struct Span {
     }
 };
 
-// Tokens [tok, tok + most) of a request's new ones.
+// Tokens [tok, tok + most) of a request's new ones. Of a tree's nodes each may see every other, and each stands
+// somewhere from the end of the history, behind which nothing is seen by all, to the last token: p0 is the
+// last token of the history.
+template <bool TREE>
 __device__ __forceinline__ Span span_of(const PagedArgs& a, const Request& r, int tok, int most) {
     Span s;
     const int left = r.n - tok, n = left < 0 ? 0 : left < most ? left : most;
     s.n = n * a.n_rep;
-    s.p0 = r.len - r.n + tok;
-    s.p1 = s.p0 + n - 1;
+    s.tok = n;
+    s.p0 = TREE ? r.len - r.n - 1 : r.len - r.n + tok;
+    s.p1 = TREE ? r.len - 1 : s.p0 + n - 1;
     s.s0 = s.ss = s.f0 = s.fs = 0;
     s.s1 = s.n && s.p1 >= 0 ? s.p1 / kKT + 1 : 0;
     s.f1 = s.p0 < 0 ? 0 : (s.p0 + 1) / kKT;
     if (a.window) {
-        const int from = s.p0 - a.window + 1, last = s.p1 - a.window;   // first token row p0 sees; last one p1 does not
+        const int from = s.p0 + (TREE ? 1 : 0) - a.window + 1, last = s.p1 - a.window;   // first token row p0 sees; last one p1 does not
         s.s0 = from > 0 ? from / kKT : 0;
         s.f0 = last >= 0 ? last / kKT + 1 : 0;
         s.ss = (int)(((int64_t)a.sinks + kKT - 1) / kKT);
@@ -151,7 +155,9 @@ __device__ __forceinline__ Span span_of(const PagedArgs& a, const Request& r, in
     return s;
 }
 
+template <bool TREE>
 __device__ __forceinline__ Tiles tile_tiles(const ChunkParams& P, const Request& r, int m) {
+    if (TREE) return visible_tiles<kKT>(P.a.window, P.a.sinks, r.len - r.n, r.len - 1);
     const int tok = m * P.tile_tok, left = r.n - tok, n = left < P.tile_tok ? left : P.tile_tok;
     return visible_tiles<kKT>(P.a.window, P.a.sinks, r.len - r.n + tok, r.len - r.n + tok + n - 1);
 }
@@ -175,12 +181,13 @@ __device__ __forceinline__ int row_tiles(const ChunkParams& P, const Request& r)
 
 // Cost of one KV head of each lane's request, and its largest tile's. All lanes call: requests of many
 // tiles are summed by the whole warp.
+template <bool TREE>
 __device__ __forceinline__ int64_t head_cost(const ChunkParams& P, const Request& r, int* largest) {
     const int lane = threadIdx.x & 31, n_m = row_tiles(P, r);
     int64_t sum = 0;
     if (n_m <= 2)
         for (int m = 0; m < n_m; m++) {
-            const int c = tile_tiles(P, r, m).count() + kTileCost;
+            const int c = tile_tiles<TREE>(P, r, m).count() + kTileCost;
             sum += c;
             *largest = max(*largest, c);
         }
@@ -192,7 +199,7 @@ __device__ __forceinline__ int64_t head_cost(const ChunkParams& P, const Request
         const int n = __shfl_sync(0xffffffffu, n_m, src);
         int64_t part = 0;
         for (int m = lane; m < n; m += 32) {
-            const int c = tile_tiles(P, q, m).count() + kTileCost;
+            const int c = tile_tiles<TREE>(P, q, m).count() + kTileCost;
             part += c;
             *largest = max(*largest, c);
         }
@@ -204,11 +211,12 @@ __device__ __forceinline__ int64_t head_cost(const ChunkParams& P, const Request
 }
 
 // Row tile of one KV head at offset *off of its line; *off becomes the offset within the tile.
+template <bool TREE>
 __device__ __forceinline__ int tile_at(const ChunkParams& P, const Request& r, int64_t* off) {
     const int lane = threadIdx.x & 31, n_m = row_tiles(P, r);
     for (int m0 = 0;; m0 += 32) {
         const int m = m0 + lane;
-        const int64_t mine = m < n_m ? tile_tiles(P, r, m).count() + kTileCost : 0;
+        const int64_t mine = m < n_m ? tile_tiles<TREE>(P, r, m).count() + kTileCost : 0;
         int64_t incl = mine;
 #pragma unroll
         for (int k = 1; k < 32; k *= 2) {
@@ -227,6 +235,7 @@ __device__ __forceinline__ int tile_at(const ChunkParams& P, const Request& r, i
 }
 
 // Walk over a share: request, KV head, row tile, key tile.
+template <bool TREE>
 struct ChunkWalk {
     int i, h, m, n_m;
     int c, take, n;       // first key tile of the current work tile, how many of it, of how many
@@ -240,11 +249,11 @@ struct ChunkWalk {
         int32_t flag = 0;
         n_m = 0;
         if (i >= P.a.n_req) return;
-        r = load_request(P.a, i, &flag);
+        r = load_request<TREE>(P.a, i, &flag);
         n_m = row_tiles(P, r);
     }
     __device__ __forceinline__ void tile(const ChunkParams& P) {
-        t = tile_tiles(P, r, m);
+        t = tile_tiles<TREE>(P, r, m);
         n = t.count();
         c = x > kTileCost ? x - kTileCost : 0;
         goes_on = n + kTileCost - x > left;
@@ -423,11 +432,12 @@ __device__ __forceinline__ uint32_t bits_between(int lo, int hi) {
 
 // A tile that not every row sees whole: the row sees the columns [lo, hi] and those below sk; the
 // others are set to -inf. 64 columns a turn.
-__device__ __noinline__ void mask_row(uint32_t s_tm, int lo, int hi, int sk) {
+template <class More>
+__device__ __forceinline__ void mask_row_but(uint32_t s_tm, int lo, int hi, int sk, More more) {
 #pragma unroll 1
     for (int c0 = 0; c0 < kKT; c0 += 64) {
-        const uint32_t see0 = bits_between(lo - c0, hi - c0) | bits_between(0, (sk - 1 < hi ? sk - 1 : hi) - c0);
-        const uint32_t see1 = bits_between(lo - c0 - 32, hi - c0 - 32) | bits_between(0, (sk - 1 < hi ? sk - 1 : hi) - c0 - 32);
+        const uint32_t see0 = bits_between(lo - c0, hi - c0) | bits_between(0, (sk - 1 < hi ? sk - 1 : hi) - c0) | more(c0);
+        const uint32_t see1 = bits_between(lo - c0 - 32, hi - c0 - 32) | bits_between(0, (sk - 1 < hi ? sk - 1 : hi) - c0 - 32) | more(c0 + 32);
         if (__all_sync(0xffffffffu, (see0 & see1) == ~0u)) continue;
         float u[32], v[32];
         tmem_ld32f(s_tm + c0, u);
@@ -444,6 +454,15 @@ __device__ __noinline__ void mask_row(uint32_t s_tm, int lo, int hi, int sk) {
         tmem_st32(s_tm + c0 + 32, r);
     }
     tmem_wait_st();
+}
+__device__ __noinline__ void mask_row(uint32_t s_tm, int lo, int hi, int sk) {
+    mask_row_but(s_tm, lo, hi, sk, [](int) { return 0u; });
+}
+// The same for a node's row: history up to column hi, and the nodes of its mask (column 0 is token t0; node -1:
+// no row, which sees nothing).
+__device__ __noinline__ void mask_node(const PagedArgs& a, const Request& r, int node, uint32_t s_tm, int t0, int lo, int sk) {
+    const int ctx = r.len - r.n;
+    mask_row_but(s_tm, lo, node < 0 ? -1 : ctx - 1 - t0, sk, [&](int c) { return node < 0 ? 0u : tree_word(a, r, node, t0 + c - ctx); });
 }
 
 // Each lane holds 8 pieces of 16 bytes of its row (128 bytes). The 8 lanes of a group transpose them
@@ -515,9 +534,9 @@ __device__ __forceinline__ float elem(uint32_t bits16) {
 
 // Adds the special values of the partial tokens that this row sees to its row of O (columns of the
 // half at o_tm, quiescent); `first`: O holds nothing yet and is set to zero first. All lanes call.
-template <bool FP16, int D>
+template <bool FP16, int D, bool TREE>
 __device__ __noinline__ void add_special(const PagedArgs& a, const Request& r, int req, int h, Span item, int t0, int pos,
-                                         uint32_t o_tm, bool first) {
+                                         int node, uint32_t o_tm, bool first) {
     for (int c0 = 0; c0 < D; c0 += 32) {
         uint32_t o[32];
         if (first) {
@@ -529,7 +548,8 @@ __device__ __noinline__ void add_special(const PagedArgs& a, const Request& r, i
         }
         for (int t = t0; t < t0 + kKT && t < r.len; t++) {
             if (!item.partial(a, t)) continue;
-            const bool see = t <= pos && (!a.window || t > pos - a.window || t < a.sinks);
+            const bool see = TREE ? node >= 0 && tree_sees(a, r, node, pos, t)
+                                  : t <= pos && (!a.window || t > pos - a.window || t < a.sinks);
             if (!__any_sync(0xffffffffu, see)) continue;
             const int pg = __ldg(a.table + (int64_t)req * a.max_pages + (t >> a.page_log2));
             if (pg < 0 || pg >= a.n_pages) continue;
@@ -562,7 +582,7 @@ __device__ __forceinline__ bool take_turn(int* turn, bool issue, const volatile 
     return __all_sync(0xffffffffu, ok);
 }
 
-template <bool FP16, int D>
+template <bool FP16, int D, bool TREE>
 __global__ void __launch_bounds__(kChunkThreads, 1)
 paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant__ CUtensorMap map,
                    const __grid_constant__ CUtensorMap qmap) {
@@ -583,8 +603,8 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
     uint32_t tiles = 0;          // of this thread's requests, up to 65535
     for (int k = 0; k < per; k++) {
         Request r{};
-        if (i_lo + k < i_hi) r = load_request(a, i_lo + k, &flag);
-        const int64_t c = head_cost(P, r, &largest);
+        if (i_lo + k < i_hi) r = load_request<TREE>(a, i_lo + k, &flag);
+        const int64_t c = head_cost<TREE>(P, r, &largest);
         if (k == 0) first_cost = c;
         mine += c * a.H;
         tiles = (uint32_t)min((int64_t)tiles + (int64_t)row_tiles(P, r) * a.H, (int64_t)65535);
@@ -662,7 +682,7 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
         if (b >= tiles_before && b < tiles_before + tiles) {
             uint32_t off = b - tiles_before;
             for (int i = i_lo; i < i_hi; i++) {
-                const Request r = load_request(a, i, &flag);
+                const Request r = load_request<TREE>(a, i, &flag);
                 const uint32_t n_m = row_tiles(P, r), n = n_m * a.H;
                 if (off < n) {
                     const int m = off % n_m;
@@ -670,7 +690,7 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                     M->start[1] = off / n_m;
                     M->start[2] = m;
                     M->start[3] = 0;
-                    M->units = tile_tiles(P, r, m).count() + kTileCost;
+                    M->units = tile_tiles<TREE>(P, r, m).count() + kTileCost;
                     break;
                 }
                 off -= n;
@@ -682,8 +702,8 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
         int64_t at = before, hc = 0, off = 0;
         for (int k = 0; k < per; k++) {
             Request q{};
-            if (i_lo + k < i_hi) q = load_request(a, i_lo + k, &flag);
-            const int64_t c = per == 1 ? first_cost : head_cost(P, q, &largest);
+            if (i_lo + k < i_hi) q = load_request<TREE>(a, i_lo + k, &flag);
+            const int64_t c = per == 1 ? first_cost : head_cost<TREE>(P, q, &largest);
             if (begin >= at && begin < at + c * a.H) {
                 req = i_lo + k;
                 r = q;
@@ -700,7 +720,7 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
         off = __shfl_sync(0xffffffffu, off, src);
         const int h = (int)(off / hc);
         off -= h * hc;
-        const int m = tile_at(P, r, &off);
+        const int m = tile_at<TREE>(P, r, &off);
         if (lane == 0) {
             M->start[0] = req;
             M->start[1] = h;
@@ -712,7 +732,7 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
     if (blockIdx.x == 0) raise_flag(a.status, flag);
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     volatile int* abort_flag = &M->abort_flag;
-    ChunkWalk w;
+    ChunkWalk<TREE> w;
     w.start(P, M->start, whole_tiles ? M->units : begin < end ? (int)(end - begin) : 0);
     const uint32_t kS = tmem, kO = tmem + 256;
 
@@ -730,7 +750,7 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
         int meta_last = -1;
         while (w.left > 0 && !dead) {
             const int tok = w.m * P.tile_tok + x * P.half_tok;   // the half's first new token
-            const Span sp = span_of(a, w.r, tok, P.half_tok), item = span_of(a, w.r, w.m * P.tile_tok, P.tile_tok);
+            const Span sp = span_of<TREE>(a, w.r, tok, P.half_tok), item = span_of<TREE>(a, w.r, w.m * P.tile_tok, P.tile_tok);
             const int take = w.take;
             if (!head_part && w.goes_on) {   // it starts here and goes on
                 meta_last = (int)(blockIdx.x + (w.rest + share - 1) / share);
@@ -738,7 +758,7 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                     ChunkMeta* m = P.meta + blockIdx.x;
                     m->last = meta_last;
                     m->tok0 = w.r.tok0 + w.m * P.tile_tok;
-                    m->n_tok = item.p1 - item.p0 + 1;
+                    m->n_tok = item.tok;
                     m->h = w.h;
                 }
             }
@@ -746,7 +766,8 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                 const int row = (warp & 3) * 32 + lane;
                 const bool have = row < sp.n;
                 const int rt = token_of(a, row), tk = tok + rt, hd = w.h * a.n_rep + (row - rt * a.n_rep);
-                const int pos = have ? sp.p0 + rt : -1;
+                const int node = TREE && have ? tk : -1;
+                const int pos = !have ? -1 : TREE ? tree_position(a, w.r, tk, &flag) : sp.p0 + rt;
                 float ref = -INFINITY, sum = 0.0f;
                 bool started = false;
                 for (int kc = 0; kc < take; kc++) {
@@ -768,7 +789,8 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                     };
                     tc_fence_after();
                     const int t0 = id * kKT;
-                    if (!sp.sees_all(id)) mask_row(s_tm, a.window ? pos - a.window + 1 - t0 : 0, pos - t0, a.sinks - t0);
+                    if (TREE && !sp.sees_all(id)) mask_node(a, w.r, node, s_tm, t0, a.window ? pos - a.window + 1 - t0 : 0, a.sinks - t0);
+                    else if (!sp.sees_all(id)) mask_row(s_tm, a.window ? pos - a.window + 1 - t0 : 0, pos - t0, a.sinks - t0);
                     float u[32], v[32];
                     const float mx = sl2 * row_max(s_tm, u, v);
                     // each row by its own scores alone: rows past the tile's end hold anything
@@ -796,7 +818,7 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                         if (dead) break;
                         if (special) {
                             if (!quiet()) break;
-                            add_special<FP16, D>(a, w.r, w.i, w.h, item, t0, pos, o_tm, !started);
+                            add_special<FP16, D, TREE>(a, w.r, w.i, w.h, item, t0, pos, node, o_tm, !started);
                             if (!started && lane == 0) *(volatile int*)&M->accum0[x] = 1;
                         }
                     }
@@ -885,6 +907,7 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
             if (sp.n <= 0) w.next(P);
         }
         if (tid == 0 && meta_last < 0) P.meta[blockIdx.x].last = -1;
+        if (TREE) raise_flag(a.status, flag);   // (positions)
         if (dead) {
             *abort_flag = 1;
             if (lane == 0) raise_flag(a.status, CG_FLAG_PIPE_TIMEOUT);
@@ -1057,7 +1080,7 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                 first = false;
             };
             while (w.left > 0 && !dead) {
-                const Span sp = span_of(a, w.r, w.m * P.tile_tok + x * P.half_tok, P.half_tok);
+                const Span sp = span_of<TREE>(a, w.r, w.m * P.tile_tok + x * P.half_tok, P.half_tok);
                 const int take = w.take;
                 bool prev = false, any = false;
                 first = true;
@@ -1158,11 +1181,11 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
             int nv = 0, nq[2] = {0, 0};
             bool dead = *abort_flag != 0, q_bytes = false;
             while (w.left > 0 && !dead) {
-                const Span item = span_of(a, w.r, w.m * P.tile_tok, P.tile_tok);
+                const Span item = span_of<TREE>(a, w.r, w.m * P.tile_tok, P.tile_tok);
                 const int take = w.take;
                 for (int x = 0; x < halves(D) && !dead; x++) {
                     const int tok = w.m * P.tile_tok + x * P.half_tok;
-                    const Span sp = span_of(a, w.r, tok, P.half_tok);
+                    const Span sp = span_of<TREE>(a, w.r, tok, P.half_tok);
                     if (sp.n <= 0) continue;
                     if (!__all_sync(0xffffffffu, mbar_wait(&M->qempty[x], (nq[x] & 1) ^ 1, abort_flag, a.wait_ns))) {
                         dead = true;
@@ -1367,14 +1390,14 @@ bool query_map(CUtensorMap* map, const PagedArgs& a) {
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <bool FP16, int D>
+template <bool FP16, int D, bool TREE>
 cudaError_t launch_chunk(ChunkParams P, bool after_rows, cudaStream_t st) {
     CUtensorMap map, qmap{};
     if (!paged_pool_map(&map, P.a, P.box_rows)) return cudaErrorInvalidValue;
     P.q_boxes = query_map(&qmap, P.a);
     constexpr size_t smem = ChunkSmem<D>::total;
     static SmemOptIn opt_in;
-    cudaError_t e = opt_in.set(reinterpret_cast<const void*>(paged_chunk_kernel<FP16, D>), (int)smem);
+    cudaError_t e = opt_in.set(reinterpret_cast<const void*>(paged_chunk_kernel<FP16, D, TREE>), (int)smem);
     if (e != cudaSuccess) return e;
     const unsigned grid = (unsigned)tc::num_sms();
     cudaLaunchConfig_t cfg{};
@@ -1389,13 +1412,20 @@ cudaError_t launch_chunk(ChunkParams P, bool after_rows, cudaStream_t st) {
     // Beside the rows kernel of the same call this one starts as soon as that one's CTAs leave room: it
     // reads none of its results (and ends after it, see its end).
     cfg.numAttrs = after_rows ? 1 : 0;
-    if ((e = cudaLaunchKernelEx(&cfg, paged_chunk_kernel<FP16, D>, P, map, qmap)) != cudaSuccess) return e;
+    if ((e = cudaLaunchKernelEx(&cfg, paged_chunk_kernel<FP16, D, TREE>, P, map, qmap)) != cudaSuccess) return e;
     // the merge is scheduled while the last shares run; it waits for them on the device
     cfg.gridDim = dim3(grid, D / 16);
     cfg.blockDim = dim3(tile_rows(D));
     cfg.dynamicSmemBytes = 0;
     cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, paged_chunk_merge_kernel<FP16, D>, P);
+}
+
+template <int D>
+cudaError_t launch_chunk(const ChunkParams& P, bool after_rows, cudaStream_t st) {
+    const bool tree = P.a.masks != nullptr;
+    if (P.a.dtype == CG_FP16) return tree ? launch_chunk<true, D, true>(P, after_rows, st) : launch_chunk<true, D, false>(P, after_rows, st);
+    return tree ? launch_chunk<false, D, true>(P, after_rows, st) : launch_chunk<false, D, false>(P, after_rows, st);
 }
 
 }  // namespace
@@ -1415,10 +1445,9 @@ cudaError_t launch_paged_chunk(const PagedArgs& a, int min_rows, bool after_rows
     P.half_tok = kHalfRows / a.n_rep;
     P.tile_tok = halves(a.d) * P.half_tok;
     P.box_rows = a.page < kKT ? a.page : kKT;
-    const bool h = a.dtype == CG_FP16;
-    if (a.d == 64) return h ? launch_chunk<true, 64>(P, after_rows, st) : launch_chunk<false, 64>(P, after_rows, st);
-    if (a.d == 256) return h ? launch_chunk<true, 256>(P, after_rows, st) : launch_chunk<false, 256>(P, after_rows, st);
-    return h ? launch_chunk<true, 128>(P, after_rows, st) : launch_chunk<false, 128>(P, after_rows, st);
+    if (a.d == 64) return launch_chunk<64>(P, after_rows, st);
+    if (a.d == 256) return launch_chunk<256>(P, after_rows, st);
+    return launch_chunk<128>(P, after_rows, st);
 }
 
 }  // namespace cg

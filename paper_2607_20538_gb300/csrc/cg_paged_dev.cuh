@@ -84,20 +84,47 @@ struct Request {
     int len, n, tok0;     // tokens in the pool, new ones, first query row
 };
 
-// Loads and checks a request: lengths that are not covered by the arrays raise the flag.
+// Loads and checks a request: lengths that are not covered by the arrays raise the flag (and, in a
+// tree's call, more new tokens than tokens).
+template <bool TREE>
 __device__ __forceinline__ Request load_request(const PagedArgs& a, int i, int32_t* flag) {
     Request r;
     const int c0 = __ldg(a.cu_new + i), c1 = __ldg(a.cu_new + i + 1);
     r.len = __ldg(a.seq_lens + i);
     r.tok0 = c0;
     r.n = c1 - c0;
-    const bool ok = c0 >= 0 && c1 >= c0 && c1 <= a.n_tok && r.n <= a.max_new && r.len >= 0 &&
+    const bool ok = c0 >= 0 && c1 >= c0 && c1 <= a.n_tok && r.n <= a.max_new && r.len >= (TREE ? r.n : 0) &&
            (int64_t)r.len <= (int64_t)a.max_pages << a.page_log2;
     if (!ok) {
         *flag |= CG_FLAG_PAGED_RANGE;
         r.n = 0;
     }
     return r;
+}
+
+// A tree's rows. Tokens below ctx = len - n are history, which every row sees (with a window: from its position
+// on); token ctx + j is node j, seen where bit j of the row's mask says so. A position outside
+// [ctx, ctx + node] raises the flag and counts as the nearest of them, so that the tiles of a request follow
+// from its lengths alone. 0 where no window asks for it.
+__device__ __forceinline__ int tree_position(const PagedArgs& a, const Request& r, int node, int32_t* flag) {
+    if (!a.window) return 0;
+    const int ctx = r.len - r.n, p = __ldg(a.positions + r.tok0 + node);
+    if (p < ctx || p > ctx + node) *flag |= CG_FLAG_PAGED_RANGE;
+    return min(max(p, ctx), ctx + node);
+}
+// Nodes [j, j + 32) of a request that the row of `node` sees, as a word; any j.
+__device__ __forceinline__ uint32_t tree_word(const PagedArgs& a, const Request& r, int node, int j) {
+    if (j <= -32 || j >= r.n) return 0u;
+    const uint32_t* row = a.masks + (int64_t)(r.tok0 + node) * a.words;
+    const int w = j >> 5;                                  // -1 for j < 0
+    const uint32_t lo = w >= 0 ? __ldg(row + w) : 0u, hi = w + 1 < a.words ? __ldg(row + w + 1) : 0u;
+    const int left = r.n - j;                              // bits past the last node are no tokens
+    return __funnelshift_r(lo, hi, j & 31) & (left >= 32 ? ~0u : (1u << left) - 1u);
+}
+// Whether the row of `node` at position p sees token t < len.
+__device__ __forceinline__ bool tree_sees(const PagedArgs& a, const Request& r, int node, int p, int t) {
+    const int j = t - (r.len - r.n);
+    return j < 0 ? !a.window || t > p - a.window || t < a.sinks : (tree_word(a, r, node, j) & 1u) != 0;
 }
 
 // Key tiles of TK tokens that rows at positions [p_first, p_last] of a request of length len see:

@@ -93,6 +93,11 @@ _ARGS = {   # the first pointers are to parameter structs
     "cg_rotary_append": [_vp, _vp, _ci32, _ci32, _vp] + [_vp] * 9,
     "cg_paged_attention_workspace_bytes": [_vp, _vp, ctypes.POINTER(ctypes.c_size_t)],
     "cg_paged_attention": [_vp, _vp] + [_vp] * 8 + [ctypes.c_size_t, _vp],
+    "cg_tree_plan": [_ci32] * 5 + [_vp] * 5 + [_ci32, _vp],
+    "cg_tree_attention": [_vp, _vp, _ci32] + [_vp] * 10 + [ctypes.c_size_t, _vp],
+    "cg_tree_commit": [_vp] + [_ci32] * 3 + [_vp] * 11,
+    "cg_block8_encode": [_ci32, _ci64, _ci64, _ci32, _vp, _ci64, _vp, _ci64, _vp, _vp],
+    "cg_block8_matmul": [_ci32, _ci64, _ci64, _ci64, _vp, _ci64, _vp, _vp, _ci64, _vp, _vp, _ci64, _vp],
 }
 _fns = {}
 _ws_bytes = {}
@@ -277,13 +282,9 @@ def _workspace(pages: Pages, how: PagedAttention, n: int, device):
     return kept
 
 
-def paged_attention(pages: Pages, how: PagedAttention, q, pool, block_table, seq_lens, cu_new, out, lse=None,
-                    workspace=None, stream=None) -> None:
-    """Attention of the new tokens' queries q [n_tok][H * n_rep][d] over their requests' pages
-    (cg_paged_attention). Without a workspace the call takes one from torch's allocator, on the
-    current stream (pass one to run on another); the default stream's is kept for the next call of the
-    same host thread, until the thread ends. A workspace that is passed serves calls made one after the
-    other: two threads must not pass the same one at the same time."""
+def _attend(name: str, pages: Pages, how: PagedAttention, q, pool, block_table, seq_lens, cu_new, out, lse, workspace, stream,
+            words=(), masks=()) -> None:
+    """The call of an attention entry point: `words` before its tensors, `masks` behind the lengths."""
     n, hq, dev = q.shape[0], pages.H * how.n_rep, _device()
     qp, qt, qh = _heads("q", q, n, hq, pages.d, pool.dtype, dev)
     op, ot, oh = _heads("out", out, n, hq, pages.d, pool.dtype, dev)
@@ -300,7 +301,17 @@ def paged_attention(pages: Pages, how: PagedAttention, q, pool, block_table, seq
     elif workspace.get_device() != dev or not workspace.is_contiguous():
         _bad(f"workspace: expected a contiguous tensor on device {dev}")
     r = pages.n_req
-    _check(_fn("cg_paged_attention")(
-        cp, ca, qp, _pool(pages, pool, dev), _i32("block_table", block_table, r * pages.max_pages, dev),
-        _i32("seq_lens", seq_lens, r, dev), _i32("cu_new", cu_new, r + 1, dev), op, lp, workspace.data_ptr(),
+    _check(_fn(name)(
+        cp, ca, *words, qp, _pool(pages, pool, dev), _i32("block_table", block_table, r * pages.max_pages, dev),
+        _i32("seq_lens", seq_lens, r, dev), _i32("cu_new", cu_new, r + 1, dev), *masks, op, lp, workspace.data_ptr(),
         workspace.nbytes, _stream(stream)))
+
+
+def paged_attention(pages: Pages, how: PagedAttention, q, pool, block_table, seq_lens, cu_new, out, lse=None,
+                    workspace=None, stream=None) -> None:
+    """Attention of the new tokens' queries q [n_tok][H * n_rep][d] over their requests' pages
+    (cg_paged_attention). Without a workspace the call takes one from torch's allocator, on the
+    current stream (pass one to run on another); the default stream's is kept for the next call of the
+    same host thread, until the thread ends. A workspace that is passed serves calls made one after the
+    other: two threads must not pass the same one at the same time."""
+    _attend("cg_paged_attention", pages, how, q, pool, block_table, seq_lens, cu_new, out, lse, workspace, stream)
