@@ -21,7 +21,8 @@ __all__ = ["CG_BLOCK_UNIFORM", "CG_KIVI", "CG_NONE", "CG_BLOCK_TILE", "CG_TILE_T
            "kivi_stream_bytes", "kivi_stream_alloc", "kivi_append", "kivi_stream_decode",
            "attention_workspace_bytes", "attention", "encode_hadamard", "decode_hadamard",
            "Pages", "Rotary", "RopeScaling", "PagedAttention", "page_plan", "page_release", "rotary_table", "rotary",
-           "rotary_append", "paged_attention_workspace_bytes", "paged_attention", "tree_plan", "tree_attention", "tree_commit"]
+           "rotary_append", "paged_attention_workspace_bytes", "paged_attention", "tree_plan", "tree_attention", "tree_commit",
+           "block8_encode", "block8_matmul"]
 
 CG_BLOCK_UNIFORM, CG_KIVI, CG_NONE, CG_BLOCK_TILE = 0, 1, 2, 3
 CG_TILE_TOKENS = 16
@@ -235,7 +236,8 @@ def alloc_outputs(shape: Shape, params: Params, device="cuda"):
 # The bindings that check torch tensors are loaded (and torch with them) on first use.
 _LAZY = {"paged": ("Pages", "PagedAttention", "RopeScaling", "Rotary", "page_plan", "page_release", "paged_attention",
                    "paged_attention_workspace_bytes", "rotary", "rotary_append", "rotary_table"),
-         "tree": ("tree_plan", "tree_attention", "tree_commit")}
+         "tree": ("tree_plan", "tree_attention", "tree_commit"),
+         "block8": ("block8_encode", "block8_matmul")}
 
 
 def __getattr__(name):

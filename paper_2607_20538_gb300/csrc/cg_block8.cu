@@ -1,0 +1,704 @@
+// cg_block8.cu -- matrices in e4m3 with a scale for each block of 128 channels: encoding, and the product of two of
+// them. Contract: include/codecgauge_block8.h.
+#include <cooperative_groups.h>
+#include <cuda_fp8.h>
+
+#include "../../include/codecgauge_block8.h"
+#include "cg_launch.h"
+#include "cg_paged.h"
+#include "cg_sm100.cuh"
+#include "cg_tc_common.cuh"
+#include "cg_tmap.h"
+
+#define CG_EXPORT __attribute__((visibility("default")))
+
+namespace cg {
+namespace {
+
+using namespace sm100;
+
+constexpr int kBlock = CG_BLOCK8;
+constexpr float kTop = 448.0f;
+
+// ------------------------------------------------------------------------------------
+// Encoding. 8 lanes a row of a block, 16 channels each: 32 bytes in, 16 bytes out. The largest |x| is found on the
+// bits (the order of non-negative numbers is that of their bits, infinities and NaN above all). A scale for one
+// row needs the 8 lanes alone, one for 128 rows a CTA, whose threads keep their 4 rows in registers. Bound: HBM, 3
+// bytes a value.
+// ------------------------------------------------------------------------------------
+constexpr int kEncThreads = 256, kGroup = 8, kEncRows = kEncThreads / kGroup;   // rows of blocks of a CTA and turn
+
+struct EncArgs {
+    const uint16_t* x;
+    uint8_t* codes;
+    float* scales;
+    int32_t* status;
+    int64_t R, K, x_stride, stride, nb;   // nb blocks a row
+};
+
+template <bool FP16>
+__device__ __forceinline__ float2 floats(uint32_t w) {
+    if (FP16) return __half22float2(*reinterpret_cast<const __half2*>(&w));
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+
+struct Piece {
+    uint32_t w[8];   // 16 values
+    __device__ __forceinline__ void load(const uint16_t* p, bool have) {
+        const uint4 zero = make_uint4(0, 0, 0, 0);
+        const uint4 a = have ? __ldg(reinterpret_cast<const uint4*>(p)) : zero, b = have ? __ldg(reinterpret_cast<const uint4*>(p) + 1) : zero;
+        w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
+        w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
+    }
+    // bits of the largest |x|
+    __device__ __forceinline__ uint32_t top() const {
+        uint32_t m = 0;
+#pragma unroll
+        for (int k = 0; k < 8; k++) m = __vmaxu2(m, w[k] & 0x7fff7fffu);
+        return max(m & 0xffffu, m >> 16);
+    }
+};
+
+// A block's scale from the bits of its largest |x|, and the codes of its values. The quotient x / s is rounded
+// as a division rounds it: q = x r with the rounded reciprocal r, then q + r (x - q s), whose residual is exact
+// (Markstein, 1990); where r or the residual could leave the normal numbers the division itself is used.
+template <bool FP16>
+struct Scale {
+    float s, r;
+    bool nonfinite, plain;
+    __device__ __forceinline__ explicit Scale(uint32_t top) {
+        nonfinite = top >= (FP16 ? 0x7c00u : 0x7f80u);
+        s = nonfinite ? __uint_as_float(0x7fffffffu) : floats<FP16>(top).x / kTop;
+        plain = !(s >= 0x1p-80f && s <= 0x1p100f);
+        r = plain ? 0.0f : __frcp_rn(s);
+    }
+    __device__ __forceinline__ float quotient(float x) const {
+        const float q = x * r;
+        return fmaf(fmaf(-q, s, x), r, q);
+    }
+    // of |x|; the signs are put in behind (the residual of -0 would lose its sign)
+    __device__ __forceinline__ uint32_t four(uint32_t w0, uint32_t w1) const {
+        const float2 x = floats<FP16>(w0 & 0x7fff7fffu), y = floats<FP16>(w1 & 0x7fff7fffu);
+        const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(quotient(x.x), quotient(x.y)), __NV_SATFINITE, __NV_E4M3);
+        const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(quotient(y.x), quotient(y.y)), __NV_SATFINITE, __NV_E4M3);
+        return (lo | hi << 16) | (__byte_perm(w0, w1, 0x7531) & 0x80808080u);
+    }
+    static __device__ __noinline__ uint32_t four_divided(uint32_t w0, uint32_t w1, float s) {
+        const float2 x = floats<FP16>(w0), y = floats<FP16>(w1);
+        const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(x.x / s, x.y / s), __NV_SATFINITE, __NV_E4M3);
+        return lo | (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(y.x / s, y.y / s), __NV_SATFINITE, __NV_E4M3) << 16;
+    }
+    __device__ __forceinline__ uint4 codes(const Piece& p) const {
+        uint32_t c[4];
+        if (!plain) {
+#pragma unroll
+            for (int k = 0; k < 4; k++) c[k] = four(p.w[2 * k], p.w[2 * k + 1]);
+        } else if (nonfinite || s == 0.0f) {
+            c[0] = c[1] = c[2] = c[3] = nonfinite ? 0x7f7f7f7fu : 0u;
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; k++) c[k] = four_divided(p.w[2 * k], p.w[2 * k + 1], s);
+        }
+        return make_uint4(c[0], c[1], c[2], c[3]);
+    }
+};
+
+// rows = 1: a group of 8 lanes a block.
+template <bool FP16>
+__global__ void __launch_bounds__(kEncThreads) encode_rows_kernel(EncArgs a) {
+    const int lane8 = threadIdx.x % kGroup;
+    const int64_t items = a.R * a.nb, step = (int64_t)gridDim.x * kEncRows;
+    int32_t flag = 0;
+    for (int64_t it = (int64_t)blockIdx.x * kEncRows + threadIdx.x / kGroup; it - threadIdx.x / kGroup < items; it += step) {
+        const bool have = it < items;
+        const int64_t row = have ? it / a.nb : 0, b = have ? it - row * a.nb : 0, ch = b * kBlock + lane8 * 16;
+        Piece p;
+        p.load(a.x + row * a.x_stride + ch, have && ch < a.K);
+        uint32_t top = p.top();
+#pragma unroll
+        for (int off = 1; off < kGroup; off *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, off));
+        const Scale<FP16> s(top);
+        if (s.nonfinite) flag = CG_FLAG_NONFINITE_INPUT;
+        if (have && ch < a.K) *reinterpret_cast<uint4*>(a.codes + row * a.stride + ch) = s.codes(p);
+        if (have && lane8 == 0) a.scales[it] = s.s;
+    }
+    raise_flag(a.status, flag);
+}
+
+// rows = 128: a CTA a block.
+template <bool FP16>
+__global__ void __launch_bounds__(kEncThreads) encode_square_kernel(EncArgs a) {
+    constexpr int kPer = kBlock / kEncRows;
+    __shared__ uint32_t tops[kEncThreads / 32];
+    const int lane8 = threadIdx.x % kGroup, r0 = threadIdx.x / kGroup, warp = threadIdx.x >> 5;
+    const int64_t rb = (a.R + kBlock - 1) / kBlock, items = rb * a.nb;
+    int32_t flag = 0;
+    for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
+        const int64_t r = it / a.nb, b = it - r * a.nb, ch = b * kBlock + lane8 * 16;
+        Piece p[kPer];
+        uint32_t top = 0;
+#pragma unroll
+        for (int k = 0; k < kPer; k++) {
+            const int64_t row = r * kBlock + r0 + k * kEncRows;
+            p[k].load(a.x + row * a.x_stride + ch, row < a.R && ch < a.K);
+        }
+#pragma unroll
+        for (int k = 0; k < kPer; k++) top = max(top, p[k].top());
+        top = __reduce_max_sync(0xffffffffu, top);
+        if ((threadIdx.x & 31) == 0) tops[warp] = top;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kEncThreads / 32; w++) top = max(top, tops[w]);
+        __syncthreads();
+        const Scale<FP16> s(top);
+        if (s.nonfinite) flag = CG_FLAG_NONFINITE_INPUT;
+#pragma unroll
+        for (int k = 0; k < kPer; k++) {
+            const int64_t row = r * kBlock + r0 + k * kEncRows;
+            if (row < a.R && ch < a.K) *reinterpret_cast<uint4*>(a.codes + row * a.stride + ch) = s.codes(p[k]);
+        }
+        if (threadIdx.x == 0) a.scales[it] = s.s;
+    }
+    raise_flag(a.status, flag);
+}
+
+// ------------------------------------------------------------------------------------
+// Product. A tile is 128 rows of one matrix (the lanes of tensor memory) by TC rows of the other (its columns). Block
+// by block of 128 channels the tensor cores (tcgen05.mma, kind f8f6f4, four instructions of 32 channels) sum the
+// products into one of two buffers of tensor memory; the accumulating warps read it, multiply by the block's two
+// scales and add to sums in registers, while the other buffer fills.
+//   warps 0 .. E-1  accumulate: warp w has lanes 32 (w % 4) .. + 31 and columns (w / 4) CW .. + CW - 1
+//   warp E          TMA: both matrices' 128-byte pieces of rows into a ring of stages (128-byte swizzle)
+//   warp E + 1      one thread issues tcgen05.mma
+// TOKENS: lanes are rows of x, so that a thread has one x scale a block and its warp one or two w scales. Otherwise
+// (few rows of x) lanes are rows of w, which fill the 128 lanes where x could not, and columns rows of x, whose
+// scales the lanes hold for one another.
+// Few tiles: the blocks of channels are cut among the CTAs of a cluster; each leaves its sums in shared memory,
+// and each adds up a part of the rows, in the order of the ranks whatever their timing.
+// ------------------------------------------------------------------------------------
+constexpr int kLanes = 128;
+
+template <int TC, bool TOKENS>
+struct Tile {
+    static constexpr int kWarps = TC >= 128 ? 8 : 4;            // accumulating
+    static constexpr int CW = TC / (kWarps / 4);                // columns of a warp
+    static constexpr int kThreads = (kWarps + 2) * 32;
+    static constexpr uint32_t kA = kLanes * 128, kStage = kA + TC * 128;
+    static constexpr int kStages = TC >= 192 ? 4 : TC == 128 ? 6 : 4;
+    static constexpr int kPitch = TC + 4;                       // floats of a row of sums, without bank conflicts in 16-byte pieces
+    static constexpr uint32_t kSums = kLanes * kPitch * 4;
+    static constexpr uint32_t misc = kStages * kStage > kSums ? kStages * kStage : kSums;
+    static constexpr uint32_t total = misc + 256;
+    static constexpr int kBuf = TC > 128 ? 256 : TC;            // columns from buffer to buffer
+    static constexpr int kCols = 2 * kBuf < 32 ? 32 : 2 * kBuf;
+    static constexpr int kCtas = total <= 76000 ? 3 : total <= 114000 ? 2 : 1;   // of an SM
+    static_assert(CW % 16 == 0 && kStage % 1024 == 0 && total <= 232448, "tile");
+};
+
+struct MatArgs {
+    const float *xs, *ws;
+    void* out;
+    int32_t* status;
+    int64_t M, N, nb, out_stride;
+    int64_t lane_tiles, col_tiles;
+    uint64_t wait_ns;
+    int fp16, vec;       // 16-byte stores are possible
+    int split;           // CTAs of a cluster
+    int group;           // lane tiles that are walked together
+};
+
+struct MatMisc {
+    uint64_t full[8], empty[8], tfull[2], tempty[2], drain;
+    int abort_flag;
+    uint32_t tmem;
+};
+static_assert(sizeof(MatMisc) <= 256, "misc block");
+
+__device__ __forceinline__ void mma_e4m3(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+        "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// Instruction descriptor (kind::f8f6f4): e4m3 A and B, both K-major, fp32 D, M x N.
+__host__ __device__ constexpr uint32_t idesc_e4m3(int M, int N) {
+    return (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, float (&r)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]),
+          "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15])
+        : "r"(taddr));
+}
+// Uses of r stay behind the wait that precedes this.
+__device__ __forceinline__ void settle16(float (&r)[16]) {
+    asm volatile("" : "+f"(r[0]), "+f"(r[1]), "+f"(r[2]), "+f"(r[3]), "+f"(r[4]), "+f"(r[5]), "+f"(r[6]), "+f"(r[7]),
+                 "+f"(r[8]), "+f"(r[9]), "+f"(r[10]), "+f"(r[11]), "+f"(r[12]), "+f"(r[13]), "+f"(r[14]), "+f"(r[15]));
+}
+
+__device__ __forceinline__ uint32_t pack(float x, float y, int fp16) {   // x in the low half
+    if (fp16) {
+        const __half2 h = __floats2half2_rn(x, y);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    }
+    const __nv_bfloat162 b = __floats2bfloat162_rn(x, y);
+    return *reinterpret_cast<const uint32_t*>(&b);
+}
+
+// Up to 8 values (16 bytes) to dst.
+__device__ __forceinline__ void store_piece(uint16_t* dst, uint4 v, int valid, bool vec) {
+    if (vec && valid >= 8) {
+        *reinterpret_cast<uint4*>(dst) = v;
+        return;
+    }
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int e = 0; e < 8; e++)
+        if (e < valid) dst[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
+}
+
+// 32 columns of each lane's row. The lanes of a group of four transpose their pieces of 16 bytes, so that a store
+// instruction covers 64 bytes of 8 rows instead of 16 of 32. row: of the output, or null; left: its columns from here on.
+__device__ __forceinline__ void store_columns(uint32_t (&b)[16], uint16_t* row, int64_t left, bool vec) {
+    const int lane = threadIdx.x & 31, j = lane & 3;
+#pragma unroll
+    for (int step = 1; step < 4; step *= 2) {
+        const bool up = lane & step;
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            if (k & step) continue;
+#pragma unroll
+            for (int e = 0; e < 4; e++) {   // pieces k of the upper lane and k + step of the lower one change places
+                uint32_t &x = b[4 * k + e], &y = b[4 * (k + step) + e];
+                const uint32_t other = __shfl_xor_sync(0xffffffffu, up ? x : y, step);
+                if (up) x = other;
+                else y = other;
+            }
+        }
+    }
+    const int valid = left - 8 * j < 8 ? (int)(left - 8 * j) : 8;
+#pragma unroll
+    for (int k = 0; k < 4; k++) {
+        const uint64_t dst = __shfl_sync(0xffffffffu, reinterpret_cast<uint64_t>(row), (lane & 28) + k);
+        if (dst && valid > 0)
+            store_piece(reinterpret_cast<uint16_t*>(dst) + 8 * j, make_uint4(b[4 * k], b[4 * k + 1], b[4 * k + 2], b[4 * k + 3]), valid, vec);
+    }
+}
+
+template <int TC, bool TOKENS>
+__global__ void __launch_bounds__(Tile<TC, TOKENS>::kThreads, Tile<TC, TOKENS>::kCtas)
+block8_matmul_kernel(const __grid_constant__ MatArgs a, const __grid_constant__ CUtensorMap lane_map, const __grid_constant__ CUtensorMap col_map) {
+    using T = Tile<TC, TOKENS>;
+    extern __shared__ __align__(1024) unsigned char smem[];
+    MatMisc* S = reinterpret_cast<MatMisc*>(smem + T::misc);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int rank = blockIdx.x % a.split;
+    const int64_t first = blockIdx.x / a.split, step = gridDim.x / a.split, tiles = a.lane_tiles * a.col_tiles;
+    const int64_t kb0 = a.nb * rank / a.split, kb1 = a.nb * (rank + 1) / a.split;
+    if (tid == 0) {
+        for (int s = 0; s < T::kStages; s++) {
+            mbar_init(&S->full[s], 1);
+            mbar_init(&S->empty[s], 1);
+        }
+        for (int s = 0; s < 2; s++) {
+            mbar_init(&S->tfull[s], 1);
+            mbar_init(&S->tempty[s], T::kWarps);
+        }
+        mbar_init(&S->drain, 1);
+        S->abort_flag = (smem_u32(smem) & 1023u) != 0;   // the swizzle needs the alignment asked for
+        fence_barrier_init();
+        prefetch_tmap(&lane_map);
+        prefetch_tmap(&col_map);
+    }
+    if (warp == T::kWarps + 1) {
+        tmem_alloc(&S->tmem, T::kCols);
+        tmem_relinquish();
+        tc_fence_before();
+    }
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = S->tmem;
+    volatile int* abort_flag = &S->abort_flag;
+    // lane tiles in groups, so that the CTAs at work share both matrices' rows in L2
+    auto place = [&](int64_t tile, int64_t* l, int64_t* c) {
+        const int64_t per = a.group * a.col_tiles, g = tile / per, in = tile - g * per;
+        const int64_t left = a.lane_tiles - g * a.group, n = left < a.group ? left : a.group;
+        *c = in / n;
+        *l = g * a.group + (in - *c * n);
+    };
+    bool dead = *abort_flag != 0;
+
+    if (warp < T::kWarps) {
+        // ------------------------------------------------------------ accumulate
+        const int col0 = (warp >> 2) * T::CW, row = 32 * (warp & 3) + lane;
+        const uint32_t t0 = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + col0;
+        int buf = 0, ph = 0;
+        for (int64_t tile = first; tile < tiles && !dead; tile += step) {
+            int64_t lt, ct;
+            place(tile, &lt, &ct);
+            const int64_t r = lt * kLanes + row, c = ct * TC + col0;    // the thread's row, and first column
+            float acc[T::CW];
+#pragma unroll
+            for (int k = 0; k < T::CW; k++) acc[k] = 0.0f;
+            // the scales of a block ahead: `mine` of the thread's row (TOKENS) or of columns lane + 32 i; `uni` of the
+            // warp's first and last columns, or of its row of w
+            constexpr int kMine = TOKENS ? 1 : (T::CW + 31) / 32;
+            const float *pm[kMine], *pu[2];
+            if (TOKENS) {
+                pm[0] = a.xs + (r < a.M ? r : a.M - 1) * a.nb;
+                const int64_t last = (a.N - 1) / kBlock, u0 = c / kBlock, u1 = (c + T::CW - 1) / kBlock;
+                pu[0] = a.ws + (u0 < last ? u0 : last) * a.nb;
+                pu[1] = a.ws + (u1 < last ? u1 : last) * a.nb;
+            } else {
+#pragma unroll
+                for (int i = 0; i < kMine; i++) {
+                    const int64_t m = c + lane + 32 * i;
+                    pm[i] = a.xs + (m < a.M ? m : a.M - 1) * a.nb;
+                }
+                pu[0] = pu[1] = a.ws + lt * a.nb;
+            }
+            float mine[kMine], uni[2];
+            auto fetch = [&](int64_t kb) {
+                if (kb >= kb1) return;
+#pragma unroll
+                for (int i = 0; i < kMine; i++) mine[i] = __ldg(pm[i] + kb);
+                uni[0] = __ldg(pu[0] + kb);
+                uni[1] = __ldg(pu[1] + kb);
+            };
+            fetch(kb0);
+            for (int64_t kb = kb0; kb < kb1; kb++) {
+                float f[kMine], f1;
+#pragma unroll
+                for (int i = 0; i < kMine; i++) f[i] = mine[i] * uni[0];
+                f1 = mine[0] * uni[1];
+                fetch(kb + 1);
+                if (!__all_sync(0xffffffffu, mbar_wait(&S->tfull[buf], ph, abort_flag, a.wait_ns))) {
+                    dead = true;
+                    break;
+                }
+                tc_fence_after();
+#pragma unroll
+                for (int q = 0; q < T::CW / 16; q++) {
+                    float v[16];
+                    tmem_ld16(t0 + buf * T::kBuf + 16 * q, v);
+                    tmem_wait_ld();
+                    settle16(v);
+                    if (16 * (q + 1) == T::CW) {   // all read
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&S->tempty[buf]);
+                    }
+                    // columns of another block of w than the first
+                    const float fq = !TOKENS ? 0.0f : T::CW % kBlock == 0 || (c + 16 * q) / kBlock == c / kBlock ? f[0] : f1;
+#pragma unroll
+                    for (int k = 0; k < 16; k++)
+                        acc[16 * q + k] = fmaf(v[k], TOKENS ? fq : __shfl_sync(0xffffffffu, f[(16 * q + k) / 32 % kMine], (16 * q + k) & 31), acc[16 * q + k]);
+                }
+                buf ^= 1;
+                ph ^= buf == 0;
+            }
+            if (dead) break;
+            if (a.split > 1) {
+                float* sums = reinterpret_cast<float*>(smem) + row * T::kPitch + col0;
+#pragma unroll
+                for (int k = 0; k < T::CW; k += 4) *reinterpret_cast<float4*>(sums + k) = make_float4(acc[k], acc[k + 1], acc[k + 2], acc[k + 3]);
+                break;
+            }
+            if (TOKENS) {
+                uint16_t* out = r < a.M ? static_cast<uint16_t*>(a.out) + r * a.out_stride + c : nullptr;
+#pragma unroll
+                for (int q = 0; q < T::CW / 32; q++) {
+                    uint32_t b[16];
+#pragma unroll
+                    for (int k = 0; k < 16; k++) b[k] = pack(acc[32 * q + 2 * k], acc[32 * q + 2 * k + 1], a.fp16);
+                    if (c + 32 * q < a.N) store_columns(b, out ? out + 32 * q : nullptr, a.N - (c + 32 * q), a.vec);
+                }
+            } else if (r < a.N) {
+                uint16_t* out = static_cast<uint16_t*>(a.out) + r;
+#pragma unroll
+                for (int k = 0; k < T::CW; k++)
+                    if (c + k < a.M) out[(c + k) * a.out_stride] = (uint16_t)pack(acc[k], 0.0f, a.fp16);
+            }
+        }
+    } else if (warp == T::kWarps) {
+        // ------------------------------------------------------------ copies
+        int st = 0, ph = 1;
+        int64_t issued = 0;
+        for (int64_t tile = first; tile < tiles && !dead; tile += step) {
+            int64_t lt, ct;
+            place(tile, &lt, &ct);
+            for (int64_t kb = kb0; kb < kb1; kb++) {
+                if (!__all_sync(0xffffffffu, mbar_wait(&S->empty[st], ph, abort_flag, a.wait_ns))) {
+                    dead = true;
+                    break;
+                }
+                if (lane == 0) {
+                    mbar_arrive_expect_tx(&S->full[st], T::kStage);
+                    tma_load_2d(smem + st * T::kStage, &lane_map, &S->full[st], (int)(kb * kBlock), (int)(lt * kLanes));
+                    tma_load_2d(smem + st * T::kStage + T::kA, &col_map, &S->full[st], (int)(kb * kBlock), (int)(ct * TC));
+                }
+                __syncwarp();
+                issued++;
+                if (++st == T::kStages) {
+                    st = 0;
+                    ph ^= 1;
+                }
+            }
+        }
+        if (dead) *abort_flag = 1;
+        // copies in flight land before the CTA ends, also where the other warps gave up on them
+        const int zero = 0;
+        for (int64_t k = issued > T::kStages ? issued - T::kStages : 0; k < issued; k++)
+            mbar_wait(&S->full[k % T::kStages], (k / T::kStages) & 1, &zero, tc::kWaitLimitNs);
+    } else {
+        // ------------------------------------------------------------ products
+        constexpr uint32_t idesc = idesc_e4m3(kLanes, TC);
+        int st = 0, ph = 0, buf = 0, tph = 1;
+        for (int64_t tile = first; tile < tiles && !dead; tile += step) {
+            for (int64_t kb = kb0; kb < kb1; kb++) {
+                if (!__all_sync(0xffffffffu, mbar_wait(&S->tempty[buf], tph, abort_flag, a.wait_ns)) ||
+                    !__all_sync(0xffffffffu, mbar_wait(&S->full[st], ph, abort_flag, a.wait_ns))) {
+                    dead = true;
+                    break;
+                }
+                tc_fence_after();
+                if (lane == 0) {
+                    const uint64_t da = sdesc_sw128(smem_u32(smem + st * T::kStage)), db = sdesc_sw128(smem_u32(smem + st * T::kStage + T::kA));
+#pragma unroll
+                    for (int k = 0; k < kBlock / 32; k++) mma_e4m3(tmem + buf * T::kBuf, da + 2 * k, db + 2 * k, idesc, k ? 1u : 0u);
+                    mma_commit(&S->empty[st]);
+                    mma_commit(&S->tfull[buf]);
+                }
+                __syncwarp();
+                buf ^= 1;
+                tph ^= buf == 0;
+                if (++st == T::kStages) {
+                    st = 0;
+                    ph ^= 1;
+                }
+            }
+        }
+        if (dead) *abort_flag = 1;
+        if (lane == 0) mma_commit(&S->drain);   // products in flight end before tensor memory is given back
+        __syncwarp();
+        const int zero = 0;
+        mbar_wait(&S->drain, 0, &zero, tc::kWaitLimitNs);
+    }
+    __syncwarp();
+    if (dead) {
+        *abort_flag = 1;
+        if (lane == 0) raise_flag(a.status, CG_FLAG_PIPE_TIMEOUT);
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == T::kWarps + 1) {
+        tc_fence_after();
+        tmem_dealloc(tmem, T::kCols);
+    }
+    if (a.split > 1) {
+        // ---- sums of the cluster: this CTA's part of the rows
+        auto cluster = cooperative_groups::this_cluster();
+        cluster.sync();
+        int64_t lt, ct;
+        place(first, &lt, &ct);
+        const int rows = kLanes / a.split, r0 = rank * rows;
+        const float* sums = reinterpret_cast<const float*>(smem);
+        if (TOKENS) {
+            for (int x = tid; x < rows * (TC / 4); x += T::kThreads) {
+                const int r = r0 + x / (TC / 4), c4 = x % (TC / 4) * 4;
+                const int64_t m = lt * kLanes + r, n = ct * TC + c4;
+                if (m >= a.M || n >= a.N) continue;
+                float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                for (int k = 0; k < a.split; k++) {
+                    const float4 v = *reinterpret_cast<const float4*>(cluster.map_shared_rank(sums, k) + r * T::kPitch + c4);
+                    s = make_float4(s.x + v.x, s.y + v.y, s.z + v.z, s.w + v.w);
+                }
+                uint16_t* dst = static_cast<uint16_t*>(a.out) + m * a.out_stride + n;
+                const uint2 w = make_uint2(pack(s.x, s.y, a.fp16), pack(s.z, s.w, a.fp16));
+                if (a.vec && n + 4 <= a.N) *reinterpret_cast<uint2*>(dst) = w;
+                else store_piece(dst, make_uint4(w.x, w.y, 0u, 0u), a.N - n < 4 ? (int)(a.N - n) : 4, false);
+            }
+        } else {
+            for (int x = tid; x < rows * TC; x += T::kThreads) {
+                const int r = r0 + x % rows, c = x / rows;
+                const int64_t n = lt * kLanes + r, m = ct * TC + c;
+                if (m >= a.M || n >= a.N) continue;
+                float s = 0.0f;
+                for (int k = 0; k < a.split; k++) s += cluster.map_shared_rank(sums, k)[r * T::kPitch + c];
+                static_cast<uint16_t*>(a.out)[m * a.out_stride + n] = (uint16_t)pack(s, 0.0f, a.fp16);
+            }
+        }
+        cluster.sync();   // no CTA ends while its sums may be read
+    }
+}
+
+// Codes [rows][K] in boxes of box_rows x 128 bytes, 128-byte swizzle; what lies outside reads as 0.
+bool codes_map(CUtensorMap* map, const void* base, int64_t rows, int64_t K, int64_t stride, uint32_t box_rows) {
+    auto fn = tmap_encode_fn();
+    if (!fn) return false;
+    cuuint64_t dims[2] = {(cuuint64_t)K, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)(rows > 1 ? stride : K)};
+    cuuint32_t box[2] = {128, box_rows}, estr[2] = {1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+struct Matrices {
+    const void *x, *w;
+    int64_t K, x_stride, w_stride;
+};
+
+template <int TC, bool TOKENS>
+cudaError_t launch_tile(MatArgs a, const Matrices& m, int split, cudaStream_t st) {
+    using T = Tile<TC, TOKENS>;
+    CUtensorMap lanes, cols;
+    const bool ok = TOKENS ? codes_map(&lanes, m.x, a.M, m.K, m.x_stride, kLanes) && codes_map(&cols, m.w, a.N, m.K, m.w_stride, TC)
+                           : codes_map(&lanes, m.w, a.N, m.K, m.w_stride, kLanes) && codes_map(&cols, m.x, a.M, m.K, m.x_stride, TC);
+    if (!ok) return cudaErrorInvalidValue;
+    a.lane_tiles = ((TOKENS ? a.M : a.N) + kLanes - 1) / kLanes;
+    a.col_tiles = ((TOKENS ? a.N : a.M) + TC - 1) / TC;
+    a.split = split;
+    a.group = 16;
+    auto* kernel = block8_matmul_kernel<TC, TOKENS>;
+    static SmemOptIn opt_in;
+    cudaError_t e = opt_in.set(reinterpret_cast<const void*>(kernel), (int)T::total);
+    if (e != cudaSuccess) return e;
+    const int64_t tiles = a.lane_tiles * a.col_tiles, room = (int64_t)tc::num_sms() * T::kCtas;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(split > 1 ? tiles * split : tiles < room ? tiles : room));
+    cfg.blockDim = dim3(T::kThreads);
+    cfg.dynamicSmemBytes = T::total;
+    cfg.stream = st;
+    cudaLaunchAttribute at{};
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = (unsigned)split;
+    at.val.clusterDim.y = at.val.clusterDim.z = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = split > 1 ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kernel, a, lanes, cols);
+}
+
+// CTAs of a cluster: as many as the GPU has room for at once, a block of channels each at least.
+int split_of(int64_t tiles, int64_t nb, int ctas) {
+    int s = 1;
+    while (s < 8 && tiles * 2 * s <= (int64_t)tc::num_sms() * ctas && 2 * s <= nb) s *= 2;
+    return s;
+}
+
+cudaError_t launch_matmul(const MatArgs& a, const Matrices& m, cudaStream_t st) {
+    const int64_t n128 = (a.N + 127) / 128, m128 = (a.M + 127) / 128;
+    if (a.M <= 16) return launch_tile<16, false>(a, m, split_of(n128, a.nb, Tile<16, false>::kCtas), st);
+    if (a.M <= 32) return launch_tile<32, false>(a, m, split_of(n128, a.nb, Tile<32, false>::kCtas), st);
+    if (a.M <= 64) return launch_tile<64, false>(a, m, split_of(n128, a.nb, Tile<64, false>::kCtas), st);
+    const int64_t t256 = m128 * ((a.N + 255) / 256);
+    if (t256 >= tc::num_sms()) return launch_tile<256, true>(a, m, 1, st);
+    return launch_tile<128, true>(a, m, split_of(m128 * n128, a.nb, Tile<128, true>::kCtas), st);
+}
+
+bool al16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+int check_type(int32_t dtype) {
+    return dtype == CG_BF16 || dtype == CG_FP16 ? CG_OK : set_error(CG_EINVAL, "dtype=%d: CG_BF16 or CG_FP16", dtype);
+}
+int check_channels(int64_t K) {
+    if (K < 16 || K % 16) return set_error(CG_EINVAL, "K=%lld: must be a multiple of 16, at least 16", (long long)K);
+    if (K > (int64_t)1 << 30) return set_error(CG_ERANGE, "K=%lld: must be at most 2^30", (long long)K);
+    return CG_OK;
+}
+int check_rows(const char* what, int64_t R) {
+    if (R < 0) return set_error(CG_EINVAL, "%s=%lld: must be >= 0", what, (long long)R);
+    if (R > (int64_t)1 << 30) return set_error(CG_ERANGE, "%s=%lld: must be at most 2^30", what, (long long)R);
+    return CG_OK;
+}
+int check_stride(const char* what, int64_t R, int64_t row, int64_t stride, int64_t of) {
+    if (R < 2) return CG_OK;
+    if (stride < row || stride % of || stride >= (int64_t)1 << 40)
+        return set_error(CG_EINVAL, "%s: a row stride must be a multiple of %lld, at least the row's %lld and below 2^40 (got %lld)", what, (long long)of,
+                         (long long)row, (long long)stride);
+    return CG_OK;
+}
+
+}  // namespace
+}  // namespace cg
+
+using namespace cg;
+
+extern "C" {
+
+CG_EXPORT int cg_block8_encode(int32_t dtype, int64_t R, int64_t K, int32_t rows, const void* x, int64_t x_stride, void* codes,
+                               int64_t stride, float* scales, void* stream) {
+    set_error(CG_OK, "%s", "");
+    int rc = check_type(dtype);
+    if (!rc) rc = check_channels(K);
+    if (!rc) rc = check_rows("R", R);
+    if (!rc && rows != 1 && rows != kBlock) rc = set_error(CG_EINVAL, "rows=%d: must be 1 or %d", rows, kBlock);
+    if (!rc) rc = check_stride("x", R, K, x_stride, 8);
+    if (!rc) rc = check_stride("codes", R, K, stride, 16);
+    if (rc) return rc;
+    if (R == 0) return CG_OK;
+    if (!x || !codes || !scales) return set_error(CG_EINVAL, "null x, codes or scales");
+    if (!al16(x) || !al16(codes) || (reinterpret_cast<uintptr_t>(scales) & 3u))
+        return set_error(CG_EINVAL, "x and codes must be 16-byte aligned, scales to 4 bytes");
+    EncArgs a{};
+    if ((rc = device_status(&a.status))) return rc;
+    a.x = static_cast<const uint16_t*>(x);
+    a.codes = static_cast<uint8_t*>(codes);
+    a.scales = scales;
+    a.R = R;
+    a.K = K;
+    a.x_stride = R > 1 ? x_stride : K;
+    a.stride = R > 1 ? stride : K;
+    a.nb = (K + kBlock - 1) / kBlock;
+    const int64_t items = rows == 1 ? (R * a.nb + kEncRows - 1) / kEncRows : (R + kBlock - 1) / kBlock * a.nb;
+    const unsigned grid = (unsigned)(items < (1 << 30) ? items : 1 << 30);
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (rows == 1) {
+        if (dtype == CG_FP16) encode_rows_kernel<true><<<grid, kEncThreads, 0, st>>>(a);
+        else encode_rows_kernel<false><<<grid, kEncThreads, 0, st>>>(a);
+    } else {
+        if (dtype == CG_FP16) encode_square_kernel<true><<<grid, kEncThreads, 0, st>>>(a);
+        else encode_square_kernel<false><<<grid, kEncThreads, 0, st>>>(a);
+    }
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return set_error(CG_ECUDA, "block encoding launch: %s", cudaGetErrorString(e));
+    return CG_OK;
+}
+
+CG_EXPORT int cg_block8_matmul(int32_t dtype, int64_t M, int64_t N, int64_t K, const void* x, int64_t x_stride, const float* x_scales,
+                               const void* w, int64_t w_stride, const float* w_scales, void* out, int64_t out_stride, void* stream) {
+    set_error(CG_OK, "%s", "");
+    int rc = check_type(dtype);
+    if (!rc) rc = check_channels(K);
+    if (!rc) rc = check_rows("M", M);
+    if (!rc) rc = check_rows("N", N);
+    if (!rc) rc = check_stride("x", M, K, x_stride, 16);
+    if (!rc) rc = check_stride("w", N, K, w_stride, 16);
+    if (!rc) rc = check_stride("out", M, N, out_stride, 1);
+    if (rc) return rc;
+    if (M == 0 || N == 0) return CG_OK;
+    if (!x || !x_scales || !w || !w_scales || !out) return set_error(CG_EINVAL, "null x, w, scales or out");
+    if (!al16(x) || !al16(w) || ((reinterpret_cast<uintptr_t>(x_scales) | reinterpret_cast<uintptr_t>(w_scales)) & 3u) ||
+        (reinterpret_cast<uintptr_t>(out) & 1u))
+        return set_error(CG_EINVAL, "x and w must be 16-byte aligned, scales and out to their type");
+    if (out == x || out == w) return set_error(CG_EINVAL, "out must not overlap the inputs");
+    MatArgs a{};
+    if ((rc = device_status(&a.status))) return rc;
+    a.xs = x_scales;
+    a.ws = w_scales;
+    a.out = out;
+    a.M = M;
+    a.N = N;
+    a.nb = (K + kBlock - 1) / kBlock;
+    a.out_stride = M > 1 ? out_stride : N;
+    a.wait_ns = wait_limit_ns();
+    a.fp16 = dtype == CG_FP16;
+    a.vec = al16(out) && (M < 2 || out_stride % 8 == 0);
+    const cudaError_t e = launch_matmul(a, Matrices{x, w, K, x_stride, w_stride}, static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return set_error(CG_ECUDA, "block product launch: %s", cudaGetErrorString(e));
+    return CG_OK;
+}
+
+}  // extern "C"
