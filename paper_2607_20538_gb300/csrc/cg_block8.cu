@@ -203,6 +203,7 @@ struct MatArgs {
     int64_t lane_tiles, col_tiles;
     uint64_t wait_ns;
     int fp16, vec;       // 16-byte stores are possible
+    int vec_scales;      // 16-byte loads of scales are possible
     int split;           // CTAs of a cluster
     int group;           // lane tiles that are walked together
 };
@@ -214,13 +215,32 @@ struct MatMisc {
 };
 static_assert(sizeof(MatMisc) <= 256, "misc block");
 
-__device__ __forceinline__ void mma_e4m3(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
-        "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
-        : "memory");
+// One step of 32 channels. Descriptors as halves (a step only adds to the low ones) that the whole warp computes, so that
+// they stay in uniform registers, and an elected thread: behind a branch on the lane number a block's issue took 500
+// cycles, as long as its products.
+template <bool PAIR>
+__device__ __forceinline__ void mma_e4m3(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t accumulate) {
+    if (PAIR)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
+            "mov.b64 da, {%1, %3};\n\tmov.b64 db, {%2, %3};\n\t"
+            "setp.ne.b32 p, %5, 0;\n\t"
+            "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], da, db, %4, p;\n\t}" ::"r"(d_tmem),
+            "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
+            "mov.b64 da, {%1, %3};\n\tmov.b64 db, {%2, %3};\n\t"
+            "setp.ne.b32 p, %5, 0;\n\t"
+            "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], da, db, %4, p;\n\t}" ::"r"(d_tmem),
+            "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate)
+            : "memory");
+}
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
 }
 // Instruction descriptor (kind::f8f6f4): e4m3 A and B, both K-major, fp32 D, M x N.
 __host__ __device__ constexpr uint32_t idesc_e4m3(int M, int N) {
@@ -457,6 +477,9 @@ block8_matmul_kernel(const __grid_constant__ MatArgs a, const __grid_constant__ 
     } else {
         // ------------------------------------------------------------ products
         constexpr uint32_t idesc = idesc_e4m3(kLanes, TC);
+        const bool issue = elect_one();
+        const uint64_t desc = sdesc_sw128(smem_u32(smem));
+        const uint32_t a_lo = (uint32_t)desc, hi = (uint32_t)(desc >> 32);
         int st = 0, ph = 0, buf = 0, tph = 1;
         for (int64_t tile = first; tile < tiles && !dead; tile += step) {
             for (int64_t kb = kb0; kb < kb1; kb++) {
@@ -466,10 +489,10 @@ block8_matmul_kernel(const __grid_constant__ MatArgs a, const __grid_constant__ 
                     break;
                 }
                 tc_fence_after();
-                if (lane == 0) {
-                    const uint64_t da = sdesc_sw128(smem_u32(smem + st * T::kStage)), db = sdesc_sw128(smem_u32(smem + st * T::kStage + T::kA));
+                const uint32_t da = a_lo + ((st * T::kStage) >> 4), db = da + (T::kA >> 4), d = tmem + buf * T::kBuf;
+                if (issue) {
 #pragma unroll
-                    for (int k = 0; k < kBlock / 32; k++) mma_e4m3(tmem + buf * T::kBuf, da + 2 * k, db + 2 * k, idesc, k ? 1u : 0u);
+                    for (int k = 0; k < kBlock / 32; k++) mma_e4m3<false>(d, da + 2 * k, db + 2 * k, hi, idesc, k ? 1u : 0u);
                     mma_commit(&S->empty[st]);
                     mma_commit(&S->tfull[buf]);
                 }
@@ -483,7 +506,7 @@ block8_matmul_kernel(const __grid_constant__ MatArgs a, const __grid_constant__ 
             }
         }
         if (dead) *abort_flag = 1;
-        if (lane == 0) mma_commit(&S->drain);   // products in flight end before tensor memory is given back
+        if (issue) mma_commit(&S->drain);   // products in flight end before tensor memory is given back
         __syncwarp();
         const int zero = 0;
         mbar_wait(&S->drain, 0, &zero, tc::kWaitLimitNs);
@@ -536,6 +559,353 @@ block8_matmul_kernel(const __grid_constant__ MatArgs a, const __grid_constant__ 
     }
 }
 
+// ------------------------------------------------------------------------------------
+// Product of many rows: pairs of CTAs (a cluster of two, tcgen05 cta_group::2). A tile is 256 rows of x by 256 rows of
+// w; each CTA of the pair copies 128 rows of x and half the rows of w, and its tensor memory takes the sums of its
+// own rows with all columns, so that a product reads 32 KB a block and SM where a CTA for itself would read 48.
+// The two halves of the columns are products, buffers and barriers of their own (N = 128): while one half's sums are
+// read, the other's products run.
+//   warps 0 - 7   accumulate, as above: a thread a row and one half's columns, in 208 registers. Results go through
+//                 shared memory and TMA stores, which run beside the next tile.
+//   warp 8        TMA of the CTA's own halves
+//   warps 9, 10   of the first CTA: one thread each issues the pair's tcgen05.mma of the even and of the odd blocks
+//                 (a buffer of tensor memory each; one warp's loop took 850 cycles a block for 512 of products)
+//   warp 11       waits for the CTA's own copies and arrives at the first one's `ready` (each CTA so waits for its own copies
+//                 alone, and can at its end; the issuing warps have one barrier to look at for both)
+// ------------------------------------------------------------------------------------
+struct Pair {
+    static constexpr int TC = 256, CW = TC / 2;
+    static constexpr int kThreads = 384;
+    static constexpr uint32_t kA = kLanes * 128, kB = CW / 2 * 128, kStage = kA + 2 * kB;
+    static constexpr int kStages = 5;
+    static constexpr uint32_t kOut = 32 * 128;                   // 32 rows x 64 columns of results, 128-byte swizzle
+    static constexpr uint32_t out = kStages * kStage;            // [warp][2]
+    static constexpr uint32_t misc = out + 16 * kOut, total = misc + 512;
+    static_assert(CW == kBlock && kB % 1024 == 0 && total <= 232448, "tile");
+};
+
+struct PairMisc {
+    uint64_t full[5], ready[5], empty[5], tfull[2][2], tempty[2][2], drain;   // (tensor memory: by buffer and half of the columns)
+    int abort_flag;
+    uint32_t tmem;
+};
+static_assert(sizeof(PairMisc) <= 512, "misc block");
+
+// A pair's tiles, from pair to pair: lane tiles in groups, so that the pairs at work share both matrices' rows in L2.
+struct PairWalk {
+    int g, in, lt, ct;      // group, tile in it; lane tile, column tile
+    __device__ __forceinline__ bool set(const MatArgs& a) {
+        for (;;) {
+            const int left = (int)a.lane_tiles - g * a.group, n = left < a.group ? left : a.group;
+            if (n <= 0) return false;
+            if (in < n * (int)a.col_tiles) {
+                ct = in / n;
+                lt = g * a.group + (in - ct * n);
+                return true;
+            }
+            in -= n * (int)a.col_tiles;
+            g++;
+        }
+    }
+    __device__ __forceinline__ bool start(const MatArgs& a) {
+        g = 0;
+        in = (int)(blockIdx.x >> 1);
+        return set(a);
+    }
+    __device__ __forceinline__ bool next(const MatArgs& a) {
+        in += (int)(gridDim.x >> 1);
+        return set(a);
+    }
+};
+
+// Address of the same place in the shared memory of a CTA of the cluster.
+__device__ __forceinline__ uint32_t at_rank(const void* p, uint32_t rank) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(p)), "r"(rank));
+    return r;
+}
+// Arrival at a barrier of either CTA. What the other side may rely on goes through tensor memory (with its fences) and
+// the copies' own barrier, not through this thread's loads and stores, so that the arrival need not wait for those:
+// with .release.cluster here and .acquire.cluster in the waits a block took 2400 cycles.
+__device__ __forceinline__ void arrive_at(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+// mbar_wait, whole in its place: where warps exchange registers a wait in the loops must not be a call.
+__device__ __forceinline__ bool pair_wait(uint64_t* bar, uint32_t parity, const volatile int* abort, uint64_t limit_ns) {
+    const bool poll = limit_ns < 1000000ull;   // the diagnostic setting of mbar_wait
+    if (!poll && mbar_try_wait(bar, parity)) return true;
+    const uint64_t t0 = globaltimer_ns();
+    for (uint32_t it = 0;; it++) {
+        if (poll ? mbar_test_wait(bar, parity) : mbar_try_wait(bar, parity)) return true;
+        if (poll || (it & 63u) == 63u) {
+            if (*abort || globaltimer_ns() - t0 > limit_ns) return false;
+        }
+    }
+}
+
+// Arrives at `bar` of both CTAs once the pair's products issued before are done.
+__device__ __forceinline__ void commit_pair(uint64_t* bar) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_u32(bar)),
+                 "h"((uint16_t)3)
+                 : "memory");
+}
+
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Pair::kThreads, 1)
+block8_pair_kernel(const __grid_constant__ MatArgs a, const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map,
+                   const __grid_constant__ CUtensorMap out_map) {
+    using T = Pair;
+    extern __shared__ __align__(1024) unsigned char smem[];
+    PairMisc* S = reinterpret_cast<PairMisc*>(smem + T::misc);
+    auto cluster = cooperative_groups::this_cluster();
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t rank = cluster.block_rank();
+    const int nb = (int)a.nb;
+    if (tid == 0) {
+        for (int s = 0; s < T::kStages; s++) {
+            mbar_init(&S->full[s], 1);
+            mbar_init(&S->ready[s], 2);
+            mbar_init(&S->empty[s], 1);
+        }
+        for (int s = 0; s < 4; s++) {
+            mbar_init(&S->tfull[s >> 1][s & 1], 1);
+            mbar_init(&S->tempty[s >> 1][s & 1], 8);
+        }
+        mbar_init(&S->drain, 2);
+        S->abort_flag = (smem_u32(smem) & 1023u) != 0;   // the swizzle needs the alignment asked for
+        fence_barrier_init();
+        prefetch_tmap(&x_map);
+        prefetch_tmap(&w_map);
+        if (a.vec) prefetch_tmap(&out_map);
+    }
+    if (warp == 9) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&S->tmem)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        tc_fence_before();
+    }
+    __syncthreads();
+    cluster.sync();
+    tc_fence_after();
+    const uint32_t tmem = S->tmem;
+    volatile int* abort_flag = &S->abort_flag;
+    bool dead = *abort_flag != 0;
+    PairWalk w;
+
+    // 168 registers a thread at launch: 256 x 208 + 128 x 88 of 384 x 168
+    if (warp < 8) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+        // ------------------------------------------------------------ accumulate
+        const int half = warp >> 2, col0 = half * T::CW, row0 = 32 * (warp & 3);
+        const uint32_t t0 = tmem + ((uint32_t)row0 << 16) + col0;
+        const uint32_t released[2] = {at_rank(&S->tempty[0][half], 0), at_rank(&S->tempty[1][half], 0)};
+        unsigned char* out_sm = smem + T::out + warp * 2 * T::kOut;
+        int buf = 0, ph = 0;
+        // scales of four blocks, fetched four blocks ahead, across tiles
+        const float *px, *pw;
+        float nx[4], nw[4], f[4];
+        auto fetch = [&](int kb) {
+            if (a.vec_scales) {   // (whole groups of four)
+                *reinterpret_cast<float4*>(nx) = __ldg(reinterpret_cast<const float4*>(px + kb));
+                *reinterpret_cast<float4*>(nw) = __ldg(reinterpret_cast<const float4*>(pw + kb));
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    const int k = kb + i < nb ? kb + i : nb - 1;
+                    nx[i] = __ldg(px + k);
+                    nw[i] = __ldg(pw + k);
+                }
+            }
+        };
+        auto scales_of_tile = [&]() {
+            const int64_t r = (int64_t)w.lt * (2 * kLanes) + rank * kLanes + row0 + lane, u = ((int64_t)w.ct * T::TC + col0) / kBlock, last = (a.N - 1) / kBlock;
+            px = a.xs + (r < a.M ? r : a.M - 1) * a.nb;
+            pw = a.ws + (u < last ? u : last) * a.nb;
+            fetch(0);
+        };
+        bool more = w.start(a);
+        if (more) scales_of_tile();
+        while (more && !dead) {
+            const int r0 = w.lt * (2 * kLanes) + (int)rank * kLanes + row0, c = w.ct * T::TC + col0;    // the warp's first row and column
+            float2 acc[T::CW / 2];
+#pragma unroll
+            for (int k = 0; k < T::CW / 2; k++) acc[k] = make_float2(0.0f, 0.0f);
+            for (int kb = 0; kb < nb; kb++) {
+                const bool fresh = (kb & 3) == 0;
+#pragma unroll
+                for (int i = 0; i < 4; i++) f[i] = fresh ? nx[i] * nw[i] : f[i < 3 ? i + 1 : 3];
+                if (fresh) {
+                    if (kb + 4 < nb) fetch(kb + 4);
+                    else if ((more = w.next(a))) scales_of_tile();
+                }
+                if (!__all_sync(0xffffffffu, pair_wait(&S->tfull[buf][half], ph, abort_flag, a.wait_ns))) {
+                    dead = true;
+                    break;
+                }
+                tc_fence_after();
+                float v[2][16];
+                tmem_ld16(t0 + buf * T::TC, v[0]);
+#pragma unroll
+                for (int q = 0; q < T::CW / 16; q++) {
+                    tmem_wait_ld();
+                    settle16(v[q & 1]);
+                    if (16 * (q + 1) < T::CW) {
+                        tmem_ld16(t0 + buf * T::TC + 16 * (q + 1), v[(q + 1) & 1]);
+                    } else {   // all read
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) arrive_at(released[buf]);
+                    }
+                    const float2 ff = make_float2(f[0], f[0]);
+#pragma unroll
+                    for (int k = 0; k < 8; k++) acc[8 * q + k] = __ffma2_rn(make_float2(v[q & 1][2 * k], v[q & 1][2 * k + 1]), ff, acc[8 * q + k]);
+                }
+                buf ^= 1;
+                ph ^= buf == 0;
+            }
+            if (dead) break;
+            if (a.vec) {
+                if (lane == 0) bulk_wait_read<0>();   // the last tile's results have left
+                __syncwarp();
+#pragma unroll
+                for (int q = 0; q < T::CW / 8; q++) {
+                    const uint4 b = make_uint4(pack(acc[4 * q].x, acc[4 * q].y, a.fp16), pack(acc[4 * q + 1].x, acc[4 * q + 1].y, a.fp16),
+                                               pack(acc[4 * q + 2].x, acc[4 * q + 2].y, a.fp16), pack(acc[4 * q + 3].x, acc[4 * q + 3].y, a.fp16));
+                    *reinterpret_cast<uint4*>(out_sm + (q >> 3) * T::kOut + lane * 128 + (((q & 7) ^ (lane & 7)) << 4)) = b;
+                }
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0 && r0 < a.M) {
+#pragma unroll
+                    for (int h = 0; h < 2; h++)
+                        if (c + 64 * h < a.N) tma_store_2d(&out_map, out_sm + h * T::kOut, c + 64 * h, r0);
+                    bulk_commit();
+                }
+            } else {
+                uint16_t* out = r0 + lane < a.M ? static_cast<uint16_t*>(a.out) + (int64_t)(r0 + lane) * a.out_stride + c : nullptr;
+#pragma unroll
+                for (int q = 0; q < T::CW / 32; q++) {
+                    uint32_t b[16];
+#pragma unroll
+                    for (int k = 0; k < 16; k++) b[k] = pack(acc[16 * q + k].x, acc[16 * q + k].y, a.fp16);
+                    if (c + 32 * q < a.N) store_columns(b, out ? out + 32 * q : nullptr, a.N - (c + 32 * q), false);
+                }
+            }
+        }
+        if (lane == 0) bulk_wait<0>();   // results are out before the CTA ends
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        if (warp == 8) {
+            // -------------------------------------------------------- copies
+            int st = 0, ph = 1;
+            int64_t issued = 0;
+            for (bool more = w.start(a); more && !dead; more = w.next(a)) {
+                const int xr = w.lt * (2 * kLanes) + (int)rank * kLanes, wr = w.ct * T::TC + (int)rank * (T::CW / 2);
+                for (int kb = 0; kb < nb; kb++) {
+                    if (!__all_sync(0xffffffffu, pair_wait(&S->empty[st], ph, abort_flag, a.wait_ns))) {
+                        dead = true;
+                        break;
+                    }
+                    if (lane == 0) {
+                        unsigned char* dst = smem + st * T::kStage;
+                        mbar_arrive_expect_tx(&S->full[st], T::kStage);
+                        tma_load_2d(dst, &x_map, &S->full[st], kb * kBlock, xr);
+#pragma unroll
+                        for (int h = 0; h < 2; h++)   // half of each half's rows of w
+                            tma_load_2d(dst + T::kA + h * T::kB, &w_map, &S->full[st], kb * kBlock, wr + h * T::CW);
+                    }
+                    __syncwarp();
+                    issued++;
+                    if (++st == T::kStages) {
+                        st = 0;
+                        ph ^= 1;
+                    }
+                }
+            }
+            if (dead) *abort_flag = 1;
+            // copies in flight land before the CTA ends, also where the other warps gave up on them
+            const int zero = 0;
+            for (int64_t k = issued > T::kStages ? issued - T::kStages : 0; k < issued; k++)
+                pair_wait(&S->full[k % T::kStages], (k / T::kStages) & 1, &zero, tc::kWaitLimitNs);
+        } else if (warp < 11) {
+            // -------------------------------------------------------- products of every other block
+            if (rank == 0) {
+                constexpr uint32_t idesc = idesc_e4m3(2 * kLanes, T::CW);
+                const bool issue = elect_one();
+                const uint64_t desc = sdesc_sw128(smem_u32(smem));
+                const uint32_t a_lo = (uint32_t)desc, hi = (uint32_t)(desc >> 32);
+                const int buf = warp - 9;
+                int st = buf, ph = 0, tph = 1, kb = buf;
+                for (bool more = w.start(a); more && !dead; more = w.next(a)) {
+                    for (; kb < nb; kb += 2) {
+                        if (!__all_sync(0xffffffffu, pair_wait(&S->ready[st], ph, abort_flag, a.wait_ns))) {
+                            dead = true;
+                            break;
+                        }
+                        const uint32_t da = a_lo + ((st * T::kStage) >> 4);
+#pragma unroll
+                        for (int h = 0; h < 2; h++) {
+                            if (!__all_sync(0xffffffffu, pair_wait(&S->tempty[buf][h], tph, abort_flag, a.wait_ns))) {
+                                dead = true;
+                                break;
+                            }
+                            tc_fence_after();
+                            const uint32_t db = da + ((T::kA + h * T::kB) >> 4), d = tmem + buf * T::TC + h * T::CW;
+                            if (issue) {
+#pragma unroll
+                                for (int k = 0; k < kBlock / 32; k++) mma_e4m3<true>(d, da + 2 * k, db + 2 * k, hi, idesc, k ? 1u : 0u);
+                                commit_pair(&S->tfull[buf][h]);
+                                if (h == 1) commit_pair(&S->empty[st]);
+                            }
+                            __syncwarp();
+                        }
+                        if (dead) break;
+                        tph ^= 1;
+                        st += 2;
+                        if (st >= T::kStages) {
+                            st -= T::kStages;
+                            ph ^= 1;
+                        }
+                    }
+                    kb -= nb;   // the warp's first block of the next tile
+                }
+                if (dead) *abort_flag = 1;
+                if (issue) commit_pair(&S->drain);   // products in flight end before tensor memory is given back
+                __syncwarp();
+            }
+            const int zero = 0;
+            pair_wait(&S->drain, 0, &zero, tc::kWaitLimitNs);
+        } else {
+            // -------------------------------------------------------- word of the CTA's stages
+            int st = 0, ph = 0;
+            for (bool more = w.start(a); more && !dead; more = w.next(a))
+                for (int kb = 0; kb < nb; kb++) {
+                    if (!__all_sync(0xffffffffu, pair_wait(&S->full[st], ph, abort_flag, a.wait_ns))) {
+                        dead = true;
+                        break;
+                    }
+                    if (lane == 0) arrive_at(at_rank(&S->ready[st], 0));
+                    __syncwarp();
+                    if (++st == T::kStages) {
+                        st = 0;
+                        ph ^= 1;
+                    }
+                }
+            if (dead) *abort_flag = 1;
+        }
+    }
+    __syncwarp();
+    if (dead) {
+        *abort_flag = 1;
+        if (lane == 0) raise_flag(a.status, CG_FLAG_PIPE_TIMEOUT);
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster.sync();   // no CTA ends, and no tensor memory goes, while the other one's products or arrivals may need it
+    if (warp == 9) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+    }
+}
+
 // Codes [rows][K] in boxes of box_rows x 128 bytes, 128-byte swizzle; what lies outside reads as 0.
 bool codes_map(CUtensorMap* map, const void* base, int64_t rows, int64_t K, int64_t stride, uint32_t box_rows) {
     auto fn = tmap_encode_fn();
@@ -544,6 +914,17 @@ bool codes_map(CUtensorMap* map, const void* base, int64_t rows, int64_t K, int6
     cuuint32_t box[2] = {128, box_rows}, estr[2] = {1, 1};
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Results [M][N] in boxes of 32 rows x 64 columns, 128-byte swizzle.
+bool results_map(CUtensorMap* map, const MatArgs& a) {
+    auto fn = tmap_encode_fn();
+    if (!fn) return false;
+    cuuint64_t dims[2] = {(cuuint64_t)a.N, (cuuint64_t)a.M}, strides[1] = {(cuuint64_t)(a.M > 1 ? a.out_stride : (a.N + 7) / 8 * 8) * 2};
+    cuuint32_t box[2] = {64, 32}, estr[2] = {1, 1};
+    return fn(map, a.fp16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, a.out, dims, strides, box, estr,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 struct Matrices {
@@ -581,6 +962,51 @@ cudaError_t launch_tile(MatArgs a, const Matrices& m, int split, cudaStream_t st
     return cudaLaunchKernelEx(&cfg, kernel, a, lanes, cols);
 }
 
+// Clusters of two CTAs of a kernel that run at the same time, asked once per device.
+cudaError_t max_pairs(const void* kernel, int threads, size_t smem, int* pairs) {
+    static std::atomic<int> known[64];
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    *pairs = dev < 64 ? known[dev].load(std::memory_order_relaxed) : 0;
+    if (*pairs) return cudaSuccess;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(tc::num_sms() / 2 * 2));
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cudaLaunchAttribute at{};
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = 2;
+    at.val.clusterDim.y = at.val.clusterDim.z = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    if ((e = cudaOccupancyMaxActiveClusters(pairs, kernel, &cfg)) != cudaSuccess) return e;
+    if (*pairs < 1) return cudaErrorInvalidConfiguration;
+    if (dev < 64) known[dev].store(*pairs, std::memory_order_relaxed);
+    return cudaSuccess;
+}
+
+cudaError_t launch_pairs(MatArgs a, const Matrices& m, cudaStream_t st) {
+    using T = Pair;
+    CUtensorMap xs, ws, out{};
+    a.vec = a.vec && a.out_stride < (int64_t)1 << 39;   // (what a tensor map can hold)
+    if (!codes_map(&xs, m.x, a.M, m.K, m.x_stride, kLanes) || !codes_map(&ws, m.w, a.N, m.K, m.w_stride, T::CW / 2) ||
+        (a.vec && !results_map(&out, a)))
+        return cudaErrorInvalidValue;
+    a.lane_tiles = (a.M + 2 * kLanes - 1) / (2 * kLanes);
+    a.col_tiles = (a.N + T::TC - 1) / T::TC;
+    a.split = 1;
+    a.group = 8;
+    static SmemOptIn opt_in;
+    cudaError_t e = opt_in.set(reinterpret_cast<const void*>(block8_pair_kernel), (int)T::total);
+    if (e != cudaSuccess) return e;
+    int pairs = 0;   // that the GPU has room for at once: one that came later would take its share when the others are done
+    if ((e = max_pairs(reinterpret_cast<const void*>(block8_pair_kernel), T::kThreads, T::total, &pairs)) != cudaSuccess) return e;
+    const int64_t tiles = a.lane_tiles * a.col_tiles;
+    block8_pair_kernel<<<(unsigned)(2 * (tiles < pairs ? tiles : pairs)), T::kThreads, T::total, st>>>(a, xs, ws, out);
+    return cudaGetLastError();
+}
+
 // CTAs of a cluster: as many as the GPU has room for at once, a block of channels each at least.
 int split_of(int64_t tiles, int64_t nb, int ctas) {
     int s = 1;
@@ -594,7 +1020,7 @@ cudaError_t launch_matmul(const MatArgs& a, const Matrices& m, cudaStream_t st) 
     if (a.M <= 32) return launch_tile<32, false>(a, m, split_of(n128, a.nb, Tile<32, false>::kCtas), st);
     if (a.M <= 64) return launch_tile<64, false>(a, m, split_of(n128, a.nb, Tile<64, false>::kCtas), st);
     const int64_t t256 = m128 * ((a.N + 255) / 256);
-    if (t256 >= tc::num_sms()) return launch_tile<256, true>(a, m, 1, st);
+    if (t256 >= tc::num_sms()) return launch_pairs(a, m, st);
     return launch_tile<128, true>(a, m, split_of(m128 * n128, a.nb, Tile<128, true>::kCtas), st);
 }
 
@@ -696,6 +1122,7 @@ CG_EXPORT int cg_block8_matmul(int32_t dtype, int64_t M, int64_t N, int64_t K, c
     a.wait_ns = wait_limit_ns();
     a.fp16 = dtype == CG_FP16;
     a.vec = al16(out) && (M < 2 || out_stride % 8 == 0);
+    a.vec_scales = a.nb % 4 == 0 && al16(x_scales) && al16(w_scales);
     const cudaError_t e = launch_matmul(a, Matrices{x, w, K, x_stride, w_stride}, static_cast<cudaStream_t>(stream));
     if (e != cudaSuccess) return set_error(CG_ECUDA, "block product launch: %s", cudaGetErrorString(e));
     return CG_OK;
