@@ -741,22 +741,24 @@ block8_pair_kernel(const __grid_constant__ MatArgs a, const __grid_constant__ CU
                     break;
                 }
                 tc_fence_after();
-                float v[2][16];
+                float v[3][16];   // read in pairs, of which the next one's first half is asked for ahead
                 tmem_ld16(t0 + buf * T::TC, v[0]);
+                tmem_ld16(t0 + buf * T::TC + 16, v[1]);
 #pragma unroll
                 for (int q = 0; q < T::CW / 16; q++) {
-                    tmem_wait_ld();
-                    settle16(v[q & 1]);
-                    if (16 * (q + 1) < T::CW) {
-                        tmem_ld16(t0 + buf * T::TC + 16 * (q + 1), v[(q + 1) & 1]);
-                    } else {   // all read
+                    if ((q & 1) == 0) tmem_wait_ld();
+                    settle16(v[q % 3]);
+                    if ((q & 1) == 0) settle16(v[(q + 1) % 3]);
+                    if (16 * (q + 2) < T::CW) {
+                        tmem_ld16(t0 + buf * T::TC + 16 * (q + 2), v[(q + 2) % 3]);
+                    } else if (q + 1 == T::CW / 16) {   // all read
                         tc_fence_before();
                         __syncwarp();
                         if (lane == 0) arrive_at(released[buf]);
                     }
                     const float2 ff = make_float2(f[0], f[0]);
 #pragma unroll
-                    for (int k = 0; k < 8; k++) acc[8 * q + k] = __ffma2_rn(make_float2(v[q & 1][2 * k], v[q & 1][2 * k + 1]), ff, acc[8 * q + k]);
+                    for (int k = 0; k < 8; k++) acc[8 * q + k] = __ffma2_rn(make_float2(v[q % 3][2 * k], v[q % 3][2 * k + 1]), ff, acc[8 * q + k]);
                 }
                 buf ^= 1;
                 ph ^= buf == 0;
@@ -906,6 +908,160 @@ block8_pair_kernel(const __grid_constant__ MatArgs a, const __grid_constant__ CU
     }
 }
 
+// ------------------------------------------------------------------------------------
+// Product of at most 8 rows of x (single tokens): HBM bounds it, a byte of w for 2 M flops. A tile is 16 rows of w; each
+// of 8 warps takes an eighth of the blocks of 128 channels, 4 mma.sync m16n8k32 each (a tcgen05 tile would be 7/8
+// padding). A warp copies its own blocks of w and x (cp.async into a ring of its own, 4 blocks ahead and on into the
+// CTA's next tile) and loads its scales 8 blocks at a time, a lane one block's, a batch ahead: no load's latency stands
+// in the loop, it waits for nobody but at a tile's end, where the warps' sums are added in their order, and the call
+// needs no tensor maps, which the host would make. All CTAs read the same few lines of x and its scales at
+// about the same time, which one slice of L2 serves: they come through L1 (scales copied block by block past it took 2 us
+// more). The order of the channels within a block is free as long as both operands have the same: a thread reads 16 bytes
+// of either.
+// Where the rows of w leave SMs idle, the blocks are cut among the CTAs of a cluster, added in the order of the ranks.
+// ------------------------------------------------------------------------------------
+constexpr int kFewThreads = 256, kFewRows = 16, kFewMost = 8, kFewWarps = kFewThreads / 32;
+constexpr int kFewAhead = 4;                                        // blocks of a warp in flight
+constexpr uint32_t kFewW = kFewRows * kBlock;                       // bytes of a block of w; x follows
+constexpr uint32_t few_slot(int M) { return kFewW + M * kBlock; }
+constexpr uint32_t few_smem(int M) { return kFewWarps * kFewAhead * few_slot(M) + kFewWarps * kFewRows * kFewMost * 4; }
+static_assert(3 * (few_smem(1) + 1024) <= 233472 && 2 * (few_smem(kFewMost) + 1024) <= 233472, "three or two CTAs an SM");
+
+struct FewArgs {
+    const uint8_t *x, *w;
+    const float *xs, *ws;
+    uint16_t* out;
+    int64_t x_stride, w_stride, out_stride, K, N;
+    int M, nb, tiles, fp16, split;
+};
+
+__device__ __forceinline__ void mma_m16n8k32(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// 16 bytes, or zeros
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool have) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(have ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copy16_l1(uint32_t dst, const void* src, bool have) {   // by way of L1
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(have ? 16 : 0) : "memory");
+}
+
+__global__ void __launch_bounds__(kFewThreads, 3) block8_few_kernel(const __grid_constant__ FewArgs a) {
+    extern __shared__ __align__(1024) unsigned char smem[];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, j = lane & 3;
+    const int rank = (int)(blockIdx.x % (unsigned)a.split), first = (int)(blockIdx.x / (unsigned)a.split), step = (int)(gridDim.x / (unsigned)a.split);
+    const int64_t part = (int64_t)kFewWarps * a.split, mine = rank * kFewWarps + warp;
+    const int lo = (int)(a.nb * mine / part), hi = (int)(a.nb * (mine + 1) / part);   // the warp's blocks
+    const uint32_t slot_bytes = few_slot(a.M);
+    const unsigned char* ring = smem + warp * kFewAhead * slot_bytes;
+    float* sums = reinterpret_cast<float*>(smem + kFewWarps * kFewAhead * slot_bytes);   // [warp][row of x][row of w]
+
+    // Block (tile, kb) into a slot of the ring: 8 lanes a row, its 16-byte pieces 4 - 7 and 0 - 3 changed in odd rows
+    // (the fragments' reads of two rows then meet no bank twice); zeros past K, the last row again past N.
+    int ct = first, ck = lo, cs = 0;   // the next block to copy, and its slot
+    auto copy = [&]() {
+        if (ck >= hi) {
+            ct += step;
+            ck = lo;
+        }
+        if (ct < a.tiles && ck < hi) {
+            const int row0 = lane >> 3;
+            const int64_t k = (int64_t)ck * kBlock + (lane & 7) * 16, n0 = (int64_t)ct * kFewRows;
+            const bool have = k < a.K;
+            const uint32_t dst = smem_u32(ring) + cs * slot_bytes, at = ((lane & 7) ^ ((row0 & 1) << 2)) << 4;
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const int row = 4 * i + row0;
+                copy16(dst + row * kBlock + at, a.w + (n0 + row < a.N ? n0 + row : a.N - 1) * a.w_stride + (have ? k : 0), have);
+            }
+#pragma unroll
+            for (int i = 0; i < kFewMost / 4; i++) {
+                const int row = 4 * i + row0;
+                if (row < a.M) copy16_l1(dst + kFewW + row * kBlock + at, a.x + row * a.x_stride + (have ? k : 0), have);
+            }
+            ck++;
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        if (++cs == kFewAhead) cs = 0;
+    };
+#pragma unroll
+    for (int i = 0; i < kFewAhead; i++) copy();
+
+    // scales of 8 blocks: lane (g, j) those of block g, for rows 2j and 2j + 1 of x; and of the batch that follows
+    float sw = 0.0f, s0 = 0.0f, s1 = 0.0f, nw = 0.0f, n0 = 0.0f, n1 = 0.0f;
+    auto fetch = [&](int tile, int kb) {
+        kb += g;
+        if (tile >= a.tiles || kb >= hi) return;
+        nw = __ldg(a.ws + (int64_t)tile * kFewRows / kBlock * a.nb + kb);
+        if (2 * j < a.M) n0 = __ldg(a.xs + (int64_t)(2 * j) * a.nb + kb);
+        if (2 * j + 1 < a.M) n1 = __ldg(a.xs + (int64_t)(2 * j + 1) * a.nb + kb);
+    };
+    fetch(first, lo);
+    int slot = 0;
+    for (int tile = first; tile < a.tiles; tile += step) {
+        float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};   // rows g, g + 8 of w, 2j, 2j + 1 of x
+        for (int kb = lo; kb < hi; kb++) {
+            if (((kb - lo) & 7) == 0) {
+                sw = nw;
+                s0 = n0;
+                s1 = n1;
+                if (kb + 8 < hi) fetch(tile, kb + 8);
+                else fetch(tile + step, lo);
+            }
+            asm volatile("cp.async.wait_group %0;" ::"n"(kFewAhead - 1) : "memory");
+            __syncwarp();
+            const unsigned char* src = ring + slot * slot_bytes;
+            uint4 wv[2][2], xv[2];
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                const unsigned char* p = src + (((4 * h + j) ^ ((g & 1) << 2)) << 4);
+                wv[0][h] = *reinterpret_cast<const uint4*>(p + g * kBlock);
+                wv[1][h] = *reinterpret_cast<const uint4*>(p + (g + 8) * kBlock);
+                xv[h] = g < a.M ? *reinterpret_cast<const uint4*>(p + kFewW + g * kBlock) : make_uint4(0, 0, 0, 0);
+            }
+            const int from = ((kb - lo) & 7) * 4 + j;
+            const float fw = __shfl_sync(0xffffffffu, sw, from), f0 = __shfl_sync(0xffffffffu, s0, from) * fw, f1 = __shfl_sync(0xffffffffu, s1, from) * fw;
+            __syncwarp();
+            copy();           // into the slot just read
+            if (++slot == kFewAhead) slot = 0;
+            float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                mma_m16n8k32(d, wv[0][h].x, wv[1][h].x, wv[0][h].y, wv[1][h].y, xv[h].x, xv[h].y);
+                mma_m16n8k32(d, wv[0][h].z, wv[1][h].z, wv[0][h].w, wv[1][h].w, xv[h].z, xv[h].w);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; e++) acc[e] = fmaf(d[e], e & 1 ? f1 : f0, acc[e]);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; e++) sums[(warp * kFewMost + 2 * j + (e & 1)) * kFewRows + g + 8 * (e >> 1)] = acc[e];
+        __syncthreads();
+        const int m = tid / kFewRows, r = tid % kFewRows;   // a thread an output
+        float total = 0.0f;
+        if (m < a.M) {
+#pragma unroll
+            for (int k = 0; k < kFewWarps; k++) total += sums[(k * kFewMost + m) * kFewRows + r];
+        }
+        if (a.split > 1) {
+            auto cluster = cooperative_groups::this_cluster();
+            __syncthreads();
+            if (m < a.M) sums[tid] = total;
+            cluster.sync();
+            if (rank == 0 && m < a.M) {
+                total = 0.0f;
+                for (int k = 0; k < a.split; k++) total += cluster.map_shared_rank(sums, k)[tid];
+            }
+            cluster.sync();   // the sums are free again, and no CTA ends while they may be read
+        }
+        const int64_t n = (int64_t)tile * kFewRows + r;
+        if (rank == 0 && m < a.M && n < a.N) a.out[m * a.out_stride + n] = (uint16_t)pack(total, 0.0f, a.fp16);
+        if (tile + step < a.tiles) __syncthreads();   // the sums are free again
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+}
+
 // Codes [rows][K] in boxes of box_rows x 128 bytes, 128-byte swizzle; what lies outside reads as 0.
 bool codes_map(CUtensorMap* map, const void* base, int64_t rows, int64_t K, int64_t stride, uint32_t box_rows) {
     auto fn = tmap_encode_fn();
@@ -1007,6 +1163,42 @@ cudaError_t launch_pairs(MatArgs a, const Matrices& m, cudaStream_t st) {
     return cudaGetLastError();
 }
 
+cudaError_t launch_few(const MatArgs& a, const Matrices& m, cudaStream_t st) {
+    FewArgs f{};
+    f.x = static_cast<const uint8_t*>(m.x);
+    f.w = static_cast<const uint8_t*>(m.w);
+    f.xs = a.xs;
+    f.ws = a.ws;
+    f.out = static_cast<uint16_t*>(a.out);
+    f.x_stride = m.x_stride;
+    f.w_stride = m.w_stride;
+    f.out_stride = a.out_stride;
+    f.K = m.K;
+    f.N = a.N;
+    f.M = (int)a.M;
+    f.nb = (int)a.nb;
+    f.fp16 = a.fp16;
+    f.tiles = (int)((a.N + kFewRows - 1) / kFewRows);
+    const int smem = (int)few_smem(f.M), room = (233472 / (smem + 1024) < 3 ? 2 : 3) * tc::num_sms();
+    f.split = 1;
+    while (f.split < 8 && (int64_t)f.tiles * 2 * f.split <= room && 2 * f.split * kFewWarps <= f.nb) f.split *= 2;
+    static SmemOptIn opt_in;
+    cudaError_t e = opt_in.set(reinterpret_cast<const void*>(block8_few_kernel), (int)few_smem(kFewMost));
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(f.split > 1 ? f.tiles * f.split : f.tiles < room ? f.tiles : room));
+    cfg.blockDim = dim3(kFewThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute at{};
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = (unsigned)f.split;
+    at.val.clusterDim.y = at.val.clusterDim.z = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = f.split > 1 ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, block8_few_kernel, f);
+}
+
 // CTAs of a cluster: as many as the GPU has room for at once, a block of channels each at least.
 int split_of(int64_t tiles, int64_t nb, int ctas) {
     int s = 1;
@@ -1016,6 +1208,7 @@ int split_of(int64_t tiles, int64_t nb, int ctas) {
 
 cudaError_t launch_matmul(const MatArgs& a, const Matrices& m, cudaStream_t st) {
     const int64_t n128 = (a.N + 127) / 128, m128 = (a.M + 127) / 128;
+    if (a.M <= kFewMost) return launch_few(a, m, st);
     if (a.M <= 16) return launch_tile<16, false>(a, m, split_of(n128, a.nb, Tile<16, false>::kCtas), st);
     if (a.M <= 32) return launch_tile<32, false>(a, m, split_of(n128, a.nb, Tile<32, false>::kCtas), st);
     if (a.M <= 64) return launch_tile<64, false>(a, m, split_of(n128, a.nb, Tile<64, false>::kCtas), st);
