@@ -34,6 +34,7 @@ struct EncArgs {
     float* scales;
     int32_t* status;
     int64_t R, K, x_stride, stride, nb;   // nb blocks a row
+    int64_t step_row, step_b;             // of all CTAs' blocks of one turn
 };
 
 template <bool FP16>
@@ -72,15 +73,14 @@ struct Scale {
         plain = !(s >= 0x1p-80f && s <= 0x1p100f);
         r = plain ? 0.0f : __frcp_rn(s);
     }
-    __device__ __forceinline__ float quotient(float x) const {
-        const float q = x * r;
-        return fmaf(fmaf(-q, s, x), r, q);
+    __device__ __forceinline__ float2 quotients(float2 x) const {
+        const float2 rr = make_float2(r, r), q = __fmul2_rn(x, rr);
+        return __ffma2_rn(__ffma2_rn(q, make_float2(-s, -s), x), rr, q);
     }
-    // of |x|; the signs are put in behind (the residual of -0 would lose its sign)
+    // the signs are put in behind: that of -0 is lost in the residual
     __device__ __forceinline__ uint32_t four(uint32_t w0, uint32_t w1) const {
-        const float2 x = floats<FP16>(w0 & 0x7fff7fffu), y = floats<FP16>(w1 & 0x7fff7fffu);
-        const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(quotient(x.x), quotient(x.y)), __NV_SATFINITE, __NV_E4M3);
-        const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(quotient(y.x), quotient(y.y)), __NV_SATFINITE, __NV_E4M3);
+        const uint32_t lo = __nv_cvt_float2_to_fp8x2(quotients(floats<FP16>(w0)), __NV_SATFINITE, __NV_E4M3);
+        const uint32_t hi = __nv_cvt_float2_to_fp8x2(quotients(floats<FP16>(w1)), __NV_SATFINITE, __NV_E4M3);
         return (lo | hi << 16) | (__byte_perm(w0, w1, 0x7531) & 0x80808080u);
     }
     static __device__ __noinline__ uint32_t four_divided(uint32_t w0, uint32_t w1, float s) {
@@ -103,24 +103,41 @@ struct Scale {
     }
 };
 
-// rows = 1: a group of 8 lanes a block.
-template <bool FP16>
+// rows = 1: a group of 8 lanes a block, U blocks at a time. A group walks from block to block in steps of (step_row, step_b).
+template <bool FP16, int U>
 __global__ void __launch_bounds__(kEncThreads) encode_rows_kernel(EncArgs a) {
     const int lane8 = threadIdx.x % kGroup;
-    const int64_t items = a.R * a.nb, step = (int64_t)gridDim.x * kEncRows;
+    const int64_t first = (int64_t)blockIdx.x * kEncRows + threadIdx.x / kGroup;
+    int64_t row = first / a.nb, b = first - row * a.nb;
     int32_t flag = 0;
-    for (int64_t it = (int64_t)blockIdx.x * kEncRows + threadIdx.x / kGroup; it - threadIdx.x / kGroup < items; it += step) {
-        const bool have = it < items;
-        const int64_t row = have ? it / a.nb : 0, b = have ? it - row * a.nb : 0, ch = b * kBlock + lane8 * 16;
-        Piece p;
-        p.load(a.x + row * a.x_stride + ch, have && ch < a.K);
-        uint32_t top = p.top();
+    while (__any_sync(0xffffffffu, row < a.R)) {
+        Piece p[U];
+        int64_t at_row[U], at_b[U];
 #pragma unroll
-        for (int off = 1; off < kGroup; off *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, off));
-        const Scale<FP16> s(top);
-        if (s.nonfinite) flag = CG_FLAG_NONFINITE_INPUT;
-        if (have && ch < a.K) *reinterpret_cast<uint4*>(a.codes + row * a.stride + ch) = s.codes(p);
-        if (have && lane8 == 0) a.scales[it] = s.s;
+        for (int u = 0; u < U; u++) {
+            at_row[u] = row;
+            at_b[u] = b;
+            const int64_t ch = b * kBlock + lane8 * 16;
+            p[u].load(a.x + row * a.x_stride + ch, row < a.R && ch < a.K);
+            row += a.step_row;
+            b += a.step_b;
+            if (b >= a.nb) {
+                b -= a.nb;
+                row++;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            uint32_t top = p[u].top();
+#pragma unroll
+            for (int off = 1; off < kGroup; off *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, off));
+            const Scale<FP16> s(top);
+            if (s.nonfinite) flag = CG_FLAG_NONFINITE_INPUT;
+            if (at_row[u] >= a.R) continue;
+            const int64_t ch = at_b[u] * kBlock + lane8 * 16;
+            if (ch < a.K) *reinterpret_cast<uint4*>(a.codes + at_row[u] * a.stride + ch) = s.codes(p[u]);
+            if (lane8 == 0) a.scales[at_row[u] * a.nb + at_b[u]] = s.s;
+        }
     }
     raise_flag(a.status, flag);
 }
@@ -163,36 +180,31 @@ __global__ void __launch_bounds__(kEncThreads) encode_square_kernel(EncArgs a) {
 }
 
 // ------------------------------------------------------------------------------------
-// Product. A tile is 128 rows of one matrix (the lanes of tensor memory) by TC rows of the other (its columns). Block
-// by block of 128 channels the tensor cores (tcgen05.mma, kind f8f6f4, four instructions of 32 channels) sum the
-// products into one of two buffers of tensor memory; the accumulating warps read it, multiply by the block's two
-// scales and add to sums in registers, while the other buffer fills.
-//   warps 0 .. E-1  accumulate: warp w has lanes 32 (w % 4) .. + 31 and columns (w / 4) CW .. + CW - 1
-//   warp E          TMA: both matrices' 128-byte pieces of rows into a ring of stages (128-byte swizzle)
-//   warp E + 1      one thread issues tcgen05.mma
-// TOKENS: lanes are rows of x, so that a thread has one x scale a block and its warp one or two w scales. Otherwise
-// (few rows of x) lanes are rows of w, which fill the 128 lanes where x could not, and columns rows of x, whose
-// scales the lanes hold for one another.
+// Product. A tile is 128 rows of x (the lanes of tensor memory) by 128 rows of w (its columns). Block by block of 128
+// channels the tensor cores (tcgen05.mma, kind f8f6f4, four instructions of 32 channels) sum the products into one of
+// four buffers of tensor memory; the accumulating warps read it, multiply by the block's two scales and add to sums in
+// registers, while the other buffers fill.
+//   warps 0 - 7   accumulate: warp w has lanes 32 (w % 4) .. + 31 and columns 64 (w / 4) .. + 63; lanes past the last row
+//                 of x are left out
+//   warp 8        TMA: both matrices' 128-byte pieces of rows into a ring of stages (128-byte swizzle)
+//   warps 9, 10   one thread each issues tcgen05.mma, of the even and of the odd blocks (one warp's loop takes 650 cycles
+//                 a block, its products 256)
+// Few rows of x: a stage holds them in whole groups of 8, and more stages fit; the lanes that they do not fill multiply
+// what lies behind, and nobody reads them.
 // Few tiles: the blocks of channels are cut among the CTAs of a cluster; each leaves its sums in shared memory,
 // and each adds up a part of the rows, in the order of the ranks whatever their timing.
 // ------------------------------------------------------------------------------------
 constexpr int kLanes = 128;
 
-template <int TC, bool TOKENS>
 struct Tile {
-    static constexpr int kWarps = TC >= 128 ? 8 : 4;            // accumulating
-    static constexpr int CW = TC / (kWarps / 4);                // columns of a warp
-    static constexpr int kThreads = (kWarps + 2) * 32;
-    static constexpr uint32_t kA = kLanes * 128, kStage = kA + TC * 128;
-    static constexpr int kStages = TC >= 192 ? 4 : TC == 128 ? 6 : 4;
+    static constexpr int TC = 128, CW = 64;                     // columns, and those of a warp
+    static constexpr int kWarps = 8, kThreads = (kWarps + 3) * 32;
+    static constexpr uint32_t kB = TC * 128, ring = 196608;
+    static constexpr int kMost = 10;                            // stages
+    static constexpr int kBufs = 4;                             // of tensor memory
     static constexpr int kPitch = TC + 4;                       // floats of a row of sums, without bank conflicts in 16-byte pieces
-    static constexpr uint32_t kSums = kLanes * kPitch * 4;
-    static constexpr uint32_t misc = kStages * kStage > kSums ? kStages * kStage : kSums;
-    static constexpr uint32_t total = misc + 256;
-    static constexpr int kBuf = TC > 128 ? 256 : TC;            // columns from buffer to buffer
-    static constexpr int kCols = 2 * kBuf < 32 ? 32 : 2 * kBuf;
-    static constexpr int kCtas = total <= 76000 ? 3 : total <= 114000 ? 2 : 1;   // of an SM
-    static_assert(CW % 16 == 0 && kStage % 1024 == 0 && total <= 232448, "tile");
+    static constexpr uint32_t misc = ring, total = misc + 512;
+    static_assert(kLanes * kPitch * 4 <= ring && kMost * (kB + 1024) <= ring && total <= 232448, "tile");
 };
 
 struct MatArgs {
@@ -206,14 +218,15 @@ struct MatArgs {
     int vec_scales;      // 16-byte loads of scales are possible
     int split;           // CTAs of a cluster
     int group;           // lane tiles that are walked together
+    int box_rows;        // of x in a stage
 };
 
 struct MatMisc {
-    uint64_t full[8], empty[8], tfull[2], tempty[2], drain;
+    uint64_t full[Tile::kMost], empty[Tile::kMost], tfull[Tile::kBufs], tempty[Tile::kBufs], drain;
     int abort_flag;
     uint32_t tmem;
 };
-static_assert(sizeof(MatMisc) <= 256, "misc block");
+static_assert(sizeof(MatMisc) <= 512, "misc block");
 
 // One step of 32 channels. Descriptors as halves (a step only adds to the low ones) that the whole warp computes, so that
 // they stay in uniform registers, and an elected thread: behind a branch on the lane number a block's issue took 500
@@ -309,33 +322,34 @@ __device__ __forceinline__ void store_columns(uint32_t (&b)[16], uint16_t* row, 
     }
 }
 
-template <int TC, bool TOKENS>
-__global__ void __launch_bounds__(Tile<TC, TOKENS>::kThreads, Tile<TC, TOKENS>::kCtas)
-block8_matmul_kernel(const __grid_constant__ MatArgs a, const __grid_constant__ CUtensorMap lane_map, const __grid_constant__ CUtensorMap col_map) {
-    using T = Tile<TC, TOKENS>;
+__global__ void __launch_bounds__(Tile::kThreads, 1)
+block8_tile_kernel(const __grid_constant__ MatArgs a, const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map) {
+    using T = Tile;
     extern __shared__ __align__(1024) unsigned char smem[];
     MatMisc* S = reinterpret_cast<MatMisc*>(smem + T::misc);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int rank = blockIdx.x % a.split;
-    const int64_t first = blockIdx.x / a.split, step = gridDim.x / a.split, tiles = a.lane_tiles * a.col_tiles;
-    const int64_t kb0 = a.nb * rank / a.split, kb1 = a.nb * (rank + 1) / a.split;
+    const int rank = (int)(blockIdx.x % (unsigned)a.split);
+    const int64_t first = blockIdx.x / (unsigned)a.split, step = gridDim.x / (unsigned)a.split, tiles = a.lane_tiles * a.col_tiles;
+    const int kb0 = (int)(a.nb * rank / a.split), kb1 = (int)(a.nb * (rank + 1) / a.split);
+    const uint32_t stage = a.box_rows * 128 + T::kB;
+    const int stages = min(T::kMost, (int)(T::ring / stage));
     if (tid == 0) {
-        for (int s = 0; s < T::kStages; s++) {
+        for (int s = 0; s < stages; s++) {
             mbar_init(&S->full[s], 1);
             mbar_init(&S->empty[s], 1);
         }
-        for (int s = 0; s < 2; s++) {
+        for (int s = 0; s < T::kBufs; s++) {
             mbar_init(&S->tfull[s], 1);
             mbar_init(&S->tempty[s], T::kWarps);
         }
-        mbar_init(&S->drain, 1);
+        mbar_init(&S->drain, 2);
         S->abort_flag = (smem_u32(smem) & 1023u) != 0;   // the swizzle needs the alignment asked for
         fence_barrier_init();
-        prefetch_tmap(&lane_map);
-        prefetch_tmap(&col_map);
+        prefetch_tmap(&x_map);
+        prefetch_tmap(&w_map);
     }
     if (warp == T::kWarps + 1) {
-        tmem_alloc(&S->tmem, T::kCols);
+        tmem_alloc(&S->tmem, T::kBufs * T::TC);
         tmem_relinquish();
         tc_fence_before();
     }
@@ -354,94 +368,79 @@ block8_matmul_kernel(const __grid_constant__ MatArgs a, const __grid_constant__ 
 
     if (warp < T::kWarps) {
         // ------------------------------------------------------------ accumulate
-        const int col0 = (warp >> 2) * T::CW, row = 32 * (warp & 3) + lane;
-        const uint32_t t0 = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + col0;
+        const int col0 = (warp >> 2) * T::CW, row0 = 32 * (warp & 3), row = row0 + lane;
+        const uint32_t t0 = tmem + ((uint32_t)row0 << 16) + col0;
         int buf = 0, ph = 0;
         for (int64_t tile = first; tile < tiles && !dead; tile += step) {
             int64_t lt, ct;
             place(tile, &lt, &ct);
-            const int64_t r = lt * kLanes + row, c = ct * TC + col0;    // the thread's row, and first column
-            float acc[T::CW];
+            const int64_t r = lt * kLanes + row, c = ct * T::TC + col0;    // the thread's row, and first column
+            const bool idle = lt * kLanes + row0 >= a.M;                   // no row of the warp's is one of x
+            float2 acc[T::CW / 2];
 #pragma unroll
-            for (int k = 0; k < T::CW; k++) acc[k] = 0.0f;
-            // the scales of a block ahead: `mine` of the thread's row (TOKENS) or of columns lane + 32 i; `uni` of the
-            // warp's first and last columns, or of its row of w
-            constexpr int kMine = TOKENS ? 1 : (T::CW + 31) / 32;
-            const float *pm[kMine], *pu[2];
-            if (TOKENS) {
-                pm[0] = a.xs + (r < a.M ? r : a.M - 1) * a.nb;
-                const int64_t last = (a.N - 1) / kBlock, u0 = c / kBlock, u1 = (c + T::CW - 1) / kBlock;
-                pu[0] = a.ws + (u0 < last ? u0 : last) * a.nb;
-                pu[1] = a.ws + (u1 < last ? u1 : last) * a.nb;
-            } else {
+            for (int k = 0; k < T::CW / 2; k++) acc[k] = make_float2(0.0f, 0.0f);
+            // scales of four blocks, fetched four blocks ahead
+            const float *px = a.xs + (r < a.M ? r : a.M - 1) * a.nb, *pw = a.ws + ct * a.nb;   // (128 columns: one block of w)
+            float nx[4], nw[4], f[4];
+            auto fetch = [&](int kb) {
 #pragma unroll
-                for (int i = 0; i < kMine; i++) {
-                    const int64_t m = c + lane + 32 * i;
-                    pm[i] = a.xs + (m < a.M ? m : a.M - 1) * a.nb;
+                for (int i = 0; i < 4; i++) {
+                    const int k = kb + i < kb1 ? kb + i : kb1 - 1;
+                    nx[i] = __ldg(px + k);
+                    nw[i] = __ldg(pw + k);
                 }
-                pu[0] = pu[1] = a.ws + lt * a.nb;
-            }
-            float mine[kMine], uni[2];
-            auto fetch = [&](int64_t kb) {
-                if (kb >= kb1) return;
-#pragma unroll
-                for (int i = 0; i < kMine; i++) mine[i] = __ldg(pm[i] + kb);
-                uni[0] = __ldg(pu[0] + kb);
-                uni[1] = __ldg(pu[1] + kb);
             };
-            fetch(kb0);
-            for (int64_t kb = kb0; kb < kb1; kb++) {
-                float f[kMine], f1;
+            if (!idle && kb0 < kb1) fetch(kb0);
+            for (int kb = kb0; kb < kb1; kb++) {
+                const bool fresh = ((kb - kb0) & 3) == 0;
 #pragma unroll
-                for (int i = 0; i < kMine; i++) f[i] = mine[i] * uni[0];
-                f1 = mine[0] * uni[1];
-                fetch(kb + 1);
+                for (int i = 0; i < 4; i++) f[i] = fresh ? nx[i] * nw[i] : f[i < 3 ? i + 1 : 3];
+                if (fresh && !idle && kb + 4 < kb1) fetch(kb + 4);
                 if (!__all_sync(0xffffffffu, mbar_wait(&S->tfull[buf], ph, abort_flag, a.wait_ns))) {
                     dead = true;
                     break;
                 }
                 tc_fence_after();
+                if (!idle) {
+                    float v[3][16];   // read in pairs, of which the next one's first half is asked for ahead
+                    tmem_ld16(t0 + buf * T::TC, v[0]);
+                    tmem_ld16(t0 + buf * T::TC + 16, v[1]);
 #pragma unroll
-                for (int q = 0; q < T::CW / 16; q++) {
-                    float v[16];
-                    tmem_ld16(t0 + buf * T::kBuf + 16 * q, v);
-                    tmem_wait_ld();
-                    settle16(v);
-                    if (16 * (q + 1) == T::CW) {   // all read
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(&S->tempty[buf]);
+                    for (int q = 0; q < T::CW / 16; q++) {
+                        if ((q & 1) == 0) tmem_wait_ld();
+                        settle16(v[q % 3]);
+                        if ((q & 1) == 0) settle16(v[(q + 1) % 3]);
+                        if (16 * (q + 2) < T::CW) tmem_ld16(t0 + buf * T::TC + 16 * (q + 2), v[(q + 2) % 3]);
+                        const float2 ff = make_float2(f[0], f[0]);
+#pragma unroll
+                        for (int k = 0; k < 8; k++) acc[8 * q + k] = __ffma2_rn(make_float2(v[q % 3][2 * k], v[q % 3][2 * k + 1]), ff, acc[8 * q + k]);
                     }
-                    // columns of another block of w than the first
-                    const float fq = !TOKENS ? 0.0f : T::CW % kBlock == 0 || (c + 16 * q) / kBlock == c / kBlock ? f[0] : f1;
-#pragma unroll
-                    for (int k = 0; k < 16; k++)
-                        acc[16 * q + k] = fmaf(v[k], TOKENS ? fq : __shfl_sync(0xffffffffu, f[(16 * q + k) / 32 % kMine], (16 * q + k) & 31), acc[16 * q + k]);
                 }
-                buf ^= 1;
-                ph ^= buf == 0;
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&S->tempty[buf]);
+                if (++buf == T::kBufs) {
+                    buf = 0;
+                    ph ^= 1;
+                }
             }
             if (dead) break;
             if (a.split > 1) {
                 float* sums = reinterpret_cast<float*>(smem) + row * T::kPitch + col0;
+                if (!idle) {
 #pragma unroll
-                for (int k = 0; k < T::CW; k += 4) *reinterpret_cast<float4*>(sums + k) = make_float4(acc[k], acc[k + 1], acc[k + 2], acc[k + 3]);
+                    for (int k = 0; k < T::CW; k += 4)
+                        *reinterpret_cast<float4*>(sums + k) = make_float4(acc[k / 2].x, acc[k / 2].y, acc[k / 2 + 1].x, acc[k / 2 + 1].y);
+                }
                 break;
             }
-            if (TOKENS) {
-                uint16_t* out = r < a.M ? static_cast<uint16_t*>(a.out) + r * a.out_stride + c : nullptr;
+            uint16_t* out = r < a.M ? static_cast<uint16_t*>(a.out) + r * a.out_stride + c : nullptr;
 #pragma unroll
-                for (int q = 0; q < T::CW / 32; q++) {
-                    uint32_t b[16];
+            for (int q = 0; q < T::CW / 32; q++) {
+                uint32_t b[16];
 #pragma unroll
-                    for (int k = 0; k < 16; k++) b[k] = pack(acc[32 * q + 2 * k], acc[32 * q + 2 * k + 1], a.fp16);
-                    if (c + 32 * q < a.N) store_columns(b, out ? out + 32 * q : nullptr, a.N - (c + 32 * q), a.vec);
-                }
-            } else if (r < a.N) {
-                uint16_t* out = static_cast<uint16_t*>(a.out) + r;
-#pragma unroll
-                for (int k = 0; k < T::CW; k++)
-                    if (c + k < a.M) out[(c + k) * a.out_stride] = (uint16_t)pack(acc[k], 0.0f, a.fp16);
+                for (int k = 0; k < 16; k++) b[k] = pack(acc[16 * q + k].x, acc[16 * q + k].y, a.fp16);
+                if (c + 32 * q < a.N) store_columns(b, out ? out + 32 * q : nullptr, a.N - (c + 32 * q), a.vec);
             }
         }
     } else if (warp == T::kWarps) {
@@ -451,19 +450,19 @@ block8_matmul_kernel(const __grid_constant__ MatArgs a, const __grid_constant__ 
         for (int64_t tile = first; tile < tiles && !dead; tile += step) {
             int64_t lt, ct;
             place(tile, &lt, &ct);
-            for (int64_t kb = kb0; kb < kb1; kb++) {
+            for (int kb = kb0; kb < kb1; kb++) {
                 if (!__all_sync(0xffffffffu, mbar_wait(&S->empty[st], ph, abort_flag, a.wait_ns))) {
                     dead = true;
                     break;
                 }
                 if (lane == 0) {
-                    mbar_arrive_expect_tx(&S->full[st], T::kStage);
-                    tma_load_2d(smem + st * T::kStage, &lane_map, &S->full[st], (int)(kb * kBlock), (int)(lt * kLanes));
-                    tma_load_2d(smem + st * T::kStage + T::kA, &col_map, &S->full[st], (int)(kb * kBlock), (int)(ct * TC));
+                    mbar_arrive_expect_tx(&S->full[st], stage);
+                    tma_load_2d(smem + st * stage + a.box_rows * 128, &w_map, &S->full[st], kb * kBlock, (int)(ct * T::TC));
+                    tma_load_2d(smem + st * stage, &x_map, &S->full[st], kb * kBlock, (int)(lt * kLanes));
                 }
                 __syncwarp();
                 issued++;
-                if (++st == T::kStages) {
+                if (++st == stages) {
                     st = 0;
                     ph ^= 1;
                 }
@@ -472,38 +471,44 @@ block8_matmul_kernel(const __grid_constant__ MatArgs a, const __grid_constant__ 
         if (dead) *abort_flag = 1;
         // copies in flight land before the CTA ends, also where the other warps gave up on them
         const int zero = 0;
-        for (int64_t k = issued > T::kStages ? issued - T::kStages : 0; k < issued; k++)
-            mbar_wait(&S->full[k % T::kStages], (k / T::kStages) & 1, &zero, tc::kWaitLimitNs);
+        for (int64_t k = issued > stages ? issued - stages : 0; k < issued; k++)
+            mbar_wait(&S->full[k % stages], (k / stages) & 1, &zero, tc::kWaitLimitNs);
     } else {
-        // ------------------------------------------------------------ products
-        constexpr uint32_t idesc = idesc_e4m3(kLanes, TC);
+        // ------------------------------------------------------------ products of every other block
+        constexpr uint32_t idesc = idesc_e4m3(kLanes, T::TC);
         const bool issue = elect_one();
         const uint64_t desc = sdesc_sw128(smem_u32(smem));
         const uint32_t a_lo = (uint32_t)desc, hi = (uint32_t)(desc >> 32);
-        int st = 0, ph = 0, buf = 0, tph = 1;
+        const int odd = warp - T::kWarps - 1, n = kb1 - kb0;
+        int st = odd % stages, ph = odd / stages & 1, buf = odd, tph = 1, k0 = odd;
         for (int64_t tile = first; tile < tiles && !dead; tile += step) {
-            for (int64_t kb = kb0; kb < kb1; kb++) {
+            for (; k0 < n; k0 += 2) {
                 if (!__all_sync(0xffffffffu, mbar_wait(&S->tempty[buf], tph, abort_flag, a.wait_ns)) ||
                     !__all_sync(0xffffffffu, mbar_wait(&S->full[st], ph, abort_flag, a.wait_ns))) {
                     dead = true;
                     break;
                 }
                 tc_fence_after();
-                const uint32_t da = a_lo + ((st * T::kStage) >> 4), db = da + (T::kA >> 4), d = tmem + buf * T::kBuf;
+                const uint32_t da = a_lo + ((st * stage) >> 4), db = da + ((a.box_rows * 128) >> 4), d = tmem + buf * T::TC;
                 if (issue) {
 #pragma unroll
                     for (int k = 0; k < kBlock / 32; k++) mma_e4m3<false>(d, da + 2 * k, db + 2 * k, hi, idesc, k ? 1u : 0u);
-                    mma_commit(&S->empty[st]);
                     mma_commit(&S->tfull[buf]);
+                    mma_commit(&S->empty[st]);
                 }
                 __syncwarp();
-                buf ^= 1;
-                tph ^= buf == 0;
-                if (++st == T::kStages) {
-                    st = 0;
+                buf += 2;
+                if (buf >= T::kBufs) {
+                    buf -= T::kBufs;
+                    tph ^= 1;
+                }
+                st += 2;
+                if (st >= stages) {
+                    st -= stages;
                     ph ^= 1;
                 }
             }
+            k0 -= n;   // the warp's first block of the next tile
         }
         if (dead) *abort_flag = 1;
         if (issue) mma_commit(&S->drain);   // products in flight end before tensor memory is given back
@@ -520,7 +525,7 @@ block8_matmul_kernel(const __grid_constant__ MatArgs a, const __grid_constant__ 
     __syncthreads();
     if (warp == T::kWarps + 1) {
         tc_fence_after();
-        tmem_dealloc(tmem, T::kCols);
+        tmem_dealloc(tmem, T::kBufs * T::TC);
     }
     if (a.split > 1) {
         // ---- sums of the cluster: this CTA's part of the rows
@@ -528,32 +533,24 @@ block8_matmul_kernel(const __grid_constant__ MatArgs a, const __grid_constant__ 
         cluster.sync();
         int64_t lt, ct;
         place(first, &lt, &ct);
-        const int rows = kLanes / a.split, r0 = rank * rows;
+        const int have = a.M - lt * kLanes < kLanes ? (int)(a.M - lt * kLanes) : kLanes;
+        const int r0 = have * rank / a.split, r1 = have * (rank + 1) / a.split;
         const float* sums = reinterpret_cast<const float*>(smem);
-        if (TOKENS) {
-            for (int x = tid; x < rows * (TC / 4); x += T::kThreads) {
-                const int r = r0 + x / (TC / 4), c4 = x % (TC / 4) * 4;
-                const int64_t m = lt * kLanes + r, n = ct * TC + c4;
-                if (m >= a.M || n >= a.N) continue;
-                float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                for (int k = 0; k < a.split; k++) {
-                    const float4 v = *reinterpret_cast<const float4*>(cluster.map_shared_rank(sums, k) + r * T::kPitch + c4);
-                    s = make_float4(s.x + v.x, s.y + v.y, s.z + v.z, s.w + v.w);
-                }
-                uint16_t* dst = static_cast<uint16_t*>(a.out) + m * a.out_stride + n;
-                const uint2 w = make_uint2(pack(s.x, s.y, a.fp16), pack(s.z, s.w, a.fp16));
-                if (a.vec && n + 4 <= a.N) *reinterpret_cast<uint2*>(dst) = w;
-                else store_piece(dst, make_uint4(w.x, w.y, 0u, 0u), a.N - n < 4 ? (int)(a.N - n) : 4, false);
+        for (int x = tid; x < (r1 - r0) * (T::TC / 4); x += T::kThreads) {
+            const int r = r0 + x / (T::TC / 4), c4 = x % (T::TC / 4) * 4;
+            const int64_t m = lt * kLanes + r, n = ct * T::TC + c4;
+            if (n >= a.N) continue;
+            float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+            for (int k = 0; k < 8; k++) {
+                if (k >= a.split) break;
+                const float4 v = *reinterpret_cast<const float4*>(cluster.map_shared_rank(sums, k) + r * T::kPitch + c4);
+                s = make_float4(s.x + v.x, s.y + v.y, s.z + v.z, s.w + v.w);
             }
-        } else {
-            for (int x = tid; x < rows * TC; x += T::kThreads) {
-                const int r = r0 + x % rows, c = x / rows;
-                const int64_t n = lt * kLanes + r, m = ct * TC + c;
-                if (m >= a.M || n >= a.N) continue;
-                float s = 0.0f;
-                for (int k = 0; k < a.split; k++) s += cluster.map_shared_rank(sums, k)[r * T::kPitch + c];
-                static_cast<uint16_t*>(a.out)[m * a.out_stride + n] = (uint16_t)pack(s, 0.0f, a.fp16);
-            }
+            uint16_t* dst = static_cast<uint16_t*>(a.out) + m * a.out_stride + n;
+            const uint2 w = make_uint2(pack(s.x, s.y, a.fp16), pack(s.z, s.w, a.fp16));
+            if (a.vec && n + 4 <= a.N) *reinterpret_cast<uint2*>(dst) = w;
+            else store_piece(dst, make_uint4(w.x, w.y, 0u, 0u), a.N - n < 4 ? (int)(a.N - n) : 4, false);
         }
         cluster.sync();   // no CTA ends while its sums may be read
     }
@@ -1088,58 +1085,76 @@ struct Matrices {
     int64_t K, x_stride, w_stride;
 };
 
-template <int TC, bool TOKENS>
-cudaError_t launch_tile(MatArgs a, const Matrices& m, int split, cudaStream_t st) {
-    using T = Tile<TC, TOKENS>;
-    CUtensorMap lanes, cols;
-    const bool ok = TOKENS ? codes_map(&lanes, m.x, a.M, m.K, m.x_stride, kLanes) && codes_map(&cols, m.w, a.N, m.K, m.w_stride, TC)
-                           : codes_map(&lanes, m.w, a.N, m.K, m.w_stride, kLanes) && codes_map(&cols, m.x, a.M, m.K, m.x_stride, TC);
-    if (!ok) return cudaErrorInvalidValue;
-    a.lane_tiles = ((TOKENS ? a.M : a.N) + kLanes - 1) / kLanes;
-    a.col_tiles = ((TOKENS ? a.N : a.M) + TC - 1) / TC;
-    a.split = split;
-    a.group = 16;
-    auto* kernel = block8_matmul_kernel<TC, TOKENS>;
+cudaError_t opt_in_tiles() {
     static SmemOptIn opt_in;
-    cudaError_t e = opt_in.set(reinterpret_cast<const void*>(kernel), (int)T::total);
+    return opt_in.set(reinterpret_cast<const void*>(block8_tile_kernel), (int)Tile::total);
+}
+
+// Clusters of `size` CTAs of a kernel that run at the same time, asked once per device and size.
+struct Clusters {
+    std::atomic<int> known[64][9];
+    cudaError_t most(const void* kernel, int threads, size_t smem, int size, int* n) {
+        int dev = 0;
+        cudaError_t e = cudaGetDevice(&dev);
+        if (e != cudaSuccess) return e;
+        *n = dev < 64 ? known[dev][size].load(std::memory_order_relaxed) : 0;
+        if (*n) return cudaSuccess;
+        cudaLaunchConfig_t cfg{};
+        cfg.gridDim = dim3((unsigned)(tc::num_sms() / size * size));
+        cfg.blockDim = dim3((unsigned)threads);
+        cfg.dynamicSmemBytes = smem;
+        cudaLaunchAttribute at{};
+        at.id = cudaLaunchAttributeClusterDimension;
+        at.val.clusterDim.x = (unsigned)size;
+        at.val.clusterDim.y = at.val.clusterDim.z = 1;
+        cfg.attrs = &at;
+        cfg.numAttrs = 1;
+        if ((e = cudaOccupancyMaxActiveClusters(n, kernel, &cfg)) != cudaSuccess) return e;
+        if (*n < 1) return cudaErrorInvalidConfiguration;
+        if (dev < 64) known[dev][size].store(*n, std::memory_order_relaxed);
+        return cudaSuccess;
+    }
+};
+
+// CTAs of a cluster of the tile kernel: as many as the GPU has room for at once, a block of channels each at least.
+cudaError_t tile_split(const MatArgs& a, int* split) {
+    static Clusters clusters;
+    const int64_t tiles = (a.M + kLanes - 1) / kLanes * ((a.N + Tile::TC - 1) / Tile::TC), room = tc::num_sms();
+    cudaError_t e = opt_in_tiles();
     if (e != cudaSuccess) return e;
-    const int64_t tiles = a.lane_tiles * a.col_tiles, room = (int64_t)tc::num_sms() * T::kCtas;
+    int s = (int)(room / tiles < 8 ? room / tiles : 8);
+    if (s > a.nb) s = (int)a.nb;
+    for (; s > 1; s--) {
+        int n = 0;
+        if ((e = clusters.most(reinterpret_cast<const void*>(block8_tile_kernel), Tile::kThreads, Tile::total, s, &n)) != cudaSuccess) return e;
+        if (n >= tiles) break;
+    }
+    *split = s < 1 ? 1 : s;
+    return cudaSuccess;
+}
+
+cudaError_t launch_tiles(MatArgs a, const Matrices& m, int split, cudaStream_t st) {
+    using T = Tile;
+    a.box_rows = a.M < kLanes ? (int)((a.M + 7) / 8 * 8) : kLanes;
+    CUtensorMap xs, ws;
+    if (!codes_map(&xs, m.x, a.M, m.K, m.x_stride, a.box_rows) || !codes_map(&ws, m.w, a.N, m.K, m.w_stride, T::TC)) return cudaErrorInvalidValue;
+    a.lane_tiles = (a.M + kLanes - 1) / kLanes;
+    a.col_tiles = (a.N + T::TC - 1) / T::TC;
+    a.group = 16;
+    a.split = split;
+    const int64_t tiles = a.lane_tiles * a.col_tiles, room = tc::num_sms();
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)(split > 1 ? tiles * split : tiles < room ? tiles : room));
+    cfg.gridDim = dim3((unsigned)(a.split > 1 ? tiles * a.split : tiles < room ? tiles : room));
     cfg.blockDim = dim3(T::kThreads);
     cfg.dynamicSmemBytes = T::total;
     cfg.stream = st;
     cudaLaunchAttribute at{};
     at.id = cudaLaunchAttributeClusterDimension;
-    at.val.clusterDim.x = (unsigned)split;
+    at.val.clusterDim.x = (unsigned)a.split;
     at.val.clusterDim.y = at.val.clusterDim.z = 1;
     cfg.attrs = &at;
-    cfg.numAttrs = split > 1 ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, kernel, a, lanes, cols);
-}
-
-// Clusters of two CTAs of a kernel that run at the same time, asked once per device.
-cudaError_t max_pairs(const void* kernel, int threads, size_t smem, int* pairs) {
-    static std::atomic<int> known[64];
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return e;
-    *pairs = dev < 64 ? known[dev].load(std::memory_order_relaxed) : 0;
-    if (*pairs) return cudaSuccess;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)(tc::num_sms() / 2 * 2));
-    cfg.blockDim = dim3((unsigned)threads);
-    cfg.dynamicSmemBytes = smem;
-    cudaLaunchAttribute at{};
-    at.id = cudaLaunchAttributeClusterDimension;
-    at.val.clusterDim.x = 2;
-    at.val.clusterDim.y = at.val.clusterDim.z = 1;
-    cfg.attrs = &at;
-    cfg.numAttrs = 1;
-    if ((e = cudaOccupancyMaxActiveClusters(pairs, kernel, &cfg)) != cudaSuccess) return e;
-    if (*pairs < 1) return cudaErrorInvalidConfiguration;
-    if (dev < 64) known[dev].store(*pairs, std::memory_order_relaxed);
-    return cudaSuccess;
+    cfg.numAttrs = a.split > 1 ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, block8_tile_kernel, a, xs, ws);
 }
 
 cudaError_t launch_pairs(MatArgs a, const Matrices& m, cudaStream_t st) {
@@ -1157,7 +1172,8 @@ cudaError_t launch_pairs(MatArgs a, const Matrices& m, cudaStream_t st) {
     cudaError_t e = opt_in.set(reinterpret_cast<const void*>(block8_pair_kernel), (int)T::total);
     if (e != cudaSuccess) return e;
     int pairs = 0;   // that the GPU has room for at once: one that came later would take its share when the others are done
-    if ((e = max_pairs(reinterpret_cast<const void*>(block8_pair_kernel), T::kThreads, T::total, &pairs)) != cudaSuccess) return e;
+    static Clusters clusters;
+    if ((e = clusters.most(reinterpret_cast<const void*>(block8_pair_kernel), T::kThreads, T::total, 2, &pairs)) != cudaSuccess) return e;
     const int64_t tiles = a.lane_tiles * a.col_tiles;
     block8_pair_kernel<<<(unsigned)(2 * (tiles < pairs ? tiles : pairs)), T::kThreads, T::total, st>>>(a, xs, ws, out);
     return cudaGetLastError();
@@ -1199,22 +1215,19 @@ cudaError_t launch_few(const MatArgs& a, const Matrices& m, cudaStream_t st) {
     return cudaLaunchKernelEx(&cfg, block8_few_kernel, f);
 }
 
-// CTAs of a cluster: as many as the GPU has room for at once, a block of channels each at least.
-int split_of(int64_t tiles, int64_t nb, int ctas) {
-    int s = 1;
-    while (s < 8 && tiles * 2 * s <= (int64_t)tc::num_sms() * ctas && 2 * s <= nb) s *= 2;
-    return s;
-}
-
+// The tile kernel takes 0.36 us a block of channels and round, 1.3 us to add up a cluster's sums, the pair kernel 0.45 us a
+// block for four times the work (6144 rows of w, 4096 channels: 256 rows of x 15.8 us on tiles and 18.8 on pairs, 512 27.7 and
+// 19.0). The smaller sum is taken.
 cudaError_t launch_matmul(const MatArgs& a, const Matrices& m, cudaStream_t st) {
-    const int64_t n128 = (a.N + 127) / 128, m128 = (a.M + 127) / 128;
     if (a.M <= kFewMost) return launch_few(a, m, st);
-    if (a.M <= 16) return launch_tile<16, false>(a, m, split_of(n128, a.nb, Tile<16, false>::kCtas), st);
-    if (a.M <= 32) return launch_tile<32, false>(a, m, split_of(n128, a.nb, Tile<32, false>::kCtas), st);
-    if (a.M <= 64) return launch_tile<64, false>(a, m, split_of(n128, a.nb, Tile<64, false>::kCtas), st);
-    const int64_t t256 = m128 * ((a.N + 255) / 256);
-    if (t256 >= tc::num_sms()) return launch_pairs(a, m, st);
-    return launch_tile<128, true>(a, m, split_of(m128 * n128, a.nb, Tile<128, true>::kCtas), st);
+    const int64_t tiles = (a.M + kLanes - 1) / kLanes * ((a.N + Tile::TC - 1) / Tile::TC), sms = tc::num_sms();
+    const int64_t pairs = (a.M + 2 * kLanes - 1) / (2 * kLanes) * ((a.N + Pair::TC - 1) / Pair::TC);
+    int split = 1;
+    const cudaError_t e = tile_split(a, &split);
+    if (e != cudaSuccess) return e;
+    const int64_t t_tiles = (tiles * split + sms - 1) / sms * ((a.nb + split - 1) / split) * 36 + (split > 1 ? 130 : 0);
+    const int64_t t_pairs = (pairs + sms / 2 - 1) / (sms / 2) * a.nb * 45;
+    return t_pairs < t_tiles ? launch_pairs(a, m, st) : launch_tiles(a, m, split, st);
 }
 
 bool al16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -1272,13 +1285,23 @@ CG_EXPORT int cg_block8_encode(int32_t dtype, int64_t R, int64_t K, int32_t rows
     a.stride = R > 1 ? stride : K;
     a.nb = (K + kBlock - 1) / kBlock;
     const int64_t items = rows == 1 ? (R * a.nb + kEncRows - 1) / kEncRows : (R + kBlock - 1) / kBlock * a.nb;
-    const unsigned grid = (unsigned)(items < (1 << 30) ? items : 1 << 30);
+    // Long matrices: 8 CTAs an SM that go on, two blocks of a row at a time (8192 x 4096: 24.4 us with a CTA for 32 blocks)
+    const int64_t room = 8 * (int64_t)tc::num_sms();
+    const unsigned grid = (unsigned)(items < room ? items : room);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const bool fp16 = dtype == CG_FP16;
     if (rows == 1) {
-        if (dtype == CG_FP16) encode_rows_kernel<true><<<grid, kEncThreads, 0, st>>>(a);
-        else encode_rows_kernel<false><<<grid, kEncThreads, 0, st>>>(a);
+        a.step_row = (int64_t)grid * kEncRows / a.nb;
+        a.step_b = (int64_t)grid * kEncRows % a.nb;
+        if (items > room) {
+            if (fp16) encode_rows_kernel<true, 2><<<grid, kEncThreads, 0, st>>>(a);
+            else encode_rows_kernel<false, 2><<<grid, kEncThreads, 0, st>>>(a);
+        } else {
+            if (fp16) encode_rows_kernel<true, 1><<<grid, kEncThreads, 0, st>>>(a);
+            else encode_rows_kernel<false, 1><<<grid, kEncThreads, 0, st>>>(a);
+        }
     } else {
-        if (dtype == CG_FP16) encode_square_kernel<true><<<grid, kEncThreads, 0, st>>>(a);
+        if (fp16) encode_square_kernel<true><<<grid, kEncThreads, 0, st>>>(a);
         else encode_square_kernel<false><<<grid, kEncThreads, 0, st>>>(a);
     }
     const cudaError_t e = cudaGetLastError();
