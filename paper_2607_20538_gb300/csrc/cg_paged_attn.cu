@@ -497,15 +497,15 @@ paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ 
                     if (TREE && edge) {
 #pragma unroll
                         for (int hf = 0; hf < 2; hf++) {
-                            const int first = t0 - (w.r.len - w.r.n);   // node of column t0
-                            const uint32_t nodes = node[hf] >= 0 ? tree_word(a, w.r, node[hf], first) : 0u;
+                            const int j0 = t0 - (w.r.len - w.r.n);      // node of column t0
+                            const uint32_t nodes = node[hf] >= 0 ? tree_word(tree_row(a, w.r, node[hf]), a.words, w.r.n, j0) : 0u;
 #pragma unroll
                             for (int n = 0; n < 2; n++)
 #pragma unroll
                                 for (int e = 0; e < 2; e++) {
                                     const int c = 8 * n + e, t = t0 + c;
                                     const bool old = !a.window || t > pos[hf] - a.window || t < a.sinks;
-                                    const bool see = first + c < 0 ? old && node[hf] >= 0 : (nodes >> c & 1u) != 0;
+                                    const bool see = j0 + c < 0 ? old && node[hf] >= 0 : (nodes >> c & 1u) != 0;
                                     s[n][2 * hf + e] = see ? s[n][2 * hf + e] : -INFINITY;
                                 }
                         }

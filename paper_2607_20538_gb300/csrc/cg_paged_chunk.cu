@@ -458,11 +458,10 @@ __device__ __forceinline__ void mask_row_but(uint32_t s_tm, int lo, int hi, int 
 __device__ __noinline__ void mask_row(uint32_t s_tm, int lo, int hi, int sk) {
     mask_row_but(s_tm, lo, hi, sk, [](int) { return 0u; });
 }
-// The same for a node's row: history up to column hi, and the nodes of its mask (column 0 is token t0; node -1:
-// no row, which sees nothing).
-__device__ __noinline__ void mask_node(const PagedArgs& a, const Request& r, int node, uint32_t s_tm, int t0, int lo, int sk) {
-    const int ctx = r.len - r.n;
-    mask_row_but(s_tm, lo, node < 0 ? -1 : ctx - 1 - t0, sk, [&](int c) { return node < 0 ? 0u : tree_word(a, r, node, t0 + c - ctx); });
+// The same for a node's row: history, which ends before column -j0, and the nodes of its mask (column 0 is node j0; row
+// null: no row, which sees nothing).
+__device__ __noinline__ void mask_node(const uint32_t* row, int words, int n, uint32_t s_tm, int j0, int lo, int sk) {
+    mask_row_but(s_tm, lo, row ? -1 - j0 : -1, sk, [&](int c) { return row ? tree_word(row, words, n, j0 + c) : 0u; });
 }
 
 // Each lane holds 8 pieces of 16 bytes of its row (128 bytes). The 8 lanes of a group transpose them
@@ -766,7 +765,6 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                 const int row = (warp & 3) * 32 + lane;
                 const bool have = row < sp.n;
                 const int rt = token_of(a, row), tk = tok + rt, hd = w.h * a.n_rep + (row - rt * a.n_rep);
-                const int node = TREE && have ? tk : -1;
                 const int pos = !have ? -1 : TREE ? tree_position(a, w.r, tk, &flag) : sp.p0 + rt;
                 float ref = -INFINITY, sum = 0.0f;
                 bool started = false;
@@ -789,7 +787,9 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                     };
                     tc_fence_after();
                     const int t0 = id * kKT;
-                    if (TREE && !sp.sees_all(id)) mask_node(a, w.r, node, s_tm, t0, a.window ? pos - a.window + 1 - t0 : 0, a.sinks - t0);
+                    if (TREE && !sp.sees_all(id))
+                        mask_node(have ? tree_row(a, w.r, tk) : nullptr, a.words, w.r.n, s_tm, t0 - (w.r.len - w.r.n), a.window ? pos - a.window + 1 - t0 : 0,
+                                  a.sinks - t0);
                     else if (!sp.sees_all(id)) mask_row(s_tm, a.window ? pos - a.window + 1 - t0 : 0, pos - t0, a.sinks - t0);
                     float u[32], v[32];
                     const float mx = sl2 * row_max(s_tm, u, v);
@@ -818,7 +818,7 @@ paged_chunk_kernel(const __grid_constant__ ChunkParams P, const __grid_constant_
                         if (dead) break;
                         if (special) {
                             if (!quiet()) break;
-                            add_special<FP16, D, TREE>(a, w.r, w.i, w.h, item, t0, pos, node, o_tm, !started);
+                            add_special<FP16, D, TREE>(a, w.r, w.i, w.h, item, t0, pos, have ? tk : -1, o_tm, !started);
                             if (!started && lane == 0) *(volatile int*)&M->accum0[x] = 1;
                         }
                     }

@@ -112,19 +112,22 @@ __device__ __forceinline__ int tree_position(const PagedArgs& a, const Request& 
     if (p < ctx || p > ctx + node) *flag |= CG_FLAG_PAGED_RANGE;
     return min(max(p, ctx), ctx + node);
 }
-// Nodes [j, j + 32) of a request that the row of `node` sees, as a word; any j.
-__device__ __forceinline__ uint32_t tree_word(const PagedArgs& a, const Request& r, int node, int j) {
-    if (j <= -32 || j >= r.n) return 0u;
-    const uint32_t* row = a.masks + (int64_t)(r.tok0 + node) * a.words;
+// A node's row of masks.
+__device__ __forceinline__ const uint32_t* tree_row(const PagedArgs& a, const Request& r, int node) {
+    return a.masks + (int64_t)(r.tok0 + node) * a.words;
+}
+// Nodes [j, j + 32) of a request of n that the row sees, as a word; any j.
+__device__ __forceinline__ uint32_t tree_word(const uint32_t* row, int words, int n, int j) {
+    if (j <= -32 || j >= n) return 0u;
     const int w = j >> 5;                                  // -1 for j < 0
-    const uint32_t lo = w >= 0 ? __ldg(row + w) : 0u, hi = w + 1 < a.words ? __ldg(row + w + 1) : 0u;
-    const int left = r.n - j;                              // bits past the last node are no tokens
+    const uint32_t lo = w >= 0 ? __ldg(row + w) : 0u, hi = w + 1 < words ? __ldg(row + w + 1) : 0u;
+    const int left = n - j;                                // bits past the last node are no tokens
     return __funnelshift_r(lo, hi, j & 31) & (left >= 32 ? ~0u : (1u << left) - 1u);
 }
 // Whether the row of `node` at position p sees token t < len.
 __device__ __forceinline__ bool tree_sees(const PagedArgs& a, const Request& r, int node, int p, int t) {
     const int j = t - (r.len - r.n);
-    return j < 0 ? !a.window || t > p - a.window || t < a.sinks : (tree_word(a, r, node, j) & 1u) != 0;
+    return j < 0 ? !a.window || t > p - a.window || t < a.sinks : (tree_word(tree_row(a, r, node), a.words, r.n, j) & 1u) != 0;
 }
 
 // Key tiles of TK tokens that rows at positions [p_first, p_last] of a request of length len see:
