@@ -191,8 +191,9 @@ __global__ void __launch_bounds__(kEncThreads) encode_square_kernel(EncArgs a) {
 //                 a block, its products 256)
 // Few rows of x: a stage holds them in whole groups of 8, and more stages fit; the lanes that they do not fill multiply
 // what lies behind, and nobody reads them.
-// Few tiles: the blocks of channels are cut among the CTAs of a cluster; each leaves its sums in shared memory,
-// and each adds up a part of the rows, in the order of the ranks whatever their timing.
+// Few tiles: the blocks of channels are cut among the CTAs of a cluster; each writes its sums of a part of the rows into the
+// shared memory of the CTA that adds those up, in the order of the ranks whatever their timing. (Left where they were and
+// read from there they cost 333 x 1000 x 4112 4.1 us of 10.7, two rounds of loads' latency and a barrier more.)
 // ------------------------------------------------------------------------------------
 constexpr int kLanes = 128;
 
@@ -200,11 +201,13 @@ struct Tile {
     static constexpr int TC = 128, CW = 64;                     // columns, and those of a warp
     static constexpr int kWarps = 8, kThreads = (kWarps + 3) * 32;
     static constexpr uint32_t kB = TC * 128, ring = 196608;
+    // a cluster's ring; the sums follow, [rank][columns / 4][rows of a part, an odd number][4]: a warp's store is 512 bytes in a
+    // row (with the columns of a row together 64 KB took 2.5 us), and the columns of a row lie in different banks
+    static constexpr uint32_t split_ring = 159744;
     static constexpr int kMost = 10;                            // stages
     static constexpr int kBufs = 4;                             // of tensor memory
-    static constexpr int kPitch = TC + 4;                       // floats of a row of sums, without bank conflicts in 16-byte pieces
-    static constexpr uint32_t misc = ring, total = misc + 512;
-    static_assert(kLanes * kPitch * 4 <= ring && kMost * (kB + 1024) <= ring && total <= 232448, "tile");
+    static constexpr uint32_t misc = 231936, total = misc + 512;
+    static_assert(split_ring % 1024 == 0 && split_ring + (kLanes + 12) * TC * 4 <= misc && ring <= misc && kMost * (kB + 1024) <= ring && total <= 232448, "tile");
 };
 
 struct MatArgs {
@@ -219,6 +222,34 @@ struct MatArgs {
     int split;           // CTAs of a cluster
     int group;           // lane tiles that are walked together
     int box_rows;        // of x in a stage
+};
+
+// The tiles of a CTA (or a pair, or a cluster), every step-th from the first: lane tiles in groups, so that those at work
+// share both matrices' rows in L2.
+struct TileWalk {
+    int g, in, lt, ct;      // group, tile in it; lane tile, column tile
+    __device__ __forceinline__ bool set(const MatArgs& a) {
+        for (;;) {
+            const int left = (int)a.lane_tiles - g * a.group, n = left < a.group ? left : a.group;
+            if (n <= 0) return false;
+            if (in < n * (int)a.col_tiles) {
+                ct = in / n;
+                lt = g * a.group + (in - ct * n);
+                return true;
+            }
+            in -= n * (int)a.col_tiles;
+            g++;
+        }
+    }
+    __device__ __forceinline__ bool start(const MatArgs& a, int first) {
+        g = 0;
+        in = first;
+        return set(a);
+    }
+    __device__ __forceinline__ bool next(const MatArgs& a, int step) {
+        in += step;
+        return set(a);
+    }
 };
 
 struct MatMisc {
@@ -259,6 +290,16 @@ __device__ __forceinline__ bool elect_one() {
 __host__ __device__ constexpr uint32_t idesc_e4m3(int M, int N) {
     return (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
 }
+
+// Address of the same place in the shared memory of a CTA of the cluster.
+__device__ __forceinline__ uint32_t at_rank(const void* p, uint32_t rank) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(p)), "r"(rank));
+    return r;
+}
+// The cluster's barrier in halves; every thread calls both, in turn.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.aligned;" ::: "memory"); }
 
 __device__ __forceinline__ void tmem_ld16(uint32_t taddr, float (&r)[16]) {
     asm volatile(
@@ -329,10 +370,11 @@ block8_tile_kernel(const __grid_constant__ MatArgs a, const __grid_constant__ CU
     MatMisc* S = reinterpret_cast<MatMisc*>(smem + T::misc);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int rank = (int)(blockIdx.x % (unsigned)a.split);
-    const int64_t first = blockIdx.x / (unsigned)a.split, step = gridDim.x / (unsigned)a.split, tiles = a.lane_tiles * a.col_tiles;
+    const int first = (int)(blockIdx.x / (unsigned)a.split), step = (int)(gridDim.x / (unsigned)a.split);
     const int kb0 = (int)(a.nb * rank / a.split), kb1 = (int)(a.nb * (rank + 1) / a.split);
     const uint32_t stage = a.box_rows * 128 + T::kB;
-    const int stages = min(T::kMost, (int)(T::ring / stage));
+    const int stages = min(T::kMost, (int)((a.split > 1 ? T::split_ring : T::ring) / stage));
+    if (a.split > 1) cluster_arrive();   // (waited for before anything is written into another CTA's shared memory: it has started then)
     if (tid == 0) {
         for (int s = 0; s < stages; s++) {
             mbar_init(&S->full[s], 1);
@@ -357,13 +399,11 @@ block8_tile_kernel(const __grid_constant__ MatArgs a, const __grid_constant__ CU
     tc_fence_after();
     const uint32_t tmem = S->tmem;
     volatile int* abort_flag = &S->abort_flag;
-    // lane tiles in groups, so that the CTAs at work share both matrices' rows in L2
-    auto place = [&](int64_t tile, int64_t* l, int64_t* c) {
-        const int64_t per = a.group * a.col_tiles, g = tile / per, in = tile - g * per;
-        const int64_t left = a.lane_tiles - g * a.group, n = left < a.group ? left : a.group;
-        *c = in / n;
-        *l = g * a.group + (in - *c * n);
-    };
+    TileWalk w;
+    bool more = w.start(a, first);
+    // of a cluster's tile: its place, its rows, and how many of them each CTA adds up
+    const int64_t m0 = (int64_t)w.lt * kLanes, n0 = (int64_t)w.ct * T::TC;
+    const int have = a.M - m0 < kLanes ? (int)(a.M - m0) : kLanes, part = (have + a.split - 1) / a.split;
     bool dead = *abort_flag != 0;
 
     if (warp < T::kWarps) {
@@ -371,16 +411,14 @@ block8_tile_kernel(const __grid_constant__ MatArgs a, const __grid_constant__ CU
         const int col0 = (warp >> 2) * T::CW, row0 = 32 * (warp & 3), row = row0 + lane;
         const uint32_t t0 = tmem + ((uint32_t)row0 << 16) + col0;
         int buf = 0, ph = 0;
-        for (int64_t tile = first; tile < tiles && !dead; tile += step) {
-            int64_t lt, ct;
-            place(tile, &lt, &ct);
-            const int64_t r = lt * kLanes + row, c = ct * T::TC + col0;    // the thread's row, and first column
-            const bool idle = lt * kLanes + row0 >= a.M;                   // no row of the warp's is one of x
+        for (; more && !dead; more = w.next(a, step)) {
+            const int64_t r = (int64_t)w.lt * kLanes + row, c = (int64_t)w.ct * T::TC + col0;    // the thread's row, and first column
+            const bool idle = (int64_t)w.lt * kLanes + row0 >= a.M;                   // no row of the warp's is one of x
             float2 acc[T::CW / 2];
 #pragma unroll
             for (int k = 0; k < T::CW / 2; k++) acc[k] = make_float2(0.0f, 0.0f);
             // scales of four blocks, fetched four blocks ahead
-            const float *px = a.xs + (r < a.M ? r : a.M - 1) * a.nb, *pw = a.ws + ct * a.nb;   // (128 columns: one block of w)
+            const float *px = a.xs + (r < a.M ? r : a.M - 1) * a.nb, *pw = a.ws + w.ct * a.nb;   // (128 columns: one block of w)
             float nx[4], nw[4], f[4];
             auto fetch = [&](int kb) {
 #pragma unroll
@@ -426,11 +464,16 @@ block8_tile_kernel(const __grid_constant__ MatArgs a, const __grid_constant__ CU
             }
             if (dead) break;
             if (a.split > 1) {
-                float* sums = reinterpret_cast<float*>(smem) + row * T::kPitch + col0;
-                if (!idle) {
+                cluster_wait();
+                if (row < have) {
+                    const int pitch = part | 1, owner = row / part;
+                    const float4* here = reinterpret_cast<const float4*>(smem + T::split_ring) + (rank * (T::TC / 4) + col0 / 4) * pitch + row - owner * part;
+                    const uint32_t dst = at_rank(here, (uint32_t)owner);
 #pragma unroll
-                    for (int k = 0; k < T::CW; k += 4)
-                        *reinterpret_cast<float4*>(sums + k) = make_float4(acc[k / 2].x, acc[k / 2].y, acc[k / 2 + 1].x, acc[k / 2 + 1].y);
+                    for (int k = 0; k < T::CW / 4; k++)
+                        asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(dst + 16 * k * pitch), "f"(acc[2 * k].x), "f"(acc[2 * k].y),
+                                     "f"(acc[2 * k + 1].x), "f"(acc[2 * k + 1].y)
+                                     : "memory");
                 }
                 break;
             }
@@ -447,9 +490,7 @@ block8_tile_kernel(const __grid_constant__ MatArgs a, const __grid_constant__ CU
         // ------------------------------------------------------------ copies
         int st = 0, ph = 1;
         int64_t issued = 0;
-        for (int64_t tile = first; tile < tiles && !dead; tile += step) {
-            int64_t lt, ct;
-            place(tile, &lt, &ct);
+        for (; more && !dead; more = w.next(a, step)) {
             for (int kb = kb0; kb < kb1; kb++) {
                 if (!__all_sync(0xffffffffu, mbar_wait(&S->empty[st], ph, abort_flag, a.wait_ns))) {
                     dead = true;
@@ -457,8 +498,8 @@ block8_tile_kernel(const __grid_constant__ MatArgs a, const __grid_constant__ CU
                 }
                 if (lane == 0) {
                     mbar_arrive_expect_tx(&S->full[st], stage);
-                    tma_load_2d(smem + st * stage + a.box_rows * 128, &w_map, &S->full[st], kb * kBlock, (int)(ct * T::TC));
-                    tma_load_2d(smem + st * stage, &x_map, &S->full[st], kb * kBlock, (int)(lt * kLanes));
+                    tma_load_2d(smem + st * stage + a.box_rows * 128, &w_map, &S->full[st], kb * kBlock, w.ct * T::TC);
+                    tma_load_2d(smem + st * stage, &x_map, &S->full[st], kb * kBlock, w.lt * kLanes);
                 }
                 __syncwarp();
                 issued++;
@@ -481,7 +522,7 @@ block8_tile_kernel(const __grid_constant__ MatArgs a, const __grid_constant__ CU
         const uint32_t a_lo = (uint32_t)desc, hi = (uint32_t)(desc >> 32);
         const int odd = warp - T::kWarps - 1, n = kb1 - kb0;
         int st = odd % stages, ph = odd / stages & 1, buf = odd, tph = 1, k0 = odd;
-        for (int64_t tile = first; tile < tiles && !dead; tile += step) {
+        for (; more && !dead; more = w.next(a, step)) {
             for (; k0 < n; k0 += 2) {
                 if (!__all_sync(0xffffffffu, mbar_wait(&S->tempty[buf], tph, abort_flag, a.wait_ns)) ||
                     !__all_sync(0xffffffffu, mbar_wait(&S->full[st], ph, abort_flag, a.wait_ns))) {
@@ -528,23 +569,18 @@ block8_tile_kernel(const __grid_constant__ MatArgs a, const __grid_constant__ CU
         tmem_dealloc(tmem, T::kBufs * T::TC);
     }
     if (a.split > 1) {
-        // ---- sums of the cluster: this CTA's part of the rows
-        auto cluster = cooperative_groups::this_cluster();
-        cluster.sync();
-        int64_t lt, ct;
-        place(first, &lt, &ct);
-        const int have = a.M - lt * kLanes < kLanes ? (int)(a.M - lt * kLanes) : kLanes;
-        const int r0 = have * rank / a.split, r1 = have * (rank + 1) / a.split;
-        const float* sums = reinterpret_cast<const float*>(smem);
-        for (int x = tid; x < (r1 - r0) * (T::TC / 4); x += T::kThreads) {
-            const int r = r0 + x / (T::TC / 4), c4 = x % (T::TC / 4) * 4;
-            const int64_t m = lt * kLanes + r, n = ct * T::TC + c4;
+        // ---- this CTA's part of the rows
+        if (warp >= T::kWarps || dead) cluster_wait();   // (the others have)
+        cooperative_groups::this_cluster().sync();
+        const int r0 = rank * part, rows = have - r0 < part ? have - r0 : part;
+        const float4* sums = reinterpret_cast<const float4*>(smem + T::split_ring);
+        for (int x = tid; x < rows * (T::TC / 4); x += T::kThreads) {
+            const int r = x / (T::TC / 4), c = x % (T::TC / 4), pitch = part | 1;
+            const int64_t m = m0 + r0 + r, n = n0 + 4 * c;
             if (n >= a.N) continue;
             float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll
-            for (int k = 0; k < 8; k++) {
-                if (k >= a.split) break;
-                const float4 v = *reinterpret_cast<const float4*>(cluster.map_shared_rank(sums, k) + r * T::kPitch + c4);
+            for (int k = 0; k < a.split; k++) {
+                const float4 v = sums[(k * (T::TC / 4) + c) * pitch + r];
                 s = make_float4(s.x + v.x, s.y + v.y, s.z + v.z, s.w + v.w);
             }
             uint16_t* dst = static_cast<uint16_t*>(a.out) + m * a.out_stride + n;
@@ -552,7 +588,6 @@ block8_tile_kernel(const __grid_constant__ MatArgs a, const __grid_constant__ CU
             if (a.vec && n + 4 <= a.N) *reinterpret_cast<uint2*>(dst) = w;
             else store_piece(dst, make_uint4(w.x, w.y, 0u, 0u), a.N - n < 4 ? (int)(a.N - n) : 4, false);
         }
-        cluster.sync();   // no CTA ends while its sums may be read
     }
 }
 
@@ -588,39 +623,6 @@ struct PairMisc {
 };
 static_assert(sizeof(PairMisc) <= 512, "misc block");
 
-// A pair's tiles, from pair to pair: lane tiles in groups, so that the pairs at work share both matrices' rows in L2.
-struct PairWalk {
-    int g, in, lt, ct;      // group, tile in it; lane tile, column tile
-    __device__ __forceinline__ bool set(const MatArgs& a) {
-        for (;;) {
-            const int left = (int)a.lane_tiles - g * a.group, n = left < a.group ? left : a.group;
-            if (n <= 0) return false;
-            if (in < n * (int)a.col_tiles) {
-                ct = in / n;
-                lt = g * a.group + (in - ct * n);
-                return true;
-            }
-            in -= n * (int)a.col_tiles;
-            g++;
-        }
-    }
-    __device__ __forceinline__ bool start(const MatArgs& a) {
-        g = 0;
-        in = (int)(blockIdx.x >> 1);
-        return set(a);
-    }
-    __device__ __forceinline__ bool next(const MatArgs& a) {
-        in += (int)(gridDim.x >> 1);
-        return set(a);
-    }
-};
-
-// Address of the same place in the shared memory of a CTA of the cluster.
-__device__ __forceinline__ uint32_t at_rank(const void* p, uint32_t rank) {
-    uint32_t r;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(p)), "r"(rank));
-    return r;
-}
 // Arrival at a barrier of either CTA. What the other side may rely on goes through tensor memory (with its fences) and
 // the copies' own barrier, not through this thread's loads and stores, so that the arrival need not wait for those:
 // with .release.cluster here and .acquire.cluster in the waits a block took 2400 cycles.
@@ -685,7 +687,7 @@ block8_pair_kernel(const __grid_constant__ MatArgs a, const __grid_constant__ CU
     const uint32_t tmem = S->tmem;
     volatile int* abort_flag = &S->abort_flag;
     bool dead = *abort_flag != 0;
-    PairWalk w;
+    TileWalk w;
 
     // 168 registers a thread at launch: 256 x 208 + 128 x 88 of 384 x 168
     if (warp < 8) {
@@ -718,7 +720,7 @@ block8_pair_kernel(const __grid_constant__ MatArgs a, const __grid_constant__ CU
             pw = a.ws + (u < last ? u : last) * a.nb;
             fetch(0);
         };
-        bool more = w.start(a);
+        bool more = w.start(a, (int)(blockIdx.x >> 1));
         if (more) scales_of_tile();
         while (more && !dead) {
             const int r0 = w.lt * (2 * kLanes) + (int)rank * kLanes + row0, c = w.ct * T::TC + col0;    // the warp's first row and column
@@ -731,7 +733,7 @@ block8_pair_kernel(const __grid_constant__ MatArgs a, const __grid_constant__ CU
                 for (int i = 0; i < 4; i++) f[i] = fresh ? nx[i] * nw[i] : f[i < 3 ? i + 1 : 3];
                 if (fresh) {
                     if (kb + 4 < nb) fetch(kb + 4);
-                    else if ((more = w.next(a))) scales_of_tile();
+                    else if ((more = w.next(a, (int)(gridDim.x >> 1)))) scales_of_tile();
                 }
                 if (!__all_sync(0xffffffffu, pair_wait(&S->tfull[buf][half], ph, abort_flag, a.wait_ns))) {
                     dead = true;
@@ -796,7 +798,7 @@ block8_pair_kernel(const __grid_constant__ MatArgs a, const __grid_constant__ CU
             // -------------------------------------------------------- copies
             int st = 0, ph = 1;
             int64_t issued = 0;
-            for (bool more = w.start(a); more && !dead; more = w.next(a)) {
+            for (bool more = w.start(a, (int)(blockIdx.x >> 1)); more && !dead; more = w.next(a, (int)(gridDim.x >> 1))) {
                 const int xr = w.lt * (2 * kLanes) + (int)rank * kLanes, wr = w.ct * T::TC + (int)rank * (T::CW / 2);
                 for (int kb = 0; kb < nb; kb++) {
                     if (!__all_sync(0xffffffffu, pair_wait(&S->empty[st], ph, abort_flag, a.wait_ns))) {
@@ -833,7 +835,7 @@ block8_pair_kernel(const __grid_constant__ MatArgs a, const __grid_constant__ CU
                 const uint32_t a_lo = (uint32_t)desc, hi = (uint32_t)(desc >> 32);
                 const int buf = warp - 9;
                 int st = buf, ph = 0, tph = 1, kb = buf;
-                for (bool more = w.start(a); more && !dead; more = w.next(a)) {
+                for (bool more = w.start(a, (int)(blockIdx.x >> 1)); more && !dead; more = w.next(a, (int)(gridDim.x >> 1))) {
                     for (; kb < nb; kb += 2) {
                         if (!__all_sync(0xffffffffu, pair_wait(&S->ready[st], ph, abort_flag, a.wait_ns))) {
                             dead = true;
@@ -875,7 +877,7 @@ block8_pair_kernel(const __grid_constant__ MatArgs a, const __grid_constant__ CU
         } else {
             // -------------------------------------------------------- word of the CTA's stages
             int st = 0, ph = 0;
-            for (bool more = w.start(a); more && !dead; more = w.next(a))
+            for (bool more = w.start(a, (int)(blockIdx.x >> 1)); more && !dead; more = w.next(a, (int)(gridDim.x >> 1)))
                 for (int kb = 0; kb < nb; kb++) {
                     if (!__all_sync(0xffffffffu, pair_wait(&S->full[st], ph, abort_flag, a.wait_ns))) {
                         dead = true;
