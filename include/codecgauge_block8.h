@@ -34,8 +34,9 @@ int cg_block8_encode(int32_t dtype, int64_t R, int64_t K, int32_t rows, const vo
 
 /* out = x w^T: out[m][n] = sum_k x[m][k] w[n][k] of the matrices that the codes stand for; x [M][K] with
  * rows = 1, w [N][K] with rows = 128. A block's products are summed in fp32 on the tensor cores; the block's sum times
- * its two scales is added in fp32; the total is rounded once to dtype (CG_BF16 or CG_FP16; beyond its
- * range it becomes infinite). NaN codes and scales reach the outputs that they enter.
+ * the product of its two scales (rounded to fp32: it should be a normal number, or 0) is added in fp32; the total is
+ * rounded once to dtype (CG_BF16 or CG_FP16; beyond its range it becomes infinite). NaN codes and scales reach the
+ * outputs that they enter, and no others.
  *   M, N >= 0;  K : a multiple of 16, >= 16;  M, N, K <= 2^30
  *   codes 16-byte aligned, strides in bytes >= K (unless one row) and multiples of 16, below 2^40;  out_stride in
  *   elements, >= N (unless M < 2);  out aligned to 2 bytes (16 with out_stride a multiple of 8 is fastest).

@@ -207,7 +207,7 @@ struct Tile {
     static constexpr int kMost = 10;                            // stages
     static constexpr int kBufs = 4;                             // of tensor memory
     static constexpr uint32_t misc = 231936, total = misc + 512;
-    static_assert(split_ring % 1024 == 0 && split_ring + (kLanes + 12) * TC * 4 <= misc && ring <= misc && kMost * (kB + 1024) <= ring && total <= 232448, "tile");
+    static_assert(split_ring % 1024 == 0 && split_ring + (kLanes + 12) * TC * 4 <= misc && ring <= misc && ring + kWarps * 4096 <= misc && kMost * (kB + 1024) <= ring && total <= 232448, "tile");
 };
 
 struct MatArgs {
@@ -335,9 +335,53 @@ __device__ __forceinline__ void store_piece(uint16_t* dst, uint4 v, int valid, b
         if (e < valid) dst[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
 }
 
+// A warp's results in shared memory: boxes of 32 rows x 64 columns (4 KB) in the 128-byte swizzle. acc: the lane's row.
+template <int COLS>
+__device__ __forceinline__ void stage_results(unsigned char* box, const float2 (&acc)[COLS / 2], int fp16) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int q = 0; q < COLS / 8; q++) {
+        const uint4 b = make_uint4(pack(acc[4 * q].x, acc[4 * q].y, fp16), pack(acc[4 * q + 1].x, acc[4 * q + 1].y, fp16),
+                                   pack(acc[4 * q + 2].x, acc[4 * q + 2].y, fp16), pack(acc[4 * q + 3].x, acc[4 * q + 3].y, fp16));
+        *reinterpret_cast<uint4*>(box + (q >> 3) * 4096 + lane * 128 + (((q & 7) ^ (lane & 7)) << 4)) = b;
+    }
+}
+// Staged results to rows that begin anywhere, 8 rows at a time: a row's words of two values from its first even place on, side
+// by side in the warp, the ends alone. (Value by value from registers 8192 x 6147 x 4096 took 356 us.) out: the first row's
+// first column; rows <= 32, n <= COLS: rows and columns there are.
+template <int COLS>
+__device__ __forceinline__ void store_staged(const unsigned char* box, uint16_t* out, int64_t stride, int rows, int n) {
+    const int lane = threadIdx.x & 31, end = n - 1;   // the last column, in word end / 2
+#pragma unroll 1
+    for (int r0 = 0; r0 < rows; r0 += 8) {
+        uint32_t v[8][COLS / 64];                     // columns 2 lane, 2 lane + 1 of each box
+#pragma unroll
+        for (int k = 0; k < 8; k++)
+#pragma unroll
+            for (int i = 0; i < COLS / 64; i++)
+                v[k][i] = *reinterpret_cast<const uint32_t*>(box + i * 4096 + (r0 + k) * 128 + ((((lane >> 2) ^ k) << 4) | ((lane & 3) << 2)));
+#pragma unroll
+        for (int k = 0; k < 8; k++) {
+            if (r0 + k >= rows) break;
+            uint16_t* row = out + (r0 + k) * stride;
+            const int odd = (int)(reinterpret_cast<uintptr_t>(row) >> 1 & 1);
+#pragma unroll
+            for (int i = 0; i < COLS / 64; i++) {
+                uint32_t w = v[k][i];
+                const uint32_t down = __shfl_down_sync(0xffffffffu, w, 1), other = i + 1 < COLS / 64 ? __shfl_sync(0xffffffffu, v[k][(i + 1) % (COLS / 64)], 0) : 0u;
+                if (odd) w = __funnelshift_r(w, lane < 31 ? down : other, 16);
+                const int e = 64 * i + 2 * lane + odd;
+                if (e + 1 < n) *reinterpret_cast<uint32_t*>(row + e) = w;
+                if (((end - odd) & 1) == 0 && (end >> 1) == 32 * i + lane) row[end] = (uint16_t)(v[k][i] >> (16 * (end & 1)));
+            }
+            if (lane == 0 && odd) row[0] = (uint16_t)v[k][0];
+        }
+    }
+}
+
 // 32 columns of each lane's row. The lanes of a group of four transpose their pieces of 16 bytes, so that a store
 // instruction covers 64 bytes of 8 rows instead of 16 of 32. row: of the output, or null; left: its columns from here on.
-__device__ __forceinline__ void store_columns(uint32_t (&b)[16], uint16_t* row, int64_t left, bool vec) {
+__device__ __forceinline__ void store_columns(uint32_t (&b)[16], uint16_t* row, int left) {
     const int lane = threadIdx.x & 31, j = lane & 3;
 #pragma unroll
     for (int step = 1; step < 4; step *= 2) {
@@ -354,12 +398,12 @@ __device__ __forceinline__ void store_columns(uint32_t (&b)[16], uint16_t* row, 
             }
         }
     }
-    const int valid = left - 8 * j < 8 ? (int)(left - 8 * j) : 8;
+    const int valid = left - 8 * j < 8 ? left - 8 * j : 8;
 #pragma unroll
     for (int k = 0; k < 4; k++) {
         const uint64_t dst = __shfl_sync(0xffffffffu, reinterpret_cast<uint64_t>(row), (lane & 28) + k);
         if (dst && valid > 0)
-            store_piece(reinterpret_cast<uint16_t*>(dst) + 8 * j, make_uint4(b[4 * k], b[4 * k + 1], b[4 * k + 2], b[4 * k + 3]), valid, vec);
+            store_piece(reinterpret_cast<uint16_t*>(dst) + 8 * j, make_uint4(b[4 * k], b[4 * k + 1], b[4 * k + 2], b[4 * k + 3]), valid, true);
     }
 }
 
@@ -477,13 +521,23 @@ block8_tile_kernel(const __grid_constant__ MatArgs a, const __grid_constant__ CU
                 }
                 break;
             }
-            uint16_t* out = r < a.M ? static_cast<uint16_t*>(a.out) + r * a.out_stride + c : nullptr;
+            const int rows = a.M - (r - lane) < 32 ? (int)(a.M - (r - lane)) : 32, n = a.N - c < T::CW ? (int)(a.N - c) : T::CW;
+            if (rows <= 0 || n <= 0) continue;
+            uint16_t* out = static_cast<uint16_t*>(a.out) + (r - lane) * a.out_stride + c;   // (the warp's first row)
+            if (a.vec) {
 #pragma unroll
-            for (int q = 0; q < T::CW / 32; q++) {
-                uint32_t b[16];
+                for (int q = 0; q < T::CW / 32; q++) {
+                    uint32_t b[16];
 #pragma unroll
-                for (int k = 0; k < 16; k++) b[k] = pack(acc[16 * q + k].x, acc[16 * q + k].y, a.fp16);
-                if (c + 32 * q < a.N) store_columns(b, out ? out + 32 * q : nullptr, a.N - (c + 32 * q), a.vec);
+                    for (int k = 0; k < 16; k++) b[k] = pack(acc[16 * q + k].x, acc[16 * q + k].y, a.fp16);
+                    if (32 * q < n) store_columns(b, lane < rows ? out + lane * a.out_stride + 32 * q : nullptr, n - 32 * q);
+                }
+            } else {
+                unsigned char* box = smem + T::ring + warp * 4096;
+                stage_results<T::CW>(box, acc, a.fp16);
+                __syncwarp();
+                store_staged<T::CW>(box, out, a.out_stride, rows, n);
+                __syncwarp();
             }
         }
     } else if (warp == T::kWarps) {
@@ -763,15 +817,10 @@ block8_pair_kernel(const __grid_constant__ MatArgs a, const __grid_constant__ CU
                 ph ^= buf == 0;
             }
             if (dead) break;
-            if (a.vec) {
+            if (a.vec && (c + T::CW <= a.N || a.N % 8 == 0)) {   // (a TMA store ends at a multiple of 16 bytes)
                 if (lane == 0) bulk_wait_read<0>();   // the last tile's results have left
                 __syncwarp();
-#pragma unroll
-                for (int q = 0; q < T::CW / 8; q++) {
-                    const uint4 b = make_uint4(pack(acc[4 * q].x, acc[4 * q].y, a.fp16), pack(acc[4 * q + 1].x, acc[4 * q + 1].y, a.fp16),
-                                               pack(acc[4 * q + 2].x, acc[4 * q + 2].y, a.fp16), pack(acc[4 * q + 3].x, acc[4 * q + 3].y, a.fp16));
-                    *reinterpret_cast<uint4*>(out_sm + (q >> 3) * T::kOut + lane * 128 + (((q & 7) ^ (lane & 7)) << 4)) = b;
-                }
+                stage_results<T::CW>(out_sm, acc, a.fp16);
                 fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0 && r0 < a.M) {
@@ -781,14 +830,13 @@ block8_pair_kernel(const __grid_constant__ MatArgs a, const __grid_constant__ CU
                     bulk_commit();
                 }
             } else {
-                uint16_t* out = r0 + lane < a.M ? static_cast<uint16_t*>(a.out) + (int64_t)(r0 + lane) * a.out_stride + c : nullptr;
-#pragma unroll
-                for (int q = 0; q < T::CW / 32; q++) {
-                    uint32_t b[16];
-#pragma unroll
-                    for (int k = 0; k < 16; k++) b[k] = pack(acc[16 * q + k].x, acc[16 * q + k].y, a.fp16);
-                    if (c + 32 * q < a.N) store_columns(b, out ? out + 32 * q : nullptr, a.N - (c + 32 * q), false);
-                }
+                if (lane == 0) bulk_wait_read<0>();
+                __syncwarp();
+                stage_results<T::CW>(out_sm, acc, a.fp16);
+                __syncwarp();
+                const int rows = a.M - r0 < 32 ? (int)(a.M - r0) : 32, n = a.N - c < T::CW ? (int)(a.N - c) : T::CW;
+                if (rows > 0 && n > 0) store_staged<T::CW>(out_sm, static_cast<uint16_t*>(a.out) + (int64_t)r0 * a.out_stride + c, a.out_stride, rows, n);
+                __syncwarp();
             }
         }
         if (lane == 0) bulk_wait<0>();   // results are out before the CTA ends
@@ -1227,8 +1275,9 @@ cudaError_t launch_matmul(const MatArgs& a, const Matrices& m, cudaStream_t st) 
     int split = 1;
     const cudaError_t e = tile_split(a, &split);
     if (e != cudaSuccess) return e;
-    const int64_t t_tiles = (tiles * split + sms - 1) / sms * ((a.nb + split - 1) / split) * 36 + (split > 1 ? 130 : 0);
-    const int64_t t_pairs = (pairs + sms / 2 - 1) / (sms / 2) * a.nb * 45;
+    auto on_tiles = [&](int s) { return (tiles * s + sms - 1) / sms * ((a.nb + s - 1) / s) * 36 + (s > 1 ? 130 : 0); };
+    if (on_tiles(1) <= on_tiles(split)) split = 1;
+    const int64_t t_tiles = on_tiles(split), t_pairs = (pairs + sms / 2 - 1) / (sms / 2) * a.nb * 45;
     return t_pairs < t_tiles ? launch_pairs(a, m, st) : launch_tiles(a, m, split, st);
 }
 

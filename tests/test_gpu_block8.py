@@ -103,7 +103,9 @@ def test_encode_many_rows():
 # ------------------------------------------------------------------------------------ product
 SIZES = [(1, 1, 16), (1, 8, 128), (1, 6144, 4096), (2, 130, 144), (5, 1000, 272), (16, 128, 128), (17, 257, 640), (31, 96, 1040), (33, 2000, 4096), (64, 129, 384),
          (65, 128, 128), (65, 7, 2048), (100, 1000, 4112), (127, 200, 48), (128, 640, 1280), (129, 384, 256), (333, 1000, 4112), (500, 8, 512), (1000, 3000, 400),
-         (2048, 2560, 512), (2049, 2561, 528), (4097, 1153, 144), (300, 20000, 256), (20000, 300, 128), (16, 40000, 128), (40, 60000, 256), (3, 512, 16384)]
+         (2048, 2560, 512), (2049, 2561, 528), (4097, 1153, 144), (300, 20000, 256), (20000, 300, 128), (16, 40000, 128), (40, 60000, 256), (3, 512, 16384),
+         (1, 20000, 1040), (8, 9000, 272), (7, 70, 96), (8, 300, 8208), (9, 300, 400), (24, 130, 2064), (100, 40000, 272), (128, 1000, 1152),
+         (20000, 2000, 128), (3000, 3000, 384)]
 
 
 def _exact_case(M, N, K, seed=0):
@@ -179,13 +181,14 @@ def test_matmul(M, N, K, dtype):
     assert torch.equal(got, _matmul(*c, dtype).double()) and cg.get_status() == 0
 
 
-@pytest.mark.parametrize("M,N,K", [(4, 300, 400), (200, 300, 400), (2200, 2600, 144)])
+@pytest.mark.parametrize("M,N,K", [(4, 300, 400), (200, 300, 400), (2200, 2600, 144), (40, 2001, 144), (2200, 2601, 144), (2200, 2567, 272)])
 def test_strides(M, N, K):
-    """Matrices within wider ones."""
+    """Matrices within wider ones, the last piece of an output's row whole or not."""
     x, xs, w, ws = _exact_case(M, N, K)
     wide = lambda t, pad: torch.cat([t.view(torch.uint8), torch.full((t.shape[0], pad), 0x7f, dtype=torch.uint8, device="cuda")], 1).view(E4M3)[:, :K]  # noqa: E731
     want = _matmul(x, xs, w, ws)
-    assert torch.equal(_matmul(wide(x, 16), xs, wide(w, 240), ws, pad=8), want)
+    for pad in (8, -N % 8, -N % 8 + 8):
+        assert torch.equal(_matmul(wide(x, 16), xs, wide(w, 240), ws, pad=pad), want)
     assert torch.equal(_matmul(x[:1], xs[:1], wide(w, 16), ws), want[:1])
 
 
@@ -215,6 +218,18 @@ def test_special_values_reach_their_rows(M):
             hit[:, 128:256] = True
         got = _matmul(**t)
         assert torch.isnan(got[hit]).all() and torch.equal(got[~hit], want[~hit]), name
+
+
+@pytest.mark.parametrize("M", [1, 3, 60, 300, 2500])
+def test_a_row_does_not_depend_on_the_others(M):
+    """The same rows of x among others that hold NaN, and rows of w alone, give the same bits in the same kernel."""
+    N, K = 2600, 528
+    x, xs, w, ws = _real_case(M, N, K)
+    want = _matmul(x, xs, w, ws)
+    y, ys = x.clone(), xs.clone()
+    keep = torch.arange(M, device="cuda") % 3 == 0
+    y.view(torch.uint8)[~keep] = 0x7f
+    assert torch.equal(_matmul(y, ys, w, ws)[keep], want[keep])
 
 
 def test_results_beyond_the_type():

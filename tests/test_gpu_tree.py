@@ -208,6 +208,36 @@ def test_special_values_reach_who_sees_them(nodes, dtype, d):
         assert (torch.isnan(got) if value != value else got == value).all()
 
 
+def test_longer_rows_of_masks():
+    """More words than the nodes need: their bits count for nothing."""
+    for nodes in ([40, 3], [4, 2]):
+        c = _case(ctx=[70, 300], nodes=nodes)
+        want, lse = _attend(c)
+        more = np.full((c["masks"].shape[0], 3), 0xffffffff, np.uint32)
+        wide = dict(c, masks=np.concatenate([c["masks"], more], 1))
+        out, l2 = _attend(wide)
+        assert torch.equal(out, want) and torch.equal(l2, lse) and cg.get_status() == 0
+
+
+def test_queries_shared_by_heads():
+    """A stride of 0: one query for all heads of a token."""
+    for nodes in ([50, 3], [4, 2]):
+        c = _case(ctx=[70, 300], nodes=nodes)
+        one = c["q"][:, :1].cuda()
+        c["q"] = one.expand(-1, c["H"] * c["rep"], -1).contiguous().cpu()
+        want, lse = _attend(c)
+        out, l2 = _attend(c, q=one.expand(-1, c["H"] * c["rep"], -1), out=torch.full_like(want, 77.0))
+        assert torch.equal(out, want) and torch.equal(l2, lse)
+        _check(c, out, lse)
+
+
+def test_plan_without_rows():
+    got = _plan([], [3, 0], [0, 0, 0], 0, 1, 0)
+    assert got[0].size == 0 and cg.get_status() == 0
+    got = _plan([], [3, 0], [0, 0, 0], 4, 1, 5)
+    assert (got[0] == 0).all() and (got[1] == 0).all() and cg.get_status() == 0
+
+
 def test_a_chain_is_paged_attention():
     """With a chain's masks the rows see what paged_attention's see."""
     for ctx, nodes in (([100, 7], [30, 50]), ([100, 7], [2, 4])):
