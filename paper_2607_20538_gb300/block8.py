@@ -15,13 +15,22 @@ BLOCK = 128
 _E4M3 = torch.float8_e4m3fn
 
 
-def _matrix(name: str, t, dtype, dev: int):
-    """Checks a matrix on the device whose rows are contiguous; its address and row stride (0 for at most one row)."""
-    if t.dim() != 2 or t.dtype is not dtype or t.get_device() != dev:
+def _matrix(name: str, t, R: int, K: int, dtype, dev: int):
+    """Checks a matrix [R][K] on the device whose rows are contiguous; its address and row stride (0 for at most one row)."""
+    if t.shape != (R, K):
+        _p._bad(f"{name}: expected shape [{R}, {K}], got {list(t.shape)}")
+    if t.dtype is not dtype or t.get_device() != dev:
         _p._bad(f"{name}: expected a {dtype} matrix on device {dev}")
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    row, one = t.stride()
+    if one != 1 and K > 1:
         _p._bad(f"{name}: the last dimension must be contiguous")
-    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else 0)
+    return t.data_ptr(), (row if R > 1 else 0)
+
+
+def _shape(name: str, t):
+    if t.dim() != 2:
+        _p._bad(f"{name}: expected a matrix, got {list(t.shape)}")
+    return t.shape
 
 
 def _scales(name: str, t, R: int, K: int, rows: int, dev: int) -> int:
@@ -37,12 +46,9 @@ def block8_encode(x, codes, scales, rows: int = 1, stream=None) -> None:
     dev = _p._device()
     if rows not in (1, BLOCK):
         _p._bad(f"rows={rows}: must be 1 or {BLOCK}")
-    elem = _p._elem(x)
-    xp, xs = _matrix("x", x, x.dtype, dev)
-    cp, cs = _matrix("codes", codes, _E4M3, dev)
-    R, K = x.shape
-    if codes.shape != x.shape:
-        _p._bad(f"codes: expected shape {list(x.shape)}, got {list(codes.shape)}")
+    elem, (R, K) = _p._elem(x), _shape("x", x)
+    xp, xs = _matrix("x", x, R, K, x.dtype, dev)
+    cp, cs = _matrix("codes", codes, R, K, _E4M3, dev)
     _check(_p._fn("cg_block8_encode")(elem, R, K, rows, xp, xs, cp, cs, _scales("scales", scales, R, K, rows, dev), _p._stream(stream)))
 
 
@@ -50,14 +56,9 @@ def block8_matmul(x, x_scales, w, w_scales, out, stream=None) -> None:
     """out [M][N] (bf16 or fp16; rows may have a stride) = x w^T of the coded matrices x [M][K] (rows=1) and
     w [N][K] (rows=128) (cg_block8_matmul)."""
     dev = _p._device()
-    elem = _p._elem(out)
-    xp, xs = _matrix("x", x, _E4M3, dev)
-    wp, ws = _matrix("w", w, _E4M3, dev)
-    op, os = _matrix("out", out, out.dtype, dev)
-    (M, K), N = x.shape, w.shape[0]
-    if w.shape[1] != K:
-        _p._bad(f"w: expected shape [N, {K}], got {list(w.shape)}")
-    if out.shape != (M, N):
-        _p._bad(f"out: expected shape [{M}, {N}], got {list(out.shape)}")
+    elem, (M, K), N = _p._elem(out), _shape("x", x), _shape("w", w)[0]
+    xp, xs = _matrix("x", x, M, K, _E4M3, dev)
+    wp, ws = _matrix("w", w, N, K, _E4M3, dev)
+    op, os = _matrix("out", out, M, N, out.dtype, dev)
     _check(_p._fn("cg_block8_matmul")(elem, M, N, K, xp, xs, _scales("x_scales", x_scales, M, K, 1, dev), wp, ws,
                                       _scales("w_scales", w_scales, N, K, BLOCK, dev), op, os, _p._stream(stream)))
