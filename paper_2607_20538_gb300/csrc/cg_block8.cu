@@ -24,7 +24,8 @@ constexpr float kTop = 448.0f;
 // Encoding. 8 lanes a row of a block, 16 channels each: 32 bytes in, 16 bytes out. The largest |x| is found on the
 // bits (the order of non-negative numbers is that of their bits, infinities and NaN above all). A scale for one
 // row needs the 8 lanes alone, one for 128 rows a CTA, whose threads keep their 4 rows in registers. Bound: HBM, 3
-// bytes a value.
+// bytes a value: 8192 x 4096 19.4 us, 5.2 TB/s; 16384 x 16384 127 us, 6.3 TB/s; by 128 rows 16384 x 8192 66 us, 6.1 TB/s. (With
+// unpacked arithmetic those took 24.4, 164 and 81 us.)
 // ------------------------------------------------------------------------------------
 constexpr int kEncThreads = 256, kGroup = 8, kEncRows = kEncThreads / kGroup;   // rows of blocks of a CTA and turn
 
@@ -193,7 +194,8 @@ __global__ void __launch_bounds__(kEncThreads) encode_square_kernel(EncArgs a) {
 // what lies behind, and nobody reads them.
 // Few tiles: the blocks of channels are cut among the CTAs of a cluster; each writes its sums of a part of the rows into the
 // shared memory of the CTA that adds those up, in the order of the ranks whatever their timing. (Left where they were and
-// read from there they cost 333 x 1000 x 4112 4.1 us of 10.7, two rounds of loads' latency and a barrier more.)
+// read from there they cost 333 x 1000 x 4112 4.1 us of 10.7, two rounds of loads' latency and a barrier more.) Bound: what an
+// SM takes in by TMA, about 70 GB/s, and the start and end, 6 us: 333 x 1000 x 4112 9.3 us, 17 x 6144 x 4096 10.1, 256 15.7.
 // ------------------------------------------------------------------------------------
 constexpr int kLanes = 128;
 
@@ -649,6 +651,8 @@ block8_tile_kernel(const __grid_constant__ MatArgs a, const __grid_constant__ CU
 // Product of many rows: pairs of CTAs (a cluster of two, tcgen05 cta_group::2). A tile is 256 rows of x by 256 rows of
 // w; each CTA of the pair copies 128 rows of x and half the rows of w, and its tensor memory takes the sums of its
 // own rows with all columns, so that a product reads 32 KB a block and SM where a CTA for itself would read 48.
+// Bound: the tensor cores (512 cycles a block), and the sums' way through registers beside them: 8192 x 6144 x 4096 158 us, 2.6
+// PFLOP/s, in long runs 173 (power cap); 8192 x 8192 x 8192 383 us, 2.9. The products alone 122 us, with the sums read 131.
 // The two halves of the columns are products, buffers and barriers of their own (N = 128): while one half's sums are
 // read, the other's products run.
 //   warps 0 - 7   accumulate, as above: a thread a row and one half's columns, in 208 registers. Results go through
@@ -964,7 +968,7 @@ block8_pair_kernel(const __grid_constant__ MatArgs a, const __grid_constant__ CU
 // needs no tensor maps, which the host would make. All CTAs read the same few lines of x and its scales at
 // about the same time, which one slice of L2 serves: they come through L1 (scales copied block by block past it took 2 us
 // more). The order of the channels within a block is free as long as both operands have the same: a thread reads 16 bytes
-// of either.
+// of either. 1 x 6144 x 4096 7.2 to 8 us (25 MB; a plain read of them 5.6), 1 x 58368 x 4096 43 us, 5.6 TB/s.
 // Where the rows of w leave SMs idle, the blocks are cut among the CTAs of a cluster, added in the order of the ranks.
 // ------------------------------------------------------------------------------------
 constexpr int kFewThreads = 256, kFewRows = 16, kFewMost = 8, kFewWarps = kFewThreads / 32;

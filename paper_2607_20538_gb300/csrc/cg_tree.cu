@@ -61,7 +61,8 @@ __device__ __forceinline__ Tree load_tree(const int32_t* lens, const int32_t* cu
 // Tree plan. A CTA per request: words climbed by a warp each, into shared memory; then a thread per node
 // climbs from word to word, once for its depth and once more, from the last word of its row to the first, for the
 // bits. The nodes of a path within a word stand in order of depth, so that a window keeps a word's highest bits and
-// sinks its lowest. Bound: launch latency and two dependent loads (lengths, parents).
+// sinks its lowest. Bound: launch latency and two dependent loads (lengths, parents). In a graph: one tree of 8 nodes 1.7 us,
+// 256 of up to 64 2.1.
 // ------------------------------------------------------------------------------------
 constexpr int kPlanThreads = 128;
 
@@ -134,7 +135,8 @@ __global__ void __launch_bounds__(kPlanThreads) tree_plan_kernel(TreePlanArgs a)
 // table, then each thread moves the same 16 bytes of row after row, in ascending order and a batch at a time.
 // Row k receives row r_k >= k, and no later row of the path is read from a place already written, so a thread that
 // goes upwards needs nobody else's leave. Bound: chains of dependent loads (lengths, parents, table, rows) for few
-// rows; HBM, 4 H d layers bytes read and written a moved row, for many.
+// rows; HBM, 4 H d layers bytes read and written a moved row, for many. In a graph: one path in one layer 4.3 us, 64 paths of
+// trees of up to 48 nodes in 16 layers (25 MB) 10.4.
 // ------------------------------------------------------------------------------------
 constexpr int kCommitThreads = 256, kMoveBatch = 8;
 
