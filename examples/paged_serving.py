@@ -4,7 +4,11 @@ Each step takes the new tokens of a batch of requests (a prompt, a chunk or one 
     page_plan        pages for them out of the free stack, positions and pool slots
     rotary_append    queries and keys turned by their positions, keys and values into their pages
     paged_attention  the new tokens over the pages of their own request
-and page_release gives a finished request's pages back. The pool is at the same time a cache of the
+and page_release gives a finished request's pages back. Drafted continuations of the requests go through
+    tree_plan        positions and masks of each tree's nodes
+    tree_attention   the nodes over their request's pages and their own ancestors
+    tree_commit      the accepted path's keys and values move up, spare pages go back
+instead of paged_attention. The pool is at the same time a cache of the
 codec (one layer, the pages as the batch): at the end all pages are encoded and restored, and the next
 token attends over the restored pages.
 
@@ -61,6 +65,26 @@ class PagedLayer:
         self.free_count, self.free_left = self.free_left, self.free_count
         return out
 
+    def verify(self, new_lens, parents, q, k, v, max_new, accept):
+        """Drafted trees of every request as one step: parents int32 [n] (a node's place in its tree, -1: the last token held), q, k,
+        v as in step. accept(o) gives each request's accepted node (int32 [n_req], -1: none) from the nodes' outputs; those on
+        its path stay. Returns o."""
+        n = k.shape[0]
+        i32 = dict(dtype=torch.int32, device=self.device)
+        positions, masks, kept = torch.empty(n, **i32), torch.empty(n, -(-max_new // 32), **i32), torch.empty_like(self.lens)
+        slots = torch.empty(n, dtype=torch.int64, device=self.device)
+        cg.page_plan(self.pages, self.lens, new_lens, self.free_pages, self.free_count, self.block_table, self.next_lens, self.cu_new,
+                     positions, slots, self.free_left)
+        cg.tree_plan(max_new, parents, self.next_lens, self.cu_new, positions, masks, self.window, self.sinks)
+        turned, out = torch.empty_like(q), torch.empty_like(q)
+        cg.rotary_append(self.pages, self.turn, q, k, v, positions, slots, self.table, turned, self.pool)
+        how = cg.PagedAttention(self.n_rep, max_new, 1.0 / math.sqrt(self.pages.d), self.window, self.sinks)
+        cg.tree_attention(self.pages, how, turned, self.pool, self.block_table, self.next_lens, self.cu_new, positions, masks, out)
+        cg.tree_commit(self.pages, max_new, parents, accept(out), self.next_lens, self.cu_new, self.block_table, self.pool, kept,
+                       self.free_pages, self.free_left, self.free_count)
+        self.lens = kept
+        return out
+
     def release(self, done):
         """Give back the pages of the requests whose flag (int32 [n_req]) is set."""
         cg.page_release(self.pages, self.lens, done, self.block_table, self.free_pages, self.free_count, self.next_lens, self.free_left)
@@ -112,6 +136,12 @@ def main(argv=None):
     layer.step(new, *tokens(93, layer, gen), max_new=90)
     print(f"after a release and a new prompt of 90: lengths {layer.lens.tolist()}, "
           f"{layer.pages.n_pages - int(layer.free_count)} pages in use")
+
+    # a drafted tree of 6 nodes for each request: two continuations of two tokens and one of one behind a common first;
+    # here the first node's second child is accepted for all, which leaves two tokens
+    parents = torch.tensor([-1, 0, 1, 0, 3, 0] * len(prompts), **i32)
+    layer.verify(6 * ones, parents, *tokens(6 * len(prompts), layer, gen), max_new=6, accept=lambda o: 3 * ones)
+    print(f"after a step of drafted trees: lengths {layer.lens.tolist()}, {layer.pages.n_pages - int(layer.free_count)} pages in use")
 
     # the same next token over the pages and over the pages as the codec restores them
     restored, ratio = layer.coded(a.bits)
