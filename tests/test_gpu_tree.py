@@ -164,6 +164,16 @@ CASES = {
 }
 
 
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_every_cut_of_a_tree(d):
+    """One tree after histories of one tile after the other: the shares of the CTAs begin and end at every place of a tile."""
+    for ctx in list(range(120, 1700, 128)) + [127, 128, 129, 255, 256, 257, 3000]:
+        c = _case(ctx=[ctx], nodes=[9], H=1, rep=3, d=d, seed=ctx)
+        out, lse = _attend(c)
+        assert cg.get_status() == 0
+        _check(c, out, lse)
+
+
 @pytest.mark.parametrize("name", list(CASES))
 def test_attention(name):
     c = _case(**CASES[name], seed=len(name))
