@@ -24,7 +24,7 @@ constexpr float kTop = 448.0f;
 // Encoding. 8 lanes a row of a block, 16 channels each: 32 bytes in, 16 bytes out. The largest |x| is found on the
 // bits (the order of non-negative numbers is that of their bits, infinities and NaN above all). A scale for one
 // row needs the 8 lanes alone, one for 128 rows a CTA, whose threads keep their 4 rows in registers. Bound: HBM, 3
-// bytes a value: 8192 x 4096 19.4 us, 5.2 TB/s; 16384 x 16384 127 us, 6.3 TB/s; by 128 rows 16384 x 8192 66 us, 6.1 TB/s. (With
+// bytes a value: 8192 x 4096 19.1 us, 5.3 TB/s; 16384 x 16384 127 us, 6.3 TB/s; by 128 rows 16384 x 8192 66 us, 6.1 TB/s. (With
 // unpacked arithmetic those took 24.4, 164 and 81 us.)
 // ------------------------------------------------------------------------------------
 constexpr int kEncThreads = 256, kGroup = 8, kEncRows = kEncThreads / kGroup;   // rows of blocks of a CTA and turn
@@ -1340,8 +1340,9 @@ CG_EXPORT int cg_block8_encode(int32_t dtype, int64_t R, int64_t K, int32_t rows
     a.stride = R > 1 ? stride : K;
     a.nb = (K + kBlock - 1) / kBlock;
     const int64_t items = rows == 1 ? (R * a.nb + kEncRows - 1) / kEncRows : (R + kBlock - 1) / kBlock * a.nb;
-    // Long matrices: 8 CTAs an SM that go on, two blocks of a row at a time (8192 x 4096: 24.4 us with a CTA for 32 blocks)
-    const int64_t room = 8 * (int64_t)tc::num_sms();
+    // Long matrices: as many CTAs as run at once go on, two blocks of a row at a time (8192 x 4096: 19.1 us, 21 with one block, 24.4
+    // with a CTA for 32 blocks; 1024 x 4096 3.8 us, 4.2 with 8 CTAs an SM)
+    const int64_t room = (rows == 1 ? 4 : 8) * (int64_t)tc::num_sms();
     const unsigned grid = (unsigned)(items < room ? items : room);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     const bool fp16 = dtype == CG_FP16;
