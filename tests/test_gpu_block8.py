@@ -249,6 +249,35 @@ def test_zeros_and_no_rows():
     assert cg.get_status() == 0
 
 
+@pytest.mark.parametrize("M,N,K", [(300000, 8192, 128), (1100000, 128, 4096), (5, 1100000, 4096), (2, 40, 1 << 20), (300, 200, 1 << 18)])
+def test_offsets_past_32_bits_and_long_rows(M, N, K):
+    """Results, codes of x and codes of w beyond 2^32 bytes, and rows of a million channels: sampled rows and columns, equal."""
+    gen = torch.Generator(device="cuda").manual_seed(K)
+    make = lambda R: torch.randint(0, 2, (R, K), generator=gen, device="cuda", dtype=torch.uint8).mul_(0x38).view(E4M3)  # noqa: E731  (0 and 1)
+    x, w = make(M), make(N)
+    xs, ws = torch.ones(M, _up(K, 128), device="cuda"), torch.ones(_up(N, 128), _up(K, 128), device="cuda")
+    xs[::2] *= 2
+    out = torch.empty(M, N, dtype=torch.bfloat16, device="cuda")
+    cg.block8_matmul(x, xs, w, ws, out)
+    r = torch.unique(torch.cat([torch.tensor([0, M - 1]), torch.randint(0, M, (40,), generator=torch.Generator().manual_seed(1))])).cuda()
+    c = torch.unique(torch.cat([torch.tensor([0, N - 1]), torch.randint(0, N, (40,), generator=torch.Generator().manual_seed(2))])).cuda()
+    # at most 2 2^20 < 2^24: exact in fp32
+    want = (x.view(torch.uint8)[r] > 0).double() @ (w.view(torch.uint8)[c] > 0).double().T * xs[r, :1].double()
+    assert torch.equal(out[r][:, c], want.to(torch.bfloat16)) and cg.get_status() == 0
+
+
+def test_encode_past_32_bits():
+    R, K = 1100000, 4096
+    x = torch.zeros(R, K, dtype=torch.bfloat16, device="cuda")
+    r = torch.tensor([0, 1, 524287, 524288, 1048575, 1048576, R - 1], device="cuda")
+    x[r] = torch.randn(len(r), K, device="cuda").bfloat16()
+    codes, scales = torch.empty(R, K, dtype=E4M3, device="cuda"), torch.empty(R, K // 128, device="cuda")
+    cg.block8_encode(x, codes, scales)
+    want, ws = _encoded(x[r].cpu(), 1)
+    assert torch.equal(codes.view(torch.uint8)[r].cpu(), want) and torch.equal(scales[r].cpu(), ws)
+    assert int((scales != 0).any(1).sum()) == len(r) and cg.get_status() == 0
+
+
 @pytest.mark.parametrize("M", [1, 100, 2500])
 def test_graph_and_streams(M):
     """Encoding and product on a side stream, then captured and replayed on other values."""

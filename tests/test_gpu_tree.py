@@ -360,6 +360,23 @@ def test_commit(n_req, page, ctx, most, layers, H, d):
     assert torch.equal(one[0].view(torch.int16), want[0][0]) and cg.get_status() == 0
 
 
+def test_commit_in_a_pool_past_32_bits():
+    """Pages of the pool's end, whose rows lie beyond 2^31 elements."""
+    H, page, d, n_pages, n = 16, 256, 256, 1100, 300
+    pool = torch.zeros(2, n_pages, H, page, d, dtype=torch.bfloat16, device="cuda")
+    table = np.array([[n_pages - 1, n_pages - 2]])
+    for j in (0, 1):
+        pool[:, table[0, j]] = torch.randn(2, H, page, d, device="cuda").bfloat16()
+    c = dict(page=page, H=H, d=d, n_pages=2, parents=ref.random_parents(np.random.default_rng(1), n), leaves=[n - 1], lens=np.array([n + 5]), cu=np.array([0, n]),
+             table=np.array([[1, 0]]), pool=pool[None, :, n_pages - 2:].cpu(), stack=np.full(2, -9), count=0, most=n)
+    want = _committed(c)
+    pages = cg.Pages(n_pages=n_pages, page=page, H=H, d=d, n_req=1, max_pages=2)
+    left, stack, free_left = i32([77]), i32(np.full(n_pages, -9)), i32([77])
+    cg.tree_commit(pages, n, i32(c["parents"]), i32(c["leaves"]), i32(c["lens"]), i32(c["cu"]), i32(table), pool, left, stack, i32([0]), free_left)
+    assert cg.get_status() == 0 and left.tolist() == want[1] and free_left.item() == want[3]
+    assert torch.equal(pool[:, n_pages - 2:].cpu().view(torch.int16), want[0][0])
+
+
 def test_commit_of_the_largest_tree():
     c = _commit_case(1, 16, 3, 8192, 1, 1, 64)
     for parents in ([-1 if k == 0 else max(0, k - 2) for k in range(8192)], [k - 1 for k in range(8192)], [-1] * 8192):
