@@ -44,6 +44,8 @@ def block8_encode(x, codes, scales, rows: int = 1, stream=None) -> None:
     """codes and scales of x [R][K] (bf16 or fp16, K a multiple of 16; rows may have a stride), a scale for each
     128 channels of a row (rows=1: activations) or of 128 rows (rows=128: weights) (cg_block8_encode)."""
     dev = _p._device()
+    if dev >= 0 and _p._took("block8_encode", x, codes, scales, rows, dev, _p._stream(stream)):
+        return
     if rows not in (1, BLOCK):
         _p._bad(f"rows={rows}: must be 1 or {BLOCK}")
     elem, (R, K) = _p._elem(x), _shape("x", x)
@@ -56,6 +58,8 @@ def block8_matmul(x, x_scales, w, w_scales, out, stream=None) -> None:
     """out [M][N] (bf16 or fp16; rows may have a stride) = x w^T of the coded matrices x [M][K] (rows=1) and
     w [N][K] (rows=128) (cg_block8_matmul)."""
     dev = _p._device()
+    if dev >= 0 and _p._took("block8_matmul", x, x_scales, w, w_scales, out, dev, _p._stream(stream)):
+        return
     elem, (M, K), N = _p._elem(out), _shape("x", x), _shape("w", w)[0]
     xp, xs = _matrix("x", x, M, K, _E4M3, dev)
     wp, ws = _matrix("w", w, N, K, _E4M3, dev)

@@ -4,11 +4,13 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcodecgauge.so")
+CALLS = os.path.join(HERE, "_calls.so")
 BUILD_DIR = os.path.join(HERE, "_build")
 SOURCES = ["cg_api.cu", "cg_simt.cu", "cg_tc.cu", "cg_tc_rows.cu", "cg_tc_dec.cu", "cg_tc_keydec.cu",
            "cg_noalloc.cu", "cg_attn.cu", "cg_paged.cu", "cg_paged_attn.cu",
@@ -64,7 +66,22 @@ def build(force: bool = False, verbose: bool = False, ptxas_verbose: bool = Fals
         tmp = LIB + f".tmp{os.getpid()}"
         subprocess.check_call([nvcc(), *ARCH, "-shared", "-o", tmp, *objs, "-lcudart"])
         os.replace(tmp, LIB)
+    _build_calls(force)
     return LIB
+
+
+def _build_calls(force: bool) -> None:
+    """The short way from Python to some entry points (csrc/cg_calls.c), for this interpreter. Where its headers are
+    missing the calls go by ctypes."""
+    src, inc = os.path.join(CSRC, "cg_calls.c"), sysconfig.get_path("include")
+    if not os.path.exists(os.path.join(inc, "Python.h")):
+        sys.stderr.write(f"no Python.h in {inc}: calls go by ctypes\n")
+        return
+    headers = [os.path.join(HERE, "..", "include", f) for f in ("codecgauge_tree.h", "codecgauge_block8.h", "codecgauge_paged.h")]
+    if force or _stale(CALLS, [src, *headers, __file__]):
+        tmp = CALLS + f".tmp{os.getpid()}"
+        subprocess.check_call(["gcc", "-O2", "-Wall", "-Werror", "-shared", "-fPIC", f"-I{inc}", src, "-o", tmp])
+        os.replace(tmp, CALLS)
 
 
 if __name__ == "__main__":

@@ -117,6 +117,36 @@ def _bad(msg: str):
     raise CodecGaugeError(-1, msg)
 
 
+_short = None
+
+
+def _short_calls():
+    """The module of the short calls (csrc/cg_calls.c), set up; False where it is not built."""
+    global _short
+    try:
+        from . import _calls
+    except ImportError:
+        _short = False
+    else:
+        at = [ctypes.cast(getattr(load(), f), _vp).value for f in (
+            "cg_tree_plan", "cg_tree_attention", "cg_tree_commit", "cg_block8_encode", "cg_block8_matmul")]
+        _calls.setup(torch.Tensor, torch.int32, torch.float32, torch.bfloat16, torch.float16, torch.float8_e4m3fn, *at)
+        _short = _calls
+    return _short
+
+
+def _took(name: str, *args) -> bool:
+    """The call by its short way (csrc/cg_calls.c), which finds the arguments as they should be and makes it, or does
+    nothing and returns False: then the caller's own checks say what is wrong, or make the call."""
+    short = _short_calls() if _short is None else _short
+    if not short:
+        return False
+    rc = getattr(short, name)(*args)
+    if rc:
+        _check(rc)
+    return rc is not None
+
+
 _INT32, _INT64, _FLOAT32 = torch.int32, torch.int64, torch.float32
 _ELEM = {torch.bfloat16: CG_BF16, torch.float16: CG_FP16}
 
@@ -282,6 +312,12 @@ def _workspace(pages: Pages, how: PagedAttention, n: int, device):
     return kept
 
 
+def _own_workspace(pages: Pages, how: PagedAttention, n: int, device, stream):
+    if stream is not None and stream != torch.cuda.current_stream():
+        _bad("workspace: needed on a stream that is not the current one")
+    return _workspace(pages, how, n, device)
+
+
 def _attend(name: str, pages: Pages, how: PagedAttention, q, pool, block_table, seq_lens, cu_new, out, lse, workspace, stream,
             words=(), masks=()) -> None:
     """The call of an attention entry point: `words` before its tensors, `masks` behind the lengths."""
@@ -295,9 +331,7 @@ def _attend(name: str, pages: Pages, how: PagedAttention, q, pool, block_table, 
         lp = lse.data_ptr()
     cp, ca = pages.c(_elem(pool)), _attn(pages, how, n, qt, qh, ot, oh)
     if workspace is None:
-        if stream is not None and stream != torch.cuda.current_stream():
-            _bad("workspace: needed on a stream that is not the current one")
-        workspace = _workspace(pages, how, n, q.device)
+        workspace = _own_workspace(pages, how, n, q.device, stream)
     elif workspace.get_device() != dev or not workspace.is_contiguous():
         _bad(f"workspace: expected a contiguous tensor on device {dev}")
     r = pages.n_req

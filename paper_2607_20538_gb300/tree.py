@@ -19,7 +19,10 @@ def _masks(masks, n: int, dev: int):
 def tree_plan(max_new: int, parents, seq_lens, cu_new, positions, masks, window: int = 0, sinks: int = 0, stream=None) -> None:
     """Positions and masks of the nodes of every request's tree (cg_tree_plan). The number of requests is
     seq_lens.numel(), of rows positions.numel(); masks int32 [rows][words], 32 words >= max_new."""
-    r, n, dev = seq_lens.numel(), positions.numel(), _p._device()
+    dev = _p._device()
+    if dev >= 0 and _p._took("tree_plan", max_new, window, sinks, parents, seq_lens, cu_new, positions, masks, dev, _p._stream(stream)):
+        return
+    r, n = seq_lens.numel(), positions.numel()
     mp, words = _masks(masks, n, dev)
     _check(_p._fn("cg_tree_plan")(
         r, n, max_new, window, sinks, _p._i32("parents", parents, n, dev), _p._i32("seq_lens", seq_lens, r, dev),
@@ -31,6 +34,11 @@ def tree_attention(pages: Pages, how: PagedAttention, q, pool, block_table, seq_
     """paged_attention of the nodes: each over its request's history and the nodes of its mask
     (cg_tree_attention). positions may be None without a window; the workspace is paged_attention's."""
     n, dev = q.shape[0], _p._device()
+    if q.get_device() == dev:
+        room = _p._own_workspace(pages, how, n, q.device, stream) if workspace is None else workspace
+        if _p._took("tree_attention", pages, how, q, pool, block_table, seq_lens, cu_new, positions, masks, out, lse, room, dev,
+                    _p._stream(stream)):
+            return
     mp, words = _masks(masks, n, dev)
     if positions is None and how.window:
         _p._bad("positions: needed with a window")
@@ -44,7 +52,11 @@ def tree_commit(pages: Pages, max_new: int, parents, leaves, seq_lens, cu_new, b
     back on the stack (cg_tree_commit). leaves: each request's accepted node, -1: none. pool: one layer's
     [2][n_pages][H][page][d], several [layers][2][n_pages][H][page][d], or None (lengths and pages alone); without
     lens_left, free_pages, free_count and free_left only rows move."""
-    n, r, dev = parents.numel(), pages.n_req, _p._device()
+    dev = _p._device()
+    if dev >= 0 and _p._took("tree_commit", pages, max_new, parents, leaves, seq_lens, cu_new, block_table, pool, lens_left,
+                             free_pages, free_count, free_left, dev, _p._stream(stream)):
+        return
+    n, r = parents.numel(), pages.n_req
     layers, pp, elem = 0, None, _p.CG_BF16
     if pool is not None:
         layers, elem = (pool.shape[0] if pool.dim() == 6 else 1), _p._elem(pool)
