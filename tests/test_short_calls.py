@@ -10,7 +10,7 @@ import pytest
 import torch
 
 import paper_2607_20538_gb300 as cg
-from paper_2607_20538_gb300 import block8, paged, tree  # noqa: F401
+from paper_2607_20538_gb300 import build, paged
 
 BF16, FP16, F32, I32, E4M3 = torch.bfloat16, torch.float16, torch.float32, torch.int32, torch.float8_e4m3fn
 NAMES = ["tree_plan", "tree_attention", "tree_commit", "block8_encode", "block8_matmul"]
@@ -23,11 +23,10 @@ class Calls:
     number as a device is -1."""
 
     def __init__(self, tmp_path, monkeypatch):
-        here = os.path.join(os.path.dirname(cg.__file__), "_calls.so")
-        if not os.path.exists(here):
+        if not os.path.exists(build.CALLS):
             pytest.skip("built where Python's headers are")
         copy = str(tmp_path / "_calls.so")
-        shutil.copy(here, copy)
+        shutil.copy(build.CALLS, copy)
         spec = importlib.util.spec_from_file_location("_calls", copy)
         self.module = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(self.module)
@@ -125,8 +124,6 @@ def test_same_call(name, calls):
     kw = KW[name]()
     short, python = calls.both(name, kw, PYTHON[name])
     assert len(short) == 1 and short == python
-    for t in (kw.values() if name != "tree_commit" else ()):
-        assert t is not None
     optional = {"tree_attention": (dict(lse=None), dict(positions=None)),
                 "tree_commit": (dict(pool=None), dict(pool=_t(2, 8, 2, 16, 128, dtype=FP16)),
                                 dict.fromkeys(("lens_left", "free_pages", "free_count", "free_left"))),
@@ -175,3 +172,53 @@ def test_a_status_raises(monkeypatch):
     with pytest.raises(cg.CodecGaugeError) as e:
         paged._took("tree_plan", -2)
     assert e.value.code == -2
+
+
+def _step(device="cuda"):
+    """One step of two trees and a product: the outputs of the five calls."""
+    g = torch.Generator().manual_seed(3)
+    i32 = lambda v: torch.tensor(v, dtype=I32, device=device)  # noqa: E731
+    rand = lambda *s: torch.randn(s, generator=g).to(device)  # noqa: E731
+    parents, lens, cu, table = i32([-1, 0, 0, -1, 0]), i32([21, 18]), i32([0, 3, 5]), i32([[3, 5, -1, -1], [1, 0, -1, -1]])
+    positions, masks = torch.full((5,), -1, dtype=I32, device=device), torch.zeros((5, 1), dtype=I32, device=device)
+    cg.tree_plan(3, parents, lens, cu, positions, masks)
+    pool, q = rand(2, 8, 2, 16, 128).to(BF16), rand(5, 8, 128).to(BF16)
+    out, lse = torch.empty_like(q), torch.empty((5, 8), dtype=F32, device=device)
+    cg.tree_attention(PAGES, HOW, q, pool, table, lens, cu, positions, masks, out, lse)
+    left, free, count, free_left = i32([0, 0]), i32([2, 4, 6, 7, 0, 0, 0, 0]), i32([4]), i32([0])
+    cg.tree_commit(PAGES, 3, parents, i32([2, -1]), lens, cu, table, pool, left, free, count, free_left)
+    x, w = rand(7, 272).to(BF16), rand(130, 272).to(BF16)
+    xc, wc = torch.empty((7, 272), dtype=E4M3, device=device), torch.empty((130, 272), dtype=E4M3, device=device)
+    xs, ws = torch.empty((7, 3), dtype=F32, device=device), torch.empty((2, 3), dtype=F32, device=device)
+    y = torch.empty((7, 130), dtype=BF16, device=device)
+    cg.block8_encode(x, xc, xs)
+    cg.block8_encode(w, wc, ws, rows=128)
+    cg.block8_matmul(xc, xs, wc, ws, y)
+    return [t.cpu() for t in (positions, masks, out, lse, pool, left, free, free_left, xc.view(torch.uint8), xs, wc.view(torch.uint8), ws, y)]
+
+
+@pytest.mark.gpu
+def test_a_step_goes_the_short_way(monkeypatch):
+    """And gives what it gives by Python and ctypes."""
+    if not os.path.exists(build.CALLS):
+        pytest.skip("built where Python's headers are")
+    by_ctypes = []
+    fn = paged._fn
+    monkeypatch.setattr(paged, "_fn", lambda name: by_ctypes.append(name) or fn(name))
+    monkeypatch.setattr(paged, "_short", None)
+    short = _step()
+    assert not [n for n in by_ctypes if "workspace_bytes" not in n]
+    monkeypatch.setattr(paged, "_short", False)
+    longer = _step()
+    assert len([n for n in by_ctypes if "workspace_bytes" not in n]) == 6
+    assert all(torch.equal(a, b) for a, b in zip(short, longer))
+    assert cg.get_status() == 0
+
+
+@pytest.mark.gpu
+def test_a_tensor_elsewhere_is_refused():
+    x, codes, scales = (t.cuda() for t in list(_encode().values())[:3])
+    with pytest.raises(cg.CodecGaugeError, match="scales"):
+        cg.block8_encode(x, codes, scales.cpu())
+    with pytest.raises(cg.CodecGaugeError, match="q:"):
+        cg.tree_attention(**dict({k: v.cuda() if isinstance(v, torch.Tensor) else v for k, v in _attention().items()}, q=_attention()["q"]))
