@@ -76,7 +76,7 @@ int cg_tree_attention(const cg_pages* pages, const cg_paged_attn* how, int32_t m
  *   pool may be NULL (layers 0): only lengths and pages, H, d and dtype ignored; lens_left may be NULL (then free_pages, free_count
  *   and free_left too): only rows. A request may be committed once: its rows have moved then.
  * A request whose lengths do not fit keeps them: lens_left[i] = seq_lens[i] (0 for a negative one).
- * lens_left and free_left must not alias the inputs. max_new: 0 .. CG_TREE_NODES. One launch. */
+ * lens_left, free_left and free_pages must not alias the inputs or one another. max_new: 0 .. CG_TREE_NODES. One launch. */
 int cg_tree_commit(const cg_pages* pages, int32_t n_tok, int32_t max_new, int32_t layers, const int32_t* parents,
                    const int32_t* leaves, const int32_t* seq_lens, const int32_t* cu_new, const int32_t* block_table,
                    void* pool, int32_t* lens_left, int32_t* free_pages, const int32_t* free_count,

@@ -1329,6 +1329,7 @@ CG_EXPORT int cg_block8_encode(int32_t dtype, int64_t R, int64_t K, int32_t rows
     if (!x || !codes || !scales) return set_error(CG_EINVAL, "null x, codes or scales");
     if (!al16(x) || !al16(codes) || (reinterpret_cast<uintptr_t>(scales) & 3u))
         return set_error(CG_EINVAL, "x and codes must be 16-byte aligned, scales to 4 bytes");
+    if (codes == x || scales == x || scales == codes) return set_error(CG_EINVAL, "the outputs must not overlap x or one another");
     EncArgs a{};
     if ((rc = device_status(&a.status))) return rc;
     a.x = static_cast<const uint16_t*>(x);
@@ -1381,7 +1382,7 @@ CG_EXPORT int cg_block8_matmul(int32_t dtype, int64_t M, int64_t N, int64_t K, c
     if (!al16(x) || !al16(w) || ((reinterpret_cast<uintptr_t>(x_scales) | reinterpret_cast<uintptr_t>(w_scales)) & 3u) ||
         (reinterpret_cast<uintptr_t>(out) & 1u))
         return set_error(CG_EINVAL, "x and w must be 16-byte aligned, scales and out to their type");
-    if (out == x || out == w) return set_error(CG_EINVAL, "out must not overlap the inputs");
+    if (out == x || out == w || out == x_scales || out == w_scales) return set_error(CG_EINVAL, "out must not overlap the inputs");
     MatArgs a{};
     if ((rc = device_status(&a.status))) return rc;
     a.xs = x_scales;

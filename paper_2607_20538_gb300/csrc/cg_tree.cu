@@ -415,9 +415,12 @@ CG_EXPORT int cg_tree_commit(const cg_pages* pages, int32_t n_tok, int32_t max_n
                           (const void*)lens_left, (const void*)free_pages, (const void*)free_count, (const void*)free_left})
         if (!al4(p)) return set_error(CG_EINVAL, "pointers must be aligned to their type");
     if (!al16(pool)) return set_error(CG_EINVAL, "pool must be 16-byte aligned");
-    if (give)
+    if (give) {
         for (const int32_t* p : {parents, leaves, seq_lens, cu_new, block_table, free_count})
-            if (p && (p == lens_left || p == free_left)) return set_error(CG_EINVAL, "lens_left and free_left must not alias the inputs");
+            if (p && (p == lens_left || p == free_left || p == free_pages)) return set_error(CG_EINVAL, "lens_left, free_left and free_pages must not alias the inputs");
+        if (lens_left == free_left || lens_left == free_pages || free_left == free_pages)
+            return set_error(CG_EINVAL, "lens_left, free_left and free_pages must not alias one another");
+    }
     if (!give && !pool) return CG_OK;
     CommitArgs a{};
     if ((rc = device_status(&a.status))) return rc;

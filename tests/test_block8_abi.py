@@ -50,6 +50,14 @@ def test_refusals(lib, call, kw, code):
     assert lib.cg_last_error().decode()
 
 
+@pytest.mark.parametrize("call,kw", [
+    (_encode, dict(codes=FAKE)), (_encode, dict(scales=FAKE)), (_encode, dict(scales=2 * FAKE)), (_matmul, dict(out=3 * FAKE)), (_matmul, dict(out=2 * FAKE)),
+    (_matmul, dict(out=4 * FAKE)),
+])
+def test_outputs_in_the_place_of_others(lib, call, kw):
+    assert call(**kw) == -1 and b"overlap" in lib.cg_last_error()
+
+
 def test_nothing_to_do(lib):
     assert _encode(R=0) == 0 and _matmul(M=0) == 0 and _matmul(N=0) == 0
     assert _encode(R=0, x=None, codes=None, scales=None) == 0

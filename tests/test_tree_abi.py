@@ -85,6 +85,13 @@ def _make(call, t, **kw):
      "commit": lambda: cg.tree_commit(pages, 5, **t, **kw)}[call]()
 
 
+@pytest.mark.parametrize("kw", [
+    *(dict([(o, i * FAKE)]) for o in ("left", "free", "free_left") for i in (1, 2, 3, 4, 5, 9)), dict(left=8 * FAKE), dict(free_left=7 * FAKE), dict(free_left=8 * FAKE),
+])
+def test_commit_in_the_place_of_others(lib, kw):
+    assert _commit(**kw) == -1 and b"alias" in lib.cg_last_error()
+
+
 @pytest.fixture
 def calls(monkeypatch):
     made = []
