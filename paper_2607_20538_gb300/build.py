@@ -1,7 +1,9 @@
 """Build libcodecgauge.so in-tree with nvcc for sm_103a (one -gencode, TUs in parallel)."""
 from __future__ import annotations
 
+import importlib.util
 import os
+import runpy
 import subprocess
 import sys
 import sysconfig
@@ -55,33 +57,46 @@ def build(force: bool = False, verbose: bool = False, ptxas_verbose: bool = Fals
         r = subprocess.run(cmd, capture_output=True, text=True)
         return cmd, r
 
-    with ThreadPoolExecutor(max_workers=len(SOURCES)) as ex:
+    with ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
+        calls = ex.submit(_build_calls, force)
         for cmd, r in ex.map(run, jobs):
             if verbose or ptxas_verbose or r.returncode:
                 sys.stderr.write(r.stdout + r.stderr)
             if r.returncode:
                 raise RuntimeError(f"nvcc failed: {' '.join(cmd)}")
+        calls.result()
     objs = [os.path.join(BUILD_DIR, s.replace(".cu", ".o")) for s in SOURCES]
     if force or jobs or _stale(LIB, objs):
         tmp = LIB + f".tmp{os.getpid()}"
         subprocess.check_call([nvcc(), *ARCH, "-shared", "-o", tmp, *objs, "-lcudart"])
         os.replace(tmp, LIB)
-    _build_calls(force)
     return LIB
 
 
 def _build_calls(force: bool) -> None:
-    """The short way from Python to some entry points (csrc/cg_calls.c), for this interpreter. Where its headers are
-    missing the calls go by ctypes."""
-    src, inc = os.path.join(CSRC, "cg_calls.c"), sysconfig.get_path("include")
-    if not os.path.exists(os.path.join(inc, "Python.h")):
-        sys.stderr.write(f"no Python.h in {inc}: calls go by ctypes\n")
-        return
+    """The short way from Python to some entry points (csrc/cg_calls.cpp), for this interpreter and torch. Where their
+    headers are missing the calls go by ctypes."""
+    src, inc = os.path.join(CSRC, "cg_calls.cpp"), sysconfig.get_path("include")
+    spec = importlib.util.find_spec("torch")
+    torch = os.path.dirname(spec.origin) if spec and spec.origin else ""
+    for h in (os.path.join(inc, "Python.h"), os.path.join(torch, "include/torch/csrc/autograd/python_variable.h")):
+        if not os.path.exists(h):
+            sys.stderr.write(f"no {h}: calls go by ctypes\n")
+            return
+    version = runpy.run_path(os.path.join(torch, "version.py"))["__version__"]
+    built_for = os.path.join(BUILD_DIR, f"calls-{version}")
     headers = [os.path.join(HERE, "..", "include", f) for f in ("codecgauge_tree.h", "codecgauge_block8.h", "codecgauge_paged.h")]
-    if force or _stale(CALLS, [src, *headers, __file__]):
-        tmp = CALLS + f".tmp{os.getpid()}"
-        subprocess.check_call(["gcc", "-O2", "-Wall", "-shared", "-fPIC", f"-I{inc}", src, "-o", tmp])
-        os.replace(tmp, CALLS)
+    if not (force or _stale(CALLS, [src, *headers, __file__]) or _stale(built_for, [CALLS])):
+        return
+    tmp = CALLS + f".tmp{os.getpid()}"
+    cmd = ["g++", "-O2", "-std=c++17", "-Wall", "-shared", "-fPIC", "-fvisibility=hidden", f'-DCG_TORCH_VERSION="{version}"',
+           f"-I{inc}", f"-I{torch}/include", f"-I{torch}/include/torch/csrc/api/include", src, f"-L{torch}/lib", "-ltorch_python",
+           "-ltorch_cpu", "-lc10", "-o", tmp]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode:
+        raise RuntimeError(f"g++ failed: {' '.join(cmd)}\n{r.stderr}")
+    os.replace(tmp, CALLS)
+    open(built_for, "w").close()
 
 
 if __name__ == "__main__":

@@ -121,22 +121,24 @@ _short = None
 
 
 def _short_calls():
-    """The module of the short calls (csrc/cg_calls.c), set up; False where it is not built."""
+    """The module of the short calls (csrc/cg_calls.cpp), set up; False where it is not built, or for another torch."""
     global _short
     try:
         from . import _calls
     except ImportError:
         _short = False
-    else:
-        at = [ctypes.cast(getattr(load(), f), _vp).value for f in (
-            "cg_tree_plan", "cg_tree_attention", "cg_tree_commit", "cg_block8_encode", "cg_block8_matmul")]
-        _calls.setup(torch.Tensor, torch.int32, torch.float32, torch.bfloat16, torch.float16, torch.float8_e4m3fn, *at)
-        _short = _calls
+        return _short
+    if _calls.torch_version != str(torch.__version__):
+        _short = False
+        return _short
+    _calls.setup(torch.Tensor, *(ctypes.cast(getattr(load(), f), _vp).value for f in (
+        "cg_tree_plan", "cg_tree_attention", "cg_tree_commit", "cg_block8_encode", "cg_block8_matmul")))
+    _short = _calls
     return _short
 
 
 def _took(name: str, *args) -> bool:
-    """The call by its short way (csrc/cg_calls.c), which finds the arguments as they should be and makes it, or does
+    """The call by its short way (csrc/cg_calls.cpp), which finds the arguments as they should be and makes it, or does
     nothing and returns False: then the caller's own checks say what is wrong, or make the call."""
     short = _short_calls() if _short is None else _short
     if not short:

@@ -1,4 +1,4 @@
-"""The short way of calls from Python (csrc/cg_calls.c) gives the library what the Python functions give it, or nothing."""
+"""The short way of calls from Python (csrc/cg_calls.cpp) gives the library what the Python functions give it, or nothing."""
 from __future__ import annotations
 
 import ctypes
@@ -24,7 +24,7 @@ class Calls:
 
     def __init__(self, tmp_path, monkeypatch):
         if not os.path.exists(build.CALLS):
-            pytest.skip("built where Python's headers are")
+            pytest.skip("built where Python's and torch's headers are")
         copy = str(tmp_path / "_calls.so")
         shutil.copy(build.CALLS, copy)
         spec = importlib.util.spec_from_file_location("_calls", copy)
@@ -32,7 +32,7 @@ class Calls:
         spec.loader.exec_module(self.module)
         self.made, self.rc = [], 0
         self._keep = [ctypes.CFUNCTYPE(ctypes.c_int, *paged._ARGS["cg_" + n])(self._note(n)) for n in NAMES]
-        self.module.setup(torch.Tensor, I32, F32, BF16, FP16, E4M3, *(ctypes.cast(f, ctypes.c_void_p).value for f in self._keep))
+        self.module.setup(torch.Tensor, *(ctypes.cast(f, ctypes.c_void_p).value for f in self._keep))
         monkeypatch.setattr(paged, "_short", False)
         monkeypatch.setattr(paged, "_device", lambda: -1)
         monkeypatch.setattr(paged, "_stream", lambda stream: 7)
@@ -201,7 +201,7 @@ def _step(device="cuda"):
 def test_a_step_goes_the_short_way(monkeypatch):
     """And gives what it gives by Python and ctypes."""
     if not os.path.exists(build.CALLS):
-        pytest.skip("built where Python's headers are")
+        pytest.skip("built where Python's and torch's headers are")
     by_ctypes = []
     fn = paged._fn
     monkeypatch.setattr(paged, "_fn", lambda name: by_ctypes.append(name) or fn(name))
