@@ -4,6 +4,7 @@
 #include <cuda_fp8.h>
 
 #include "../../include/codecgauge_block8.h"
+#include "cg_follow.cuh"
 #include "cg_launch.h"
 #include "cg_paged.h"
 #include "cg_sm100.cuh"
@@ -24,7 +25,7 @@ constexpr float kTop = 448.0f;
 // Encoding. 8 lanes a row of a block, 16 channels each: 32 bytes in, 16 bytes out. The largest |x| is found on the
 // bits (the order of non-negative numbers is that of their bits, infinities and NaN above all). A scale for one
 // row needs the 8 lanes alone, one for 128 rows a CTA, whose threads keep their 4 rows in registers. Bound: HBM, 3
-// bytes a value: 8192 x 4096 19.1 us, 5.3 TB/s; 16384 x 16384 127 us, 6.3 TB/s; by 128 rows 16384 x 8192 66 us, 6.1 TB/s. (With
+// bytes a value: 8192 x 4096 18.4 us, 5.5 TB/s; 16384 x 16384 128 us, 6.3 TB/s; by 128 rows 16384 x 8192 65 us, 6.2 TB/s. (With
 // unpacked arithmetic those took 24.4, 164 and 81 us.)
 // ------------------------------------------------------------------------------------
 constexpr int kEncThreads = 256, kGroup = 8, kEncRows = kEncThreads / kGroup;   // rows of blocks of a CTA and turn
@@ -48,7 +49,7 @@ struct Piece {
     uint32_t w[8];   // 16 values
     __device__ __forceinline__ void load(const uint16_t* p, bool have) {
         const uint4 zero = make_uint4(0, 0, 0, 0);
-        const uint4 a = have ? __ldg(reinterpret_cast<const uint4*>(p)) : zero, b = have ? __ldg(reinterpret_cast<const uint4*>(p) + 1) : zero;
+        const uint4 a = have ? *reinterpret_cast<const uint4*>(p) : zero, b = have ? *(reinterpret_cast<const uint4*>(p) + 1) : zero;
         w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
         w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
     }
@@ -111,6 +112,7 @@ __global__ void __launch_bounds__(kEncThreads) encode_rows_kernel(EncArgs a) {
     const int64_t first = (int64_t)blockIdx.x * kEncRows + threadIdx.x / kGroup;
     int64_t row = first / a.nb, b = first - row * a.nb;
     int32_t flag = 0;
+    follow();
     while (__any_sync(0xffffffffu, row < a.R)) {
         Piece p[U];
         int64_t at_row[U], at_b[U];
@@ -151,6 +153,7 @@ __global__ void __launch_bounds__(kEncThreads) encode_square_kernel(EncArgs a) {
     const int lane8 = threadIdx.x % kGroup, r0 = threadIdx.x / kGroup, warp = threadIdx.x >> 5;
     const int64_t rb = (a.R + kBlock - 1) / kBlock, items = rb * a.nb;
     int32_t flag = 0;
+    follow();
     for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
         const int64_t r = it / a.nb, b = it - r * a.nb, ch = b * kBlock + lane8 * 16;
         Piece p[kPer];
@@ -195,7 +198,7 @@ __global__ void __launch_bounds__(kEncThreads) encode_square_kernel(EncArgs a) {
 // Few tiles: the blocks of channels are cut among the CTAs of a cluster; each writes its sums of a part of the rows into the
 // shared memory of the CTA that adds those up, in the order of the ranks whatever their timing. (Left where they were and
 // read from there they cost 333 x 1000 x 4112 4.1 us of 10.7, two rounds of loads' latency and a barrier more.) Bound: what an
-// SM takes in by TMA, about 70 GB/s, and the start and end, 6 us: 333 x 1000 x 4112 9.3 us, 17 x 6144 x 4096 10.1, 256 15.7.
+// SM takes in by TMA, about 70 GB/s, and the start and end, 6 us: 333 x 1000 x 4112 8.4 us, 17 x 6144 x 4096 9.1, 256 14.5.
 // ------------------------------------------------------------------------------------
 constexpr int kLanes = 128;
 
@@ -443,6 +446,8 @@ block8_tile_kernel(const __grid_constant__ MatArgs a, const __grid_constant__ CU
     }
     __syncthreads();
     tc_fence_after();
+    follow();
+    let_follow();
     const uint32_t tmem = S->tmem;
     volatile int* abort_flag = &S->abort_flag;
     TileWalk w;
@@ -470,8 +475,8 @@ block8_tile_kernel(const __grid_constant__ MatArgs a, const __grid_constant__ CU
 #pragma unroll
                 for (int i = 0; i < 4; i++) {
                     const int k = kb + i < kb1 ? kb + i : kb1 - 1;
-                    nx[i] = __ldg(px + k);
-                    nw[i] = __ldg(pw + k);
+                    nx[i] = px[k];
+                    nw[i] = pw[k];
                 }
             };
             if (!idle && kb0 < kb1) fetch(kb0);
@@ -742,6 +747,7 @@ block8_pair_kernel(const __grid_constant__ MatArgs a, const __grid_constant__ CU
     __syncthreads();
     cluster.sync();
     tc_fence_after();
+    follow();
     const uint32_t tmem = S->tmem;
     volatile int* abort_flag = &S->abort_flag;
     bool dead = *abort_flag != 0;
@@ -761,14 +767,14 @@ block8_pair_kernel(const __grid_constant__ MatArgs a, const __grid_constant__ CU
         float nx[4], nw[4], f[4];
         auto fetch = [&](int kb) {
             if (a.vec_scales) {   // (whole groups of four)
-                *reinterpret_cast<float4*>(nx) = __ldg(reinterpret_cast<const float4*>(px + kb));
-                *reinterpret_cast<float4*>(nw) = __ldg(reinterpret_cast<const float4*>(pw + kb));
+                *reinterpret_cast<float4*>(nx) = *reinterpret_cast<const float4*>(px + kb);
+                *reinterpret_cast<float4*>(nw) = *reinterpret_cast<const float4*>(pw + kb);
             } else {
 #pragma unroll
                 for (int i = 0; i < 4; i++) {
                     const int k = kb + i < nb ? kb + i : nb - 1;
-                    nx[i] = __ldg(px + k);
-                    nw[i] = __ldg(pw + k);
+                    nx[i] = px[k];
+                    nw[i] = pw[k];
                 }
             }
         };
@@ -968,7 +974,7 @@ block8_pair_kernel(const __grid_constant__ MatArgs a, const __grid_constant__ CU
 // needs no tensor maps, which the host would make. All CTAs read the same few lines of x and its scales at
 // about the same time, which one slice of L2 serves: they come through L1 (scales copied block by block past it took 2 us
 // more). The order of the channels within a block is free as long as both operands have the same: a thread reads 16 bytes
-// of either. 1 x 6144 x 4096 7.2 to 8 us (25 MB; a plain read of them 5.6), 1 x 58368 x 4096 43 us, 5.6 TB/s.
+// of either. 1 x 6144 x 4096 6.4 us (25 MB; a plain read of them 5.6), 1 x 58368 x 4096 42 us, 5.7 TB/s.
 // Where the rows of w leave SMs idle, the blocks are cut among the CTAs of a cluster, added in the order of the ranks.
 // ------------------------------------------------------------------------------------
 constexpr int kFewThreads = 256, kFewRows = 16, kFewMost = 8, kFewWarps = kFewThreads / 32;
@@ -1037,6 +1043,7 @@ __global__ void __launch_bounds__(kFewThreads, 3) block8_few_kernel(const __grid
         asm volatile("cp.async.commit_group;" ::: "memory");
         if (++cs == kFewAhead) cs = 0;
     };
+    follow();
 #pragma unroll
     for (int i = 0; i < kFewAhead; i++) copy();
 
@@ -1045,9 +1052,9 @@ __global__ void __launch_bounds__(kFewThreads, 3) block8_few_kernel(const __grid
     auto fetch = [&](int tile, int kb) {
         kb += g;
         if (tile >= a.tiles || kb >= hi) return;
-        nw = __ldg(a.ws + (int64_t)tile * kFewRows / kBlock * a.nb + kb);
-        if (2 * j < a.M) n0 = __ldg(a.xs + (int64_t)(2 * j) * a.nb + kb);
-        if (2 * j + 1 < a.M) n1 = __ldg(a.xs + (int64_t)(2 * j + 1) * a.nb + kb);
+        nw = a.ws[(int64_t)tile * kFewRows / kBlock * a.nb + kb];
+        if (2 * j < a.M) n0 = a.xs[(int64_t)(2 * j) * a.nb + kb];
+        if (2 * j + 1 < a.M) n1 = a.xs[(int64_t)(2 * j + 1) * a.nb + kb];
     };
     fetch(first, lo);
     int slot = 0;
@@ -1197,18 +1204,8 @@ cudaError_t launch_tiles(MatArgs a, const Matrices& m, int split, cudaStream_t s
     a.group = 16;
     a.split = split;
     const int64_t tiles = a.lane_tiles * a.col_tiles, room = tc::num_sms();
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)(a.split > 1 ? tiles * a.split : tiles < room ? tiles : room));
-    cfg.blockDim = dim3(T::kThreads);
-    cfg.dynamicSmemBytes = T::total;
-    cfg.stream = st;
-    cudaLaunchAttribute at{};
-    at.id = cudaLaunchAttributeClusterDimension;
-    at.val.clusterDim.x = (unsigned)a.split;
-    at.val.clusterDim.y = at.val.clusterDim.z = 1;
-    cfg.attrs = &at;
-    cfg.numAttrs = a.split > 1 ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, block8_tile_kernel, a, xs, ws);
+    return launch_following(block8_tile_kernel, (unsigned)(a.split > 1 ? tiles * a.split : tiles < room ? tiles : room), T::kThreads, T::total, st, a.split, a, xs,
+                            ws);
 }
 
 cudaError_t launch_pairs(MatArgs a, const Matrices& m, cudaStream_t st) {
@@ -1229,8 +1226,7 @@ cudaError_t launch_pairs(MatArgs a, const Matrices& m, cudaStream_t st) {
     static Clusters clusters;
     if ((e = clusters.most(reinterpret_cast<const void*>(block8_pair_kernel), T::kThreads, T::total, 2, &pairs)) != cudaSuccess) return e;
     const int64_t tiles = a.lane_tiles * a.col_tiles;
-    block8_pair_kernel<<<(unsigned)(2 * (tiles < pairs ? tiles : pairs)), T::kThreads, T::total, st>>>(a, xs, ws, out);
-    return cudaGetLastError();
+    return launch_following(block8_pair_kernel, (unsigned)(2 * (tiles < pairs ? tiles : pairs)), T::kThreads, T::total, st, 0, a, xs, ws, out);
 }
 
 cudaError_t launch_few(const MatArgs& a, const Matrices& m, cudaStream_t st) {
@@ -1255,18 +1251,7 @@ cudaError_t launch_few(const MatArgs& a, const Matrices& m, cudaStream_t st) {
     static SmemOptIn opt_in;
     cudaError_t e = opt_in.set(reinterpret_cast<const void*>(block8_few_kernel), (int)few_smem(kFewMost));
     if (e != cudaSuccess) return e;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)(f.split > 1 ? f.tiles * f.split : f.tiles < room ? f.tiles : room));
-    cfg.blockDim = dim3(kFewThreads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cudaLaunchAttribute at{};
-    at.id = cudaLaunchAttributeClusterDimension;
-    at.val.clusterDim.x = (unsigned)f.split;
-    at.val.clusterDim.y = at.val.clusterDim.z = 1;
-    cfg.attrs = &at;
-    cfg.numAttrs = f.split > 1 ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, block8_few_kernel, f);
+    return launch_following(block8_few_kernel, (unsigned)(f.split > 1 ? f.tiles * f.split : f.tiles < room ? f.tiles : room), kFewThreads, (size_t)smem, st, f.split, f);
 }
 
 // The tile kernel takes 0.36 us a block of channels and round, 1.3 us to add up a cluster's sums, the pair kernel 0.45 us a
@@ -1347,21 +1332,16 @@ CG_EXPORT int cg_block8_encode(int32_t dtype, int64_t R, int64_t K, int32_t rows
     const unsigned grid = (unsigned)(items < room ? items : room);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     const bool fp16 = dtype == CG_FP16;
+    auto launch = [&](void (*kernel)(EncArgs)) { return launch_following(kernel, grid, kEncThreads, 0, st, 0, a); };
+    cudaError_t e;
     if (rows == 1) {
         a.step_row = (int64_t)grid * kEncRows / a.nb;
         a.step_b = (int64_t)grid * kEncRows % a.nb;
-        if (items > room) {
-            if (fp16) encode_rows_kernel<true, 2><<<grid, kEncThreads, 0, st>>>(a);
-            else encode_rows_kernel<false, 2><<<grid, kEncThreads, 0, st>>>(a);
-        } else {
-            if (fp16) encode_rows_kernel<true, 1><<<grid, kEncThreads, 0, st>>>(a);
-            else encode_rows_kernel<false, 1><<<grid, kEncThreads, 0, st>>>(a);
-        }
+        if (items > room) e = launch(fp16 ? encode_rows_kernel<true, 2> : encode_rows_kernel<false, 2>);
+        else e = launch(fp16 ? encode_rows_kernel<true, 1> : encode_rows_kernel<false, 1>);
     } else {
-        if (fp16) encode_square_kernel<true><<<grid, kEncThreads, 0, st>>>(a);
-        else encode_square_kernel<false><<<grid, kEncThreads, 0, st>>>(a);
+        e = launch(fp16 ? encode_square_kernel<true> : encode_square_kernel<false>);
     }
-    const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return set_error(CG_ECUDA, "block encoding launch: %s", cudaGetErrorString(e));
     return CG_OK;
 }

@@ -21,6 +21,7 @@
 // faster (4 query heads, 5 tokens = 20 rows: two tiles here read the keys twice).
 #include <chrono>
 
+#include "cg_follow.cuh"
 #include "cg_paged_dev.cuh"
 #include "cg_tc_common.cuh"
 #include "cg_tmap.h"
@@ -279,7 +280,8 @@ template <bool FP16, int D, bool TREE>
 __global__ void __launch_bounds__(kThreads, RowsSmem<D>::kCtas)
 paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ CUtensorMap map) {
     using L = RowsSmem<D>;
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the tiles kernel of the call may come beside
+    if (TREE) follow();
+    else asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the tiles kernel of the call may come beside
     extern __shared__ __align__(1024) unsigned char smem[];
     RowsMisc* M = reinterpret_cast<RowsMisc*>(smem + L::misc);
     float* merge = reinterpret_cast<float*>(smem + L::merge);
@@ -376,7 +378,7 @@ paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ 
                 if (k >= take) return -1;
                 const int t = w.t.id(first + k) * kTK + mybox * P.box_rows;
                 if (!(t < w.r.len && (t + P.box_rows > wlo || t < a.sinks))) return -1;
-                const int pg = __ldg(row + (t >> a.page_log2));
+                const int pg = load_input<TREE>(row + (t >> a.page_log2));
                 if (pg < 0 || pg >= a.n_pages) {
                     pflag |= CG_FLAG_PAGED_RANGE;
                     return -1;
@@ -449,8 +451,8 @@ paged_rows_kernel(const __grid_constant__ RowsParams P, const __grid_constant__ 
                 const uint16_t* src = a.q + (int64_t)(w.r.tok0 + tk) * a.q_tok + hd * a.q_head + 2 * j;
 #pragma unroll
                 for (int k = 0; k < D / 16; k++) {
-                    q[k][hf] = have ? __ldg(reinterpret_cast<const uint32_t*>(src + 16 * k)) : 0u;
-                    q[k][2 + hf] = have ? __ldg(reinterpret_cast<const uint32_t*>(src + 16 * k + 8)) : 0u;
+                    q[k][hf] = have ? load_input<TREE>(reinterpret_cast<const uint32_t*>(src + 16 * k)) : 0u;
+                    q[k][2 + hf] = have ? load_input<TREE>(reinterpret_cast<const uint32_t*>(src + 16 * k + 8)) : 0u;
                 }
             }
             float o[D / 8][4];
@@ -752,6 +754,7 @@ cudaError_t launch_rows(const RowsParams& P, cudaStream_t st) {
     cudaError_t e = opt_in.set(reinterpret_cast<const void*>(paged_rows_kernel<FP16, D, TREE>), (int)smem);
     if (e != cudaSuccess) return e;
     const unsigned grid = (unsigned)rows_ctas(D);
+    if (TREE) return launch_following(paged_rows_kernel<FP16, D, TREE>, grid, kThreads, smem, st, 0, P, map);
     paged_rows_kernel<FP16, D, TREE><<<grid, kThreads, smem, st>>>(P, map);
     return cudaGetLastError();
 }

@@ -84,13 +84,20 @@ struct Request {
     int len, n, tok0;     // tokens in the pool, new ones, first query row
 };
 
+// What a kernel before this one may have written: a tree's kernels come while that one ends (cg_follow.cuh), and
+// their loads stay behind the wait for it.
+template <bool TREE, class T>
+__device__ __forceinline__ T load_input(const T* p) {
+    return TREE ? *p : __ldg(p);
+}
+
 // Loads and checks a request: lengths that are not covered by the arrays raise the flag (and, in a
 // tree's call, more new tokens than tokens).
 template <bool TREE>
 __device__ __forceinline__ Request load_request(const PagedArgs& a, int i, int32_t* flag) {
     Request r;
-    const int c0 = __ldg(a.cu_new + i), c1 = __ldg(a.cu_new + i + 1);
-    r.len = __ldg(a.seq_lens + i);
+    const int c0 = load_input<TREE>(a.cu_new + i), c1 = load_input<TREE>(a.cu_new + i + 1);
+    r.len = load_input<TREE>(a.seq_lens + i);
     r.tok0 = c0;
     r.n = c1 - c0;
     const bool ok = c0 >= 0 && c1 >= c0 && c1 <= a.n_tok && r.n <= a.max_new && r.len >= (TREE ? r.n : 0) &&
@@ -108,7 +115,7 @@ __device__ __forceinline__ Request load_request(const PagedArgs& a, int i, int32
 // from its lengths alone. 0 where no window asks for it.
 __device__ __forceinline__ int tree_position(const PagedArgs& a, const Request& r, int node, int32_t* flag) {
     if (!a.window) return 0;
-    const int ctx = r.len - r.n, p = __ldg(a.positions + r.tok0 + node);
+    const int ctx = r.len - r.n, p = a.positions[r.tok0 + node];
     if (p < ctx || p > ctx + node) *flag |= CG_FLAG_PAGED_RANGE;
     return min(max(p, ctx), ctx + node);
 }
@@ -120,7 +127,7 @@ __device__ __forceinline__ const uint32_t* tree_row(const PagedArgs& a, const Re
 __device__ __forceinline__ uint32_t tree_word(const uint32_t* row, int words, int n, int j) {
     if (j <= -32 || j >= n) return 0u;
     const int w = j >> 5;                                  // -1 for j < 0
-    const uint32_t lo = w >= 0 ? __ldg(row + w) : 0u, hi = w + 1 < words ? __ldg(row + w + 1) : 0u;
+    const uint32_t lo = w >= 0 ? row[w] : 0u, hi = w + 1 < words ? row[w + 1] : 0u;
     const int left = n - j;                                // bits past the last node are no tokens
     return __funnelshift_r(lo, hi, j & 31) & (left >= 32 ? ~0u : (1u << left) - 1u);
 }

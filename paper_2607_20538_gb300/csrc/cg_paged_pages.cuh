@@ -68,7 +68,7 @@ __device__ __forceinline__ void push_pages(const PushArgs& a, PushSmem<THREADS, 
     constexpr int kRound = THREADS * kPushPer, kWarps = THREADS / 32;
     auto cluster = cooperative_groups::this_cluster();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = (int)cluster.block_rank();
-    int64_t count = __ldg(a.count_in);   // pages on the stack
+    int64_t count = *a.count_in;   // pages on the stack
     if (count < 0 || count > a.n_pages) {
         *flag |= CG_FLAG_PAGED_RANGE;
         count = count < 0 ? 0 : a.n_pages;
@@ -121,7 +121,7 @@ __device__ __forceinline__ void push_pages(const PushArgs& a, PushSmem<THREADS, 
                 if (f >= hi) continue;
                 if (r < 0 || S.first[r + 1] <= f) r = find_request(S.first, n, f);
                 const int col = Lines::kFromStart ? 0 : S.col[r];
-                id[k] = __ldg(a.table + (int64_t)(base + r) * a.max_pages + col + (f - S.first[r]));
+                id[k] = a.table[(int64_t)(base + r) * a.max_pages + col + (f - S.first[r])];
             }
 #pragma unroll
             for (int k = 0; k < 4; k++)

@@ -2,6 +2,7 @@
 // entry point (its kernels are those of the paged attention), and the commit of an accepted path.
 // Contract: include/codecgauge_tree.h.
 #include "../../include/codecgauge_tree.h"
+#include "cg_follow.cuh"
 #include "cg_paged.h"
 #include "cg_paged_pages.cuh"
 #include "cg_tc_common.cuh"
@@ -24,7 +25,7 @@ constexpr int kBadParent = -2;   // ends a path like -1, and raises the flag
 // Node 32 w + lane of `n`: its bit and those of its ancestors in the word, and the ancestor that follows.
 __device__ __forceinline__ void climb_word(const int32_t* parents, int w, int n, uint32_t* mask, int* up) {
     const int lane = threadIdx.x & 31, k = 32 * w + lane;
-    int u = k < n ? __ldg(parents + k) : -1;
+    int u = k < n ? *(parents + k) : -1;
     if (u < -1 || u >= k) u = k < n ? kBadParent : -1;
     uint32_t m = 1u << lane;
 #pragma unroll
@@ -51,7 +52,7 @@ struct Tree {
 };
 // most: tokens that a request may have. What does not fit counts as without nodes, behind all its tokens.
 __device__ __forceinline__ Tree load_tree(const int32_t* lens, const int32_t* cu, int i, int n_tok, int max_new, int64_t most, int32_t* flag) {
-    const int len = __ldg(lens + i), c0 = __ldg(cu + i), c1 = __ldg(cu + i + 1);
+    const int len = *(lens + i), c0 = *(cu + i), c1 = *(cu + i + 1);
     if (c0 >= 0 && c1 >= c0 && c1 <= n_tok && c1 - c0 <= max_new && len >= c1 - c0 && len <= most) return Tree{len - (c1 - c0), c1 - c0, c0};
     *flag |= CG_FLAG_PAGED_RANGE;
     return Tree{len < 0 ? 0 : len, 0, 0};
@@ -61,8 +62,8 @@ __device__ __forceinline__ Tree load_tree(const int32_t* lens, const int32_t* cu
 // Tree plan. A CTA per request: words climbed by a warp each, into shared memory; then a thread per node
 // climbs from word to word, once for its depth and once more, from the last word of its row to the first, for the
 // bits. The nodes of a path within a word stand in order of depth, so that a window keeps a word's highest bits and
-// sinks its lowest. Bound: launch latency and two dependent loads (lengths, parents). In a graph: one tree of 8 nodes 1.7 us,
-// 256 of up to 64 2.1.
+// sinks its lowest. Bound: launch latency and two dependent loads (lengths, parents). In a graph: one tree of 8 nodes 1.5 us,
+// 256 of up to 64 1.9.
 // ------------------------------------------------------------------------------------
 constexpr int kPlanThreads = 128;
 
@@ -80,7 +81,8 @@ __global__ void __launch_bounds__(kPlanThreads) tree_plan_kernel(TreePlanArgs a)
     int* up = reinterpret_cast<int*>(plan_sm + a.max_new);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     int32_t flag = 0;
-    const int end = __ldg(a.cu + a.n_req);
+    follow();
+    const int end = *(a.cu + a.n_req);
     const Tree t = load_tree(a.lens, a.cu, blockIdx.x, a.n_tok, a.max_new, 0x7fffffff, &flag);
     for (int w = warp; 32 * w < t.n; w += kPlanThreads / 32) {
         uint32_t m;
@@ -135,8 +137,8 @@ __global__ void __launch_bounds__(kPlanThreads) tree_plan_kernel(TreePlanArgs a)
 // table, then each thread moves the same 16 bytes of row after row, in ascending order and a batch at a time.
 // Row k receives row r_k >= k, and no later row of the path is read from a place already written, so a thread that
 // goes upwards needs nobody else's leave. Bound: chains of dependent loads (lengths, parents, table, rows) for few
-// rows; HBM, 4 H d layers bytes read and written a moved row, for many. In a graph: one path in one layer 4.3 us, 64 paths of
-// trees of up to 48 nodes in 16 layers (25 MB) 10.4.
+// rows; HBM, 4 H d layers bytes read and written a moved row, for many. In a graph: one path in one layer 4.1 us, 64 paths of
+// trees of up to 48 nodes in 16 layers (25 MB) 9.9.
 // ------------------------------------------------------------------------------------
 constexpr int kCommitThreads = 256, kMoveBatch = 8;
 
@@ -151,7 +153,7 @@ struct CommitArgs {
     }
     // The accepted node, or -1.
     __device__ __forceinline__ int leaf(int i, const Tree& t, int32_t* flag) const {
-        const int e = __ldg(leaves + i);
+        const int e = *(leaves + i);
         if (e >= -1 && e < t.n) return e;
         *flag |= CG_FLAG_PAGED_RANGE;
         return -1;
@@ -257,7 +259,7 @@ __device__ __forceinline__ void move_rows(const CommitArgs& a, unsigned char* sm
         int src = -1, dst = -1;
         if (at != k) {
             const int s = t.ctx + k, d = t.ctx + at;
-            const int sp = __ldg(row + (s >> a.page_log2)), dp = __ldg(row + (d >> a.page_log2));
+            const int sp = *(row + (s >> a.page_log2)), dp = *(row + (d >> a.page_log2));
             if (sp >= 0 && sp < a.n_pages && dp >= 0 && dp < a.n_pages) {
                 src = (sp << a.page_log2) + (s & (a.page - 1));
                 dst = (dp << a.page_log2) + (d & (a.page - 1));
@@ -292,6 +294,7 @@ __device__ __forceinline__ void move_rows(const CommitArgs& a, unsigned char* sm
 __global__ void __cluster_dims__(kPushCtas, 1, 1) __launch_bounds__(kCommitThreads) tree_commit_kernel(CommitArgs a) {
     extern __shared__ __align__(16) unsigned char commit_sm[];
     int32_t flag = 0;
+    follow();
     const int pages_ctas = a.lens_left ? kPushCtas : 0, b = (int)blockIdx.x - pages_ctas;
     if (b < 0) {
         CommitSmem& S = *reinterpret_cast<CommitSmem*>(commit_sm);
@@ -370,10 +373,7 @@ CG_EXPORT int cg_tree_plan(int32_t n_req, int32_t n_tok, int32_t max_new, int32_
         static SmemOptIn opt_in;
         e = opt_in.set(reinterpret_cast<const void*>(tree_plan_kernel), CG_TREE_NODES * 8);
     }
-    if (e == cudaSuccess) {
-        tree_plan_kernel<<<n_req, kPlanThreads, smem, static_cast<cudaStream_t>(stream)>>>(a);
-        e = cudaGetLastError();
-    }
+    if (e == cudaSuccess) e = launch_following(tree_plan_kernel, (unsigned)n_req, kPlanThreads, smem, static_cast<cudaStream_t>(stream), 0, a);
     if (e != cudaSuccess) return set_error(CG_ECUDA, "tree plan launch: %s", cudaGetErrorString(e));
     return CG_OK;
 }
@@ -449,10 +449,8 @@ CG_EXPORT int cg_tree_commit(const cg_pages* pages, int32_t n_tok, int32_t max_n
     const int64_t ctas = (give ? kPushCtas : 0) + (int64_t)a.n_req * a.parts, grid = (ctas + kPushCtas - 1) / kPushCtas * kPushCtas;
     static SmemOptIn opt_in;
     cudaError_t e = opt_in.set(reinterpret_cast<const void*>(tree_commit_kernel), (int)commit_smem(CG_TREE_NODES, true));
-    if (e == cudaSuccess) {
-        tree_commit_kernel<<<(unsigned)grid, kCommitThreads, commit_smem(max_new, give), static_cast<cudaStream_t>(stream)>>>(a);
-        e = cudaGetLastError();
-    }
+    if (e == cudaSuccess)
+        e = launch_following(tree_commit_kernel, (unsigned)grid, kCommitThreads, commit_smem(max_new, give), static_cast<cudaStream_t>(stream), 0, a);
     if (e != cudaSuccess) return set_error(CG_ECUDA, "tree commit launch: %s", cudaGetErrorString(e));
     return CG_OK;
 }
