@@ -2,6 +2,8 @@
 what it reads is not written over early. Against the same calls with the GPU waited for after each."""
 from __future__ import annotations
 
+import threading
+
 import pytest
 import torch
 
@@ -194,4 +196,36 @@ def test_over_two_streams(rows, captured):
             t["y"].fill_(7.0)
             run()
             assert torch.equal(t["y"].clone(), want)
+    assert cg.get_status() == 0
+
+
+def test_four_threads():
+    """Each with a stream and buffers of its own."""
+    chains = [Chain(*s) for s in ((3, 5), (20, 300), (7, 60), (20, 5))]
+    want = [_waited(c) for c in chains]
+    got, failed = [None] * len(chains), []
+
+    def run(k):
+        try:
+            stream = torch.cuda.Stream()
+            with torch.cuda.stream(stream):
+                for _ in range(3):
+                    got[k] = []
+                    for n in range(STEPS):
+                        chains[k].seed.fill_(float(n + 1))
+                        chains[k].step()
+                        got[k].append(chains[k].results())
+            stream.synchronize()
+        except Exception as e:  # noqa: BLE001
+            failed.append(e)
+
+    torch.cuda.synchronize()
+    threads = [threading.Thread(target=run, args=(k,)) for k in range(len(chains))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failed
+    for g, w in zip(got, want):
+        _same(g, w)
     assert cg.get_status() == 0
