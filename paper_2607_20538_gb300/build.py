@@ -64,39 +64,51 @@ def build(force: bool = False, verbose: bool = False, ptxas_verbose: bool = Fals
                 sys.stderr.write(r.stdout + r.stderr)
             if r.returncode:
                 raise RuntimeError(f"nvcc failed: {' '.join(cmd)}")
+        objs = [os.path.join(BUILD_DIR, s.replace(".cu", ".o")) for s in SOURCES]
+        if force or jobs or _stale(LIB, objs):
+            tmp = LIB + f".tmp{os.getpid()}"
+            subprocess.check_call([nvcc(), *ARCH, "-shared", "-o", tmp, *objs, "-lcudart"])
+            os.replace(tmp, LIB)
         calls.result()
-    objs = [os.path.join(BUILD_DIR, s.replace(".cu", ".o")) for s in SOURCES]
-    if force or jobs or _stale(LIB, objs):
-        tmp = LIB + f".tmp{os.getpid()}"
-        subprocess.check_call([nvcc(), *ARCH, "-shared", "-o", tmp, *objs, "-lcudart"])
-        os.replace(tmp, LIB)
     return LIB
 
 
 def _build_calls(force: bool) -> None:
-    """The short way from Python to some entry points (csrc/cg_calls.cpp), for this interpreter and torch. Where their
-    headers are missing the calls go by ctypes."""
+    """The short way from Python to some entry points (csrc/cg_calls.cpp), for this interpreter and torch. The library does
+    without it: where it cannot be built, none is left (an older one might make the calls of then), and the calls go by ctypes."""
+    try:
+        why = _compile_calls(force)
+    except OSError as e:   # (no compiler, no torch.version, ...)
+        why = str(e)
+    if why:
+        sys.stderr.write(f"{why}\ncalls go by ctypes\n")
+        if os.path.exists(CALLS):
+            os.remove(CALLS)
+
+
+def _compile_calls(force: bool) -> str:
+    """Why the module could not be built; empty: it is there."""
     src, inc = os.path.join(CSRC, "cg_calls.cpp"), sysconfig.get_path("include")
     spec = importlib.util.find_spec("torch")
     torch = os.path.dirname(spec.origin) if spec and spec.origin else ""
     for h in (os.path.join(inc, "Python.h"), os.path.join(torch, "include/torch/csrc/autograd/python_variable.h")):
         if not os.path.exists(h):
-            sys.stderr.write(f"no {h}: calls go by ctypes\n")
-            return
+            return f"no {h}"
     version = runpy.run_path(os.path.join(torch, "version.py"))["__version__"]
     built_for = os.path.join(BUILD_DIR, f"calls-{version}")
     headers = [os.path.join(HERE, "..", "include", f) for f in ("codecgauge_tree.h", "codecgauge_block8.h", "codecgauge_paged.h")]
     if not (force or _stale(CALLS, [src, *headers, __file__]) or _stale(built_for, [CALLS])):
-        return
+        return ""
     tmp = CALLS + f".tmp{os.getpid()}"
     cmd = ["g++", "-O2", "-std=c++17", "-Wall", "-shared", "-fPIC", "-fvisibility=hidden", f'-DCG_TORCH_VERSION="{version}"',
            f"-I{inc}", f"-I{torch}/include", f"-I{torch}/include/torch/csrc/api/include", src, f"-L{torch}/lib", "-ltorch_python",
            "-ltorch_cpu", "-lc10", "-o", tmp]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode:
-        raise RuntimeError(f"g++ failed: {' '.join(cmd)}\n{r.stderr}")
+        return f"g++ failed: {' '.join(cmd)}\n{r.stderr}"
     os.replace(tmp, CALLS)
     open(built_for, "w").close()
+    return ""
 
 
 if __name__ == "__main__":
