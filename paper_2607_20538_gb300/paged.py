@@ -300,7 +300,9 @@ class _Kept(threading.local):
 _kept = _Kept()
 
 
-def _workspace(pages: Pages, how: PagedAttention, n: int, device):
+def _workspace(pages: Pages, how: PagedAttention, n: int, device, stream=None):
+    if stream is not None and stream != torch.cuda.current_stream():
+        _bad("workspace: needed on a stream that is not the current one")
     key = (pages.d, how.n_rep, how.max_new, device)   # all that the size depends on
     nbytes = _ws_bytes.get(key)
     if nbytes is None:
@@ -314,15 +316,14 @@ def _workspace(pages: Pages, how: PagedAttention, n: int, device):
     return kept
 
 
-def _own_workspace(pages: Pages, how: PagedAttention, n: int, device, stream):
-    if stream is not None and stream != torch.cuda.current_stream():
-        _bad("workspace: needed on a stream that is not the current one")
-    return _workspace(pages, how, n, device)
-
-
-def _attend(name: str, pages: Pages, how: PagedAttention, q, pool, block_table, seq_lens, cu_new, out, lse, workspace, stream,
-            words=(), masks=()) -> None:
-    """The call of an attention entry point: `words` before its tensors, `masks` behind the lengths."""
+def paged_attention(pages: Pages, how: PagedAttention, q, pool, block_table, seq_lens, cu_new, out, lse=None,
+                    workspace=None, stream=None, _tree=None) -> None:
+    """Attention of the new tokens' queries q [n_tok][H * n_rep][d] over their requests' pages
+    (cg_paged_attention). Without a workspace the call takes one from torch's allocator, on the
+    current stream (pass one to run on another); the default stream's is kept for the next call of the
+    same host thread, until the thread ends. A workspace that is passed serves calls made one after the
+    other: two threads must not pass the same one at the same time."""
+    # (_tree: of tree_attention, whose checks are these: words of a row of masks, positions, masks)
     n, hq, dev = q.shape[0], pages.H * how.n_rep, _device()
     qp, qt, qh = _heads("q", q, n, hq, pages.d, pool.dtype, dev)
     op, ot, oh = _heads("out", out, n, hq, pages.d, pool.dtype, dev)
@@ -333,21 +334,15 @@ def _attend(name: str, pages: Pages, how: PagedAttention, q, pool, block_table, 
         lp = lse.data_ptr()
     cp, ca = pages.c(_elem(pool)), _attn(pages, how, n, qt, qh, ot, oh)
     if workspace is None:
-        workspace = _own_workspace(pages, how, n, q.device, stream)
+        workspace = _workspace(pages, how, n, q.device, stream)
     elif workspace.get_device() != dev or not workspace.is_contiguous():
         _bad(f"workspace: expected a contiguous tensor on device {dev}")
     r = pages.n_req
-    _check(_fn(name)(
-        cp, ca, *words, qp, _pool(pages, pool, dev), _i32("block_table", block_table, r * pages.max_pages, dev),
-        _i32("seq_lens", seq_lens, r, dev), _i32("cu_new", cu_new, r + 1, dev), *masks, op, lp, workspace.data_ptr(),
-        workspace.nbytes, _stream(stream)))
-
-
-def paged_attention(pages: Pages, how: PagedAttention, q, pool, block_table, seq_lens, cu_new, out, lse=None,
-                    workspace=None, stream=None) -> None:
-    """Attention of the new tokens' queries q [n_tok][H * n_rep][d] over their requests' pages
-    (cg_paged_attention). Without a workspace the call takes one from torch's allocator, on the
-    current stream (pass one to run on another); the default stream's is kept for the next call of the
-    same host thread, until the thread ends. A workspace that is passed serves calls made one after the
-    other: two threads must not pass the same one at the same time."""
-    _attend("cg_paged_attention", pages, how, q, pool, block_table, seq_lens, cu_new, out, lse, workspace, stream)
+    kv, bt = _pool(pages, pool, dev), _i32("block_table", block_table, r * pages.max_pages, dev)
+    sl, cu = _i32("seq_lens", seq_lens, r, dev), _i32("cu_new", cu_new, r + 1, dev)
+    if _tree is None:
+        _check(_fn("cg_paged_attention")(cp, ca, qp, kv, bt, sl, cu, op, lp, workspace.data_ptr(), workspace.nbytes, _stream(stream)))
+    else:
+        words, positions, masks = _tree
+        _check(_fn("cg_tree_attention")(cp, ca, words, qp, kv, bt, sl, cu, positions, masks, op, lp, workspace.data_ptr(), workspace.nbytes,
+                                        _stream(stream)))

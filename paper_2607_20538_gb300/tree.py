@@ -35,7 +35,7 @@ def tree_attention(pages: Pages, how: PagedAttention, q, pool, block_table, seq_
     (cg_tree_attention). positions may be None without a window; the workspace is paged_attention's."""
     n, dev = q.shape[0], _p._device()
     if q.get_device() == dev:
-        room = _p._own_workspace(pages, how, n, q.device, stream) if workspace is None else workspace
+        room = _p._workspace(pages, how, n, q.device, stream) if workspace is None else workspace
         if _p._took("tree_attention", pages, how, q, pool, block_table, seq_lens, cu_new, positions, masks, out, lse, room, dev,
                     _p._stream(stream)):
             return
@@ -43,7 +43,7 @@ def tree_attention(pages: Pages, how: PagedAttention, q, pool, block_table, seq_
     if positions is None and how.window:
         _p._bad("positions: needed with a window")
     pp = None if positions is None else _p._i32("positions", positions, n, dev)
-    _p._attend("cg_tree_attention", pages, how, q, pool, block_table, seq_lens, cu_new, out, lse, workspace, stream, (words,), (pp, mp))
+    _p.paged_attention(pages, how, q, pool, block_table, seq_lens, cu_new, out, lse, workspace, stream, _tree=(words, pp, mp))
 
 
 def tree_commit(pages: Pages, max_new: int, parents, leaves, seq_lens, cu_new, block_table, pool, lens_left=None, free_pages=None,
