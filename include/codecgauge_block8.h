@@ -28,7 +28,8 @@ extern "C" {
  * codes NaN.
  *   rows : 1 or 128;  K : a multiple of 16, >= 16;  R >= 0
  *   x 16-byte aligned, x_stride >= K (unless R < 2) a multiple of 8;  codes 16-byte aligned, stride >= K
- *   (unless R < 2) a multiple of 16. The outputs must not overlap x or one another. One launch. */
+ *   (unless R < 2) a multiple of 16. The outputs must not overlap x or one another (rows may lie between another
+ *   matrix's rows). One launch. */
 int cg_block8_encode(int32_t dtype, int64_t R, int64_t K, int32_t rows, const void* x, int64_t x_stride, void* codes,
                      int64_t stride, float* scales, void* stream);
 
@@ -40,7 +41,7 @@ int cg_block8_encode(int32_t dtype, int64_t R, int64_t K, int32_t rows, const vo
  *   M, N >= 0;  K : a multiple of 16, >= 16;  M, N, K <= 2^30
  *   codes 16-byte aligned, strides in bytes >= K (unless one row) and multiples of 16, below 2^40;  out_stride in
  *   elements, >= N (unless M < 2);  out aligned to 2 bytes (16 with out_stride a multiple of 8 is fastest).
- *   out must not overlap the inputs. One launch. The same call gives the same bits each time. */
+ *   out must not overlap the inputs (its rows may lie between theirs). One launch. The same call gives the same bits each time. */
 int cg_block8_matmul(int32_t dtype, int64_t M, int64_t N, int64_t K, const void* x, int64_t x_stride, const float* x_scales,
                      const void* w, int64_t w_stride, const float* w_scales, void* out, int64_t out_stride, void* stream);
 

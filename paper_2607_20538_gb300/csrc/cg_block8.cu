@@ -6,6 +6,7 @@
 #include "../../include/codecgauge_block8.h"
 #include "cg_follow.cuh"
 #include "cg_launch.h"
+#include "cg_overlap.h"
 #include "cg_paged.h"
 #include "cg_sm100.cuh"
 #include "cg_tc_common.cuh"
@@ -1314,7 +1315,9 @@ CG_EXPORT int cg_block8_encode(int32_t dtype, int64_t R, int64_t K, int32_t rows
     if (!x || !codes || !scales) return set_error(CG_EINVAL, "null x, codes or scales");
     if (!al16(x) || !al16(codes) || (reinterpret_cast<uintptr_t>(scales) & 3u))
         return set_error(CG_EINVAL, "x and codes must be 16-byte aligned, scales to 4 bytes");
-    if (codes == x || scales == x || scales == codes) return set_error(CG_EINVAL, "the outputs must not overlap x or one another");
+    const int64_t blocks = (K + kBlock - 1) / kBlock;
+    const Rows in{x, R, 2 * K, 2 * x_stride}, coded{codes, R, K, stride}, scaled = span(scales, (__int128)((R + rows - 1) / rows) * blocks * 4);
+    if (overlap(coded, in) || overlap(scaled, in) || overlap(scaled, coded)) return set_error(CG_EINVAL, "the outputs must not overlap x or one another");
     EncArgs a{};
     if ((rc = device_status(&a.status))) return rc;
     a.x = static_cast<const uint16_t*>(x);
@@ -1324,7 +1327,7 @@ CG_EXPORT int cg_block8_encode(int32_t dtype, int64_t R, int64_t K, int32_t rows
     a.K = K;
     a.x_stride = R > 1 ? x_stride : K;
     a.stride = R > 1 ? stride : K;
-    a.nb = (K + kBlock - 1) / kBlock;
+    a.nb = blocks;
     const int64_t items = rows == 1 ? (R * a.nb + kEncRows - 1) / kEncRows : (R + kBlock - 1) / kBlock * a.nb;
     // Long matrices: as many CTAs as run at once go on, two blocks of a row at a time (8192 x 4096: 19.1 us, 21 with one block, 24.4
     // with a CTA for 32 blocks; 1024 x 4096 3.8 us, 4.2 with 8 CTAs an SM)
@@ -1362,7 +1365,10 @@ CG_EXPORT int cg_block8_matmul(int32_t dtype, int64_t M, int64_t N, int64_t K, c
     if (!al16(x) || !al16(w) || ((reinterpret_cast<uintptr_t>(x_scales) | reinterpret_cast<uintptr_t>(w_scales)) & 3u) ||
         (reinterpret_cast<uintptr_t>(out) & 1u))
         return set_error(CG_EINVAL, "x and w must be 16-byte aligned, scales and out to their type");
-    if (out == x || out == w || out == x_scales || out == w_scales) return set_error(CG_EINVAL, "out must not overlap the inputs");
+    const int64_t blocks = (K + kBlock - 1) / kBlock;
+    for (const Rows& in : {Rows{x, M, K, x_stride}, Rows{w, N, K, w_stride}, span(x_scales, (__int128)M * blocks * 4),
+                           span(w_scales, (__int128)((N + kBlock - 1) / kBlock) * blocks * 4)})
+        if (overlap(Rows{out, M, 2 * N, 2 * out_stride}, in)) return set_error(CG_EINVAL, "out must not overlap the inputs");
     MatArgs a{};
     if ((rc = device_status(&a.status))) return rc;
     a.xs = x_scales;
@@ -1370,7 +1376,7 @@ CG_EXPORT int cg_block8_matmul(int32_t dtype, int64_t M, int64_t N, int64_t K, c
     a.out = out;
     a.M = M;
     a.N = N;
-    a.nb = (K + kBlock - 1) / kBlock;
+    a.nb = blocks;
     a.out_stride = M > 1 ? out_stride : N;
     a.wait_ns = wait_limit_ns();
     a.fp16 = dtype == CG_FP16;

@@ -3,6 +3,7 @@
 // Contract: include/codecgauge_tree.h.
 #include "../../include/codecgauge_tree.h"
 #include "cg_follow.cuh"
+#include "cg_overlap.h"
 #include "cg_paged.h"
 #include "cg_paged_pages.cuh"
 #include "cg_tc_common.cuh"
@@ -351,9 +352,11 @@ CG_EXPORT int cg_tree_plan(int32_t n_req, int32_t n_tok, int32_t max_new, int32_
     if (!seq_lens || !cu_new || (n_tok && (!parents || !positions || !masks))) return set_error(CG_EINVAL, "null pointer");
     for (const void* p : {(const void*)parents, (const void*)seq_lens, (const void*)cu_new, (const void*)positions, (const void*)masks})
         if (!al4(p)) return set_error(CG_EINVAL, "pointers must be aligned to their type");
-    for (const void* p : {(const void*)positions, (const void*)masks})
-        if (p && (p == parents || p == seq_lens || p == cu_new || (const void*)positions == (const void*)masks))
-            return set_error(CG_EINVAL, "positions and masks must not alias the inputs or one another");
+    const Rows pos = span(positions, 4 * (int64_t)n_tok), bits = span(masks, (__int128)n_tok * mask_words * 4);
+    bool alias = overlap(pos, bits);
+    for (const Rows& in : {span(parents, 4 * (int64_t)n_tok), span(seq_lens, 4 * (int64_t)n_req), span(cu_new, 4 * ((int64_t)n_req + 1))})
+        alias = alias || overlap(pos, in) || overlap(bits, in);
+    if (alias) return set_error(CG_EINVAL, "positions and masks must not alias the inputs or one another");
     TreePlanArgs a{};
     if ((rc = device_status(&a.status))) return rc;
     a.parents = parents;
@@ -416,9 +419,15 @@ CG_EXPORT int cg_tree_commit(const cg_pages* pages, int32_t n_tok, int32_t max_n
         if (!al4(p)) return set_error(CG_EINVAL, "pointers must be aligned to their type");
     if (!al16(pool)) return set_error(CG_EINVAL, "pool must be 16-byte aligned");
     if (give) {
-        for (const int32_t* p : {parents, leaves, seq_lens, cu_new, block_table, free_count})
-            if (p && (p == lens_left || p == free_left || p == free_pages)) return set_error(CG_EINVAL, "lens_left, free_left and free_pages must not alias the inputs");
-        if (lens_left == free_left || lens_left == free_pages || free_left == free_pages)
+        const int64_t req = 4 * (int64_t)pages->n_req;
+        const Rows in[] = {span(parents, 4 * (int64_t)n_tok), span(leaves, req), span(seq_lens, req), span(cu_new, req + 4),
+                           span(block_table, (__int128)req * pages->max_pages), span(free_count, 4),
+                           span(pool, (__int128)layers * 4 * pages->n_pages * pages->page * ((int64_t)pages->H * pages->d))};
+        const Rows out[] = {span(lens_left, req), span(free_pages, 4 * (int64_t)pages->n_pages), span(free_left, 4)};
+        for (const Rows& o : out)
+            for (const Rows& i : in)
+                if (overlap(o, i)) return set_error(CG_EINVAL, "lens_left, free_left and free_pages must not alias the inputs");
+        if (overlap(out[0], out[1]) || overlap(out[0], out[2]) || overlap(out[1], out[2]))
             return set_error(CG_EINVAL, "lens_left, free_left and free_pages must not alias one another");
     }
     if (!give && !pool) return CG_OK;
