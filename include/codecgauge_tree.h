@@ -29,7 +29,8 @@
 extern "C" {
 #endif
 
-/* Nodes of one tree at most (cg_tree_plan, cg_tree_commit). */
+/* Nodes of one tree at most (cg_tree_plan, cg_tree_commit). The plan is made for trees of up to some hundred: its time
+ * grows with the square of the nodes, and one of 8192 takes a millisecond. */
 #define CG_TREE_NODES 8192
 
 /* ---- Positions and masks of the nodes ----

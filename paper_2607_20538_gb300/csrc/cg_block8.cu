@@ -26,8 +26,8 @@ constexpr float kTop = 448.0f;
 // Encoding. 8 lanes a row of a block, 16 channels each: 32 bytes in, 16 bytes out. The largest |x| is found on the
 // bits (the order of non-negative numbers is that of their bits, infinities and NaN above all). A scale for one
 // row needs the 8 lanes alone, one for 128 rows a CTA, whose threads keep their 4 rows in registers. Bound: HBM, 3
-// bytes a value: 8192 x 4096 18.4 us, 5.5 TB/s; 16384 x 16384 128 us, 6.3 TB/s; by 128 rows 16384 x 8192 65 us, 6.2 TB/s. (With
-// unpacked arithmetic those took 24.4, 164 and 81 us.)
+// bytes a value, and 3 us of start and end: 8192 x 4096 18.4 us, 5.5 TB/s; 16384 x 16384 128 us, 6.3 TB/s; 131072 x 4096 250 us, 6.5 TB/s;
+// by 128 rows 16384 x 8192 65 us, 6.2 TB/s. (With unpacked arithmetic the first took 24.4, the second 164, the last 81 us.)
 // ------------------------------------------------------------------------------------
 constexpr int kEncThreads = 256, kGroup = 8, kEncRows = kEncThreads / kGroup;   // rows of blocks of a CTA and turn
 
@@ -198,8 +198,9 @@ __global__ void __launch_bounds__(kEncThreads) encode_square_kernel(EncArgs a) {
 // what lies behind, and nobody reads them.
 // Few tiles: the blocks of channels are cut among the CTAs of a cluster; each writes its sums of a part of the rows into the
 // shared memory of the CTA that adds those up, in the order of the ranks whatever their timing. (Left where they were and
-// read from there they cost 333 x 1000 x 4112 4.1 us of 10.7, two rounds of loads' latency and a barrier more.) Bound: what an
-// SM takes in by TMA, about 70 GB/s, and the start and end, 6 us: 333 x 1000 x 4112 8.4 us, 17 x 6144 x 4096 9.1, 256 14.5.
+// read from there they cost 333 x 1000 x 4112 4.1 us of 10.7, two rounds of loads' latency and a barrier more.) Bound: latency, of the
+// start, the first block and a cluster's sums (5.6 of 8.4 us at 333 x 1000 x 4112), and, with few rows, that the warps of their lanes alone
+// read, scale and send: 17 x 6144 x 4096 9.1 us, where the kernel for up to 8 rows takes in the same bytes in 6.4; 64 rows 9.8, 256 14.6.
 // ------------------------------------------------------------------------------------
 constexpr int kLanes = 128;
 
@@ -1256,8 +1257,10 @@ cudaError_t launch_few(const MatArgs& a, const Matrices& m, cudaStream_t st) {
 }
 
 // The tile kernel takes 0.36 us a block of channels and round, 1.3 us to add up a cluster's sums, the pair kernel 0.45 us a
-// block for four times the work (6144 rows of w, 4096 channels: 256 rows of x 15.8 us on tiles and 18.8 on pairs, 512 27.7 and
-// 19.0). The smaller sum is taken.
+// block for four times the work. The smaller sum is taken. (6144 rows of w, 4096 channels: 256 rows of x 14.8 us on tiles and 17.7 on
+// pairs, 384 15.0 and 18.1, 448 26.8 and 18.1, 1024 38.7 and 32.8; 28672 rows of w: 128 33 and 39, 200 39.7 and 35.2; 14336 channels, 4096
+// rows of w: 512 39.4 and 50.3, 640 74.8 and 51.3. Of 7 matrices w and 16 numbers of rows, 17 to 8192, with each the faster one was taken
+// every time, or one within 3 % of it.)
 cudaError_t launch_matmul(const MatArgs& a, const Matrices& m, cudaStream_t st) {
     if (a.M <= kFewMost) return launch_few(a, m, st);
     const int64_t tiles = (a.M + kLanes - 1) / kLanes * ((a.N + Tile::TC - 1) / Tile::TC), sms = tc::num_sms();
@@ -1329,8 +1332,9 @@ CG_EXPORT int cg_block8_encode(int32_t dtype, int64_t R, int64_t K, int32_t rows
     a.stride = R > 1 ? stride : K;
     a.nb = blocks;
     const int64_t items = rows == 1 ? (R * a.nb + kEncRows - 1) / kEncRows : (R + kBlock - 1) / kBlock * a.nb;
-    // Long matrices: as many CTAs as run at once go on, two blocks of a row at a time (8192 x 4096: 19.1 us, 21 with one block, 24.4
-    // with a CTA for 32 blocks; 1024 x 4096 3.8 us, 4.2 with 8 CTAs an SM)
+    // Long matrices: as many CTAs as run at once go on, two blocks of a row at a time (131072 x 4096: 250 us, 292 with one block or with
+    // a CTA for 32 blocks; 8192 x 4096, half of it in L2, 16.2, 17.2 and 18.9; 4096 rows 9.1, 8.8 and 9.0, 1024 3.1, 3.4 and 3.2; 8 CTAs
+    // an SM: within 0.2 us but for 8192 rows, 16.9)
     const int64_t room = (rows == 1 ? 4 : 8) * (int64_t)tc::num_sms();
     const unsigned grid = (unsigned)(items < room ? items : room);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);

@@ -1,7 +1,11 @@
 // cg_follow.cuh -- launches that come while the stream's last kernel ends: the kernel's CTAs are on their SMs, and what
 // needs no memory of others is done, when the last one's results are there (programmatic launch). In a row of the
-// same call, with and without: a plan 3.1 us and 4.1, a commit 5.1 and 6.2, an encoding of 8192 x 4096 18.4 and 20.6, a product of one
-// row 6.4 and 8.2, the attention of one small tree 15.5 and 17.9. CTAs that wait here hold their place on the SM.
+// same call that the host is ahead of, with and without: a plan 1.6 us and 4.1, a commit 4.0 and 6.2, an encoding of 8192 x 4096 (half
+// of it in L2) 16.8 and 19.1, a product of one row 6.4 and 8.2, of 333 8.6 and 11.2, the attention of one small tree 15.5 and 17.9; in a
+// graph a plan 1.6 and 1.9, a commit 4.0 both ways, the products 6.4 and 6.8, 8.4 and 9.0. CTAs that wait here hold their place on the
+// SM: behind a paged attention of few rows, which lets the next kernel come from its first instruction on, both calls together take
+// 1 % less (16 requests after 4096 tokens, then a product of one row: 65.5 us and 66.2) to 1 % more (then a product of 2048 rows:
+// 112.1 and 110.8; 64 requests after 8192 tokens, then an encoding of 64 rows: 327.6 and 325.7).
 #pragma once
 
 #include <cuda_runtime.h>

@@ -1443,7 +1443,10 @@ cudaError_t launch_paged_chunk(const PagedArgs& a, int min_rows, bool after_rows
     P.parts = static_cast<float*>(workspace);
     P.meta = reinterpret_cast<ChunkMeta*>(P.parts + (size_t)tc::num_sms() * 2 * chunk_part_floats(a.d));
     P.min_rows = min_rows;
-    P.min_share = a.masks ? 2 : 4;   // a tree of 8 nodes alone after 1000 tokens: 15.7 us with 2, 16.9 with 3, 17.5 with 4
+    // Matters where few trees leave SMs idle. With 2, 3 and 4: a tree of 8 nodes alone after 1000 tokens 15.2, 16.0 and 16.4 us, after 4000
+    // 18.6, 18.0 and 18.4, of 32 nodes after 1000 17.4, 17.3 and 18.5, two of 16 16.1, 16.5 and 17.2; one after 8000 tokens and more,
+    // three after 3000 and batches of four and more take the same with each, to 0.3 us.
+    P.min_share = a.masks ? 2 : 4;
     P.half_tok = kHalfRows / a.n_rep;
     P.tile_tok = halves(a.d) * P.half_tok;
     P.box_rows = a.page < kKT ? a.page : kKT;
